@@ -348,6 +348,49 @@ lc_status batchnorm_fwd_pair_t(lc_dtype dtype, const void* x, const float* gamma
                                float* save_invstd2, int n, int c, int h, int w, float eps, int relu, lc_layout layout, void* workspace,
                                size_t workspace_bytes, void* hip_stream);
 
+/* ---- The output side of a token model ----
+ * What training and serving a model over tokens needs beside the layers above: the norm in front of its classifier (a 1x1
+ * convolution over one pixel per token), the log probabilities of given tokens with their gradient, and an AdamW step over the
+ * list of parameter tensors.  The paper trains image classifiers and has none of these; they follow the textbook definitions below.
+ * Common to the group: activations are LC_F32 or LC_BF16 (fp32 arithmetic on the widened values, one rounding to nearest even where
+ * a result is stored as bf16), pointers need the alignment of one element only (rows that start on 16-byte boundaries are
+ * fastest), any width is taken, zero rows or tensors are no work and LC_OK, sums run in a fixed order (bit-identical reruns).
+ */
+
+/* rows x c values; x_ld and residual_ld: elements from one row of x / residual to the next (0: c; otherwise >= c). */
+typedef struct {
+    int64_t rows;
+    int c;            /* at most 2^30 */
+    int64_t x_ld, residual_ld;
+    float eps;        /* >= 0, inside the root */
+    lc_dtype dtype;   /* type of x, residual, total, y and of the gradients dy, dtotal, dx; gamma, rstd and dgamma are fp32 */
+} lc_rmsnorm_desc;
+
+/* Root-mean-square norm with the residual's addition: total = x + residual (rounded to dtype; x where residual is NULL),
+ *     rstd = 1/sqrt(mean over the row of total^2 + eps),   y = (total * rstd) * gamma.
+ * The statistics are those of total as stored.  total ([rows][c], contiguous) may be NULL (not stored) and must be NULL without a
+ * residual (LC_ERR_UNSUPPORTED); it may be the residual's or x's own buffer where that is contiguous, otherwise buffers must not
+ * overlap.  save_rstd: rows floats for the backward pass, or NULL.  y: [rows][c], contiguous.
+ * A row that holds an infinity or a NaN gets NaN where the formula gives it. */
+lc_status rmsnorm_fwd(const lc_rmsnorm_desc* desc, const void* x, const void* residual, const float* gamma, void* total, void* y,
+                      float* save_rstd, void* hip_stream);
+
+/* The same with y in 8 bits: for each group of `group` columns of a row (a power of two from 32 to 512, the last group of a row
+ * may be shorter; 0: the whole row) scale = max(amax |y| / 448, 2^-126) and y8 = y / scale as e4m3 (4 exponent bits, bias 7, 3 mantissa
+ * bits, no infinities, largest 448), rounded to nearest even; a NaN keeps the code of NaN and takes no part in amax.  y8: [rows][c] bytes;
+ * scales: [rows][ceil(c/group)] floats ([rows] for group 0): y is about y8 * scale. */
+lc_status rmsnorm_fwd_q8(const lc_rmsnorm_desc* desc, const void* x, const void* residual, const float* gamma, void* total, uint8_t* y8,
+                         float* scales, int group, float* save_rstd, void* hip_stream);
+
+/* Gradient: with a = dy * gamma and n = total * rstd (total: what the forward pass stored, or its x where there was no residual; h_ld
+ * elements from row to row, 0: c),
+ *     dx = rstd * (a - n * mean over the row of (a * n)) + dtotal,      dgamma = sum over the rows of dy * n.
+ * dtotal is the gradient that reaches total by the other way (the residual stream), or NULL; dx is the gradient of x and of residual
+ * alike.  dy, dtotal, dx: [rows][c], contiguous.  x_ld and residual_ld of desc are not used.  Buffers must not overlap. */
+size_t rmsnorm_bwd_workspace_bytes(const lc_rmsnorm_desc* desc);
+lc_status rmsnorm_bwd(const lc_rmsnorm_desc* desc, const void* total, int64_t h_ld, const void* dy, const void* dtotal, const float* gamma,
+                      const float* save_rstd, void* dx, float* dgamma, void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* Static, human-readable name of a status code. */
 const char* lc_status_string(lc_status status);
 

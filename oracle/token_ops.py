@@ -1,0 +1,81 @@
+"""Definitions of the operators of a token model's output side in numpy float64: the RMS norm with the residual's addition, its 8-bit
+output and its gradient; the log probabilities of given tokens with entropy, top alternatives and gradient; the AdamW step with states
+in 32 bits or in 8.  Shares no code with the GPU path; test infrastructure only."""
+import numpy as np
+
+
+# ---- small floating-point formats ----
+
+def grid_step(x, mantissa, least):
+    """The distance of neighbours around x of a format with `mantissa` bits whose least normal exponent is `least`."""
+    e = np.frexp(np.abs(x))[1] - 1
+    return np.exp2(np.maximum(e, least).astype(np.float64) - mantissa)
+
+
+def round_to(x, mantissa, least):
+    """Nearest value of the format, ties to even (np.rint), no upper limit."""
+    x = np.asarray(x, dtype=np.float64)
+    step = grid_step(x, mantissa, least)
+    return np.rint(x / step) * step
+
+
+def e4m3(x):
+    """Values of e4m3 (largest 448, least 2^-9); the caller keeps |x| at most 448 but for rounding."""
+    return round_to(x, 3, -6)
+
+
+def bf16(x):
+    return round_to(np.asarray(x, dtype=np.float64), 7, -126)
+
+
+def dither21(index, seed):
+    """21 bits for element `index` of a tensor: two rounds of shift and odd product modulo 2^32 (the golden ratio's and root two's bits)."""
+    m = (1 << 32) - 1
+    u = [(int(i) + seed * 0x9E3779B1 + 0x7F4A7C15) & m for i in np.ravel(index)]
+    u = [((v ^ (v >> 16)) * 0x9E3779B1) & m for v in u]
+    u = [((v ^ (v >> 15)) * 0x6A09E667) & m for v in u]
+    return np.array([v >> 11 for v in u], dtype=np.float64).reshape(np.shape(index))
+
+
+def e5m2_dithered(x, bits):
+    """x >= 0 on the grid of e5m2: up where the dropped part of a step and the dither, bits / 2^21, come to one; never from above zero to zero."""
+    step = grid_step(x, 2, -14)
+    q = np.floor(x / step + bits / 2.0 ** 21) * step
+    return np.where(x > 0, np.maximum(q, 2.0 ** -16), 0.0)
+
+
+def power_scale(amax, most):
+    """The smallest power of two s >= 2^-126 with amax / s <= most; 1 for amax = 0."""
+    if amax == 0:
+        return 1.0
+    f, e = np.frexp(amax / most)
+    return float(2.0 ** max(-126, e - 1 if f == 0.5 else e))
+
+
+# ---- RMS norm ----
+
+def rmsnorm(x, residual, gamma, eps, store=lambda v: v):
+    """(total, rstd, y) with y unrounded; `store` is the rounding total goes through."""
+    h = np.asarray(x, np.float64) if residual is None else store(np.asarray(x, np.float64) + np.asarray(residual, np.float64))
+    rstd = 1.0 / np.sqrt(np.mean(h * h, axis=1) + eps)
+    return h, rstd, h * rstd[:, None] * np.asarray(gamma, np.float64)
+
+
+def quantise_rows(y, group):
+    """(values of the codes, scales): scale = max(amax/448, 2^-126) for each group of columns."""
+    rows, c = y.shape
+    w = group or c
+    q, scales = np.zeros_like(y), np.zeros((rows, -(-c // w)))
+    for j, at in enumerate(range(0, c, w)):
+        part = y[:, at:at + w]
+        scales[:, j] = np.maximum(np.max(np.abs(part), axis=1) / 448.0, 2.0 ** -126)
+        q[:, at:at + w] = e4m3(part / scales[:, j:j + 1])
+    return q, scales
+
+
+def rmsnorm_bwd(h, rstd, gamma, dy, dtotal=None):
+    h, dy = np.asarray(h, np.float64), np.asarray(dy, np.float64)
+    n = h * rstd[:, None]
+    a = dy * gamma
+    dx = rstd[:, None] * (a - n * np.mean(a * n, axis=1, keepdims=True))
+    return dx if dtotal is None else dx + dtotal, np.sum(dy * n, axis=0)

@@ -1,0 +1,481 @@
+// Root-mean-square norm with the residual's addition, its output in the storage type or in 8 bits, and its gradient, for gfx950.
+//
+// total = x + residual, rstd = 1/sqrt(mean total^2 + eps), y = (total * rstd) * gamma; with a = dy * gamma and n = total * rstd,
+// dx = rstd * (a - n * mean(a * n)) + dtotal and dgamma = sum over rows of dy * n.  Bound by memory: a row is read once into registers,
+// summed, and written from there.  A thread owns eight neighbouring columns at a time for either type, so that a group of 32 to 512
+// columns with a scale of its own is 4 to 64 neighbouring lanes of one wave.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "internal.h"
+#include "token_common.h"
+
+namespace {
+
+struct NormArgs {
+    const void* x;
+    const void* r;           // residual or null
+    const float* gamma;
+    void* total;             // or null
+    void* y;                 // T, or e4m3 codes
+    float* scales;           // 8 bits only
+    float* rstd;             // or null
+    long long rows, x_ld, r_ld;
+    int c, group;
+    float eps;
+};
+
+constexpr float kE4m3Max = 448.f, kLeastScale = 0x1p-126f;
+
+// eight e4m3 codes of v * inv, nearest even (the conversion instruction's own rounding; NaN keeps the code of NaN)
+__device__ __forceinline__ void store8_e4m3(uint8_t* p, const float* v, float inv, int n) {
+    uint32_t w[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        int u = 0;
+        u = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * k] * inv, v[4 * k + 1] * inv, u, false);
+        u = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * k + 2] * inv, v[4 * k + 3] * inv, u, true);
+        w[k] = (uint32_t)u;
+    }
+    if (n >= 8) {
+        __builtin_memcpy(p, w, 8);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < n) p[j] = (uint8_t)(w[j >> 2] >> (8 * (j & 3)));
+    }
+}
+
+__device__ __forceinline__ float scale_of(float amax) { return fmaxf(amax / kE4m3Max, kLeastScale); }
+
+template <typename T>
+__device__ __forceinline__ void load8(Packed<T>& to, const T* row, int col, int c) {
+    if (col + 8 <= c) to.load(row + col);
+    else to.load_some(row + col, c - col);
+}
+
+// A block per row (rows dealt round the grid), CH times eight columns a thread.
+template <typename T, int WAVES, int CH, bool Q8>
+__global__ void __launch_bounds__(WAVES * 64) rmsnorm_fwd_kernel(const NormArgs p) {
+    __shared__ float red[2][2][WAVES];
+    const int tid = threadIdx.x, c = p.c;
+    int parity = 0;
+    for (long long row = blockIdx.x; row < p.rows; row += gridDim.x, parity ^= 1) {
+        const T* x = static_cast<const T*>(p.x) + row * p.x_ld;
+        Packed<T> px[CH], pr[CH];
+        Packed<float> pg[CH];
+        float h[CH][8];
+#pragma unroll
+        for (int i = 0; i < CH; ++i) load8(px[i], x, (i * WAVES * 64 + tid) * 8, c);
+        if (p.r) {
+            const T* r = static_cast<const T*>(p.r) + row * p.r_ld;
+#pragma unroll
+            for (int i = 0; i < CH; ++i) load8(pr[i], r, (i * WAVES * 64 + tid) * 8, c);
+        }
+#pragma unroll
+        for (int i = 0; i < CH; ++i) load8(pg[i], p.gamma, (i * WAVES * 64 + tid) * 8, c);
+        float ss = 0.f;
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) h[i][j] = p.r ? lc_as_stored<T>(px[i].get(j) + pr[i].get(j)) : px[i].get(j);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) ss = fmaf(h[i][j], h[i][j], ss);
+        }
+        if (p.total) {
+            T* t = static_cast<T*>(p.total) + row * (long long)c;
+#pragma unroll
+            for (int i = 0; i < CH; ++i) {
+                const int col = (i * WAVES * 64 + tid) * 8;
+                lc_store8(t + col, h[i], c - col);
+            }
+        }
+        ss = lc_block_sum<WAVES>(ss, red[parity][0]);
+        const float rstd = 1.f / sqrtf(ss / (float)c + p.eps);
+        if (p.rstd && tid == 0) p.rstd[row] = rstd;
+        float amax = 0.f;
+#pragma unroll
+        for (int i = 0; i < CH; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                h[i][j] = h[i][j] * rstd * pg[i].get(j);
+                if (Q8) amax = fmaxf(amax, fabsf(h[i][j]));
+            }
+        if constexpr (!Q8) {
+            T* y = static_cast<T*>(p.y) + row * (long long)c;
+#pragma unroll
+            for (int i = 0; i < CH; ++i) {
+                const int col = (i * WAVES * 64 + tid) * 8;
+                lc_store8(y + col, h[i], c - col);
+            }
+        } else {
+            uint8_t* y = static_cast<uint8_t*>(p.y) + row * (long long)c;
+            if (p.group == 0) {
+                const float scale = scale_of(lc_block_max<WAVES>(amax, red[parity][1]));
+                if (tid == 0) p.scales[row] = scale;
+                const float inv = 1.f / scale;
+#pragma unroll
+                for (int i = 0; i < CH; ++i) {
+                    const int col = (i * WAVES * 64 + tid) * 8;
+                    store8_e4m3(y + col, h[i], inv, c - col);
+                }
+            } else {
+                const int lanes = p.group >> 3;
+                const long long groups = (c + p.group - 1) / p.group;
+#pragma unroll
+                for (int i = 0; i < CH; ++i) {
+                    const int col = (i * WAVES * 64 + tid) * 8;
+                    float m = 0.f;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) m = fmaxf(m, fabsf(h[i][j]));
+                    for (int off = 1; off < lanes; off <<= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
+                    const float scale = scale_of(m);
+                    if (col < c && (tid & (lanes - 1)) == 0) p.scales[row * groups + col / p.group] = scale;
+                    store8_e4m3(y + col, h[i], 1.f / scale, c - col);
+                }
+            }
+        }
+    }
+}
+
+// Rows too wide for the registers of a block: the same in passes over the row, which the caches hold.
+template <typename T, bool Q8>
+__global__ void __launch_bounds__(1024) rmsnorm_fwd_wide_kernel(const NormArgs p) {
+    constexpr int WAVES = 16, kSpan = WAVES * 64 * 8;
+    __shared__ float red[2][2][WAVES];
+    const int tid = threadIdx.x, c = p.c;
+    int parity = 0;
+    for (long long row = blockIdx.x; row < p.rows; row += gridDim.x, parity ^= 1) {
+        const T* x = static_cast<const T*>(p.x) + row * p.x_ld;
+        const T* r = p.r ? static_cast<const T*>(p.r) + row * p.r_ld : nullptr;
+        T* t = p.total ? static_cast<T*>(p.total) + row * (long long)c : nullptr;
+        // the stored sum is what later passes read (total may be x's or the residual's own buffer)
+        auto value = [&](int col, float* h, bool first) __attribute__((always_inline)) {
+            Packed<T> a, b;
+            if (!first && t) {
+                load8(a, const_cast<const T*>(t), col, c);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) h[j] = a.get(j);
+                return;
+            }
+            load8(a, x, col, c);
+            if (r) load8(b, r, col, c);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) h[j] = r ? lc_as_stored<T>(a.get(j) + b.get(j)) : a.get(j);
+        };
+        float ss = 0.f, h[8];
+        for (long long at = tid * 8; at < c; at += kSpan) {
+            const int col = (int)at;
+            value(col, h, true);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) ss = fmaf(h[j], h[j], ss);
+            if (t) lc_store8(t + col, h, c - col);
+        }
+        ss = lc_block_sum<WAVES>(ss, red[parity][0]);
+        const float rstd = 1.f / sqrtf(ss / (float)c + p.eps);
+        if (p.rstd && tid == 0) p.rstd[row] = rstd;
+        auto normed = [&](int col, float* y) __attribute__((always_inline)) {
+            Packed<float> g;
+            load8(g, p.gamma, col, c);
+            value(col, y, false);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] = y[j] * rstd * g.get(j);
+        };
+        if constexpr (!Q8) {
+            for (long long at = tid * 8; at < c; at += kSpan) {
+                normed((int)at, h);
+                lc_store8(static_cast<T*>(p.y) + row * (long long)c + at, h, c - (int)at);
+            }
+        } else {
+            uint8_t* y = static_cast<uint8_t*>(p.y) + row * (long long)c;
+            const int lanes = p.group >> 3;
+            const long long groups = p.group ? (c + p.group - 1) / p.group : 1;
+            float scale = 0.f;
+            if (p.group == 0) {
+                float m = 0.f;
+                for (long long at = tid * 8; at < c; at += kSpan) {
+                    normed((int)at, h);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) m = fmaxf(m, fabsf(h[j]));
+                }
+                scale = scale_of(lc_block_max<WAVES>(m, red[parity][1]));
+                if (tid == 0) p.scales[row] = scale;
+            }
+            for (long long base = 0; base < c; base += kSpan) {     // every lane of a group takes part in its maximum
+                const long long at = base + tid * 8;
+                const int col = at < c ? (int)at : c;
+                normed(col, h);
+                if (p.group) {
+                    float m = 0.f;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) m = fmaxf(m, fabsf(h[j]));
+                    for (int off = 1; off < lanes; off <<= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
+                    scale = scale_of(m);
+                    if (col < c && (tid & (lanes - 1)) == 0) p.scales[row * groups + col / p.group] = scale;
+                }
+                store8_e4m3(y + col, h, 1.f / scale, c - col);
+            }
+        }
+    }
+}
+
+struct NormBwdArgs {
+    const void* h;
+    const void* dy;
+    const void* dh;          // or null
+    const float* gamma;
+    const float* rstd;
+    void* dx;
+    float* part;             // [blocks][c]: each block's rows' share of dgamma
+    long long rows, h_ld;
+    int c;
+};
+
+// A block walks rows blockIdx, blockIdx + gridDim, ...; a thread's columns stay the same, so that its share of dgamma stays in registers.
+template <typename T, int WAVES, int CH>
+__global__ void __launch_bounds__(WAVES * 64) rmsnorm_bwd_kernel(const NormBwdArgs p) {
+    __shared__ float red[2][WAVES];
+    const int tid = threadIdx.x, c = p.c;
+    Packed<float> pg[CH];
+    float acc[CH][8] = {};
+#pragma unroll
+    for (int i = 0; i < CH; ++i) load8(pg[i], p.gamma, (i * WAVES * 64 + tid) * 8, c);
+    int parity = 0;
+    for (long long row = blockIdx.x; row < p.rows; row += gridDim.x, parity ^= 1) {
+        const T* h = static_cast<const T*>(p.h) + row * p.h_ld;
+        const T* dy = static_cast<const T*>(p.dy) + row * (long long)c;
+        Packed<T> ph[CH], pd[CH], pt[CH];
+#pragma unroll
+        for (int i = 0; i < CH; ++i) load8(ph[i], h, (i * WAVES * 64 + tid) * 8, c);
+#pragma unroll
+        for (int i = 0; i < CH; ++i) load8(pd[i], dy, (i * WAVES * 64 + tid) * 8, c);
+        if (p.dh) {
+            const T* dh = static_cast<const T*>(p.dh) + row * (long long)c;
+#pragma unroll
+            for (int i = 0; i < CH; ++i) load8(pt[i], dh, (i * WAVES * 64 + tid) * 8, c);
+        }
+        const float rstd = p.rstd[row];
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < CH; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float n = ph[i].get(j) * rstd, d = pd[i].get(j);
+                s = fmaf(d * pg[i].get(j), n, s);
+                acc[i][j] = fmaf(d, n, acc[i][j]);
+            }
+        const float mean = lc_block_sum<WAVES>(s, red[parity]) / (float)c;
+        T* dx = static_cast<T*>(p.dx) + row * (long long)c;
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            const int col = (i * WAVES * 64 + tid) * 8;
+            float o[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float n = ph[i].get(j) * rstd;
+                o[j] = (pd[i].get(j) * pg[i].get(j) - n * mean) * rstd;
+                if (p.dh) o[j] += pt[i].get(j);
+            }
+            lc_store8(dx + col, o, c - col);
+        }
+    }
+    float* part = p.part + (long long)blockIdx.x * c;
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+        const int col = (i * WAVES * 64 + tid) * 8;
+        lc_store8(part + col, acc[i], c - col);
+    }
+}
+
+// Wide rows: dgamma's shares by column tiles and ranges of rows (blockIdx.y), and dx in two passes over a row.
+template <typename T>
+__global__ void __launch_bounds__(256) rmsnorm_dgamma_wide_kernel(const NormBwdArgs p) {
+    const long long at = ((long long)blockIdx.x * 256 + threadIdx.x) * 8;
+    if (at >= p.c) return;
+    const int col = (int)at;
+    float acc[8] = {};
+    for (long long row = blockIdx.y; row < p.rows; row += gridDim.y) {
+        Packed<T> h, d;
+        load8(h, static_cast<const T*>(p.h) + row * p.h_ld, col, p.c);
+        load8(d, static_cast<const T*>(p.dy) + row * (long long)p.c, col, p.c);
+        const float rstd = p.rstd[row];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[j] = fmaf(d.get(j), h.get(j) * rstd, acc[j]);
+    }
+    lc_store8(p.part + (long long)blockIdx.y * p.c + col, acc, p.c - col);
+}
+
+template <typename T>
+__global__ void __launch_bounds__(1024) rmsnorm_bwd_wide_kernel(const NormBwdArgs p) {
+    constexpr int WAVES = 16, kSpan = WAVES * 64 * 8;
+    __shared__ float red[2][WAVES];
+    const int tid = threadIdx.x, c = p.c;
+    int parity = 0;
+    for (long long row = blockIdx.x; row < p.rows; row += gridDim.x, parity ^= 1) {
+        const T* h = static_cast<const T*>(p.h) + row * p.h_ld;
+        const T* dy = static_cast<const T*>(p.dy) + row * (long long)c;
+        const T* dh = p.dh ? static_cast<const T*>(p.dh) + row * (long long)c : nullptr;
+        T* dx = static_cast<T*>(p.dx) + row * (long long)c;
+        const float rstd = p.rstd[row];
+        Packed<T> a, b, t;
+        Packed<float> g;
+        float s = 0.f;
+        for (long long at = tid * 8; at < c; at += kSpan) {
+            load8(a, h, (int)at, c);
+            load8(b, dy, (int)at, c);
+            load8(g, p.gamma, (int)at, c);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s = fmaf(b.get(j) * g.get(j), a.get(j) * rstd, s);
+        }
+        const float mean = lc_block_sum<WAVES>(s, red[parity]) / (float)c;
+        for (long long at = tid * 8; at < c; at += kSpan) {
+            load8(a, h, (int)at, c);
+            load8(b, dy, (int)at, c);
+            load8(g, p.gamma, (int)at, c);
+            if (dh) load8(t, dh, (int)at, c);
+            float o[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                o[j] = (b.get(j) * g.get(j) - a.get(j) * rstd * mean) * rstd;
+                if (dh) o[j] += t.get(j);
+            }
+            lc_store8(dx + at, o, c - (int)at);
+        }
+    }
+}
+
+// dgamma[k] = the blocks' shares added in a fixed order: 64 columns a block, a wave takes every 16th share.
+__global__ void __launch_bounds__(1024) rmsnorm_dgamma_kernel(const float* __restrict__ part, float* __restrict__ dgamma, int parts, int c) {
+    __shared__ float sum[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const long long k = (long long)blockIdx.x * 64 + lane;
+    float s[4] = {};
+    if (k < c) {
+        int i = wave;
+        for (; i + 48 < parts; i += 64)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) s[u] += part[(long long)(i + 16 * u) * c + k];
+        for (; i < parts; i += 16) s[0] += part[(long long)i * c + k];
+    }
+    sum[wave][lane] = (s[0] + s[1]) + (s[2] + s[3]);
+    __syncthreads();
+    if (wave == 0 && k < c) {
+        float t = 0.f;
+#pragma unroll
+        for (int w = 0; w < 16; ++w) t += sum[w][lane];
+        dgamma[k] = t;
+    }
+}
+
+constexpr int kMostColumns = 16384;          // what a block's registers hold of a row
+constexpr int kMostWidth = 1 << 30;          // columns are counted in 32 bits, eight past the end among them
+constexpr long long kMostBlocks = 1 << 20;   // rows beyond are dealt round
+
+lc_status check_desc(const lc_rmsnorm_desc* d) {
+    if (!d) return LC_ERR_NULL;
+    if (d->dtype != LC_F32 && d->dtype != LC_BF16) return LC_ERR_UNSUPPORTED;
+    if (d->rows < 0 || d->c <= 0 || d->c > kMostWidth) return LC_ERR_SHAPE;
+    if ((d->x_ld && d->x_ld < d->c) || (d->residual_ld && d->residual_ld < d->c)) return LC_ERR_SHAPE;
+    const long long widest = std::max<long long>({d->c, d->x_ld, d->residual_ld});
+    long long bytes;
+    if (__builtin_mul_overflow((long long)d->rows, widest, &bytes) || __builtin_mul_overflow(bytes, 4ll, &bytes)) return LC_ERR_SHAPE;
+    if (!(d->eps >= 0.f)) return LC_ERR_UNSUPPORTED;
+    return LC_OK;
+}
+
+template <typename T, bool Q8>
+void launch_fwd(const NormArgs& a, hipStream_t stream) {
+    const dim3 grid((unsigned)std::min(a.rows, kMostBlocks));
+    if (a.c <= 2048) hipLaunchKernelGGL((rmsnorm_fwd_kernel<T, 4, 1, Q8>), grid, dim3(256), 0, stream, a);
+    else if (a.c <= 4096) hipLaunchKernelGGL((rmsnorm_fwd_kernel<T, 4, 2, Q8>), grid, dim3(256), 0, stream, a);
+    else if (a.c <= 8192) hipLaunchKernelGGL((rmsnorm_fwd_kernel<T, 8, 2, Q8>), grid, dim3(512), 0, stream, a);
+    else if (a.c <= kMostColumns) hipLaunchKernelGGL((rmsnorm_fwd_kernel<T, 16, 2, Q8>), grid, dim3(1024), 0, stream, a);
+    else hipLaunchKernelGGL((rmsnorm_fwd_wide_kernel<T, Q8>), grid, dim3(1024), 0, stream, a);
+}
+
+lc_status run_fwd(const lc_rmsnorm_desc* d, const void* x, const void* residual, const float* gamma, void* total, void* y, float* scales,
+                  int group, float* save_rstd, bool q8, void* hip_stream) {
+    const lc_status st = check_desc(d);
+    if (st != LC_OK) return st;
+    if (q8 && group != 0 && (group < 32 || group > 512 || (group & (group - 1)))) return LC_ERR_UNSUPPORTED;
+    if (!residual && total) return LC_ERR_UNSUPPORTED;
+    if (d->rows == 0) return LC_OK;
+    if (!x || !gamma || !y || (q8 && !scales)) return LC_ERR_NULL;
+    const size_t e = d->dtype == LC_BF16 ? 2 : 4;
+    if (lc_off_element(x, e) || lc_off_element(residual, e) || lc_off_element(total, e) || (!q8 && lc_off_element(y, e)) ||
+        lc_off_element(gamma, 4) || lc_off_element(scales, 4) || lc_off_element(save_rstd, 4))
+        return LC_ERR_ALIGN;
+    NormArgs a{x, residual, gamma, total, y, scales, save_rstd, d->rows, d->x_ld ? d->x_ld : d->c, d->residual_ld ? d->residual_ld : d->c,
+               d->c, group, d->eps};
+    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    lc_begin_call();
+    if (d->dtype == LC_BF16) q8 ? launch_fwd<uint16_t, true>(a, stream) : launch_fwd<uint16_t, false>(a, stream);
+    else q8 ? launch_fwd<float, true>(a, stream) : launch_fwd<float, false>(a, stream);
+    return lc_end_call();
+}
+
+// Blocks of the backward pass, each with a share of dgamma: four a compute unit, or one a row.
+long long bwd_blocks(const lc_rmsnorm_desc* d) { return std::min<long long>(d->rows, d->c <= kMostColumns ? 1024 : 64); }
+
+template <typename T>
+void launch_bwd(const NormBwdArgs& a, int blocks, hipStream_t stream) {
+    const dim3 grid((unsigned)blocks);
+    if (a.c <= 2048) hipLaunchKernelGGL((rmsnorm_bwd_kernel<T, 4, 1>), grid, dim3(256), 0, stream, a);
+    else if (a.c <= 4096) hipLaunchKernelGGL((rmsnorm_bwd_kernel<T, 8, 1>), grid, dim3(512), 0, stream, a);
+    else if (a.c <= 8192) hipLaunchKernelGGL((rmsnorm_bwd_kernel<T, 16, 1>), grid, dim3(1024), 0, stream, a);
+    else if (a.c <= kMostColumns) hipLaunchKernelGGL((rmsnorm_bwd_kernel<T, 16, 2>), grid, dim3(1024), 0, stream, a);
+    else {
+        hipLaunchKernelGGL((rmsnorm_dgamma_wide_kernel<T>), dim3((unsigned)(((long long)a.c + 2047) / 2048), (unsigned)blocks), dim3(256), 0, stream, a);
+        hipLaunchKernelGGL((rmsnorm_bwd_wide_kernel<T>), dim3((unsigned)std::min(a.rows, kMostBlocks)), dim3(1024), 0, stream, a);
+    }
+}
+
+}  // namespace
+
+extern "C" lc_status rmsnorm_fwd(const lc_rmsnorm_desc* desc, const void* x, const void* residual, const float* gamma, void* total, void* y,
+                                 float* save_rstd, void* hip_stream) {
+    return run_fwd(desc, x, residual, gamma, total, y, nullptr, 0, save_rstd, false, hip_stream);
+}
+
+extern "C" lc_status rmsnorm_fwd_q8(const lc_rmsnorm_desc* desc, const void* x, const void* residual, const float* gamma, void* total,
+                                    uint8_t* y8, float* scales, int group, float* save_rstd, void* hip_stream) {
+    return run_fwd(desc, x, residual, gamma, total, y8, scales, group, save_rstd, true, hip_stream);
+}
+
+extern "C" size_t rmsnorm_bwd_workspace_bytes(const lc_rmsnorm_desc* desc) {
+    if (check_desc(desc) != LC_OK) return 0;
+    return ((size_t)bwd_blocks(desc) * desc->c * sizeof(float) + 255) & ~(size_t)255;
+}
+
+extern "C" lc_status rmsnorm_bwd(const lc_rmsnorm_desc* desc, const void* total, int64_t h_ld, const void* dy, const void* dtotal,
+                                 const float* gamma, const float* save_rstd, void* dx, float* dgamma, void* workspace,
+                                 size_t workspace_bytes, void* hip_stream) {
+    const lc_status st = check_desc(desc);
+    if (st != LC_OK) return st;
+    if (h_ld && h_ld < desc->c) return LC_ERR_SHAPE;
+    long long span;
+    if (__builtin_mul_overflow((long long)desc->rows, (long long)h_ld, &span) || __builtin_mul_overflow(span, 4ll, &span)) return LC_ERR_SHAPE;
+    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    if (!dgamma) return LC_ERR_NULL;
+    if (lc_off_element(dgamma, 4)) return LC_ERR_ALIGN;
+    if (desc->rows == 0) {                   // a sum over no rows
+        lc_begin_call();
+        lc_fill_f32(dgamma, 0.f, (size_t)desc->c, stream);
+        return lc_end_call();
+    }
+    if (!total || !dy || !gamma || !save_rstd || !dx) return LC_ERR_NULL;
+    const size_t e = desc->dtype == LC_BF16 ? 2 : 4;
+    if (lc_off_element(total, e) || lc_off_element(dy, e) || lc_off_element(dtotal, e) || lc_off_element(dx, e) || lc_off_element(gamma, 4) ||
+        lc_off_element(save_rstd, 4))
+        return LC_ERR_ALIGN;
+    if (!workspace || (((uintptr_t)workspace) & 255) || workspace_bytes < rmsnorm_bwd_workspace_bytes(desc)) return LC_ERR_WORKSPACE;
+    const int blocks = (int)bwd_blocks(desc);
+    NormBwdArgs a{total, dy, dtotal, gamma, save_rstd, dx, static_cast<float*>(workspace), desc->rows, h_ld ? h_ld : desc->c, desc->c};
+    lc_begin_call();
+    if (desc->dtype == LC_BF16) launch_bwd<uint16_t>(a, blocks, stream);
+    else launch_bwd<float>(a, blocks, stream);
+    hipLaunchKernelGGL(rmsnorm_dgamma_kernel, dim3((unsigned)(((long long)desc->c + 63) / 64)), dim3(1024), 0, stream, a.part, dgamma, blocks, desc->c);
+    return lc_end_call();
+}

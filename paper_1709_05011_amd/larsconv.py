@@ -28,6 +28,7 @@ EXPORTS = ["conv2d_out_shape", "conv2d_workspace_bytes", "conv2d_fwd", "conv2d_b
            "batchnorm_fwd_t", "batchnorm_bwd_t", "maxpool_fwd_t", "maxpool_bwd_t", "relu_add_bwd_t", "global_avgpool_fwd_t",
            "global_avgpool_bwd_t", "relu_add_bwd_bnsums_t", "relu_add_bwd_bnsums_grid_t", "batchnorm_bwd_presummed_t",
            "conv2d_fwd_stats_count", "conv2d_fwd_stats", "batchnorm_fwd_pre", "batchnorm_fwd_pair_t",
+           "rmsnorm_fwd", "rmsnorm_fwd_q8", "rmsnorm_bwd_workspace_bytes", "rmsnorm_bwd",
            "lc_status_string", "lc_last_error_detail"]
 
 
@@ -63,6 +64,24 @@ class ConvDesc:
     def c_struct(self) -> lc_conv_desc:
         return lc_conv_desc(self.n, self.c, self.h, self.w, self.k, self.r, self.s, self.stride_h, self.stride_w,
                             self.pad_h, self.pad_w, self.dtype, self.layout, self.groups)
+
+
+class lc_rmsnorm_desc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("c", ctypes.c_int), ("x_ld", ctypes.c_int64), ("residual_ld", ctypes.c_int64),
+                ("eps", ctypes.c_float), ("dtype", ctypes.c_int)]
+
+
+@dataclass(frozen=True)
+class RmsNormDesc:
+    rows: int
+    c: int
+    x_ld: int = 0
+    residual_ld: int = 0
+    eps: float = 1e-5
+    dtype: int = LC_F32
+
+    def c_struct(self) -> lc_rmsnorm_desc:
+        return lc_rmsnorm_desc(self.rows, self.c, self.x_ld, self.residual_ld, self.eps, self.dtype)
 
 
 _lib = None
@@ -161,6 +180,15 @@ def lib() -> ctypes.CDLL:
                                            i32, i32, vp, sz, vp]
         L.batchnorm_fwd_pre.restype = i32
         L.batchnorm_fwd_pre.argtypes = [i32, vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, ctypes.c_float, i32, i32, vp, sz, vp, sz, vp]
+        rp = ctypes.POINTER(lc_rmsnorm_desc)
+        L.rmsnorm_fwd.restype = i32
+        L.rmsnorm_fwd.argtypes = [rp, vp, vp, vp, vp, vp, vp, vp]
+        L.rmsnorm_fwd_q8.restype = i32
+        L.rmsnorm_fwd_q8.argtypes = [rp, vp, vp, vp, vp, vp, vp, i32, vp, vp]
+        L.rmsnorm_bwd_workspace_bytes.restype = sz
+        L.rmsnorm_bwd_workspace_bytes.argtypes = [rp]
+        L.rmsnorm_bwd.restype = i32
+        L.rmsnorm_bwd.argtypes = [rp, vp, ctypes.c_int64, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.lc_status_string.restype = ctypes.c_char_p
         L.lc_status_string.argtypes = [i32]
         L.lc_last_error_detail.restype = ctypes.c_char_p
@@ -520,3 +548,31 @@ def batchnorm_fwd_pre(dtype: int, x, gamma, beta, residual, y, save_mean, save_i
     _check(lib().batchnorm_fwd_pre(dtype, _ptr(x), _ptr(gamma), _ptr(beta), _ptr(residual), _ptr(y), _ptr(save_mean),
                                    _ptr(save_invstd), n, c, h, w, eps, int(bool(relu)), layout, _ptr(stats), stats_tiles,
                                    _ptr(workspace), _nbytes(workspace), _stream(stream)), "batchnorm_fwd_pre")
+
+
+# ---- the output side of a token model: RMS norm with the residual's addition ----
+
+def _c(desc):
+    """The C structure of a descriptor dataclass (or the structure itself)."""
+    return ctypes.byref(desc.c_struct() if hasattr(desc, "c_struct") else desc)
+
+
+def rmsnorm_fwd(desc, x, residual, gamma, total, y, save_rstd=None, stream=None) -> None:
+    _check(lib().rmsnorm_fwd(_c(desc), _ptr(x), _ptr(residual), _ptr(gamma), _ptr(total), _ptr(y), _ptr(save_rstd), _stream(stream)),
+           "rmsnorm_fwd")
+
+
+def rmsnorm_fwd_q8(desc, x, residual, gamma, total, y8, scales, group: int = 0, save_rstd=None, stream=None) -> None:
+    _check(lib().rmsnorm_fwd_q8(_c(desc), _ptr(x), _ptr(residual), _ptr(gamma), _ptr(total), _ptr(y8), _ptr(scales), group,
+                                _ptr(save_rstd), _stream(stream)), "rmsnorm_fwd_q8")
+
+
+def rmsnorm_bwd_workspace_bytes(desc) -> int:
+    return int(lib().rmsnorm_bwd_workspace_bytes(_c(desc)))
+
+
+def rmsnorm_bwd(desc, total, dy, dtotal, gamma, save_rstd, dx, dgamma, workspace=None, h_ld: int = 0, stream=None,
+                workspace_bytes: Optional[int] = None) -> None:
+    nb = _nbytes(workspace) if workspace_bytes is None else workspace_bytes
+    _check(lib().rmsnorm_bwd(_c(desc), _ptr(total), h_ld, _ptr(dy), _ptr(dtotal), _ptr(gamma), _ptr(save_rstd), _ptr(dx),
+                             _ptr(dgamma), _ptr(workspace), nb, _stream(stream)), "rmsnorm_bwd")

@@ -1,0 +1,50 @@
+"""Pins of the float64 definitions in oracle/token_ops.py: hand-worked values, other people's casts (torch), finite differences."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import token_ops as ops
+
+
+def test_e4m3_and_bf16_are_the_formats_torch_knows():
+    codes = torch.arange(256, dtype=torch.uint8).view(torch.float8_e4m3fn).float().numpy()
+    values = np.unique(codes[np.isfinite(codes)])
+    assert values.max() == 448.0
+    assert np.array_equal(ops.e4m3(values), values)
+    x = np.concatenate([(values[1:] + values[:-1]) / 2, values * 1.0301, np.float32([1e-4, 3e-3, 447.9])]).astype(np.float32)
+    x = x[np.abs(x) <= 448]
+    assert np.array_equal(ops.e4m3(x), torch.from_numpy(x).to(torch.float8_e4m3fn).double().numpy())
+    y = np.random.default_rng(0).normal(size=1000).astype(np.float32)
+    assert np.array_equal(ops.bf16(y), torch.from_numpy(y).bfloat16().double().numpy())
+
+
+def test_rmsnorm_by_hand():
+    h, rstd, y = ops.rmsnorm(np.array([[1.0, 2.0]]), np.array([[2.0, 2.0]]), np.array([1.0, 10.0]), 0.0)
+    assert np.array_equal(h, [[3.0, 4.0]])
+    assert np.allclose(rstd, 1 / np.sqrt(12.5)) and np.allclose(y, [[3 / np.sqrt(12.5), 40 / np.sqrt(12.5)]])
+    q, s = ops.quantise_rows(np.array([[1.0, -3.5, 0.01, 0.0]]), 2)
+    assert np.allclose(s, [[3.5 / 448, 0.01 / 448]]) and np.array_equal(q, [[128.0, -448.0, 448.0, 0.0]])
+    assert np.array_equal(ops.quantise_rows(np.zeros((1, 3)), 0)[1], [[2.0 ** -126]])
+
+
+def test_rmsnorm_gradient_against_differences_and_autograd():
+    rng = np.random.default_rng(1)
+    x, r, g, dy, dt = rng.normal(size=(3, 7)), rng.normal(size=(3, 7)), rng.normal(size=7), rng.normal(size=(3, 7)), rng.normal(size=(3, 7))
+    f = lambda x, g: float(np.sum(ops.rmsnorm(x, r, g, 1e-3)[2] * dy) + np.sum((x + r) * dt))
+    h, rstd, _ = ops.rmsnorm(x, r, g, 1e-3)
+    dx, dg = ops.rmsnorm_bwd(h, rstd, g, dy, dt)
+    e = 1e-6
+    for i in range(3):
+        for j in range(7):
+            d = np.zeros_like(x)
+            d[i, j] = e
+            assert abs((f(x + d, g) - f(x - d, g)) / (2 * e) - dx[i, j]) < 1e-7
+    for j in range(7):
+        d = np.zeros_like(g)
+        d[j] = e
+        assert abs((f(x, g + d) - f(x, g - d)) / (2 * e) - dg[j]) < 1e-7
+    tx, tg = torch.tensor(x, requires_grad=True), torch.tensor(g, requires_grad=True)
+    th = tx + torch.tensor(r)
+    ty = th * torch.rsqrt((th * th).mean(1, keepdim=True) + 1e-3) * tg
+    ((ty * torch.tensor(dy)).sum() + (th * torch.tensor(dt)).sum()).backward()
+    assert np.allclose(tx.grad.numpy(), dx, atol=1e-12) and np.allclose(tg.grad.numpy(), dg, atol=1e-12)
