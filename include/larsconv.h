@@ -391,6 +391,37 @@ size_t rmsnorm_bwd_workspace_bytes(const lc_rmsnorm_desc* desc);
 lc_status rmsnorm_bwd(const lc_rmsnorm_desc* desc, const void* total, int64_t h_ld, const void* dy, const void* dtotal, const float* gamma,
                       const float* save_rstd, void* dx, float* dgamma, void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/* rows x vocab logits, `ld` elements from one row to the next (0: vocab; otherwise >= vocab: a padded vocabulary's pad is not read). */
+typedef struct {
+    int64_t rows;
+    int vocab;        /* at most 2^30 */
+    int64_t ld;
+    lc_dtype dtype;   /* type of logits and dlogits; everything else is fp32 */
+    int top;          /* alternatives listed per row, 0 to 32 */
+} lc_token_desc;
+
+/* Log probability of a given token in each row of logits z, with the row's entropy and its likeliest tokens:
+ *     lse = log sum_j exp(z_j),   logprob = z_token - lse,   entropy = -sum_j p_j log p_j with p_j = exp(z_j - lse)  (in nats).
+ * tokens: DEVICE, rows int32 values; a token outside [0, vocab) marks a position that does not count: logprob 0.
+ * top_tokens, top_logprobs: [rows][top], the top largest logits in falling order, equal ones by rising token, with their log
+ * probabilities; both NULL if and only if top is 0.  Masked logits are -infinity: probability 0, no part in the entropy, never listed
+ * (places left over hold token -1 and -infinity).  A row whose logits are all masked has lse -infinity, entropy 0, logprob -infinity
+ * (0 where the token does not count).  A row with a NaN or +infinity has NaN in lse, entropy and log probabilities (a NaN is never listed).
+ * logprob, entropy, lse: rows floats each; entropy may be NULL, and lse where no backward pass follows.  Sums are fp32 within a slice of a
+ * row and double across slices; logprob is formed from the difference to the row's maximum, so that large logits do not cancel in it. */
+size_t token_logprob_workspace_bytes(const lc_token_desc* desc);
+lc_status token_logprob_fwd(const lc_token_desc* desc, const void* logits, const int32_t* tokens, float* logprob, float* entropy, float* lse,
+                            int32_t* top_tokens, float* top_logprobs, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Gradient with respect to the logits of  sum over rows of  dlogprob * logprob + dentropy * entropy  (DEVICE, rows floats each; either may
+ * be NULL for zero, not both):
+ *     dlogits_j = dlogprob * ([j = token] - p_j) - dentropy * p_j * (log p_j + entropy).
+ * lse and entropy: what the forward pass gave (entropy may be NULL without dentropy).  dlogprob has no effect where the token does not
+ * count; masked logits, and rows that are masked entirely, get 0.  p_j is formed from lse as stored (relative error about |lse| 2^-24).  dlogits_ld: elements from row to row (0: vocab; otherwise >= vocab; the pad is
+ * not written).  dlogits may be the logits' own buffer if its ld is theirs; otherwise they must not overlap. */
+lc_status token_logprob_bwd(const lc_token_desc* desc, const void* logits, const int32_t* tokens, const float* lse, const float* entropy,
+                            const float* dlogprob, const float* dentropy, void* dlogits, int64_t dlogits_ld, void* hip_stream);
+
 /* Static, human-readable name of a status code. */
 const char* lc_status_string(lc_status status);
 

@@ -79,3 +79,45 @@ def rmsnorm_bwd(h, rstd, gamma, dy, dtotal=None):
     a = dy * gamma
     dx = rstd[:, None] * (a - n * np.mean(a * n, axis=1, keepdims=True))
     return dx if dtotal is None else dx + dtotal, np.sum(dy * n, axis=0)
+
+
+# ---- log probabilities of given tokens ----
+
+def token_logprob(z, tokens, top=0):
+    """(logprob, entropy, lse, top tokens, top log probabilities); masked logits are -inf, a token outside the vocabulary does not count."""
+    z = np.asarray(z, np.float64)
+    rows, k = z.shape
+    m = z.max(axis=1)
+    empty = m == -np.inf
+    from_ = np.where(empty, 0.0, m)
+    e = np.exp(z - from_[:, None])
+    with np.errstate(divide="ignore", invalid="ignore"):
+        log_s = np.log(e.sum(axis=1))
+        logp = np.where(empty[:, None], -np.inf, z - from_[:, None] - log_s[:, None])
+    p = np.where(empty[:, None], 0.0, np.exp(logp))
+    entropy = -np.sum(p * np.where(p > 0, logp, 0.0), axis=1)
+    lse = np.where(empty, -np.inf, from_ + log_s)
+    counts = (tokens >= 0) & (tokens < k)
+    logprob = np.where(counts, logp[np.arange(rows), np.clip(tokens, 0, k - 1)], 0.0)
+    order = np.argsort(-z, axis=1, kind="stable")[:, :top]
+    ids, lp = np.full((rows, top), -1, np.int64), np.full((rows, top), -np.inf)
+    n = order.shape[1]
+    there = np.take_along_axis(z, order, 1) > -np.inf
+    ids[:, :n] = np.where(there, order, -1)
+    lp[:, :n] = np.where(there, np.take_along_axis(logp, order, 1), -np.inf)
+    return logprob, entropy, lse, ids, lp
+
+
+def token_logprob_bwd(z, tokens, dlogprob, dentropy):
+    z = np.asarray(z, np.float64)
+    rows, k = z.shape
+    _, entropy, lse, _, _ = token_logprob(z, tokens)
+    empty = lse == -np.inf
+    logp = z - np.where(empty, 0.0, lse)[:, None]
+    p = np.exp(logp)
+    hot = np.zeros_like(z)
+    counts = (tokens >= 0) & (tokens < k)
+    hot[np.arange(rows)[counts], tokens[counts]] = 1.0
+    a = np.where(counts, dlogprob, 0.0)[:, None]
+    dz = a * (hot - p) - dentropy[:, None] * p * (np.where(p > 0, logp, 0.0) + entropy[:, None])
+    return np.where(empty[:, None], 0.0, dz)

@@ -50,12 +50,6 @@ __device__ __forceinline__ void store8_e4m3(uint8_t* p, const float* v, float in
 
 __device__ __forceinline__ float scale_of(float amax) { return fmaxf(amax / kE4m3Max, kLeastScale); }
 
-template <typename T>
-__device__ __forceinline__ void load8(Packed<T>& to, const T* row, int col, int c) {
-    if (col + 8 <= c) to.load(row + col);
-    else to.load_some(row + col, c - col);
-}
-
 // A block per row (rows dealt round the grid), CH times eight columns a thread.
 template <typename T, int WAVES, int CH, bool Q8>
 __global__ void __launch_bounds__(WAVES * 64) rmsnorm_fwd_kernel(const NormArgs p) {
@@ -68,14 +62,14 @@ __global__ void __launch_bounds__(WAVES * 64) rmsnorm_fwd_kernel(const NormArgs 
         Packed<float> pg[CH];
         float h[CH][8];
 #pragma unroll
-        for (int i = 0; i < CH; ++i) load8(px[i], x, (i * WAVES * 64 + tid) * 8, c);
+        for (int i = 0; i < CH; ++i) lc_load8(px[i], x, (i * WAVES * 64 + tid) * 8, c);
         if (p.r) {
             const T* r = static_cast<const T*>(p.r) + row * p.r_ld;
 #pragma unroll
-            for (int i = 0; i < CH; ++i) load8(pr[i], r, (i * WAVES * 64 + tid) * 8, c);
+            for (int i = 0; i < CH; ++i) lc_load8(pr[i], r, (i * WAVES * 64 + tid) * 8, c);
         }
 #pragma unroll
-        for (int i = 0; i < CH; ++i) load8(pg[i], p.gamma, (i * WAVES * 64 + tid) * 8, c);
+        for (int i = 0; i < CH; ++i) lc_load8(pg[i], p.gamma, (i * WAVES * 64 + tid) * 8, c);
         float ss = 0.f;
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
@@ -155,13 +149,13 @@ __global__ void __launch_bounds__(1024) rmsnorm_fwd_wide_kernel(const NormArgs p
         auto value = [&](int col, float* h, bool first) __attribute__((always_inline)) {
             Packed<T> a, b;
             if (!first && t) {
-                load8(a, const_cast<const T*>(t), col, c);
+                lc_load8(a, const_cast<const T*>(t), col, c);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) h[j] = a.get(j);
                 return;
             }
-            load8(a, x, col, c);
-            if (r) load8(b, r, col, c);
+            lc_load8(a, x, col, c);
+            if (r) lc_load8(b, r, col, c);
 #pragma unroll
             for (int j = 0; j < 8; ++j) h[j] = r ? lc_as_stored<T>(a.get(j) + b.get(j)) : a.get(j);
         };
@@ -178,7 +172,7 @@ __global__ void __launch_bounds__(1024) rmsnorm_fwd_wide_kernel(const NormArgs p
         if (p.rstd && tid == 0) p.rstd[row] = rstd;
         auto normed = [&](int col, float* y) __attribute__((always_inline)) {
             Packed<float> g;
-            load8(g, p.gamma, col, c);
+            lc_load8(g, p.gamma, col, c);
             value(col, y, false);
 #pragma unroll
             for (int j = 0; j < 8; ++j) y[j] = y[j] * rstd * g.get(j);
@@ -241,20 +235,20 @@ __global__ void __launch_bounds__(WAVES * 64) rmsnorm_bwd_kernel(const NormBwdAr
     Packed<float> pg[CH];
     float acc[CH][8] = {};
 #pragma unroll
-    for (int i = 0; i < CH; ++i) load8(pg[i], p.gamma, (i * WAVES * 64 + tid) * 8, c);
+    for (int i = 0; i < CH; ++i) lc_load8(pg[i], p.gamma, (i * WAVES * 64 + tid) * 8, c);
     int parity = 0;
     for (long long row = blockIdx.x; row < p.rows; row += gridDim.x, parity ^= 1) {
         const T* h = static_cast<const T*>(p.h) + row * p.h_ld;
         const T* dy = static_cast<const T*>(p.dy) + row * (long long)c;
         Packed<T> ph[CH], pd[CH], pt[CH];
 #pragma unroll
-        for (int i = 0; i < CH; ++i) load8(ph[i], h, (i * WAVES * 64 + tid) * 8, c);
+        for (int i = 0; i < CH; ++i) lc_load8(ph[i], h, (i * WAVES * 64 + tid) * 8, c);
 #pragma unroll
-        for (int i = 0; i < CH; ++i) load8(pd[i], dy, (i * WAVES * 64 + tid) * 8, c);
+        for (int i = 0; i < CH; ++i) lc_load8(pd[i], dy, (i * WAVES * 64 + tid) * 8, c);
         if (p.dh) {
             const T* dh = static_cast<const T*>(p.dh) + row * (long long)c;
 #pragma unroll
-            for (int i = 0; i < CH; ++i) load8(pt[i], dh, (i * WAVES * 64 + tid) * 8, c);
+            for (int i = 0; i < CH; ++i) lc_load8(pt[i], dh, (i * WAVES * 64 + tid) * 8, c);
         }
         const float rstd = p.rstd[row];
         float s = 0.f;
@@ -298,8 +292,8 @@ __global__ void __launch_bounds__(256) rmsnorm_dgamma_wide_kernel(const NormBwdA
     float acc[8] = {};
     for (long long row = blockIdx.y; row < p.rows; row += gridDim.y) {
         Packed<T> h, d;
-        load8(h, static_cast<const T*>(p.h) + row * p.h_ld, col, p.c);
-        load8(d, static_cast<const T*>(p.dy) + row * (long long)p.c, col, p.c);
+        lc_load8(h, static_cast<const T*>(p.h) + row * p.h_ld, col, p.c);
+        lc_load8(d, static_cast<const T*>(p.dy) + row * (long long)p.c, col, p.c);
         const float rstd = p.rstd[row];
 #pragma unroll
         for (int j = 0; j < 8; ++j) acc[j] = fmaf(d.get(j), h.get(j) * rstd, acc[j]);
@@ -323,18 +317,18 @@ __global__ void __launch_bounds__(1024) rmsnorm_bwd_wide_kernel(const NormBwdArg
         Packed<float> g;
         float s = 0.f;
         for (long long at = tid * 8; at < c; at += kSpan) {
-            load8(a, h, (int)at, c);
-            load8(b, dy, (int)at, c);
-            load8(g, p.gamma, (int)at, c);
+            lc_load8(a, h, (int)at, c);
+            lc_load8(b, dy, (int)at, c);
+            lc_load8(g, p.gamma, (int)at, c);
 #pragma unroll
             for (int j = 0; j < 8; ++j) s = fmaf(b.get(j) * g.get(j), a.get(j) * rstd, s);
         }
         const float mean = lc_block_sum<WAVES>(s, red[parity]) / (float)c;
         for (long long at = tid * 8; at < c; at += kSpan) {
-            load8(a, h, (int)at, c);
-            load8(b, dy, (int)at, c);
-            load8(g, p.gamma, (int)at, c);
-            if (dh) load8(t, dh, (int)at, c);
+            lc_load8(a, h, (int)at, c);
+            lc_load8(b, dy, (int)at, c);
+            lc_load8(g, p.gamma, (int)at, c);
+            if (dh) lc_load8(t, dh, (int)at, c);
             float o[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {

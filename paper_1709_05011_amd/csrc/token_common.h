@@ -19,11 +19,11 @@ struct Packed<float> {
         __builtin_memcpy(&a, p, 16);
         __builtin_memcpy(&b, p + 4, 16);
     }
-    __device__ __forceinline__ void load_some(const float* p, int n) {
+    __device__ __forceinline__ void load_some(const float* p, int n, uint32_t fill = 0) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            a[j] = j < n ? __float_as_uint(p[j]) : 0u;
-            b[j] = j + 4 < n ? __float_as_uint(p[j + 4]) : 0u;
+            a[j] = j < n ? __float_as_uint(p[j]) : fill;
+            b[j] = j + 4 < n ? __float_as_uint(p[j + 4]) : fill;
         }
     }
     __device__ __forceinline__ float get(int j) const { return __uint_as_float(j < 4 ? a[j] : b[j - 4]); }
@@ -32,13 +32,20 @@ template <>
 struct Packed<uint16_t> {
     lc_u32x4 a;
     __device__ __forceinline__ void load(const uint16_t* p) { __builtin_memcpy(&a, p, 16); }
-    __device__ __forceinline__ void load_some(const uint16_t* p, int n) {
+    __device__ __forceinline__ void load_some(const uint16_t* p, int n, uint32_t fill = 0) {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-            a[j] = (2 * j < n ? (uint32_t)p[2 * j] : 0u) | (2 * j + 1 < n ? (uint32_t)p[2 * j + 1] << 16 : 0u);
+            a[j] = (2 * j < n ? (uint32_t)p[2 * j] : fill) | (2 * j + 1 < n ? (uint32_t)p[2 * j + 1] : fill) << 16;
     }
     __device__ __forceinline__ float get(int j) const { return __uint_as_float(j & 1 ? a[j >> 1] & 0xffff0000u : a[j >> 1] << 16); }
 };
+
+// Columns col .. col + 7 of a row of c; what lies past its end is `fill` (the type's own bit pattern).
+template <typename T>
+__device__ __forceinline__ void lc_load8(Packed<T>& to, const T* row, int col, int c, uint32_t fill = 0) {
+    if (col + 8 <= c) to.load(row + col);
+    else to.load_some(row + col, c - col, fill);
+}
 
 // Eight results, rounded once.
 __device__ __forceinline__ void lc_store8(float* p, const float* v, int n) {

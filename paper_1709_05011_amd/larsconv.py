@@ -29,6 +29,7 @@ EXPORTS = ["conv2d_out_shape", "conv2d_workspace_bytes", "conv2d_fwd", "conv2d_b
            "global_avgpool_bwd_t", "relu_add_bwd_bnsums_t", "relu_add_bwd_bnsums_grid_t", "batchnorm_bwd_presummed_t",
            "conv2d_fwd_stats_count", "conv2d_fwd_stats", "batchnorm_fwd_pre", "batchnorm_fwd_pair_t",
            "rmsnorm_fwd", "rmsnorm_fwd_q8", "rmsnorm_bwd_workspace_bytes", "rmsnorm_bwd",
+           "token_logprob_workspace_bytes", "token_logprob_fwd", "token_logprob_bwd",
            "lc_status_string", "lc_last_error_detail"]
 
 
@@ -82,6 +83,22 @@ class RmsNormDesc:
 
     def c_struct(self) -> lc_rmsnorm_desc:
         return lc_rmsnorm_desc(self.rows, self.c, self.x_ld, self.residual_ld, self.eps, self.dtype)
+
+
+class lc_token_desc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("vocab", ctypes.c_int), ("ld", ctypes.c_int64), ("dtype", ctypes.c_int), ("top", ctypes.c_int)]
+
+
+@dataclass(frozen=True)
+class TokenDesc:
+    rows: int
+    vocab: int
+    ld: int = 0
+    dtype: int = LC_F32
+    top: int = 0
+
+    def c_struct(self) -> lc_token_desc:
+        return lc_token_desc(self.rows, self.vocab, self.ld, self.dtype, self.top)
 
 
 _lib = None
@@ -189,6 +206,13 @@ def lib() -> ctypes.CDLL:
         L.rmsnorm_bwd_workspace_bytes.argtypes = [rp]
         L.rmsnorm_bwd.restype = i32
         L.rmsnorm_bwd.argtypes = [rp, vp, ctypes.c_int64, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        tp = ctypes.POINTER(lc_token_desc)
+        L.token_logprob_workspace_bytes.restype = sz
+        L.token_logprob_workspace_bytes.argtypes = [tp]
+        L.token_logprob_fwd.restype = i32
+        L.token_logprob_fwd.argtypes = [tp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.token_logprob_bwd.restype = i32
+        L.token_logprob_bwd.argtypes = [tp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_int64, vp]
         L.lc_status_string.restype = ctypes.c_char_p
         L.lc_status_string.argtypes = [i32]
         L.lc_last_error_detail.restype = ctypes.c_char_p
@@ -576,3 +600,21 @@ def rmsnorm_bwd(desc, total, dy, dtotal, gamma, save_rstd, dx, dgamma, workspace
     nb = _nbytes(workspace) if workspace_bytes is None else workspace_bytes
     _check(lib().rmsnorm_bwd(_c(desc), _ptr(total), h_ld, _ptr(dy), _ptr(dtotal), _ptr(gamma), _ptr(save_rstd), _ptr(dx),
                              _ptr(dgamma), _ptr(workspace), nb, _stream(stream)), "rmsnorm_bwd")
+
+
+# ---- log probabilities of given tokens, entropy, likeliest alternatives ----
+
+def token_logprob_workspace_bytes(desc) -> int:
+    return int(lib().token_logprob_workspace_bytes(_c(desc)))
+
+
+def token_logprob_fwd(desc, logits, tokens, logprob, entropy=None, lse=None, top_tokens=None, top_logprobs=None, workspace=None, stream=None,
+                      workspace_bytes: Optional[int] = None) -> None:
+    nb = _nbytes(workspace) if workspace_bytes is None else workspace_bytes
+    _check(lib().token_logprob_fwd(_c(desc), _ptr(logits), _ptr(tokens), _ptr(logprob), _ptr(entropy), _ptr(lse), _ptr(top_tokens),
+                                   _ptr(top_logprobs), _ptr(workspace), nb, _stream(stream)), "token_logprob_fwd")
+
+
+def token_logprob_bwd(desc, logits, tokens, lse, entropy, dlogprob, dentropy, dlogits, dlogits_ld: int = 0, stream=None) -> None:
+    _check(lib().token_logprob_bwd(_c(desc), _ptr(logits), _ptr(tokens), _ptr(lse), _ptr(entropy), _ptr(dlogprob), _ptr(dentropy),
+                                   _ptr(dlogits), dlogits_ld, _stream(stream)), "token_logprob_bwd")

@@ -1,0 +1,195 @@
+"""GPU parity of the token log probabilities (entropy, alternatives, gradient) against oracle/token_ops.py in float64.
+
+Tolerances count roundings of u = 2^-24 (fp32).  An exponential of a distance d carries 3|d| + 4 of them (the distance, its product with log2 e, the
+instruction), weighted sums of them at most 40 more in a block's order, so that log S is off by at most (40 + 4 + 3 E|d|) u, E over p, and E|d| is
+at most log(vocab) + 1 for the distances from the maximum; lse adds one rounding of its own size.  bf16 stores add half a step, 2^-8."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import token_ops as ops
+from paper_1709_05011_amd import larsconv as lc
+from paper_1709_05011_amd import synth
+
+import gpu_util as gu
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+TYPES = {"f32": (lc.LC_F32, torch.float32, 0.0), "bf16": (lc.LC_BF16, torch.bfloat16, 2.0 ** -8)}
+# one token to several slices, odd widths, widths at the edges of a block's registers and of a slice
+SHAPES = [(1, 1), (2, 2), (3, 7), (5, 100), (2, 511), (3, 1000), (2, 2048), (2, 2049), (1, 4097), (2, 8192), (2, 8193), (1, 16391), (3, 50021), (1, 131072),
+          (300, 33)]
+
+
+def tol(vocab):
+    return (48 + 4 * (np.log(vocab) + 2)) * U
+
+
+def f64(t):
+    return t.double().cpu().numpy()
+
+
+def logits_of(rows, vocab, seed, dtype, pad=0, offset=0, masked=0.0, std=3.0):
+    whole = torch.full((rows * (vocab + pad) + offset,), float("nan"), dtype=dtype, device=gu.DEV)
+    view = whole[offset:].view(rows, vocab + pad)[:, :vocab]
+    z = synth.normal((rows, vocab), seed, std=std)
+    if masked:
+        z[np.random.default_rng(seed).random((rows, vocab)) < masked] = -np.inf
+    view.copy_(torch.from_numpy(z))
+    return view, view.double().cpu().numpy()
+
+
+def tokens_of(rows, vocab, seed):
+    t = np.random.default_rng(seed).integers(0, vocab, rows)
+    if rows > 2:
+        t[1], t[2] = -1, vocab                      # two kinds of positions that do not count
+    return t, gu.dev(t.astype(np.int32))
+
+
+def run(dtype, z, tokens, vocab, top=0):
+    rows = z.shape[0]
+    d = lc.TokenDesc(rows, vocab, ld=z.stride(0) if rows > 1 else 0, dtype=dtype, top=top)
+    out = [gu.guarded((rows,), torch.float32) for _ in range(3)]
+    ids = gu.guarded((rows, top), torch.float32) if top else None
+    lps = gu.guarded((rows, top), torch.float32) if top else None
+    lc.token_logprob_fwd(d, z, tokens, out[0][0], out[1][0], out[2][0], ids[0] if top else None, lps[0] if top else None,
+                         gu.workspace(lc.token_logprob_workspace_bytes(d)))
+    torch.cuda.synchronize()
+    for _, check in out + ([ids, lps] if top else []):
+        check()
+    return d, [o for o, _ in out], ids[0].view(torch.int32).cpu().numpy() if top else None, f64(lps[0]) if top else None
+
+
+def close(got, want, bound):
+    fine = np.isfinite(want)
+    return np.array_equal(got[~fine], want[~fine]) and np.all(np.abs(got[fine] - want[fine]) <= np.broadcast_to(bound, want.shape)[fine])
+
+
+def check_forward(vocab, got, want, top):
+    (lp, ent, lse), ids, lps = [f64(x) for x in got[1]], got[2], got[3]
+    wlp, went, wlse, wids, wlps = want
+    e = tol(vocab)
+    assert close(lp, wlp, e + 3 * U * np.abs(wlp))
+    assert close(lse, wlse, e + U * np.abs(wlse))
+    assert close(ent, went, 2 * e + 4 * U * went + e * went)
+    if top:
+        assert np.array_equal(ids, wids)
+        assert close(lps, wlps, e + 3 * U * np.abs(wlps))
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,vocab", SHAPES)
+@pytest.mark.parametrize("top", [0, 1, 5, 32])
+@pytest.mark.parametrize("pad,offset,masked", [(0, 0, 0.0), (5, 1, 0.4)])
+def test_forward(kind, rows, vocab, top, pad, offset, masked):
+    dtype, t, _ = TYPES[kind]
+    z, z64 = logits_of(rows, vocab, 1, t, pad, offset, masked)
+    t64, tokens = tokens_of(rows, vocab, 2)
+    got = run(dtype, z, tokens, vocab, top)
+    check_forward(vocab, got, ops.token_logprob(z64, t64, top), top)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab", [40, 700, 5000, 30000])
+@pytest.mark.parametrize("case", ["equal", "falling", "rising", "two_values", "one_lane", "all_masked", "one_left", "lowest", "large"])
+def test_alternatives_of_unusual_rows(kind, vocab, case):
+    """Equal values (more than there is room for), orders that put the largest into one lane or slice, masks that leave nothing or one, the
+    type's lowest value in place of a mask, logits far from zero."""
+    dtype, t, _ = TYPES[kind]
+    rows, top = 2, 20
+    place = np.arange(vocab, dtype=np.float64)
+    z = {"equal": np.full(vocab, 1.5), "falling": -place / 64, "rising": place / 64, "two_values": np.where(place % 3 == 1, 2.0, -1.0),
+         "one_lane": np.where(place % 2048 < 8, 5 + place / 4096, -place / 4096), "all_masked": np.full(vocab, -np.inf),
+         "one_left": np.where(place == vocab - 2, -7.0, -np.inf), "lowest": np.where(place % 5 == 0, place / 512, float(torch.finfo(t).min)),
+         "large": 3e4 + place % 17}[case]
+    z = torch.from_numpy(np.stack([z, z[::-1]])).to(t).to(gu.DEV).contiguous()
+    t64, tokens = np.array([0, vocab - 1]), gu.dev(np.array([0, vocab - 1], np.int32))
+    got = run(dtype, z, tokens, vocab, top)
+    check_forward(vocab, got, ops.token_logprob(f64(z), t64, top), top)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab", [50, 20000])
+def test_nan_and_infinity_stay_in_their_rows(kind, vocab):
+    dtype, t, _ = TYPES[kind]
+    z, _ = logits_of(4, vocab, 3, t)
+    z[1, vocab // 2] = float("nan")
+    z[2, 3] = float("inf")
+    tokens = gu.dev(np.array([1, 2, 4, 5], np.int32))
+    d, (lp, ent, lse), ids, lps = run(dtype, z, tokens, vocab, 3)
+    for x in (lp, ent, lse):
+        assert x[[1, 2]].isnan().all() and x[[0, 3]].isfinite().all()
+    assert ids[2, 0] == 3 and vocab // 2 not in ids[1] and np.isnan(lps[[1, 2]]).all() and np.isfinite(lps[[0, 3]]).all()
+    dz, one = torch.empty_like(z), torch.ones(4, device=gu.DEV)
+    lc.token_logprob_bwd(d, z, tokens, lse, ent, one, one, dz)
+    torch.cuda.synchronize()
+    assert dz[[1, 2]].isnan().all() and dz[[0, 3]].isfinite().all()
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,vocab", SHAPES)
+@pytest.mark.parametrize("parts", ["both", "logprob", "entropy"])
+def test_backward(kind, rows, vocab, parts):
+    dtype, t, half = TYPES[kind]
+    pad = vocab % 4
+    z, z64 = logits_of(rows, vocab, 4, t, pad, pad, 0.2 if vocab > 50 else 0.0)
+    t64, tokens = tokens_of(rows, vocab, 5)
+    d, (lp, ent, lse), _, _ = run(dtype, z, tokens, vocab)
+    a64, b64 = np.float32([0.5 + i % 3 for i in range(rows)]), np.float32([-0.25 * (1 + i % 2) for i in range(rows)])
+    a64, b64 = (a64 if parts != "entropy" else 0 * a64), (b64 if parts != "logprob" else 0 * b64)
+    whole, check = gu.guarded((rows, vocab + 3), t, offset=2 * pad * (2 if kind == "f32" else 1))
+    before = whole.clone()
+    lc.token_logprob_bwd(d, z, tokens, lse, ent if parts != "logprob" else None, gu.dev(a64) if parts != "entropy" else None,
+                         gu.dev(b64) if parts != "logprob" else None, whole, dlogits_ld=vocab + 3)
+    torch.cuda.synchronize()
+    check()
+    dz = f64(whole[:, :vocab])
+    assert whole[:, vocab:].isnan().all() and before.isnan().all()           # the pad is not written
+    want = ops.token_logprob_bwd(z64, t64, a64.astype(np.float64), b64.astype(np.float64))
+    _, e64, l64, _, _ = ops.token_logprob(z64, t64)
+    d64 = np.where(np.isfinite(z64), np.abs(z64 - l64[:, None]), 0.0)
+    p = np.where(np.isfinite(z64), np.exp(-d64), 0.0)
+    size = p * (np.abs(a64)[:, None] + np.abs(b64)[:, None] * (d64 + e64[:, None]))
+    # p by the rounding of lse, of the distance and of the exponential; the entropy's and the token's own term besides
+    bound = size * (tol(vocab) + U * (np.abs(l64)[:, None] + 3 * d64 + 8)) + p * np.abs(b64)[:, None] * (2 * tol(vocab) + 5 * U * e64[:, None]
+            + tol(vocab) * e64[:, None] + U * np.abs(l64)[:, None]) + U * np.abs(a64)[:, None]
+    assert np.all(np.abs(dz - want) <= half * (1 + half) * np.abs(want) + (1 + half) * bound)
+
+
+def test_the_gradient_against_differences():
+    """Central differences of the float64 sum over the kernel's own forward outputs, fp32: a step of 2^-6 keeps its rounding under 1e-3."""
+    z = synth.normal((2, 50), 6)
+    tokens, a, b = gu.dev(np.array([7, 49], np.int32)), np.float32([1.0, -0.5]), np.float32([0.5, 2.0])
+    forward = lambda y: sum(float(np.dot(f64(o), c)) for o, c in zip(run(lc.LC_F32, gu.dev(y), tokens, 50)[1][:2], (a, b)))
+    d, (lp, ent, lse), _, _ = run(lc.LC_F32, gu.dev(z), tokens, 50)
+    dz = torch.empty((2, 50), device=gu.DEV)
+    lc.token_logprob_bwd(d, gu.dev(z), tokens, lse, ent, gu.dev(a), gu.dev(b), dz)
+    got = f64(dz)
+    for i, j in [(0, 7), (0, 0), (1, 49), (1, 20)]:
+        up, down = z.copy(), z.copy()
+        up[i, j] += np.float32(2.0 ** -6)
+        down[i, j] -= np.float32(2.0 ** -6)
+        numeric = (forward(up) - forward(down)) / float(up[i, j].astype(np.float64) - down[i, j].astype(np.float64))
+        assert abs(numeric - got[i, j]) < 1e-3
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_gradient_in_the_logits_own_buffer_on_another_stream(kind):
+    dtype, t, _ = TYPES[kind]
+    rows, vocab = 40, 1001
+    z, _ = logits_of(rows, vocab, 7, t)
+    _, tokens = tokens_of(rows, vocab, 8)
+    d, (lp, ent, lse), _, _ = run(dtype, z, tokens, vocab)
+    one, dz, side = torch.ones(rows, device=gu.DEV), torch.empty_like(z), torch.cuda.Stream()
+    lc.token_logprob_bwd(d, z, tokens, lse, ent, one, one, dz)
+    torch.cuda.synchronize()
+    lc.token_logprob_bwd(d, z, tokens, lse, ent, one, one, z, stream=side)
+    torch.cuda.synchronize()
+    assert torch.equal(z, dz)
+
+
+def test_many_rows_of_one_element_and_bit_identical_reruns():
+    z, _ = logits_of(3000, 9000, 9, torch.bfloat16)
+    _, tokens = tokens_of(3000, 9000, 10)
+    first, again = run(lc.LC_BF16, z, tokens, 9000, 8), run(lc.LC_BF16, z, tokens, 9000, 8)
+    assert all(torch.equal(x, y) for x, y in zip(first[1], again[1])) and np.array_equal(first[2], again[2]) and np.array_equal(first[3], again[3])

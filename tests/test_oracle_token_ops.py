@@ -48,3 +48,32 @@ def test_rmsnorm_gradient_against_differences_and_autograd():
     ty = th * torch.rsqrt((th * th).mean(1, keepdim=True) + 1e-3) * tg
     ((ty * torch.tensor(dy)).sum() + (th * torch.tensor(dt)).sum()).backward()
     assert np.allclose(tx.grad.numpy(), dx, atol=1e-12) and np.allclose(tg.grad.numpy(), dg, atol=1e-12)
+
+
+def test_token_logprob_by_hand():
+    z = np.log(np.array([[1.0, 2.0, 4.0, 1.0]]))
+    lp, ent, lse, ids, top = ops.token_logprob(z, np.array([2]), 3)
+    p = np.array([1, 2, 4, 1]) / 8
+    assert np.allclose(lp, np.log(0.5)) and np.allclose(lse, np.log(8)) and np.allclose(ent, -np.sum(p * np.log(p)))
+    assert np.array_equal(ids, [[2, 1, 0]]) and np.allclose(top, np.log(p[[2, 1, 0]]))
+    lp, ent, lse, ids, top = ops.token_logprob(np.array([[0.0, -np.inf], [-np.inf, -np.inf]]), np.array([1, -1]), 2)
+    assert lp[0] == -np.inf and ent[0] == 0 and lse[0] == 0 and np.array_equal(ids, [[0, -1], [-1, -1]])
+    assert lp[1] == 0 and ent[1] == 0 and lse[1] == -np.inf
+    assert not ops.token_logprob_bwd(np.array([[-np.inf] * 2]), np.array([0]), np.ones(1), np.ones(1)).any()
+
+
+def test_token_logprob_gradient_against_differences_and_autograd():
+    rng = np.random.default_rng(2)
+    z, t, a, b = rng.normal(size=(4, 9)), np.array([0, 8, -1, 9]), rng.normal(size=4), rng.normal(size=4)
+    f = lambda z: float(np.dot(a, ops.token_logprob(z, t)[0]) + np.dot(b, ops.token_logprob(z, t)[1]))
+    dz, e = ops.token_logprob_bwd(z, t, a, b), 1e-6
+    for i in range(4):
+        for j in range(9):
+            d = np.zeros_like(z)
+            d[i, j] = e
+            assert abs((f(z + d) - f(z - d)) / (2 * e) - dz[i, j]) < 1e-8
+    tz = torch.tensor(z, requires_grad=True)
+    logp = torch.log_softmax(tz, 1)
+    loss = a[0] * logp[0, 0] + a[1] * logp[1, 8] - (torch.tensor(b) * (logp.exp() * logp).sum(1)).sum()
+    loss.backward()
+    assert np.allclose(tz.grad.numpy(), dz, atol=1e-12)
