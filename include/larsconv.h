@@ -422,6 +422,35 @@ lc_status token_logprob_fwd(const lc_token_desc* desc, const void* logits, const
 lc_status token_logprob_bwd(const lc_token_desc* desc, const void* logits, const int32_t* tokens, const float* lse, const float* entropy,
                             const float* dlogprob, const float* dentropy, void* dlogits, int64_t dlogits_ld, void* hip_stream);
 
+/* One AdamW step over a list of parameter tensors (decoupled weight decay).  For every element, with t = step (1 for the first):
+ *     g' = grad_scale * g,   m <- beta1 m + (1 - beta1) g',   v <- beta2 v + (1 - beta2) g'^2,
+ *     w <- w - lr * decay * w - lr * (m / (1 - beta1^t)) / (sqrt(v) / sqrt(1 - beta2^t) + eps).
+ * w, m, v: HOST arrays of n_tensors DEVICE pointers to fp32 data, updated in place; g: pointers to gradients of type g_dtype, read only; numel: HOST
+ * array of element counts (0 allowed).  weight_decay_per_tensor: HOST array replacing the scalar, or NULL.  grad_scale: DEVICE, one float (a clip
+ * factor, the inverse of a loss scale or token count), or NULL for 1.  w_lowp_out: as lars_step.  Alignment: one element.  Each product and each sum of m and v
+ * is rounded by itself (no fused multiply-add), so that any fp32 program gets their bits.  The betas are double because 1 - beta is what matters: in
+ * [0, 1); eps > 0; step >= 1 -- LC_ERR_UNSUPPORTED otherwise.  n_tensors = 0 is a no-op.  No workspace; results do not depend on the other
+ * tensors of the list.  Host arrays are read during the call and travel as launch arguments, lr and step with them: a captured graph
+ * replays the step of the capture. */
+lc_status adamw_step(int n_tensors, float* const* w, const void* const* g, lc_dtype g_dtype, float* const* m, float* const* v,
+                     const int64_t* numel, float lr, double beta1, double beta2, float eps, float weight_decay, int64_t step,
+                     const float* weight_decay_per_tensor, const float* grad_scale, void* const* w_lowp_out, void* hip_stream);
+
+/* The same with the states in 8 bits, a scale for every ADAMW_Q8_BLOCK consecutive elements of a tensor (the last block may be shorter):
+ * m as e4m3 (largest 448) rounded to nearest even, v as e5m2 (5 exponent bits, 2 mantissa bits, largest 57344).  The scales are powers of two, the
+ * smallest (at least 2^-126) that keep a block's largest magnitude in range, 1 for a block of zeros, so that scaling rounds nothing; the update uses the
+ * new m and v before they are rounded.  beta2 near 1 moves v by less per step than half of e5m2's distance, and to nearest it would stay where it
+ * is for good; v is rounded up or down with the probabilities that keep its mean, by 21 bits made from the element's number in its tensor and `seed` (a
+ * pure function of both: pass another seed every step, the step's number for instance).  What is above zero is never rounded to zero, where the root in the denominator
+ * would vanish.  A NaN or infinity becomes the code of NaN (0x7f, or 0xff for a negative m) and takes no part in its block's scale.
+ * m, v: HOST arrays of DEVICE pointers to numel bytes (any alignment); m_scale, v_scale: to ceil(numel / ADAMW_Q8_BLOCK) floats.  States start as zero
+ * bytes with any finite scales. */
+#define ADAMW_Q8_BLOCK 256
+lc_status adamw_step_q8(int n_tensors, float* const* w, const void* const* g, lc_dtype g_dtype, uint8_t* const* m, float* const* m_scale,
+                        uint8_t* const* v, float* const* v_scale, const int64_t* numel, float lr, double beta1, double beta2, float eps,
+                        float weight_decay, int64_t step, uint32_t seed, const float* weight_decay_per_tensor, const float* grad_scale,
+                        void* const* w_lowp_out, void* hip_stream);
+
 /* Static, human-readable name of a status code. */
 const char* lc_status_string(lc_status status);
 

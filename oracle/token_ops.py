@@ -121,3 +121,35 @@ def token_logprob_bwd(z, tokens, dlogprob, dentropy):
     a = np.where(counts, dlogprob, 0.0)[:, None]
     dz = a * (hot - p) - dentropy[:, None] * p * (np.where(p > 0, logp, 0.0) + entropy[:, None])
     return np.where(empty[:, None], 0.0, dz)
+
+
+# ---- AdamW ----
+
+def adamw(w, g, m, v, lr, beta1, beta2, eps, decay, step, scale=1.0):
+    """(w, m, v) after one step, float64."""
+    w, g, m, v = (np.asarray(a, np.float64) for a in (w, g, m, v))
+    g = g * scale
+    m = beta1 * m + (1 - beta1) * g
+    v = beta2 * v + (1 - beta2) * g * g
+    update = (m / (1 - beta1 ** step)) / (np.sqrt(v / (1 - beta2 ** step)) + eps)
+    return w - lr * decay * w - lr * update, m, v
+
+
+def adam_states_as_rounded(g, m, v, beta1, beta2, scale=1.0):
+    """m and v with every product and sum rounded to fp32 by itself, as the step defines them."""
+    f = np.float32
+    g, m, v = (np.asarray(a, f) for a in (g, m, v))
+    x = g * f(scale)
+    return f(beta1) * m + f(1 - beta1) * x, f(beta2) * v + f(1 - beta2) * (x * x)
+
+
+def states_in_8_bits(m, v, seed, block=256):
+    """((values of m's codes, scales), (values of v's codes, scales)) of one tensor."""
+    m, v = np.asarray(m, np.float64), np.asarray(v, np.float64)
+    out = []
+    bits = dither21(np.arange(m.size), seed)
+    for x, most, code in ((m, 448.0, lambda x, b: e4m3(x)), (v, 57344.0, e5m2_dithered)):
+        scales = np.array([power_scale(np.max(np.abs(x[i:i + block])), most) for i in range(0, x.size, block)])
+        wide = np.repeat(scales, block)[:x.size]
+        out.append((code(x / wide, bits), scales))
+    return out

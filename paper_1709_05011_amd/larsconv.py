@@ -30,6 +30,7 @@ EXPORTS = ["conv2d_out_shape", "conv2d_workspace_bytes", "conv2d_fwd", "conv2d_b
            "conv2d_fwd_stats_count", "conv2d_fwd_stats", "batchnorm_fwd_pre", "batchnorm_fwd_pair_t",
            "rmsnorm_fwd", "rmsnorm_fwd_q8", "rmsnorm_bwd_workspace_bytes", "rmsnorm_bwd",
            "token_logprob_workspace_bytes", "token_logprob_fwd", "token_logprob_bwd",
+           "adamw_step", "adamw_step_q8",
            "lc_status_string", "lc_last_error_detail"]
 
 
@@ -213,6 +214,11 @@ def lib() -> ctypes.CDLL:
         L.token_logprob_fwd.argtypes = [tp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.token_logprob_bwd.restype = i32
         L.token_logprob_bwd.argtypes = [tp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_int64, vp]
+        f32, f64, i64 = ctypes.c_float, ctypes.c_double, ctypes.c_int64
+        L.adamw_step.restype = i32
+        L.adamw_step.argtypes = [i32, vp, vp, i32, vp, vp, vp, f32, f64, f64, f32, f32, i64, vp, vp, vp, vp]
+        L.adamw_step_q8.restype = i32
+        L.adamw_step_q8.argtypes = [i32, vp, vp, i32, vp, vp, vp, vp, vp, f32, f64, f64, f32, f32, i64, ctypes.c_uint32, vp, vp, vp, vp]
         L.lc_status_string.restype = ctypes.c_char_p
         L.lc_status_string.argtypes = [i32]
         L.lc_last_error_detail.restype = ctypes.c_char_p
@@ -618,3 +624,53 @@ def token_logprob_fwd(desc, logits, tokens, logprob, entropy=None, lse=None, top
 def token_logprob_bwd(desc, logits, tokens, lse, entropy, dlogprob, dentropy, dlogits, dlogits_ld: int = 0, stream=None) -> None:
     _check(lib().token_logprob_bwd(_c(desc), _ptr(logits), _ptr(tokens), _ptr(lse), _ptr(entropy), _ptr(dlogprob), _ptr(dentropy),
                                    _ptr(dlogits), dlogits_ld, _stream(stream)), "token_logprob_bwd")
+
+
+# ---- AdamW over a list of tensors ----
+
+ADAMW_Q8_BLOCK = 256
+
+
+class AdamWArgs:
+    """Host-side pointer and size arrays of one parameter list (fp32 states), marshalled once and reusable."""
+
+    def __init__(self, w: Sequence, g: Sequence, m: Sequence, v: Sequence, numel: Optional[Sequence[int]] = None,
+                 w_lowp: Optional[Sequence] = None, g_dtype: int = LC_F32):
+        if numel is None:
+            numel = [t.numel() for t in w]
+        self.n, self.numel, self.g_dtype = len(w), list(numel), g_dtype
+        self.w, self.g, self.m, self.v = _ptr_array(w), _ptr_array(g), _ptr_array(m), _ptr_array(v)
+        self.numel_arr = _i64_array(self.numel)
+        self.w_lowp = _ptr_array(w_lowp) if w_lowp is not None else None
+        self._keep = [list(a) for a in (w, g, m, v, w_lowp or [])]
+
+
+class AdamWQ8Args(AdamWArgs):
+    """The same with the states in 8 bits (bytes) and a scale for every ADAMW_Q8_BLOCK elements."""
+
+    def __init__(self, w: Sequence, g: Sequence, m: Sequence, m_scale: Sequence, v: Sequence, v_scale: Sequence,
+                 numel: Optional[Sequence[int]] = None, w_lowp: Optional[Sequence] = None, g_dtype: int = LC_F32):
+        super().__init__(w, g, m, v, numel, w_lowp, g_dtype)
+        self.m_scale, self.v_scale = _ptr_array(m_scale), _ptr_array(v_scale)
+        self._keep += [list(m_scale), list(v_scale)]
+
+
+def _decays(args: AdamWArgs, weight_decay_per_tensor):
+    if weight_decay_per_tensor is None:
+        return None
+    if len(weight_decay_per_tensor) != args.n:
+        raise ValueError("per-tensor array of the wrong length")
+    return (ctypes.c_float * max(args.n, 1))(*[float(x) for x in weight_decay_per_tensor])
+
+
+def adamw_step(args: AdamWArgs, lr: float, beta1: float, beta2: float, eps: float, weight_decay: float, step: int,
+               weight_decay_per_tensor=None, grad_scale=None, stream=None) -> None:
+    _check(lib().adamw_step(args.n, args.w, args.g, args.g_dtype, args.m, args.v, args.numel_arr, lr, beta1, beta2, eps, weight_decay, step,
+                            _decays(args, weight_decay_per_tensor), _ptr(grad_scale), args.w_lowp, _stream(stream)), "adamw_step")
+
+
+def adamw_step_q8(args: AdamWQ8Args, lr: float, beta1: float, beta2: float, eps: float, weight_decay: float, step: int, seed: int,
+                  weight_decay_per_tensor=None, grad_scale=None, stream=None) -> None:
+    _check(lib().adamw_step_q8(args.n, args.w, args.g, args.g_dtype, args.m, args.m_scale, args.v, args.v_scale, args.numel_arr, lr, beta1, beta2,
+                               eps, weight_decay, step, seed & 0xFFFFFFFF, _decays(args, weight_decay_per_tensor), _ptr(grad_scale), args.w_lowp,
+                               _stream(stream)), "adamw_step_q8")

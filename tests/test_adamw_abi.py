@@ -1,0 +1,63 @@
+"""AdamW entry points on a machine without a GPU: every refusal comes before any launch."""
+import pytest
+
+from paper_1709_05011_amd import larsconv as lc
+
+FAKE = 0x10000000  # never dereferenced: every call below fails validation first, or has no work
+
+
+def args(q8=False, g_dtype=lc.LC_F32, numel=(100, 5000), lowp=None, **swap):
+    a = {k: [FAKE, FAKE] for k in ("w", "g", "m", "v", "m_scale", "v_scale")} | swap
+    if q8:
+        return lc.AdamWQ8Args(a["w"], a["g"], a["m"], a["m_scale"], a["v"], a["v_scale"], list(numel), lowp, g_dtype)
+    return lc.AdamWArgs(a["w"], a["g"], a["m"], a["v"], list(numel), lowp, g_dtype)
+
+
+def status(a, q8=False, beta1=0.9, beta2=0.99, eps=1e-8, step=1, grad_scale=None):
+    with pytest.raises(lc.LarsConvError) as e:
+        if q8:
+            lc.adamw_step_q8(a, 1e-3, beta1, beta2, eps, 0.1, step, 7, grad_scale=grad_scale, stream=0)
+        else:
+            lc.adamw_step(a, 1e-3, beta1, beta2, eps, 0.1, step, grad_scale=grad_scale, stream=0)
+    return e.value.status
+
+
+@pytest.mark.parametrize("q8", [False, True])
+def test_refusals(q8):
+    a = args(q8)
+    for bad in (dict(beta1=1.0), dict(beta1=-0.1), dict(beta2=1.0), dict(beta2=float("nan")), dict(eps=0.0), dict(eps=-1e-8), dict(step=0), dict(step=-3)):
+        assert status(a, q8, **bad) == lc.LC_ERR_UNSUPPORTED, bad
+    assert status(args(q8, g_dtype=5), q8) == lc.LC_ERR_UNSUPPORTED
+    assert status(args(q8, numel=(100, -1)), q8) == lc.LC_ERR_SHAPE
+    assert status(args(q8, numel=(100, (1 << 40) + 1)), q8) == lc.LC_ERR_SHAPE
+    assert status(a, q8, grad_scale=FAKE + 2) == lc.LC_ERR_ALIGN
+    for name in ("w", "g", "m", "v") + (("m_scale", "v_scale") if q8 else ()):
+        assert status(args(q8, **{name: [FAKE, None]}), q8) == lc.LC_ERR_NULL, name
+        if not (q8 and name in ("m", "v")):
+            assert status(args(q8, **{name: [FAKE, FAKE + 2]}), q8) == lc.LC_ERR_ALIGN, name
+    assert status(args(q8, g_dtype=lc.LC_BF16, g=[FAKE, FAKE + 1]), q8) == lc.LC_ERR_ALIGN
+    assert status(args(q8, lowp=[None, FAKE + 1]), q8) == lc.LC_ERR_ALIGN
+
+
+def test_lists_of_the_abi():
+    L = lc.lib()
+    a = args()
+    assert L.adamw_step(-1, a.w, a.g, 0, a.m, a.v, a.numel_arr, 0.1, 0.9, 0.9, 1e-8, 0.0, 1, None, None, None, None) == lc.LC_ERR_SHAPE
+    for i in (1, 2, 4, 5, 6):
+        call = [2, a.w, a.g, 0, a.m, a.v, a.numel_arr, 0.1, 0.9, 0.9, 1e-8, 0.0, 1, None, None, None, None]
+        call[i] = None
+        assert L.adamw_step(*call) == lc.LC_ERR_NULL
+    b = args(True)
+    for i in (4, 5, 6, 7):
+        call = [2, b.w, b.g, 0, b.m, b.m_scale, b.v, b.v_scale, b.numel_arr, 0.1, 0.9, 0.9, 1e-8, 0.0, 1, 3, None, None, None, None]
+        call[i] = None
+        assert L.adamw_step_q8(*call) == lc.LC_ERR_NULL
+    with pytest.raises(ValueError):
+        lc.adamw_step(a, 0.1, 0.9, 0.9, 1e-8, 0.0, 1, weight_decay_per_tensor=[0.1], stream=0)
+
+
+def test_nothing_to_do():
+    lc.adamw_step(lc.AdamWArgs([], [], [], []), 0.1, 0.9, 0.9, 1e-8, 0.0, 1, stream=0)
+    lc.adamw_step_q8(lc.AdamWQ8Args([], [], [], [], [], []), 0.1, 0.9, 0.9, 1e-8, 0.0, 1, 1, stream=0)
+    none = [None, None]
+    lc.adamw_step(lc.AdamWArgs(none, none, none, none, [0, 0]), 0.1, 0.9, 0.9, 1e-8, 0.0, 1, stream=0)

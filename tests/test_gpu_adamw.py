@@ -1,0 +1,181 @@
+"""GPU parity of the AdamW step against oracle/token_ops.py.  m and v are defined to the bit in fp32 and compared so, and the 8-bit states made from
+them exactly; w is compared with the float64 rule: the new value takes three sums and a product of its own (4 u = 4 * 2^-24 relative to the largest of
+them) and the update 12 u of its size (root, products, quotient, the rounded coefficients, m and v: three roundings of terms of one sign or, in m,
+of the sizes of its two terms)."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import token_ops as ops
+from paper_1709_05011_amd import larsconv as lc
+from paper_1709_05011_amd import synth
+
+import gpu_util as gu
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+SIZES = [1, 3, 4, 5, 0, 255, 256, 257, 1023, 1024, 1025, 2048 + 77, 0, 70001]
+LR, B1, B2, EPS, DECAY = 3e-3, 0.9, 0.999, 1e-8, 0.1
+f32 = lambda x: float(np.float32(x))
+
+
+def put(a, dtype, offset):
+    buf = torch.empty(a.size + offset, dtype=dtype, device=gu.DEV)
+    buf[offset:].copy_(torch.from_numpy(a))
+    return buf[offset:]
+
+
+def lists(sizes, seed, g_type, offset):
+    w = [synth.normal((n,), seed + 4 * i, std=0.05) for i, n in enumerate(sizes)]
+    g = [synth.normal((n,), seed + 4 * i + 1, std=10.0 ** -(i % 5)) for i, n in enumerate(sizes)]
+    m = [synth.normal((n,), seed + 4 * i + 2, std=0.1 * 10.0 ** -(i % 5)) for i, n in enumerate(sizes)]
+    v = [synth.normal((n,), seed + 4 * i + 3, std=0.1 * 10.0 ** -(i % 5)) ** 2 for i, n in enumerate(sizes)]
+    dg = [put(a, g_type, offset) for a in g]
+    return w, [t.float().cpu().numpy() for t in dg], m, v, [put(a, torch.float32, offset) for a in w], dg
+
+
+def check_w(got, w, g, m, v, decay, step, scale):
+    want, _, _ = ops.adamw(w, g, m, v, f32(LR), B1, B2, f32(EPS), f32(decay), step, scale)
+    _, m1, v1 = ops.adamw(w, g, np.abs(m), v, 0, B1, B2, EPS, 0, step, scale)
+    m1 = B1 * np.abs(m) + (1 - B1) * np.abs(np.float64(g) * scale)
+    update = LR * (m1 / (1 - B1 ** step)) / (np.sqrt(v1 / (1 - B2 ** step)) + EPS)
+    assert np.all(np.abs(got - want) <= U * (4 * np.abs(w) + 4 * np.abs(want)) + 16 * U * update)
+
+
+@pytest.mark.parametrize("g_type", ["f32", "bf16"])
+@pytest.mark.parametrize("offset", [0, 1])
+@pytest.mark.parametrize("scaled,lowp,step", [(False, False, 1), (True, True, 1000)])
+def test_fp32_states(g_type, offset, scaled, lowp, step):
+    t = torch.bfloat16 if g_type == "bf16" else torch.float32
+    w, g, m, v, dw, dg = lists(SIZES, 100, t, offset)
+    dm, dv = [put(a, torch.float32, offset) for a in m], [put(a, torch.float32, offset) for a in v]
+    lp = [torch.zeros(n, dtype=torch.bfloat16, device=gu.DEV) if i % 3 else None for i, n in enumerate(SIZES)] if lowp else None
+    decays = [0.01 * i for i in range(len(SIZES))]
+    scale = 0.3125 if scaled else 1.0
+    args = lc.AdamWArgs(dw, dg, dm, dv, SIZES, lp, lc.LC_BF16 if g_type == "bf16" else lc.LC_F32)
+    lc.adamw_step(args, LR, B1, B2, EPS, DECAY, step, weight_decay_per_tensor=decays, grad_scale=torch.full((1,), scale, device=gu.DEV) if scaled else None)
+    torch.cuda.synchronize()
+    for i in range(len(SIZES)):
+        wm, wv = ops.adam_states_as_rounded(g[i], m[i], v[i], B1, B2, scale)
+        assert np.array_equal(dm[i].cpu().numpy(), wm) and np.array_equal(dv[i].cpu().numpy(), wv), i
+        check_w(dw[i].double().cpu().numpy(), w[i], g[i], m[i], v[i], decays[i], step, scale)
+        if lowp and lp[i] is not None:
+            assert torch.equal(lp[i], dw[i].bfloat16())
+
+
+def in_8_bits(m, v, seed):
+    (qm, sm), (qv, sv) = ops.states_in_8_bits(m, v, seed) if m.size else ((m, m), (v, v))
+    return [torch.from_numpy(np.ascontiguousarray(q)).to(gu.DEV).to(t).view(torch.uint8) for q, t in ((qm, torch.float8_e4m3fn), (qv, torch.float8_e5m2))] + \
+        [gu.dev(np.float32(sm)), gu.dev(np.float32(sv))]
+
+
+def values(codes, t, scales):
+    return codes.view(t).float().cpu().numpy() * np.repeat(scales.cpu().numpy(), 256)[:codes.numel()]
+
+
+@pytest.mark.parametrize("g_type", ["f32", "bf16"])
+@pytest.mark.parametrize("offset", [0, 1])
+@pytest.mark.parametrize("scaled,lowp,step", [(False, False, 1), (True, True, 1000)])
+def test_8_bit_states(g_type, offset, scaled, lowp, step):
+    t = torch.bfloat16 if g_type == "bf16" else torch.float32
+    w, g, m, v, dw, dg = lists(SIZES, 500, t, offset)
+    start = [in_8_bits(a, b, 3) for a, b in zip(m, v)]
+    m = [values(s[0], torch.float8_e4m3fn, s[2]) for s in start]              # what the states stand for
+    v = [values(s[1], torch.float8_e5m2, s[3]) for s in start]
+    guard = [[gu.guarded((x.numel(),), torch.float8_e5m2 if x.dtype == torch.uint8 else x.dtype, offset=offset * x.element_size()) for x in s] for s in start]
+    for s, gs in zip(start, guard):
+        for x, (room, _) in zip(s, gs):
+            room.view(x.dtype).copy_(x)
+    dm, dv, sm, sv = ([gs[k][0].view(torch.uint8) if k < 2 else gs[k][0] for gs in guard] for k in range(4))
+    lp = [torch.zeros(n, dtype=torch.bfloat16, device=gu.DEV) if i % 3 else None for i, n in enumerate(SIZES)] if lowp else None
+    scale, seed = (0.3125 if scaled else 1.0), 0xFFFFFFF0 + step % 7
+    args = lc.AdamWQ8Args(dw, dg, dm, sm, dv, sv, SIZES, lp, lc.LC_BF16 if g_type == "bf16" else lc.LC_F32)
+    lc.adamw_step_q8(args, LR, B1, B2, EPS, DECAY, step, seed, grad_scale=torch.full((1,), scale, device=gu.DEV) if scaled else None)
+    torch.cuda.synchronize()
+    for i, n in enumerate(SIZES):
+        for _, check in guard[i]:
+            check()
+        if n == 0:
+            continue
+        (qm, wsm), (qv, wsv) = ops.states_in_8_bits(*ops.adam_states_as_rounded(g[i], m[i], v[i], B1, B2, scale), seed)
+        assert np.array_equal(sm[i].cpu().numpy(), wsm) and np.array_equal(sv[i].cpu().numpy(), wsv), i
+        assert np.array_equal(dm[i].view(torch.float8_e4m3fn).double().cpu().numpy(), qm), i
+        assert np.array_equal(dv[i].view(torch.float8_e5m2).double().cpu().numpy(), qv), i
+        check_w(dw[i].double().cpu().numpy(), w[i], g[i], m[i], v[i], DECAY, step, scale)
+        if lowp and lp[i] is not None:
+            assert torch.equal(lp[i], dw[i].bfloat16())
+
+
+@pytest.mark.parametrize("q8", [False, True])
+def test_long_lists_with_empty_tensors(q8):
+    """More tensors than one launch describes; each comes out as it does alone."""
+    sizes = [(7 * i) % 613 if i % 5 else 0 for i in range(500)]
+    got = []
+    for alone in (False, True):
+        w, g, m, v, dw, dg = lists(sizes, 900, torch.float32, 0)
+        dm, dv = ([torch.zeros(n, dtype=torch.uint8 if q8 else torch.float32, device=gu.DEV) for n in sizes] for _ in range(2))
+        sm, sv = ([torch.ones(-(-n // 256), device=gu.DEV) for n in sizes] for _ in range(2))
+        for at in ([[i] for i in range(len(sizes))] if alone else [range(len(sizes))]):
+            pick = lambda a: [a[i] for i in at]
+            if q8:
+                lc.adamw_step_q8(lc.AdamWQ8Args(pick(dw), pick(dg), pick(dm), pick(sm), pick(dv), pick(sv)), LR, B1, B2, EPS, DECAY, 1, 5)
+            else:
+                lc.adamw_step(lc.AdamWArgs(pick(dw), pick(dg), pick(dm), pick(dv)), LR, B1, B2, EPS, DECAY, 1)
+        torch.cuda.synchronize()
+        got.append([torch.cat(a) for a in (dw, dm, dv, sm, sv)])
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+    assert not torch.equal(got[0][0], torch.from_numpy(np.concatenate(w)).to(gu.DEV))
+
+
+def test_nothing_moves_but_the_decay_where_gradient_and_states_are_zero():
+    w = gu.dev(synth.normal((700,), 1))
+    before, z8, ones = w.clone(), torch.zeros(700, dtype=torch.uint8, device=gu.DEV), torch.full((3,), 7.0, device=gu.DEV)
+    lc.adamw_step_q8(lc.AdamWQ8Args([w], [torch.zeros(700, device=gu.DEV)], [z8.clone()], [ones.clone()], [z8.clone()], [ones]), LR, B1, B2, EPS, DECAY, 1, 1)
+    torch.cuda.synchronize()
+    assert torch.equal(w, before - np.float32(f32(LR) * f32(DECAY)) * before) and bool((ones == 1).all())
+
+
+def test_nan_and_infinity_in_a_gradient_stay_with_their_elements():
+    n = 1000
+    g = synth.normal((n,), 2)
+    g[300], g[301], g[302] = np.nan, np.inf, -np.inf
+    w, m, v = gu.dev(synth.normal((n,), 3)), torch.zeros(n, dtype=torch.uint8, device=gu.DEV), torch.zeros(n, dtype=torch.uint8, device=gu.DEV)
+    sm, sv = torch.ones(4, device=gu.DEV), torch.ones(4, device=gu.DEV)
+    lc.adamw_step_q8(lc.AdamWQ8Args([w], [gu.dev(g)], [m], [sm], [v], [sv]), LR, B1, B2, EPS, DECAY, 1, 1)
+    torch.cuda.synchronize()
+    bad = np.zeros(n, bool)
+    bad[300:303] = True
+    for codes, t in ((m, torch.float8_e4m3fn), (v, torch.float8_e5m2)):
+        assert np.array_equal(codes.view(t).float().isnan().cpu().numpy(), bad)
+    assert np.array_equal(w.isnan().cpu().numpy(), bad) and sm.isfinite().all() and sv.isfinite().all()
+
+
+def test_the_second_moment_in_8_bits_decays_as_it_should():
+    """beta2 = 0.999 and no gradient: 700 steps take v to 0.999^700 = 0.496 of its start, where rounding to nearest would keep it at 1.  A step's
+    rounding adds at most 0.001 * 0.25 to the relative variance, 700 of them 0.175: 0.42 / 256 over 65536 elements, five of which are 0.8 %."""
+    n = 65536
+    v, m, w = torch.from_numpy(np.full(n, 1.0)).to(torch.float8_e5m2).view(torch.uint8).to(gu.DEV), torch.zeros(n, dtype=torch.uint8, device=gu.DEV), torch.zeros(n, device=gu.DEV)
+    sm, sv = torch.ones(n // 256, device=gu.DEV), torch.ones(n // 256, device=gu.DEV)
+    args = lc.AdamWQ8Args([w], [torch.zeros(n, device=gu.DEV)], [m], [sm], [v], [sv])
+    for t in range(700):
+        lc.adamw_step_q8(args, LR, B1, 0.999, EPS, DECAY, t + 1, t)
+    torch.cuda.synchronize()
+    mean = float((v.view(torch.float8_e5m2).double() * sv.double().repeat_interleave(256)).mean())
+    assert abs(mean / 0.999 ** 700 - 1) < 0.01, mean
+
+
+@pytest.mark.parametrize("q8", [False, True])
+def test_another_stream(q8):
+    n, got = 5000, []
+    for stream in (None, torch.cuda.Stream()):
+        w, g = gu.dev(synth.normal((n,), 5)), gu.dev(synth.normal((n,), 6))
+        m, v = (torch.zeros(n, dtype=torch.uint8 if q8 else torch.float32, device=gu.DEV) for _ in range(2))
+        sm, sv = (torch.ones(20, device=gu.DEV) for _ in range(2))
+        torch.cuda.synchronize()
+        if q8:
+            lc.adamw_step_q8(lc.AdamWQ8Args([w], [g], [m], [sm], [v], [sv]), LR, B1, B2, EPS, DECAY, 1, 9, stream=stream)
+        else:
+            lc.adamw_step(lc.AdamWArgs([w], [g], [m], [v]), LR, B1, B2, EPS, DECAY, 1, stream=stream)
+        torch.cuda.synchronize()
+        got.append((w, m, v))
+    assert all(torch.equal(a, b) for a, b in zip(*got))

@@ -77,3 +77,45 @@ def test_token_logprob_gradient_against_differences_and_autograd():
     loss = a[0] * logp[0, 0] + a[1] * logp[1, 8] - (torch.tensor(b) * (logp.exp() * logp).sum(1)).sum()
     loss.backward()
     assert np.allclose(tz.grad.numpy(), dz, atol=1e-12)
+
+
+def test_adamw_against_torchs_own():
+    rng = np.random.default_rng(3)
+    w, g = rng.normal(size=20), rng.normal(size=(3, 20))
+    p = torch.tensor(w, requires_grad=True)
+    opt = torch.optim.AdamW([p], lr=0.02, betas=(0.8, 0.95), eps=1e-6, weight_decay=0.1)
+    m = v = np.zeros(20)
+    for t in range(3):
+        p.grad = torch.tensor(g[t])
+        opt.step()
+        w, m, v = ops.adamw(w, g[t], m, v, 0.02, 0.8, 0.95, 1e-6, 0.1, t + 1)
+    assert np.allclose(w, p.detach().numpy(), rtol=1e-12, atol=1e-14)
+    by_32, v_32 = ops.adam_states_as_rounded(g[0], m, v, 0.8, 0.95, 0.5)
+    _, m, v = ops.adamw(w, g[0], np.float32(m), np.float32(v), 0, 0.8, 0.95, 1e-6, 0, 4, 0.5)
+    assert by_32.dtype == np.float32 and np.allclose(by_32, m, rtol=1e-6, atol=1e-7) and np.allclose(v_32, v, rtol=1e-6)
+
+
+def test_power_scales():
+    for amax, most, want in [(0.0, 448.0, 1.0), (448.0, 448.0, 1.0), (449.0, 448.0, 2.0), (224.0, 448.0, 0.5), (1.0, 448.0, 2.0 ** -8), (1e-300, 448.0, 2.0 ** -126),
+                             (57344.0 * 8, 57344.0, 8.0)]:
+        assert ops.power_scale(amax, most) == want
+
+
+def test_dithered_e5m2():
+    values = torch.arange(124, dtype=torch.uint8).view(torch.float8_e5m2).double().numpy()      # 0 .. 57344
+    assert np.array_equal(ops.e5m2_dithered(values, 0), values)                   # on the grid nothing moves, whatever the bits
+    assert np.array_equal(ops.e5m2_dithered(values, 2.0 ** 21 - 1), values)
+    assert ops.e5m2_dithered(np.array([1e-30]), 0)[0] == 2.0 ** -16               # above zero stays above zero
+    x = 1.25 + 0.25 * 0.3                                                          # between 1.25 and 1.5
+    bits = ops.dither21(np.arange(20000), 7)
+    assert bits.min() >= 0 and bits.max() < 2 ** 21
+    got = ops.e5m2_dithered(np.full(20000, x), bits)
+    assert set(np.unique(got)) == {1.25, 1.5} and abs(np.mean(got) - x) < 5 * 0.25 * np.sqrt(0.3 * 0.7 / 20000)
+
+
+def test_dither_is_even_and_differs_by_seed():
+    a, b = ops.dither21(np.arange(30000), 1), ops.dither21(np.arange(30000), 2)
+    for bits in (a, b, (a + b) % 2 ** 21, (a[1:] - a[:-1]) % 2 ** 21, (a - b) % 2 ** 21):
+        count = np.bincount((bits // 2 ** 17).astype(int), minlength=16)
+        expected = bits.size / 16
+        assert np.sum((count - expected) ** 2 / expected) < 60                     # chi-square of 15 degrees: mean 15, P(> 60) below 1e-6
