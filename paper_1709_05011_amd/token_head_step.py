@@ -1,0 +1,114 @@
+"""The output side of a token model on the device: RMS norm with the residual's addition, a classifier over the vocabulary (a 1x1 convolution over one
+pixel per token), the log probabilities of given tokens, and the way back to the norm's inputs with an AdamW update of the classifier and the
+norm's scale.  Every operator is a call into the C library; this module only owns buffers and the order of calls, and torch is used for device memory.
+
+    head = TokenHeadStep(width=1024, vocab=32000, dtype=lc.LC_BF16)
+    logprob, entropy, dx = head.step(x, residual, tokens, dlogprob)     # dlogprob: the loss's gradient with respect to each log probability
+    logprob, entropy, ids, top = head.score(x, residual, tokens, top=5) # one token or many, nothing is updated
+    total, codes, scales = head.packed(x, residual)                     # the norm's output in 8 bits, for a product or a wire that takes it so
+
+The vocabulary is padded to a multiple of 8 rows of the classifier (what the bf16 products take without copies); the pad's logits are never read and their
+gradient stays zero.
+"""
+from __future__ import annotations
+
+from typing import Dict, Optional, Tuple
+
+import torch
+
+from . import larsconv as lc
+
+
+class TokenHeadStep:
+    def __init__(self, width: int, vocab: int, dtype: int = lc.LC_BF16, states_in_8_bits: bool = False, eps: float = 1e-5, lr: float = 1e-3,
+                 beta1: float = 0.9, beta2: float = 0.95, adam_eps: float = 1e-8, weight_decay: float = 0.1, device: str = "cuda:0"):
+        lc.lib()                     # fails here, loudly, when the library has not been built
+        self.dev, self.width, self.vocab, self.dtype, self.eps = device, width, vocab, dtype, eps
+        self.type = torch.bfloat16 if dtype == lc.LC_BF16 else torch.float32
+        self.padded = (vocab + 7) // 8 * 8
+        self.lr, self.betas, self.adam_eps, self.weight_decay, self.steps = lr, (beta1, beta2), adam_eps, weight_decay, 0
+        f32 = dict(dtype=torch.float32, device=device)
+        self.params: Dict[str, torch.Tensor] = {"w": torch.zeros((self.padded, width), **f32), "gamma": torch.ones(width, **f32)}
+        self.grads = {k: torch.zeros_like(p) for k, p in self.params.items()}
+        self.w_lowp = torch.zeros((self.padded, width), dtype=self.type, device=device) if dtype == lc.LC_BF16 else None
+        names = list(self.params)
+        lists = [[d[k] for k in names] for d in (self.params, self.grads)]
+        lowp = [self.w_lowp, None] if self.w_lowp is not None else None
+        self.states_in_8_bits = states_in_8_bits
+        sizes = [self.params[k].numel() for k in names]
+        if states_in_8_bits:
+            self.m, self.v = ([torch.zeros(n, dtype=torch.uint8, device=device) for n in sizes] for _ in range(2))
+            self.m_scale, self.v_scale = ([torch.ones(-(-n // lc.ADAMW_Q8_BLOCK), **f32) for n in sizes] for _ in range(2))
+            self._adam = lc.AdamWQ8Args(*lists, self.m, self.m_scale, self.v, self.v_scale, w_lowp=lowp)
+        else:
+            self.m, self.v = ([torch.zeros(n, **f32) for n in sizes] for _ in range(2))
+            self._adam = lc.AdamWArgs(*lists, self.m, self.v, w_lowp=lowp)
+        self._rows: Dict[Tuple[int, int], dict] = {}
+
+    def load(self, w: torch.Tensor, gamma: torch.Tensor) -> None:
+        """Sets the classifier ([vocab][width]) and the norm's scale."""
+        self.params["w"].zero_()
+        self.params["w"][:self.vocab].copy_(w)
+        self.params["gamma"].copy_(gamma)
+        if self.w_lowp is not None:
+            self.w_lowp.copy_(self.params["w"])
+
+    def _buffers(self, rows: int, top: int) -> dict:
+        """What a call over `rows` tokens works in, made once for each (rows, top)."""
+        if (rows, top) not in self._rows:
+            e = lambda *shape, dtype=torch.float32: torch.empty(shape, dtype=dtype, device=self.dev)
+            norm = lc.RmsNormDesc(rows, self.width, eps=self.eps, dtype=self.dtype)
+            token = lc.TokenDesc(rows, self.vocab, ld=self.padded, dtype=self.dtype, top=top)
+            product = lc.ConvDesc(rows, self.width, 1, 1, self.padded, 1, 1, dtype=self.dtype)
+            need = max([lc.rmsnorm_bwd_workspace_bytes(norm), lc.token_logprob_workspace_bytes(token), 256] +
+                       [lc.conv2d_workspace_bytes(product, p) for p in (lc.LC_PASS_FWD, lc.LC_PASS_BWD_DATA, lc.LC_PASS_BWD_WEIGHT)])
+            self._rows[rows, top] = dict(
+                norm=norm, token=token, product=product, ws=e(need, dtype=torch.uint8), total=e(rows, self.width, dtype=self.type),
+                y=e(rows, self.width, dtype=self.type), rstd=e(rows), logits=e(rows, self.padded, dtype=self.type), logprob=e(rows), entropy=e(rows),
+                lse=e(rows), ids=e(rows, top, dtype=torch.int32) if top else None, top=e(rows, top) if top else None)
+        return self._rows[rows, top]
+
+    def _forward(self, b: dict, x: torch.Tensor, residual: Optional[torch.Tensor], tokens: torch.Tensor) -> None:
+        w = self.params["w"] if self.w_lowp is None else self.w_lowp
+        lc.rmsnorm_fwd(b["norm"], x, residual, self.params["gamma"], b["total"] if residual is not None else None, b["y"], b["rstd"])
+        lc.conv2d_fwd(b["product"], b["y"], w, b["logits"], b["ws"])
+        lc.token_logprob_fwd(b["token"], b["logits"], tokens, b["logprob"], b["entropy"], b["lse"], b["ids"], b["top"], b["ws"])
+
+    def score(self, x, residual, tokens, top: int = 0):
+        """Log probability and entropy of each row's token (int32; outside the vocabulary: does not count), and the `top` likeliest tokens with
+        theirs.  The tensors returned are this object's buffers: the next call over as many rows writes them again."""
+        b = self._buffers(x.shape[0], top)
+        self._forward(b, x, residual, tokens)
+        return b["logprob"], b["entropy"], b["ids"], b["top"]
+
+    def step(self, x, residual, tokens, dlogprob, dentropy=None, dtotal=None, grad_scale=None):
+        """Forward, backward and update.  dlogprob, dentropy: gradient of the loss with respect to each row's log probability and entropy (a mean
+        cross-entropy: -1/rows); dtotal: gradient that reaches x + residual by another way; grad_scale: one float on the device, multiplies the
+        parameters' gradients.  Returns the rows' log probabilities and entropies and the gradient with respect to x (and to residual)."""
+        b = self._buffers(x.shape[0], 0)
+        if "dlogits" not in b:
+            b["dlogits"] = torch.zeros_like(b["logits"])          # the pad stays zero
+            b["dy"], b["dx"] = torch.empty_like(b["y"]), torch.empty_like(b["y"])
+        self._forward(b, x, residual, tokens)
+        lc.token_logprob_bwd(b["token"], b["logits"], tokens, b["lse"], b["entropy"], dlogprob, dentropy, b["dlogits"], self.padded)
+        w = self.params["w"] if self.w_lowp is None else self.w_lowp
+        lc.conv2d_bwd_data(b["product"], b["dlogits"], w, b["dy"], b["ws"])
+        lc.conv2d_bwd_weight(b["product"], b["y"], b["dlogits"], self.grads["w"], b["ws"])
+        lc.rmsnorm_bwd(b["norm"], b["total"] if residual is not None else x, b["dy"], dtotal, self.params["gamma"], b["rstd"], b["dx"],
+                       self.grads["gamma"], b["ws"])
+        self.steps += 1
+        decays = [self.weight_decay, 0.0]                         # the norm's scale is not decayed
+        if self.states_in_8_bits:
+            lc.adamw_step_q8(self._adam, self.lr, *self.betas, self.adam_eps, self.weight_decay, self.steps, self.steps, decays, grad_scale)
+        else:
+            lc.adamw_step(self._adam, self.lr, *self.betas, self.adam_eps, self.weight_decay, self.steps, decays, grad_scale)
+        return b["logprob"], b["entropy"], b["dx"]
+
+    def packed(self, x, residual, group: int = 128):
+        """x + residual and its norm as e4m3 codes with a scale for every `group` columns (0: one a row)."""
+        rows = x.shape[0]
+        total = torch.empty((rows, self.width), dtype=self.type, device=self.dev) if residual is not None else None
+        codes = torch.empty((rows, self.width), dtype=torch.float8_e4m3fn, device=self.dev)
+        scales = torch.empty((rows, -(-self.width // group) if group else 1), device=self.dev)
+        lc.rmsnorm_fwd_q8(lc.RmsNormDesc(rows, self.width, eps=self.eps, dtype=self.dtype), x, residual, self.params["gamma"], total, codes, scales, group)
+        return total, codes, scales

@@ -1,0 +1,124 @@
+"""The token model's output side as one path (paper_1709_05011_amd/token_head_step.py) against the float64 definitions chained with numpy products, its
+training, and its capture in a HIP graph."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import token_ops as ops
+from paper_1709_05011_amd import larsconv as lc
+from paper_1709_05011_amd import synth
+from paper_1709_05011_amd.token_head_step import TokenHeadStep
+
+import gpu_util as gu
+
+pytestmark = pytest.mark.gpu
+# relative to the largest value of each tensor: fp32 products over 64 to 96 columns and 300 tokens stay under 1e-4 of it (the parity bound of the
+# convolutions); bf16 rounds y, the logits, their gradient and dy once each (2^-8 of the value, |logits| about 8 and weights of order 1 behind them): 5 %
+TOL = {"f32": 1e-4, "bf16": 0.05}
+f64 = lambda t: t.double().cpu().numpy()
+
+
+def setup(kind, rows, width, vocab, **kw):
+    t = torch.bfloat16 if kind == "bf16" else torch.float32
+    head = TokenHeadStep(width, vocab, lc.LC_BF16 if kind == "bf16" else lc.LC_F32, **kw)
+    head.load(gu.dev(synth.normal((vocab, width), 1, std=2.0 / np.sqrt(width))), gu.dev(1 + synth.normal((width,), 2, std=0.2)))
+    x, r = (gu.dev(synth.normal((rows, width), s)).to(t) for s in (3, 4))
+    tokens = np.random.default_rng(5).integers(0, vocab, rows)
+    tokens[0] = -1
+    return head, x, r, tokens, gu.dev(tokens.astype(np.int32))
+
+
+def chain(head, x, r, tokens, a, b, kind):
+    """The same in float64 from the values the device holds."""
+    store = (lambda v: ops.bf16(v.astype(np.float32))) if kind == "bf16" else (lambda v: v)
+    w, gamma = f64(head.params["w"] if head.w_lowp is None else head.w_lowp)[:head.vocab], f64(head.params["gamma"])
+    h, rstd, y = ops.rmsnorm(f64(x), f64(r), gamma, 1e-5, store)
+    z = y @ w.T
+    lp, ent, _, ids, top = ops.token_logprob(z, tokens, 5)
+    dz = ops.token_logprob_bwd(z, tokens, a, b)
+    dx, dgamma = ops.rmsnorm_bwd(h, rstd, gamma, dz @ w)
+    return lp, ent, ids, top, dx, dz.T @ y, dgamma
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,width,vocab", [(1, 64, 40), (7, 96, 1003), (300, 64, 517)])
+def test_score_and_step(kind, rows, width, vocab):
+    head, x, r, tokens, dev_tokens = setup(kind, rows, width, vocab)
+    a, b = np.full(rows, -1.0 / rows), np.full(rows, -0.05 / rows)
+    lp, ent, ids, top, dx, dw, dgamma = chain(head, x, r, tokens, a, b, kind)
+    near = lambda got, want: float(np.max(np.abs(f64(got) - want))) <= TOL[kind] * max(1e-12, float(np.max(np.abs(want))))
+    got = head.score(x, r, dev_tokens, top=5)
+    torch.cuda.synchronize()
+    assert near(got[0], lp) and near(got[1], ent) and near(got[3], top)
+    before = {k: p.clone() for k, p in head.params.items()}
+    got = head.step(x, r, dev_tokens, gu.dev(np.float32(a)), gu.dev(np.float32(b)))
+    torch.cuda.synchronize()
+    assert near(got[0], lp) and near(got[1], ent) and near(got[2], dx)
+    assert near(head.grads["w"][:vocab], dw) and near(head.grads["gamma"], dgamma) and not head.grads["w"][vocab:].any()
+    for k, decay in (("w", 0.1), ("gamma", 0.0)):             # the update by the gradients the device made
+        g = f64(head.grads[k])
+        want, _, _ = ops.adamw(f64(before[k]), g, 0 * g, 0 * g, 1e-3, 0.9, 0.95, 1e-8, decay, 1)
+        assert np.max(np.abs(f64(head.params[k]) - want)) < 1e-5 * 1e-3 + 2.0 ** -22 * np.max(np.abs(want))
+    if head.w_lowp is not None:
+        assert torch.equal(head.w_lowp, head.params["w"].bfloat16())
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("states_in_8_bits", [False, True])
+def test_training_learns_the_tokens(kind, states_in_8_bits):
+    """64 tokens of their own hidden states: forty steps bring the mean log probability from under -4 to over -1, with states of either width."""
+    rows = 64
+    head, x, r, tokens, dev_tokens = setup(kind, rows, 128, 200, states_in_8_bits=states_in_8_bits, lr=0.02)
+    a = torch.full((rows,), -1.0 / rows, device=gu.DEV)
+    first = f64(head.score(x, r, dev_tokens)[0])[1:].mean()
+    for _ in range(40):
+        head.step(x, r, dev_tokens, a)
+    last = f64(head.score(x, r, dev_tokens)[0])[1:].mean()
+    assert first < -4 and last > -1, (first, last)
+
+
+def test_packed():
+    head, x, r, _, _ = setup("bf16", 9, 200, 40)
+    total, codes, scales = head.packed(x, r)
+    torch.cuda.synchronize()
+    h, _, y = ops.rmsnorm(f64(x), f64(r), f64(head.params["gamma"]), 1e-5, lambda v: ops.bf16(v.astype(np.float32)))
+    assert np.array_equal(f64(total), h) and scales.shape == (9, 2)
+    back = codes.float().double().cpu().numpy() * np.repeat(f64(scales), 128, axis=1)[:, :200]
+    assert np.max(np.abs(back - y)) < 2.0 ** -4 * 1.001 * np.max(np.abs(y))
+
+
+@pytest.mark.parametrize("states_in_8_bits", [False, True])
+def test_the_step_in_a_graph(states_in_8_bits):
+    """Captured once and replayed with eager work between: every replay from the same start gives the eager step's bits."""
+    rows = 50
+    head, x, r, tokens, dev_tokens = setup("bf16", rows, 128, 9000, states_in_8_bits=states_in_8_bits)
+    a, b = torch.full((rows,), -1.0 / rows, device=gu.DEV), torch.full((rows,), -0.01 / rows, device=gu.DEV)
+    state = [*head.params.values(), *head.m, *head.v, head.w_lowp] + ([*head.m_scale, *head.v_scale] if states_in_8_bits else [])
+    start = [t.clone() for t in state]
+
+    def restore():
+        for t, s in zip(state, start):
+            t.copy_(s)
+        head.steps = 0
+
+    def results():
+        torch.cuda.synchronize()
+        return [t.clone() for t in (*state, *out, *head.grads.values())]
+
+    out = head.step(x, r, dev_tokens, a, b)
+    want = results()
+    side = torch.cuda.Stream()
+    restore()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        head.step(x, r, dev_tokens, a, b)
+    for _ in range(3):
+        restore()
+        junk = [torch.randn(1000, 1000, device=gu.DEV) @ torch.randn(1000, 1000, device=gu.DEV) for _ in range(3)]
+        for t in (*out, *head.grads.values()):
+            t.fill_(float("nan"))
+        torch.cuda.synchronize()
+        graph.replay()
+        assert all(torch.equal(g, w) for g, w in zip(results(), want))
+        del junk
