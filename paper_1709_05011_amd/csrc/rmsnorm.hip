@@ -55,24 +55,26 @@ template <typename T, int WAVES, int CH, bool Q8>
 __global__ void __launch_bounds__(WAVES * 64) rmsnorm_fwd_kernel(const NormArgs p) {
     __shared__ float red[2][2][WAVES];
     const int tid = threadIdx.x, c = p.c;
+    const auto column = [tid](int i) { return (i * WAVES * 64 + tid) * 8; };
     int parity = 0;
     for (long long row = blockIdx.x; row < p.rows; row += gridDim.x, parity ^= 1) {
         const T* x = static_cast<const T*>(p.x) + row * p.x_ld;
         Packed<T> px[CH], pr[CH];
         Packed<float> pg[CH];
         float h[CH][8];
-#pragma unroll
-        for (int i = 0; i < CH; ++i) lc_load8(px[i], x, (i * WAVES * 64 + tid) * 8, c);
+        lc_issue8(px, x, column, c);
         if (p.r) {
             const T* r = static_cast<const T*>(p.r) + row * p.r_ld;
-#pragma unroll
-            for (int i = 0; i < CH; ++i) lc_load8(pr[i], r, (i * WAVES * 64 + tid) * 8, c);
+            lc_issue8(pr, r, column, c);
         }
-#pragma unroll
-        for (int i = 0; i < CH; ++i) lc_load8(pg[i], p.gamma, (i * WAVES * 64 + tid) * 8, c);
+        lc_issue8(pg, p.gamma, column, c);
         float ss = 0.f;
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
+            const int col = column(i);
+            lc_settle8(px[i], col, c, c);
+            if (p.r) lc_settle8(pr[i], col, c, c);
+            lc_settle8(pg[i], col, c, c);
 #pragma unroll
             for (int j = 0; j < 8; ++j) h[i][j] = p.r ? lc_as_stored<T>(px[i].get(j) + pr[i].get(j)) : px[i].get(j);
 #pragma unroll
@@ -82,7 +84,7 @@ __global__ void __launch_bounds__(WAVES * 64) rmsnorm_fwd_kernel(const NormArgs 
             T* t = static_cast<T*>(p.total) + row * (long long)c;
 #pragma unroll
             for (int i = 0; i < CH; ++i) {
-                const int col = (i * WAVES * 64 + tid) * 8;
+                const int col = column(i);
                 lc_store8(t + col, h[i], c - col);
             }
         }
@@ -101,7 +103,7 @@ __global__ void __launch_bounds__(WAVES * 64) rmsnorm_fwd_kernel(const NormArgs 
             T* y = static_cast<T*>(p.y) + row * (long long)c;
 #pragma unroll
             for (int i = 0; i < CH; ++i) {
-                const int col = (i * WAVES * 64 + tid) * 8;
+                const int col = column(i);
                 lc_store8(y + col, h[i], c - col);
             }
         } else {
@@ -112,7 +114,7 @@ __global__ void __launch_bounds__(WAVES * 64) rmsnorm_fwd_kernel(const NormArgs 
                 const float inv = 1.f / scale;
 #pragma unroll
                 for (int i = 0; i < CH; ++i) {
-                    const int col = (i * WAVES * 64 + tid) * 8;
+                    const int col = column(i);
                     store8_e4m3(y + col, h[i], inv, c - col);
                 }
             } else {
@@ -120,7 +122,7 @@ __global__ void __launch_bounds__(WAVES * 64) rmsnorm_fwd_kernel(const NormArgs 
                 const long long groups = (c + p.group - 1) / p.group;
 #pragma unroll
                 for (int i = 0; i < CH; ++i) {
-                    const int col = (i * WAVES * 64 + tid) * 8;
+                    const int col = column(i);
                     float m = 0.f;
 #pragma unroll
                     for (int j = 0; j < 8; ++j) m = fmaxf(m, fabsf(h[i][j]));
@@ -232,39 +234,43 @@ template <typename T, int WAVES, int CH>
 __global__ void __launch_bounds__(WAVES * 64) rmsnorm_bwd_kernel(const NormBwdArgs p) {
     __shared__ float red[2][WAVES];
     const int tid = threadIdx.x, c = p.c;
+    const auto column = [tid](int i) { return (i * WAVES * 64 + tid) * 8; };
     Packed<float> pg[CH];
     float acc[CH][8] = {};
+    lc_issue8(pg, p.gamma, column, c);
 #pragma unroll
-    for (int i = 0; i < CH; ++i) lc_load8(pg[i], p.gamma, (i * WAVES * 64 + tid) * 8, c);
+    for (int i = 0; i < CH; ++i) lc_settle8(pg[i], column(i), c, c);
     int parity = 0;
     for (long long row = blockIdx.x; row < p.rows; row += gridDim.x, parity ^= 1) {
         const T* h = static_cast<const T*>(p.h) + row * p.h_ld;
         const T* dy = static_cast<const T*>(p.dy) + row * (long long)c;
         Packed<T> ph[CH], pd[CH], pt[CH];
-#pragma unroll
-        for (int i = 0; i < CH; ++i) lc_load8(ph[i], h, (i * WAVES * 64 + tid) * 8, c);
-#pragma unroll
-        for (int i = 0; i < CH; ++i) lc_load8(pd[i], dy, (i * WAVES * 64 + tid) * 8, c);
+        lc_issue8(ph, h, column, c);
+        lc_issue8(pd, dy, column, c);
         if (p.dh) {
             const T* dh = static_cast<const T*>(p.dh) + row * (long long)c;
-#pragma unroll
-            for (int i = 0; i < CH; ++i) lc_load8(pt[i], dh, (i * WAVES * 64 + tid) * 8, c);
+            lc_issue8(pt, dh, column, c);
         }
         const float rstd = p.rstd[row];
         float s = 0.f;
 #pragma unroll
-        for (int i = 0; i < CH; ++i)
+        for (int i = 0; i < CH; ++i) {
+            const int col = column(i);
+            lc_settle8(ph[i], col, c, c);
+            lc_settle8(pd[i], col, c, c);
+            if (p.dh) lc_settle8(pt[i], col, c, c);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const float n = ph[i].get(j) * rstd, d = pd[i].get(j);
                 s = fmaf(d * pg[i].get(j), n, s);
                 acc[i][j] = fmaf(d, n, acc[i][j]);
             }
+        }
         const float mean = lc_block_sum<WAVES>(s, red[parity]) / (float)c;
         T* dx = static_cast<T*>(p.dx) + row * (long long)c;
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
-            const int col = (i * WAVES * 64 + tid) * 8;
+            const int col = column(i);
             float o[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
@@ -278,7 +284,7 @@ __global__ void __launch_bounds__(WAVES * 64) rmsnorm_bwd_kernel(const NormBwdAr
     float* part = p.part + (long long)blockIdx.x * c;
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
-        const int col = (i * WAVES * 64 + tid) * 8;
+        const int col = column(i);
         lc_store8(part + col, acc[i], c - col);
     }
 }

@@ -9,9 +9,10 @@
 
 namespace {
 
-// Global accesses of 16 bytes need no alignment beyond the element's on gfx950 (the unaligned access mode that HSA code objects run in).
+// Eight elements of a row as loaded.  Global accesses of 16 bytes need no alignment beyond the element's on gfx950 (the unaligned access mode that HSA code objects
+// run in).  shift(): drops the first k elements and fills up at the end.
 template <typename T>
-struct Packed;      // eight elements as loaded
+struct Packed;
 template <>
 struct Packed<float> {
     lc_u32x4 a, b;
@@ -19,11 +20,27 @@ struct Packed<float> {
         __builtin_memcpy(&a, p, 16);
         __builtin_memcpy(&b, p + 4, 16);
     }
-    __device__ __forceinline__ void load_some(const float* p, int n, uint32_t fill = 0) {
+    __device__ __forceinline__ void load_some(const float* p, int n, uint32_t fill) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             a[j] = j < n ? __float_as_uint(p[j]) : fill;
             b[j] = j + 4 < n ? __float_as_uint(p[j + 4]) : fill;
+        }
+    }
+    __device__ __forceinline__ void shift(int k, uint32_t fill) {
+        const lc_u32x4 f = {fill, fill, fill, fill};
+        if (k >= 8) a = b = f;
+        if (k & 4) {
+            a = b;
+            b = f;
+        }
+        if (k & 2) {
+            a = lc_u32x4{a[2], a[3], b[0], b[1]};
+            b = lc_u32x4{b[2], b[3], fill, fill};
+        }
+        if (k & 1) {
+            a = lc_u32x4{a[1], a[2], a[3], b[0]};
+            b = lc_u32x4{b[1], b[2], b[3], fill};
         }
     }
     __device__ __forceinline__ float get(int j) const { return __uint_as_float(j < 4 ? a[j] : b[j - 4]); }
@@ -32,19 +49,48 @@ template <>
 struct Packed<uint16_t> {
     lc_u32x4 a;
     __device__ __forceinline__ void load(const uint16_t* p) { __builtin_memcpy(&a, p, 16); }
-    __device__ __forceinline__ void load_some(const uint16_t* p, int n, uint32_t fill = 0) {
+    __device__ __forceinline__ void load_some(const uint16_t* p, int n, uint32_t fill) {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
             a[j] = (2 * j < n ? (uint32_t)p[2 * j] : fill) | (2 * j + 1 < n ? (uint32_t)p[2 * j + 1] : fill) << 16;
     }
+    __device__ __forceinline__ void shift(int k, uint32_t fill) {
+        const uint32_t f = fill | fill << 16;
+        if (k >= 8) a = lc_u32x4{f, f, f, f};
+        if (k & 4) a = lc_u32x4{a[2], a[3], f, f};
+        if (k & 2) a = lc_u32x4{a[1], a[2], a[3], f};
+        if (k & 1)
+            a = lc_u32x4{__builtin_amdgcn_alignbit(a[1], a[0], 16), __builtin_amdgcn_alignbit(a[2], a[1], 16), __builtin_amdgcn_alignbit(a[3], a[2], 16),
+                         __builtin_amdgcn_alignbit(f, a[3], 16)};
+    }
     __device__ __forceinline__ float get(int j) const { return __uint_as_float(j & 1 ? a[j >> 1] & 0xffff0000u : a[j >> 1] << 16); }
 };
 
-// Columns col .. col + 7 of a row of c; what lies past its end is `fill` (the type's own bit pattern).
+// Columns col(i) .. col(i) + 7 of a row of c for i < CH in two steps, so that all of a thread's loads are under way before the first is looked at: lc_issue8()
+// loads the row's last eight columns in place of what would pass its end (no branch, nothing outside the row), lc_settle8() moves those to their places and
+// puts `fill` (the type's own bits) where a column lies at `end` or past it; end is c, or a multiple of 8 before it.  Rows under eight columns, one
+// thread's at most, are read one by one.
+template <int CH, typename T, typename F>
+__device__ __forceinline__ void lc_issue8(Packed<T> (&to)[CH], const T* row, F&& col, int c, uint32_t fill = 0) {
+    if (c >= 8) {
+#pragma unroll
+        for (int i = 0; i < CH; ++i) to[i].load(row + min(col(i), c - 8));
+    } else {
+        to[0].load_some(row + col(0), c - col(0), fill);
+#pragma unroll
+        for (int i = 1; i < CH; ++i) to[i].shift(8, fill);
+    }
+}
 template <typename T>
-__device__ __forceinline__ void lc_load8(Packed<T>& to, const T* row, int col, int c, uint32_t fill = 0) {
-    if (col + 8 <= c) to.load(row + col);
-    else to.load_some(row + col, c - col, fill);
+__device__ __forceinline__ void lc_settle8(Packed<T>& to, int col, int c, int end, uint32_t fill = 0) {
+    if (end - col < 8 && c >= 8) to.shift(min(8 - (end - col), 8), fill);
+}
+template <typename T>
+__device__ __forceinline__ void lc_load8(Packed<T>& to, const T* row, int col, int c) {
+    Packed<T> one[1];
+    lc_issue8(one, row, [&](int) { return col; }, c);
+    to = one[0];
+    lc_settle8(to, col, c, c);
 }
 
 // Eight results, rounded once.
@@ -78,15 +124,27 @@ __device__ __forceinline__ float lc_as_stored(float x) {
     else return x;
 }
 
+// Sum and maximum over a wave, every lane with the result: five exchanges inside the vector unit (neighbours, pairs, halves of 8 and of 16 lanes, a row's last lane to the
+// next row, the first two rows' to the last two) and one lane read back as a scalar, where a shuffle through LDS takes some 100 cycles for each of six.
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ float lc_dpp(float other, float x) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(other), __float_as_int(x), CTRL, ROWS, 0xf, false));
+}
+template <typename F>
+__device__ __forceinline__ float lc_wave_join(float x, float neutral, F&& f) {
+    x = f(x, lc_dpp<0xB1>(neutral, x));              // quad_perm 1 0 3 2
+    x = f(x, lc_dpp<0x4E>(neutral, x));              // quad_perm 2 3 0 1
+    x = f(x, lc_dpp<0x141>(neutral, x));             // row_half_mirror
+    x = f(x, lc_dpp<0x140>(neutral, x));             // row_mirror
+    x = f(x, lc_dpp<0x142, 0xa>(neutral, x));        // row_bcast:15 into rows 1 and 3
+    x = f(x, lc_dpp<0x143, 0xc>(neutral, x));        // row_bcast:31 into rows 2 and 3
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
+}
 __device__ __forceinline__ float lc_wave_sum(float x) {
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) x += __shfl_xor(x, off, 64);
-    return x;
+    return lc_wave_join(x, 0.f, [](float a, float b) { return a + b; });
 }
 __device__ __forceinline__ float lc_wave_max(float x) {
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) x = fmaxf(x, __shfl_xor(x, off, 64));
-    return x;
+    return lc_wave_join(x, -INFINITY, [](float a, float b) { return fmaxf(a, b); });
 }
 // Over a block of WAVES waves, every thread with the result; `red` (WAVES floats) must not be in use by an earlier call that a slower wave may still read.
 template <int WAVES>

@@ -1,15 +1,15 @@
 // Log probabilities of given tokens over a vocabulary, with entropy and the likeliest alternatives, and the gradient, for gfx950.
 //
 // Per row of logits z: m = max z, S = sum e^(z-m), T = sum e^(z-m) (z-m); lse = m + log S, log p = z - m - log S, entropy = log S - T/S.
-// Bound by memory: the logits are read once.  A row is cut into slices of up to 8192 values that a block holds in registers, so that the
-// maximum is known before the first exponential and nothing is rescaled on the way; slices leave (m, S, T) and their own list of
-// alternatives, and a second launch joins them (rows of one slice finish where they are).
+// Bound by memory: the logits are read once.  A row is cut into slices that a wave holds in registers, so that the maximum is known before
+// the first exponential, nothing is rescaled on the way and no wave waits for another; slices leave (m, S, T) and their own list of
+// alternatives, and a second launch joins them, a wave a row (rows of one slice finish where they are).
 //
 // Alternatives: a value and its place make one 64-bit key (the value's order in the upper half, the complement of its place in the
 // lower: equal values by rising place), all different.  A lower bound on the N-th largest of a slice comes from the lanes' own maxima -- N lanes
 // have one at least as large -- found by halving over their order with a ballot a step; what reaches it, a few more than N as a
-// rule, is gathered in LDS and ranked by one wave.  More than LDS has room for (many equal values): the bound is raised by
-// halving over the keys themselves, which ends, as no two are equal.
+// rule, is gathered in LDS and ranked.  More than LDS has room for (many equal values): the bound is raised by halving over
+// the keys themselves, which ends, as no two are equal.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -20,11 +20,10 @@
 
 namespace {
 
-constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kMostTop = 32;
-constexpr int kCandidates = 512;            // keys that LDS has room for
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kFar = -150.f;              // e^-150 is 0 in fp32: distances are no longer than this where 0 * infinity would be formed
+constexpr int kCandidates = 256;            // keys that a wave's LDS has room for
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kFar = -150.f;              // 2^-150 is 0 in fp32: distances are no longer than this where 0 * infinity would be formed
 
 typedef unsigned long long Key;
 
@@ -36,8 +35,8 @@ struct TokenArgs {
     float* lse;              // or null
     int32_t* top_tokens;
     float* top_logprobs;
-    float* stats;            // [rows][slices][4]: m, S, T
-    Key* keys;               // [rows][slices][top]
+    float* stats;            // [rows][slices][4]: m, S, T (T in units of log 2, as the slices' own exponentials)
+    Key* keys;               // [rows][slices][top], falling; 0 where a slice has fewer
     long long rows, ld;
     int vocab, top, slices, slice;      // slice: values of one, a multiple of 8
 };
@@ -59,26 +58,22 @@ __device__ __forceinline__ float as_float(T v) {
 
 struct Row {
     float m, log_s;          // maximum (0 where there is none) and log S
-    bool empty;              // every logit is masked
 };
 
-// What a row gives but for its alternatives, from its m, S and T (one thread).
+// What a row gives but for its alternatives, from its m, S and T; a whole wave with the same values, lane 0 writes.
 template <typename T>
-__device__ __forceinline__ Row finish_row(const TokenArgs& p, long long row, float m, double s, double t) {
-    Row r;
-    r.empty = s == 0.0;
-    r.m = m == -INFINITY ? 0.f : m;
-    const double log_s = log(s);
-    r.log_s = (float)log_s;
+__device__ __forceinline__ Row finish_row(const TokenArgs& p, long long row, float m, float s, float t) {
     const int token = p.tokens[row];
-    float lp = 0.f;
-    if (token >= 0 && token < p.vocab) {
-        const float z = as_float<T>(static_cast<const T*>(p.z)[row * p.ld + token]);
-        lp = r.empty ? -INFINITY : (float)((double)(z - r.m) - log_s);
+    const bool counts = token >= 0 && token < p.vocab, empty = s == 0.f;
+    const float z = counts ? as_float<T>(static_cast<const T*>(p.z)[row * p.ld + token]) : 0.f;
+    Row r;
+    r.m = m == -INFINITY ? 0.f : m;
+    r.log_s = logf(s);
+    if ((threadIdx.x & 63) == 0) {
+        p.logprob[row] = !counts ? 0.f : empty ? -INFINITY : (z - r.m) - r.log_s;
+        if (p.entropy) p.entropy[row] = empty ? 0.f : r.log_s - kLn2 * (t / s);
+        if (p.lse) p.lse[row] = empty ? -INFINITY : r.m + r.log_s;
     }
-    p.logprob[row] = lp;
-    if (p.entropy) p.entropy[row] = r.empty ? 0.f : (float)(log_s - t / s);
-    if (p.lse) p.lse[row] = r.empty ? -INFINITY : (float)((double)r.m + log_s);
     return r;
 }
 
@@ -87,153 +82,133 @@ __device__ __forceinline__ void put_alternative(const TokenArgs& p, long long ro
     p.top_logprobs[row * p.top + place] = key ? (value_of((uint32_t)(key >> 32)) - r.m) - r.log_s : -INFINITY;
 }
 
-// Ranks `count` different keys in LDS with one wave; emit(place, key) for the first `top` places, key 0 where there are fewer.
+// Order of a value that at least `need` lanes of the wave reach with theirs, and few more; the least of all values where fewer lanes hold one.
+__device__ __forceinline__ uint32_t lanes_bound(uint32_t mine, bool holds, int need) {
+    uint32_t lo = 0x00800000u;                        // order of the lowest finite float
+    if (__popcll(__ballot(holds)) < need) return lo;
+    uint32_t hi = 0xff800001u;                        // above the order of infinity
+    while (hi - lo > 1) {
+        const uint32_t mid = lo + ((hi - lo) >> 1);
+        const int n = __popcll(__ballot(holds && mine >= mid));
+        if (n >= need) {
+            lo = mid;
+            if (n <= need + need / 4) break;
+        } else {
+            hi = mid;
+        }
+    }
+    return lo;
+}
+
+// Appends the keys of the lanes that have one to `keys` (a wave's own); returns the new count, which may pass kCandidates.
+__device__ __forceinline__ int append(Key* keys, int held, bool has, Key key) {
+    const unsigned long long mask = __ballot(has);
+    const int at = held + __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+    if (has && at < kCandidates) keys[at] = key;
+    return held + __popcll(mask);
+}
+
+// Ranks `count` different keys of a wave in LDS; emit(place, key) for the first `top` places, key 0 where there are fewer.
 template <typename F>
 __device__ __forceinline__ void rank_keys(const Key* keys, int count, int top, F&& emit) {
     const int lane = threadIdx.x & 63;
-    for (int i = lane; i < count; i += 64) {
-        const Key mine = keys[i];
+    for (int base = 0; base < count; base += 64) {
+        const Key mine = base + lane < count ? keys[base + lane] : 0;
         int place = 0;
+#pragma unroll 8
         for (int j = 0; j < count; ++j) place += keys[j] > mine;
-        if (place < top) emit(place, mine);
+        if (base + lane < count && place < top) emit(place, mine);
     }
     for (int i = count + lane; i < top; i += 64) emit(i, (Key)0);
 }
 
+// A wave a slice: 512 * CH values.  T is summed in units of log 2 from the exponentials' own arguments; a masked value makes it 0 * infinity there,
+// and such a slice sums again with the distances bounded (NaN and infinity among the logits come out NaN either way).
 template <typename T, int CH, bool TOP>
-__global__ void __launch_bounds__(kThreads) token_slice_kernel(const TokenArgs p) {
-    __shared__ float sums[kWaves][3];
-    __shared__ Row joined;
-    __shared__ uint32_t bound[kWaves];
-    __shared__ int counts[2];
+__global__ void __launch_bounds__(64) token_slice_kernel(const TokenArgs p) {
     __shared__ Key keys[TOP ? kCandidates : 1];
     constexpr uint32_t kMaskedBits = sizeof(T) == 2 ? 0xff80u : 0xff800000u;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const long long units = p.rows * p.slices;
-    for (long long unit = blockIdx.x; unit < units; unit += gridDim.x) {
-        const long long row = p.slices == 1 ? unit : unit / p.slices;
-        const int part = (int)(unit - row * p.slices);
-        const int first = part * p.slice, end = min(p.vocab - first, p.slice) + first;
+    const int lane = threadIdx.x, part = blockIdx.x;
+    const int first = part * p.slice, end = min(p.vocab - first, p.slice) + first;
+    for (long long row = blockIdx.y; row < p.rows; row += gridDim.y) {
+        const long long unit = row * p.slices + part;
         const T* z = static_cast<const T*>(p.z) + row * p.ld;
-        Packed<T> v[CH];
+        Packed<T> packed[CH];
+        lc_issue8(packed, z, [&](int i) { return first + (i * 64 + lane) * 8; }, p.vocab, kMaskedBits);
+        float v[CH][8], most = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < CH; ++i) lc_load8(v[i], z, first + (i * kThreads + tid) * 8, end, kMaskedBits);
-
-        float most = -INFINITY;
+        for (int i = 0; i < CH; ++i) {
+            lc_settle8(packed[i], first + (i * 64 + lane) * 8, p.vocab, end, kMaskedBits);
 #pragma unroll
-        for (int i = 0; i < CH; ++i)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) most = fmaxf(most, v[i].get(j));
-        const float m = lc_wave_max(most), from = m == -INFINITY ? 0.f : m;
+            for (int j = 0; j < 8; ++j) {
+                v[i][j] = packed[i].get(j);
+                most = fmaxf(most, v[i][j]);
+            }
+        }
+        const float m = lc_wave_max(most), from = m == -INFINITY ? 0.f : m, less = -from * kLog2e;
         float s = 0.f, t = 0.f;
 #pragma unroll
         for (int i = 0; i < CH; ++i)
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float d = v[i].get(j) - from;
-                const float e = __builtin_amdgcn_exp2f(d * kLog2e);
+                const float d = fmaf(v[i][j], kLog2e, less);
+                const float e = __builtin_amdgcn_exp2f(d);
                 s += e;
-                t = fmaf(e, fmaxf(d, kFar), t);
+                t = fmaf(e, d, t);
             }
+        if (__ballot(t != t)) {
+            t = 0.f;
+#pragma unroll
+            for (int i = 0; i < CH; ++i)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float d = fmaf(v[i][j], kLog2e, less);
+                    t = fmaf(__builtin_amdgcn_exp2f(d), fmaxf(d, kFar), t);
+                }
+        }
         s = lc_wave_sum(s);
         t = lc_wave_sum(t);
-        if (lane == 0) {
-            sums[wave][0] = m;
-            sums[wave][1] = s;
-            sums[wave][2] = t;
+        // every exponent was off by what rounding m log2 e took: 2^off on all terms
+        const float off = fmaf(from, kLog2e, less), back = __builtin_amdgcn_exp2f(-off);
+        t = fmaf(-off, s, t) * back;
+        s *= back;
+        Row r;
+        if (p.slices == 1) {
+            r = finish_row<T>(p, row, m, s, t);
+        } else if (lane == 0) {
+            *reinterpret_cast<float4*>(p.stats + unit * 4) = make_float4(m, s, t, 0.f);
         }
         if constexpr (TOP) {
-            // the largest order lo that `top` lanes of the wave reach, nearly; without so many lanes that hold a value, the least order
-            const uint32_t mine = order_of(most);
-            uint32_t lo = order_of(-3.402823466e38f), hi = order_of(m) + 1;
-            if (__popcll(__ballot(listable(most))) >= p.top) {
-                while (hi - lo > 1) {
-                    const uint32_t mid = lo + ((hi - lo) >> 1);
-                    const int n = __popcll(__ballot(listable(most) && mine >= mid));
-                    if (n >= p.top) {
-                        lo = mid;
-                        if (n <= p.top + 4) break;
-                    } else {
-                        hi = mid;
-                    }
-                }
-            }
-            if (lane == 0) bound[wave] = lo;
-            if (tid == 0) counts[0] = 0;
-        }
-        __syncthreads();
-        if (tid == 0) {
-            float bm = sums[0][0];
-#pragma unroll
-            for (int w = 1; w < kWaves; ++w) bm = fmaxf(bm, sums[w][0]);
-            double bs = 0.0, bt = 0.0;
-#pragma unroll
-            for (int w = 0; w < kWaves; ++w) {
-                // (a wave without a value keeps its sums: 0, or NaN)
-                const double shift = sums[w][0] == -INFINITY ? 0.0 : (double)sums[w][0] - (double)bm;
-                const double f = exp(shift);
-                bs += f * sums[w][1];
-                bt += f * (sums[w][2] + shift * sums[w][1]);
-            }
-            if (p.slices == 1) {
-                joined = finish_row<T>(p, row, bm, bs, bt);
-            } else {
-                float* out = p.stats + unit * 4;
-                out[0] = bm;
-                out[1] = (float)bs;
-                out[2] = (float)bt;
-            }
-        }
-        if constexpr (TOP) {
-            Key least = (Key)max(max(bound[0], bound[1]), max(bound[2], bound[3])) << 32;
             auto each = [&](auto&& f) __attribute__((always_inline)) {
 #pragma unroll
                 for (int i = 0; i < CH; ++i)
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const float x = v[i].get(j);
-                        if (listable(x)) f(key_of(x, first + (i * kThreads + tid) * 8 + j));
-                    }
+                    for (int j = 0; j < 8; ++j) f(v[i][j], first + (i * 64 + lane) * 8 + j);
             };
-            auto gather = [&]() __attribute__((always_inline)) {
-                each([&](Key k) {
-                    if (k >= least) {
-                        const int at = atomicAdd(&counts[0], 1);
-                        if (at < kCandidates) keys[at] = k;
-                    }
-                });
-            };
-            gather();
-            __syncthreads();
-            if (counts[0] > kCandidates) {          // the same for every thread
-                Key hi = ~(Key)0;                   // fewer than `top` keys reach hi, more than there is room for reach least
-                while (true) {
+            const float bound = value_of(lanes_bound(order_of(most), listable(most), p.top));
+            int held = 0;
+            each([&](float x, int at) {
+                if (__ballot(x >= bound)) held = append(keys, held, x >= bound, key_of(x, at));
+            });
+            if (held > kCandidates) {
+                Key least = (Key)order_of(bound) << 32, hi = ~(Key)0;        // fewer than `top` keys reach hi, more than there is room for reach least
+                while (hi - least > 1) {
                     const Key mid = least + ((hi - least) >> 1);
-                    __syncthreads();
-                    if (tid == 0) counts[1] = 0;
-                    __syncthreads();
                     int n = 0;
-                    each([&](Key k) { n += k >= mid; });
-                    if (n) atomicAdd(&counts[1], n);
-                    __syncthreads();
-                    n = counts[1];
+                    each([&](float x, int at) { n += __popcll(__ballot(listable(x) && key_of(x, at) >= mid)); });
                     if (n >= p.top) least = mid;
                     else hi = mid;
-                    if ((n >= p.top && n <= kCandidates) || hi - least <= 1) break;
+                    if (n >= p.top && n <= kCandidates) break;
                 }
-                __syncthreads();
-                if (tid == 0) counts[0] = 0;
-                __syncthreads();
-                gather();
-                __syncthreads();
+                held = 0;
+                each([&](float x, int at) { held = append(keys, held, listable(x) && key_of(x, at) >= least, key_of(x, at)); });
             }
-            if (wave == 0) {
-                const int count = min(counts[0], kCandidates);
-                if (p.slices == 1) rank_keys(keys, count, p.top, [&](int place, Key k) { put_alternative(p, row, place, k, joined); });
-                else rank_keys(keys, count, p.top, [&](int place, Key k) { p.keys[unit * p.top + place] = k; });
-            }
+            __syncthreads();
+            const int count = min(held, kCandidates);
+            if (p.slices == 1) rank_keys(keys, count, p.top, [&](int place, Key k) { put_alternative(p, row, place, k, r); });
+            else rank_keys(keys, count, p.top, [&](int place, Key k) { p.keys[unit * p.top + place] = k; });
+            __syncthreads();
         }
-        __syncthreads();
     }
 }
 
@@ -241,66 +216,52 @@ __global__ void __launch_bounds__(kThreads) token_slice_kernel(const TokenArgs p
 template <typename T>
 __global__ void __launch_bounds__(64) token_join_kernel(const TokenArgs p) {
     __shared__ Key keys[kCandidates];
-    __shared__ int held;
     const int lane = threadIdx.x;
     for (long long row = blockIdx.x; row < p.rows; row += gridDim.x) {
-        const float* stats = p.stats + row * p.slices * 4;
+        const float4* stats = reinterpret_cast<const float4*>(p.stats) + row * p.slices;
         float m = -INFINITY;
-        for (int i = lane; i < p.slices; i += 64) m = fmaxf(m, stats[4 * i]);
+        for (int i = lane; i < p.slices; i += 64) m = fmaxf(m, stats[i].x);
         m = lc_wave_max(m);
-        double s = 0.0, t = 0.0;
+        float s = 0.f, t = 0.f;
         for (int i = lane; i < p.slices; i += 64) {
-            const double shift = stats[4 * i] == -INFINITY ? 0.0 : (double)stats[4 * i] - (double)m;
-            const double f = exp(shift);
-            s += f * stats[4 * i + 1];
-            t += f * (stats[4 * i + 2] + shift * stats[4 * i + 1]);
+            const float4 a = stats[i];
+            const float shift = a.x == -INFINITY ? 0.f : (a.x - m) * kLog2e;      // (a slice without a value keeps its sums: 0, or NaN)
+            const float f = __builtin_amdgcn_exp2f(shift);
+            s = fmaf(f, a.y, s);
+            t = fmaf(f, fmaf(fmaxf(shift, kFar), a.y, a.z), t);
         }
-#pragma unroll
-        for (int off = 32; off > 0; off >>= 1) {
-            s += __shfl_xor(s, off, 64);
-            t += __shfl_xor(t, off, 64);
-        }
-        Row r;
-        if (lane == 0) r = finish_row<T>(p, row, m, s, t);
+        s = lc_wave_sum(s);
+        t = lc_wave_sum(t);
+        const Row r = finish_row<T>(p, row, m, s, t);
         if (p.top) {
-            r.m = __shfl(r.m, 0, 64);
-            r.log_s = __shfl(r.log_s, 0, 64);
             const Key* lists = p.keys + row * p.slices * p.top;
             const long long all = (long long)p.slices * p.top;
-            // slices * k keys are no smaller than the least of the lists' k-th ones
-            const int k = (p.top + p.slices - 1) / p.slices;
-            Key least = ~(Key)0;
-            for (int i = lane; i < p.slices; i += 64) least = min(least, lists[(long long)i * p.top + k - 1]);
-#pragma unroll
-            for (int off = 32; off > 0; off >>= 1) least = min(least, (Key)__shfl_xor(least, off, 64));
-            least = max(least, (Key)1);             // (0: a place left over)
-            auto count = [&](Key bound) __attribute__((always_inline)) {
-                int n = 0;
-                for (long long i = lane; i < all; i += 64) n += lists[i] >= bound;
-#pragma unroll
-                for (int off = 32; off > 0; off >>= 1) n += __shfl_xor(n, off, 64);
-                return n;
+            // every lane answers for k keys no smaller than its own: the k-th of a list, or the first of the largest of its lists
+            const int lanes = min(p.slices, 64), k = (p.top + lanes - 1) / lanes;
+            Key own = 0;
+            for (int i = lane; i < p.slices; i += 64) own = max(own, lists[(long long)i * p.top + k - 1]);
+            const uint32_t bound = lanes_bound((uint32_t)(own >> 32), own != 0, (p.top + k - 1) / k);
+            Key least = max((Key)bound << 32, (Key)1);
+            int held = 0;
+            auto gather = [&]() __attribute__((always_inline)) {
+                held = 0;
+                for (long long base = 0; base < all; base += 64) {
+                    const Key key = base + lane < all ? lists[base + lane] : 0;
+                    if (__ballot(key >= least)) held = append(keys, held, key >= least, key);
+                }
             };
-            int n = count(least);
-            Key hi = ~(Key)0;
-            while (n > kCandidates && hi - least > 1) {
-                const Key mid = least + ((hi - least) >> 1);
-                const int c = count(mid);
-                if (c >= p.top) {
-                    least = mid;
-                    n = c;
-                } else {
-                    hi = mid;
+            gather();
+            if (held > kCandidates) {
+                Key hi = ~(Key)0;
+                while (hi - least > 1) {
+                    const Key mid = least + ((hi - least) >> 1);
+                    int n = 0;
+                    for (long long base = 0; base < all; base += 64) n += __popcll(__ballot(base + lane < all && lists[base + lane] >= mid));
+                    if (n >= p.top) least = mid;
+                    else hi = mid;
+                    if (n >= p.top && n <= kCandidates) break;
                 }
-            }
-            if (lane == 0) held = 0;
-            __syncthreads();
-            for (long long i = lane; i < all; i += 64) {
-                const Key key = lists[i];
-                if (key >= least) {
-                    const int at = atomicAdd(&held, 1);
-                    if (at < kCandidates) keys[at] = key;
-                }
+                gather();
             }
             __syncthreads();
             rank_keys(keys, min(held, kCandidates), p.top, [&](int place, Key key) { put_alternative(p, row, place, key, r); });
@@ -317,17 +278,16 @@ struct TokenBwdArgs {
     const float* dlogprob;
     const float* dentropy;
     void* dz;
-    long long rows, ld, dld, units;
-    int vocab, parts;        // parts of 512 columns a row has
+    long long rows, ld, dld;
+    int vocab;
 };
 
 // One wave a block, eight columns a lane.
 template <typename T>
 __global__ void __launch_bounds__(64) token_bwd_kernel(const TokenBwdArgs p) {
-    for (long long unit = blockIdx.x; unit < p.units; unit += gridDim.x) {
-        const long long row = p.parts == 1 ? unit : unit / p.parts;
-        const int col = ((int)(unit - row * p.parts) * 64 + (int)threadIdx.x) * 8;
-        if (col >= p.vocab) continue;
+    const int col = (int)(blockIdx.x * 64 + threadIdx.x) * 8;
+    if (col >= p.vocab) return;
+    for (long long row = blockIdx.y; row < p.rows; row += gridDim.y) {
         Packed<T> v;
         lc_load8(v, static_cast<const T*>(p.z) + row * p.ld, col, p.vocab);
         const float lse = p.lse[row];
@@ -349,7 +309,7 @@ __global__ void __launch_bounds__(64) token_bwd_kernel(const TokenBwdArgs p) {
 }
 
 constexpr int kMostWidth = 1 << 30;
-constexpr long long kMostBlocks = 1 << 22;          // of 256 threads; more units are dealt round
+constexpr long long kMostBlocks = 1 << 25;          // of a wave (a launch holds fewer than 2^32 threads); rows beyond are dealt round
 
 lc_status check_desc(const lc_token_desc* d) {
     if (!d) return LC_ERR_NULL;
@@ -370,8 +330,8 @@ struct TokenPlan {
 // Even slices, so that no last one is short of values.
 TokenPlan plan_of(const lc_token_desc* d) {
     TokenPlan p;
-    p.chunks = d->vocab <= kThreads * 8 ? 1 : d->vocab <= kThreads * 16 ? 2 : 4;
-    const int most = kThreads * 8 * p.chunks;
+    p.chunks = d->vocab <= 512 ? 1 : d->vocab <= 1024 ? 2 : 4;
+    const int most = 512 * p.chunks;
     p.slices = (d->vocab + most - 1) / most;
     p.slice = ((d->vocab + p.slices - 1) / p.slices + 7) & ~7;
     p.slices = (d->vocab + p.slice - 1) / p.slice;
@@ -382,12 +342,17 @@ TokenPlan plan_of(const lc_token_desc* d) {
     return p;
 }
 
+// A block for every part of every row; as many rows as a grid's second dimension and kMostBlocks take, the others dealt round.
+dim3 grid_of(int parts, long long rows) {
+    return dim3((unsigned)parts, (unsigned)std::max(1ll, std::min<long long>({rows, 65535, kMostBlocks / parts})));
+}
+
 template <typename T, bool TOP>
 void launch_slices(const TokenArgs& a, int chunks, hipStream_t stream) {
-    const dim3 grid((unsigned)std::min(a.rows * a.slices, kMostBlocks));
-    if (chunks == 1) hipLaunchKernelGGL((token_slice_kernel<T, 1, TOP>), grid, dim3(kThreads), 0, stream, a);
-    else if (chunks == 2) hipLaunchKernelGGL((token_slice_kernel<T, 2, TOP>), grid, dim3(kThreads), 0, stream, a);
-    else hipLaunchKernelGGL((token_slice_kernel<T, 4, TOP>), grid, dim3(kThreads), 0, stream, a);
+    const dim3 grid = grid_of(a.slices, a.rows);
+    if (chunks == 1) hipLaunchKernelGGL((token_slice_kernel<T, 1, TOP>), grid, dim3(64), 0, stream, a);
+    else if (chunks == 2) hipLaunchKernelGGL((token_slice_kernel<T, 2, TOP>), grid, dim3(64), 0, stream, a);
+    else hipLaunchKernelGGL((token_slice_kernel<T, 4, TOP>), grid, dim3(64), 0, stream, a);
 }
 
 template <typename T>
@@ -442,9 +407,8 @@ extern "C" lc_status token_logprob_bwd(const lc_token_desc* desc, const void* lo
         lc_off_element(dlogprob, 4) || lc_off_element(dentropy, 4))
         return LC_ERR_ALIGN;
     TokenBwdArgs a{logits, tokens, lse, entropy, dlogprob, dentropy, dlogits, desc->rows, desc->ld ? desc->ld : desc->vocab,
-                   dlogits_ld ? dlogits_ld : desc->vocab, 0, desc->vocab, (desc->vocab + 511) / 512};
-    a.units = a.rows * a.parts;
-    const dim3 grid((unsigned)std::min(a.units, 4 * kMostBlocks));
+                   dlogits_ld ? dlogits_ld : desc->vocab, desc->vocab};
+    const dim3 grid = grid_of((desc->vocab + 511) / 512, a.rows);
     lc_begin_call();
     if (desc->dtype == LC_BF16) hipLaunchKernelGGL((token_bwd_kernel<uint16_t>), grid, dim3(64), 0, static_cast<hipStream_t>(hip_stream), a);
     else hipLaunchKernelGGL((token_bwd_kernel<float>), grid, dim3(64), 0, static_cast<hipStream_t>(hip_stream), a);
