@@ -56,25 +56,25 @@ __global__ void __launch_bounds__(WAVES * 64) rmsnorm_fwd_kernel(const NormArgs 
     __shared__ float red[2][2][WAVES];
     const int tid = threadIdx.x, c = p.c;
     const auto column = [tid](int i) { return (i * WAVES * 64 + tid) * 8; };
+    const bool full = c == CH * WAVES * 512;
     int parity = 0;
     for (long long row = blockIdx.x; row < p.rows; row += gridDim.x, parity ^= 1) {
         const T* x = static_cast<const T*>(p.x) + row * p.x_ld;
         Packed<T> px[CH], pr[CH];
         Packed<float> pg[CH];
         float h[CH][8];
-        lc_issue8(px, x, column, c);
+        lc_issue8(px, x, column, c, full);
         if (p.r) {
             const T* r = static_cast<const T*>(p.r) + row * p.r_ld;
-            lc_issue8(pr, r, column, c);
+            lc_issue8(pr, r, column, c, full);
         }
-        lc_issue8(pg, p.gamma, column, c);
+        lc_issue8(pg, p.gamma, column, c, full);
         float ss = 0.f;
+        lc_settle8(px, column, c, c, full);
+        if (p.r) lc_settle8(pr, column, c, c, full);
+        lc_settle8(pg, column, c, c, full);
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
-            const int col = column(i);
-            lc_settle8(px[i], col, c, c);
-            if (p.r) lc_settle8(pr[i], col, c, c);
-            lc_settle8(pg[i], col, c, c);
 #pragma unroll
             for (int j = 0; j < 8; ++j) h[i][j] = p.r ? lc_as_stored<T>(px[i].get(j) + pr[i].get(j)) : px[i].get(j);
 #pragma unroll
@@ -235,30 +235,29 @@ __global__ void __launch_bounds__(WAVES * 64) rmsnorm_bwd_kernel(const NormBwdAr
     __shared__ float red[2][WAVES];
     const int tid = threadIdx.x, c = p.c;
     const auto column = [tid](int i) { return (i * WAVES * 64 + tid) * 8; };
+    const bool full = c == CH * WAVES * 512;
     Packed<float> pg[CH];
     float acc[CH][8] = {};
-    lc_issue8(pg, p.gamma, column, c);
-#pragma unroll
-    for (int i = 0; i < CH; ++i) lc_settle8(pg[i], column(i), c, c);
+    lc_issue8(pg, p.gamma, column, c, full);
+    lc_settle8(pg, column, c, c, full);
     int parity = 0;
     for (long long row = blockIdx.x; row < p.rows; row += gridDim.x, parity ^= 1) {
         const T* h = static_cast<const T*>(p.h) + row * p.h_ld;
         const T* dy = static_cast<const T*>(p.dy) + row * (long long)c;
         Packed<T> ph[CH], pd[CH], pt[CH];
-        lc_issue8(ph, h, column, c);
-        lc_issue8(pd, dy, column, c);
+        lc_issue8(ph, h, column, c, full);
+        lc_issue8(pd, dy, column, c, full);
         if (p.dh) {
             const T* dh = static_cast<const T*>(p.dh) + row * (long long)c;
-            lc_issue8(pt, dh, column, c);
+            lc_issue8(pt, dh, column, c, full);
         }
         const float rstd = p.rstd[row];
         float s = 0.f;
+        lc_settle8(ph, column, c, c, full);
+        lc_settle8(pd, column, c, c, full);
+        if (p.dh) lc_settle8(pt, column, c, c, full);
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
-            const int col = column(i);
-            lc_settle8(ph[i], col, c, c);
-            lc_settle8(pd[i], col, c, c);
-            if (p.dh) lc_settle8(pt[i], col, c, c);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const float n = ph[i].get(j) * rstd, d = pd[i].get(j);

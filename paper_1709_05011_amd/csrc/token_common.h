@@ -9,6 +9,19 @@
 
 namespace {
 
+// 16 bytes at any element's alignment, past the caches' usual keeping with NT.
+typedef lc_u32x4 lc_u32x4_any __attribute__((aligned(2)));
+template <bool NT = false>
+__device__ __forceinline__ lc_u32x4 lc_load16(const void* p) {
+    if constexpr (NT) return __builtin_nontemporal_load(static_cast<const lc_u32x4_any*>(p));
+    else return *static_cast<const lc_u32x4_any*>(p);
+}
+template <bool NT = false>
+__device__ __forceinline__ void lc_store16(void* p, const lc_u32x4& v) {
+    if constexpr (NT) __builtin_nontemporal_store(v, static_cast<lc_u32x4_any*>(p));
+    else *static_cast<lc_u32x4_any*>(p) = v;
+}
+
 // Eight elements of a row as loaded.  Global accesses of 16 bytes need no alignment beyond the element's on gfx950 (the unaligned access mode that HSA code objects
 // run in).  shift(): drops the first k elements and fills up at the end.
 template <typename T>
@@ -16,9 +29,10 @@ struct Packed;
 template <>
 struct Packed<float> {
     lc_u32x4 a, b;
+    template <bool NT = false>
     __device__ __forceinline__ void load(const float* p) {
-        __builtin_memcpy(&a, p, 16);
-        __builtin_memcpy(&b, p + 4, 16);
+        a = lc_load16<NT>(p);
+        b = lc_load16<NT>(p + 4);
     }
     __device__ __forceinline__ void load_some(const float* p, int n, uint32_t fill) {
 #pragma unroll
@@ -48,7 +62,8 @@ struct Packed<float> {
 template <>
 struct Packed<uint16_t> {
     lc_u32x4 a;
-    __device__ __forceinline__ void load(const uint16_t* p) { __builtin_memcpy(&a, p, 16); }
+    template <bool NT = false>
+    __device__ __forceinline__ void load(const uint16_t* p) { a = lc_load16<NT>(p); }
     __device__ __forceinline__ void load_some(const uint16_t* p, int n, uint32_t fill) {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
@@ -69,47 +84,57 @@ struct Packed<uint16_t> {
 // Columns col(i) .. col(i) + 7 of a row of c for i < CH in two steps, so that all of a thread's loads are under way before the first is looked at: lc_issue8()
 // loads the row's last eight columns in place of what would pass its end (no branch, nothing outside the row), lc_settle8() moves those to their places and
 // puts `fill` (the type's own bits) where a column lies at `end` or past it; end is c, or a multiple of 8 before it.  Rows under eight columns, one
-// thread's at most, are read one by one.
-template <int CH, typename T, typename F>
-__device__ __forceinline__ void lc_issue8(Packed<T> (&to)[CH], const T* row, F&& col, int c, uint32_t fill = 0) {
-    if (c >= 8) {
+// thread's at most, are read one by one.  full (the same for a wave): every column asked for lies before `end`; the plain addresses are a quarter of the
+// instructions of the others.
+template <bool NT = false, int CH, typename T, typename F>
+__device__ __forceinline__ void lc_issue8(Packed<T> (&to)[CH], const T* row, F&& col, int c, bool full, uint32_t fill = 0) {
+    if (full) {
 #pragma unroll
-        for (int i = 0; i < CH; ++i) to[i].load(row + min(col(i), c - 8));
+        for (int i = 0; i < CH; ++i) to[i].template load<NT>(row + col(i));
+    } else if (c >= 8) {
+#pragma unroll
+        for (int i = 0; i < CH; ++i) to[i].template load<NT>(row + min(col(i), c - 8));
     } else {
         to[0].load_some(row + col(0), c - col(0), fill);
 #pragma unroll
         for (int i = 1; i < CH; ++i) to[i].shift(8, fill);
     }
 }
-template <typename T>
-__device__ __forceinline__ void lc_settle8(Packed<T>& to, int col, int c, int end, uint32_t fill = 0) {
-    if (end - col < 8 && c >= 8) to.shift(min(8 - (end - col), 8), fill);
+template <int CH, typename T, typename F>
+__device__ __forceinline__ void lc_settle8(Packed<T> (&to)[CH], F&& col, int c, int end, bool full, uint32_t fill = 0) {
+    if (full || c < 8) return;
+#pragma unroll
+    for (int i = 0; i < CH; ++i)
+        if (end - col(i) < 8) to[i].shift(min(8 - (end - col(i)), 8), fill);
 }
-template <typename T>
+template <bool NT = false, typename T>
 __device__ __forceinline__ void lc_load8(Packed<T>& to, const T* row, int col, int c) {
     Packed<T> one[1];
-    lc_issue8(one, row, [&](int) { return col; }, c);
+    const auto column = [&](int) { return col; };
+    lc_issue8<NT>(one, row, column, c, false);
+    lc_settle8(one, column, c, c, false);
     to = one[0];
-    lc_settle8(to, col, c, c);
 }
 
 // Eight results, rounded once.
+template <bool NT = false>
 __device__ __forceinline__ void lc_store8(float* p, const float* v, int n) {
     if (n >= 8) {
         const lc_u32x4 a = {__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
         const lc_u32x4 b = {__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])};
-        __builtin_memcpy(p, &a, 16);
-        __builtin_memcpy(p + 4, &b, 16);
+        lc_store16<NT>(p, a);
+        lc_store16<NT>(p + 4, b);
     } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
             if (j < n) p[j] = v[j];
     }
 }
+template <bool NT = false>
 __device__ __forceinline__ void lc_store8(uint16_t* p, const float* v, int n) {
     if (n >= 8) {
         const lc_u32x4 a = {lc_bf16x2_rne(v[0], v[1]), lc_bf16x2_rne(v[2], v[3]), lc_bf16x2_rne(v[4], v[5]), lc_bf16x2_rne(v[6], v[7])};
-        __builtin_memcpy(p, &a, 16);
+        lc_store16<NT>(p, a);
     } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j)

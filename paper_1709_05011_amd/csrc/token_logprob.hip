@@ -122,11 +122,127 @@ __device__ __forceinline__ void rank_keys(const Key* keys, int count, int top, F
     for (int i = count + lane; i < top; i += 64) emit(i, (Key)0);
 }
 
-// A wave a slice: 512 * CH values.  T is summed in units of log 2 from the exponentials' own arguments; a masked value makes it 0 * infinity there,
-// and such a slice sums again with the distances bounded (NaN and infinity among the logits come out NaN either way).
-template <typename T, int CH, bool TOP>
-__global__ void __launch_bounds__(64) token_slice_kernel(const TokenArgs p) {
-    __shared__ Key keys[TOP ? kCandidates : 1];
+// The sums of one slice or row by a wave, from memory and from the distances themselves: where they cannot be had from products with log2 e.
+template <typename T>
+__device__ __attribute__((noinline)) float3 sums_by_distances(const T* z, int first, int end) {
+    const int lane = threadIdx.x & 63;
+    float m = -INFINITY, s = 0.f, t = 0.f;
+    for (int i = first + lane; i < end; i += 64) m = fmaxf(m, as_float(z[i]));
+    m = lc_wave_max(m);
+    const float from = m == -INFINITY ? 0.f : m;
+    for (int i = first + lane; i < end; i += 64) {
+        const float d = (as_float(z[i]) - from) * kLog2e, e = __builtin_amdgcn_exp2f(d);
+        s += e;
+        t = fmaf(e, fmaxf(d, kFar), t);
+    }
+    return make_float3(m, lc_wave_sum(s), lc_wave_sum(t));
+}
+constexpr float kProductsEnd = 2.3e38f;      // largest magnitude whose product with log2 e is finite
+
+// Larger of three, a NaN ignored: without the instruction that the compiler puts before fmaxf() for each operand from memory, against signalling NaN
+// (one of those may cost a lane its maximum here; its row is NaN either way).
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+
+// What a lane has summed: S and T = sum e d over e = 2^d, d = z log2 e - ref, with ref the product m log2 e as rounded for the largest m so far.  One fused
+// multiply-add a value, exact to its rounding because ref is.  A masked value makes T 0 * infinity: the sum is then made again with the distance
+// bounded (NaN and infinity among the logits come out NaN either way).
+template <bool ENT>
+struct LaneSums {
+    float m = -INFINITY, ref = -INFINITY, s = 0.f, t = 0.f;      // (t only with ENT)
+
+    template <int N>
+    __device__ __forceinline__ void add(const float (&v)[N]) {
+        static_assert(N % 2 == 0, "in pairs");
+        float most = m;
+#pragma unroll
+        for (int j = 0; j < N; j += 2) most = max3(v[j], v[j + 1], most);
+        m = most;
+        const float now = fmaxf(ref, most * kLog2e), less = now == -INFINITY ? 0.f : -now;
+        const float shift = fmaxf(ref + less, kFar), f = __builtin_amdgcn_exp2f(ref + less);
+        if (ENT) t = f * fmaf(shift, s, t);
+        s *= f;
+        ref = now;
+        float ds = 0.f, dt = 0.f;
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const float d = fmaf(v[j], kLog2e, less), e = __builtin_amdgcn_exp2f(d);
+            ds += e;
+            if (ENT) dt = fmaf(e, d, dt);
+        }
+        if (ENT && __ballot(dt != dt)) {
+            dt = 0.f;
+            float again = less;
+            asm("" : "+v"(again));                 // (the first sum's terms are not kept in registers for this one)
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const float d = fmaf(v[j], kLog2e, again);
+                dt = fmaf(__builtin_amdgcn_exp2f(d), fmaxf(d, kFar), dt);
+            }
+        }
+        s += ds;
+        t += dt;
+    }
+
+    // The wave's m, S and T about m itself.
+    template <typename T>
+    __device__ __forceinline__ float3 join(const T* z, int first, int end) const {
+        const float all = lc_wave_max(m);
+        if (fabsf(all) > kProductsEnd && fabsf(all) < INFINITY) return sums_by_distances(z, first, end);
+        const float most = all * kLog2e, less = all == -INFINITY ? 0.f : -most;
+        const bool none = ref == -INFINITY;             // (a lane without a value keeps its sums: 0, or NaN)
+        const float shift = none ? 0.f : fmaxf(ref + less, kFar), f = none ? 1.f : __builtin_amdgcn_exp2f(ref + less);
+        const float ws = lc_wave_sum(f * s), wt = lc_wave_sum(f * fmaf(shift, s, t));
+        // every exponent is off by what rounding the product took
+        const float off = less == 0.f ? 0.f : fmaf(all, kLog2e, less), back = __builtin_amdgcn_exp2f(-off);
+        return make_float3(all, ws * back, fmaf(-off, ws, wt) * back);
+    }
+};
+
+// A wave a slice, in rounds of 512 * CH values, the next round's loads under way while one is summed.
+template <typename T, int CH, bool ENT>
+__global__ void __launch_bounds__(64) token_sums_kernel(const TokenArgs p) {
+    constexpr uint32_t kMaskedBits = sizeof(T) == 2 ? 0xff80u : 0xff800000u;
+    constexpr int kRound = 512 * CH;
+    const int lane = threadIdx.x, part = blockIdx.x;
+    const int first = part * p.slice, end = min(p.vocab - first, p.slice) + first;
+    for (long long row = blockIdx.y; row < p.rows; row += gridDim.y) {
+        const T* z = static_cast<const T*>(p.z) + row * p.ld;
+        LaneSums<ENT> sums;
+        Packed<T> a[CH], b[CH];
+        const auto issue = [&](Packed<T>(&to)[CH], int at) __attribute__((always_inline)) {
+            if (at < end) lc_issue8(to, z, [&](int i) { return at + (i * 64 + lane) * 8; }, p.vocab, at + kRound <= end, kMaskedBits);
+        };
+        const auto add = [&](Packed<T>(&from)[CH], int at) __attribute__((always_inline)) {
+            if (at >= end) return;
+            lc_settle8(from, [&](int i) { return at + (i * 64 + lane) * 8; }, p.vocab, end, at + kRound <= end, kMaskedBits);
+            float v[CH * 8];
+#pragma unroll
+            for (int i = 0; i < CH; ++i)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[8 * i + j] = from[i].get(j);
+            sums.add(v);
+        };
+        issue(a, first);
+        for (int at = first; at < end; at += 2 * kRound) {
+            issue(b, at + kRound);
+            add(a, at);
+            issue(a, at + 2 * kRound);
+            add(b, at + kRound);
+        }
+        const float3 w = sums.join(z, first, end);
+        if (p.slices == 1) finish_row<T>(p, row, w.x, w.y, w.z);
+        else if (lane == 0) *reinterpret_cast<float4*>(p.stats + (row * p.slices + part) * 4) = make_float4(w.x, w.y, w.z, 0.f);
+    }
+}
+
+// The same with the slice's alternatives, which its values stay in registers for: 512 * CH of them.
+template <typename T, int CH>
+__global__ void __launch_bounds__(64) token_top_kernel(const TokenArgs p) {
+    __shared__ Key keys[kCandidates];
     constexpr uint32_t kMaskedBits = sizeof(T) == 2 ? 0xff80u : 0xff800000u;
     const int lane = threadIdx.x, part = blockIdx.x;
     const int first = part * p.slice, end = min(p.vocab - first, p.slice) + first;
@@ -134,81 +250,54 @@ __global__ void __launch_bounds__(64) token_slice_kernel(const TokenArgs p) {
         const long long unit = row * p.slices + part;
         const T* z = static_cast<const T*>(p.z) + row * p.ld;
         Packed<T> packed[CH];
-        lc_issue8(packed, z, [&](int i) { return first + (i * 64 + lane) * 8; }, p.vocab, kMaskedBits);
-        float v[CH][8], most = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < CH; ++i) {
-            lc_settle8(packed[i], first + (i * 64 + lane) * 8, p.vocab, end, kMaskedBits);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                v[i][j] = packed[i].get(j);
-                most = fmaxf(most, v[i][j]);
-            }
-        }
-        const float m = lc_wave_max(most), from = m == -INFINITY ? 0.f : m, less = -from * kLog2e;
-        float s = 0.f, t = 0.f;
+        const auto column = [&](int i) { return first + (i * 64 + lane) * 8; };
+        const bool full = end - first == 512 * CH;
+        lc_issue8(packed, z, column, p.vocab, full, kMaskedBits);
+        lc_settle8(packed, column, p.vocab, end, full, kMaskedBits);
+        float v[CH * 8], most = -INFINITY;
 #pragma unroll
         for (int i = 0; i < CH; ++i)
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float d = fmaf(v[i][j], kLog2e, less);
-                const float e = __builtin_amdgcn_exp2f(d);
-                s += e;
-                t = fmaf(e, d, t);
+                v[8 * i + j] = packed[i].get(j);
+                most = fmaxf(most, v[8 * i + j]);
             }
-        if (__ballot(t != t)) {
-            t = 0.f;
+        LaneSums<true> sums;
+        sums.add(v);
+        const float3 w = sums.join(z, first, end);
+        Row r;
+        if (p.slices == 1) r = finish_row<T>(p, row, w.x, w.y, w.z);
+        else if (lane == 0) *reinterpret_cast<float4*>(p.stats + unit * 4) = make_float4(w.x, w.y, w.z, 0.f);
+
+        auto each = [&](auto&& f) __attribute__((always_inline)) {
 #pragma unroll
             for (int i = 0; i < CH; ++i)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float d = fmaf(v[i][j], kLog2e, less);
-                    t = fmaf(__builtin_amdgcn_exp2f(d), fmaxf(d, kFar), t);
-                }
-        }
-        s = lc_wave_sum(s);
-        t = lc_wave_sum(t);
-        // every exponent was off by what rounding m log2 e took: 2^off on all terms
-        const float off = fmaf(from, kLog2e, less), back = __builtin_amdgcn_exp2f(-off);
-        t = fmaf(-off, s, t) * back;
-        s *= back;
-        Row r;
-        if (p.slices == 1) {
-            r = finish_row<T>(p, row, m, s, t);
-        } else if (lane == 0) {
-            *reinterpret_cast<float4*>(p.stats + unit * 4) = make_float4(m, s, t, 0.f);
-        }
-        if constexpr (TOP) {
-            auto each = [&](auto&& f) __attribute__((always_inline)) {
-#pragma unroll
-                for (int i = 0; i < CH; ++i)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) f(v[i][j], first + (i * 64 + lane) * 8 + j);
-            };
-            const float bound = value_of(lanes_bound(order_of(most), listable(most), p.top));
-            int held = 0;
-            each([&](float x, int at) {
-                if (__ballot(x >= bound)) held = append(keys, held, x >= bound, key_of(x, at));
-            });
-            if (held > kCandidates) {
-                Key least = (Key)order_of(bound) << 32, hi = ~(Key)0;        // fewer than `top` keys reach hi, more than there is room for reach least
-                while (hi - least > 1) {
-                    const Key mid = least + ((hi - least) >> 1);
-                    int n = 0;
-                    each([&](float x, int at) { n += __popcll(__ballot(listable(x) && key_of(x, at) >= mid)); });
-                    if (n >= p.top) least = mid;
-                    else hi = mid;
-                    if (n >= p.top && n <= kCandidates) break;
-                }
-                held = 0;
-                each([&](float x, int at) { held = append(keys, held, listable(x) && key_of(x, at) >= least, key_of(x, at)); });
+                for (int j = 0; j < 8; ++j) f(v[8 * i + j], first + (i * 64 + lane) * 8 + j);
+        };
+        const float bound = value_of(lanes_bound(order_of(most), listable(most), p.top));
+        int held = 0;
+        each([&](float x, int at) {
+            if (__ballot(x >= bound)) held = append(keys, held, x >= bound, key_of(x, at));
+        });
+        if (held > kCandidates) {
+            Key least = (Key)order_of(bound) << 32, hi = ~(Key)0;        // fewer than `top` keys reach hi, more than there is room for reach least
+            while (hi - least > 1) {
+                const Key mid = least + ((hi - least) >> 1);
+                int n = 0;
+                each([&](float x, int at) { n += __popcll(__ballot(listable(x) && key_of(x, at) >= mid)); });
+                if (n >= p.top) least = mid;
+                else hi = mid;
+                if (n >= p.top && n <= kCandidates) break;
             }
-            __syncthreads();
-            const int count = min(held, kCandidates);
-            if (p.slices == 1) rank_keys(keys, count, p.top, [&](int place, Key k) { put_alternative(p, row, place, k, r); });
-            else rank_keys(keys, count, p.top, [&](int place, Key k) { p.keys[unit * p.top + place] = k; });
-            __syncthreads();
+            held = 0;
+            each([&](float x, int at) { held = append(keys, held, listable(x) && key_of(x, at) >= least, key_of(x, at)); });
         }
+        __syncthreads();
+        const int count = min(held, kCandidates);
+        if (p.slices == 1) rank_keys(keys, count, p.top, [&](int place, Key k) { put_alternative(p, row, place, k, r); });
+        else rank_keys(keys, count, p.top, [&](int place, Key k) { p.keys[unit * p.top + place] = k; });
+        __syncthreads();
     }
 }
 
@@ -282,29 +371,70 @@ struct TokenBwdArgs {
     int vocab;
 };
 
-// One wave a block, eight columns a lane.
+// Beyond these magnitudes the rounding of lse (2^-24 of it) shows in p: such a row's sums are made again by every wave of it.
 template <typename T>
+constexpr float kLseEnd = sizeof(T) == 2 ? 16384.f : 256.f;
+
+// One wave a block, CH times eight columns a lane, the rows from the last to the first: the forward pass read them in the other order, and what it left in the
+// memory-side cache is met before it is pushed out.  With d = (z - lse) log2 e the result is 2^d (A + B d): a fused multiply-add, an exponential, another
+// multiply-add and a product a value, the token's own term apart.
+template <typename T, int CH>
 __global__ void __launch_bounds__(64) token_bwd_kernel(const TokenBwdArgs p) {
-    const int col = (int)(blockIdx.x * 64 + threadIdx.x) * 8;
-    if (col >= p.vocab) return;
-    for (long long row = blockIdx.y; row < p.rows; row += gridDim.y) {
-        Packed<T> v;
-        lc_load8(v, static_cast<const T*>(p.z) + row * p.ld, col, p.vocab);
+    const int lane = threadIdx.x, first = blockIdx.x * 512 * CH;
+    const auto column = [&](int i) { return first + (i * 64 + lane) * 8; };
+    const bool full = first + 512 * CH <= p.vocab;
+    for (long long back = blockIdx.y; back < p.rows; back += gridDim.y) {
+        const long long row = p.rows - 1 - back;
+        const T* z = static_cast<const T*>(p.z) + row * p.ld;
+        Packed<T> v[CH];
+        lc_issue8(v, z, column, p.vocab, full);
         const float lse = p.lse[row];
         const int token = p.tokens[row];
         const bool empty = lse == -INFINITY, counts = token >= 0 && token < p.vocab;
         const float a = p.dlogprob && counts && !empty ? p.dlogprob[row] : 0.f;
         const float b = p.dentropy && !empty ? p.dentropy[row] : 0.f;
         const float ent = p.dentropy ? p.entropy[row] : 0.f;
-        float o[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float d = v.get(j) - lse;
-            const float e = __builtin_amdgcn_exp2f(d * kLog2e);
-            o[j] = empty ? 0.f : -e * (a + b * (fmaxf(d, kFar) + ent));
-            if (col + j == token) o[j] += a;
+        float from = lse, log_s = 0.f;
+        if (fabsf(lse) > kLseEnd<T> && !empty) {
+            const float3 w = sums_by_distances(z, 0, p.vocab);
+            from = w.x;
+            log_s = logf(w.y);
         }
-        lc_store8(static_cast<T*>(p.dz) + row * p.dld + col, o, p.vocab - col);
+        lc_settle8(v, column, p.vocab, p.vocab, full);
+        T* out = static_cast<T*>(p.dz) + row * p.dld;
+        // (as in the forward pass: every exponent is off by what rounding the product takes; with the row's log S it goes into the factors)
+        const bool far = fabsf(from) > kProductsEnd;
+        const float less = -from * kLog2e, off = far ? 0.f : fmaf(from, kLog2e, less) + log_s * kLog2e, scale = -__builtin_amdgcn_exp2f(-off);
+        const float A = scale * (a + b * (ent - off * kLn2)), B = scale * (b * kLn2);
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            const int col = column(i);
+            float o[8];
+            if (empty) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) o[j] = 0.f;
+            } else if (far) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float d = (v[i].get(j) - from) - log_s;
+                    o[j] = -__builtin_amdgcn_exp2f(d * kLog2e) * (a + b * (fmaxf(d, kFar) + ent));
+                }
+            } else if (b != 0.f) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float d = fmaf(v[i].get(j), kLog2e, less);
+                    o[j] = __builtin_amdgcn_exp2f(d) * fmaf(B, fmaxf(d, kFar), A);
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) o[j] = __builtin_amdgcn_exp2f(fmaf(v[i].get(j), kLog2e, less)) * A;
+            }
+            if (token >= col && token < col + 8) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) o[j] += col + j == token ? a : 0.f;
+            }
+            lc_store8<true>(out + col, o, full ? 8 : p.vocab - col);
+        }
     }
 }
 
@@ -327,12 +457,17 @@ struct TokenPlan {
     size_t stats, keys, total;
 };
 
-// Even slices, so that no last one is short of values.
+constexpr long long kUnits = 8192;                  // slices that fill the chip: rows are cut no finer than that takes
+
+// Even slices of whole rounds.
 TokenPlan plan_of(const lc_token_desc* d) {
     TokenPlan p;
     p.chunks = d->vocab <= 512 ? 1 : d->vocab <= 1024 ? 2 : 4;
-    const int most = 512 * p.chunks;
-    p.slices = (d->vocab + most - 1) / most;
+    const int round = 512 * p.chunks, rounds = (d->vocab + round - 1) / round;
+    int most = 1;                                   // rounds of a slice
+    if (d->top == 0)
+        while (most < rounds && d->rows * ((rounds + 2 * most - 1) / (2 * most)) >= kUnits) most *= 2;
+    p.slices = (rounds + most - 1) / most;
     p.slice = ((d->vocab + p.slices - 1) / p.slices + 7) & ~7;
     p.slices = (d->vocab + p.slice - 1) / p.slice;
     const size_t units = (size_t)d->rows * p.slices;
@@ -347,17 +482,23 @@ dim3 grid_of(int parts, long long rows) {
     return dim3((unsigned)parts, (unsigned)std::max(1ll, std::min<long long>({rows, 65535, kMostBlocks / parts})));
 }
 
-template <typename T, bool TOP>
-void launch_slices(const TokenArgs& a, int chunks, hipStream_t stream) {
-    const dim3 grid = grid_of(a.slices, a.rows);
-    if (chunks == 1) hipLaunchKernelGGL((token_slice_kernel<T, 1, TOP>), grid, dim3(64), 0, stream, a);
-    else if (chunks == 2) hipLaunchKernelGGL((token_slice_kernel<T, 2, TOP>), grid, dim3(64), 0, stream, a);
-    else hipLaunchKernelGGL((token_slice_kernel<T, 4, TOP>), grid, dim3(64), 0, stream, a);
+template <typename T, bool ENT>
+void launch_sums(const TokenArgs& a, int chunks, dim3 grid, hipStream_t stream) {
+    if (chunks == 1) hipLaunchKernelGGL((token_sums_kernel<T, 1, ENT>), grid, dim3(64), 0, stream, a);
+    else if (chunks == 2) hipLaunchKernelGGL((token_sums_kernel<T, 2, ENT>), grid, dim3(64), 0, stream, a);
+    else hipLaunchKernelGGL((token_sums_kernel<T, 4, ENT>), grid, dim3(64), 0, stream, a);
 }
 
 template <typename T>
 void launch_fwd(const TokenArgs& a, int chunks, hipStream_t stream) {
-    a.top ? launch_slices<T, true>(a, chunks, stream) : launch_slices<T, false>(a, chunks, stream);
+    const dim3 grid = grid_of(a.slices, a.rows), block(64);
+    if (a.top) {
+        if (chunks == 1) hipLaunchKernelGGL((token_top_kernel<T, 1>), grid, block, 0, stream, a);
+        else if (chunks == 2) hipLaunchKernelGGL((token_top_kernel<T, 2>), grid, block, 0, stream, a);
+        else hipLaunchKernelGGL((token_top_kernel<T, 4>), grid, block, 0, stream, a);
+    } else {
+        a.entropy ? launch_sums<T, true>(a, chunks, grid, stream) : launch_sums<T, false>(a, chunks, grid, stream);
+    }
     if (a.slices > 1) hipLaunchKernelGGL((token_join_kernel<T>), dim3((unsigned)std::min(a.rows, kMostBlocks)), dim3(64), 0, stream, a);
 }
 
@@ -408,9 +549,9 @@ extern "C" lc_status token_logprob_bwd(const lc_token_desc* desc, const void* lo
         return LC_ERR_ALIGN;
     TokenBwdArgs a{logits, tokens, lse, entropy, dlogprob, dentropy, dlogits, desc->rows, desc->ld ? desc->ld : desc->vocab,
                    dlogits_ld ? dlogits_ld : desc->vocab, desc->vocab};
-    const dim3 grid = grid_of((desc->vocab + 511) / 512, a.rows);
+    const dim3 grid = grid_of((desc->vocab + 1023) / 1024, a.rows);
     lc_begin_call();
-    if (desc->dtype == LC_BF16) hipLaunchKernelGGL((token_bwd_kernel<uint16_t>), grid, dim3(64), 0, static_cast<hipStream_t>(hip_stream), a);
-    else hipLaunchKernelGGL((token_bwd_kernel<float>), grid, dim3(64), 0, static_cast<hipStream_t>(hip_stream), a);
+    if (desc->dtype == LC_BF16) hipLaunchKernelGGL((token_bwd_kernel<uint16_t, 2>), grid, dim3(64), 0, static_cast<hipStream_t>(hip_stream), a);
+    else hipLaunchKernelGGL((token_bwd_kernel<float, 2>), grid, dim3(64), 0, static_cast<hipStream_t>(hip_stream), a);
     return lc_end_call();
 }
