@@ -407,8 +407,8 @@ typedef struct {
  * probabilities; both NULL if and only if top is 0.  Masked logits are -infinity: probability 0, no part in the entropy, never listed
  * (places left over hold token -1 and -infinity).  A row whose logits are all masked has lse -infinity, entropy 0, logprob -infinity
  * (0 where the token does not count).  A row with a NaN or +infinity has NaN in lse, entropy and log probabilities (a NaN is never listed).
- * logprob, entropy, lse: rows floats each; entropy may be NULL, and lse where no backward pass follows.  Sums are fp32 within a slice of a
- * row and double across slices; logprob is formed from the difference to the row's maximum, so that large logits do not cancel in it. */
+ * logprob, entropy, lse: rows floats each; entropy may be NULL, and lse where no backward pass follows.  Sums are
+ * fp32; logprob is formed from the difference to the row's maximum, so that large logits do not cancel in it. */
 size_t token_logprob_workspace_bytes(const lc_token_desc* desc);
 lc_status token_logprob_fwd(const lc_token_desc* desc, const void* logits, const int32_t* tokens, float* logprob, float* entropy, float* lse,
                             int32_t* top_tokens, float* top_logprobs, void* workspace, size_t workspace_bytes, void* hip_stream);
@@ -417,7 +417,8 @@ lc_status token_logprob_fwd(const lc_token_desc* desc, const void* logits, const
  * be NULL for zero, not both):
  *     dlogits_j = dlogprob * ([j = token] - p_j) - dentropy * p_j * (log p_j + entropy).
  * lse and entropy: what the forward pass gave (entropy may be NULL without dentropy).  dlogprob has no effect where the token does not
- * count; masked logits, and rows that are masked entirely, get 0.  p_j is formed from lse as stored (relative error about |lse| 2^-24).  dlogits_ld: elements from row to row (0: vocab; otherwise >= vocab; the pad is
+ * count; masked logits, and rows that are masked entirely, get 0.  p_j is formed from lse as stored (relative error about |lse| 2^-24)
+ * while |lse| is at most 256 (fp32 logits) or 16384 (bf16); rows beyond are summed again by every 1024 columns of theirs (right, and slow).  dlogits_ld: elements from row to row (0: vocab; otherwise >= vocab; the pad is
  * not written).  dlogits may be the logits' own buffer if its ld is theirs; otherwise they must not overlap. */
 lc_status token_logprob_bwd(const lc_token_desc* desc, const void* logits, const int32_t* tokens, const float* lse, const float* entropy,
                             const float* dlogprob, const float* dentropy, void* dlogits, int64_t dlogits_ld, void* hip_stream);

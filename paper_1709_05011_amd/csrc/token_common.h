@@ -23,7 +23,8 @@ __device__ __forceinline__ void lc_store16(void* p, const lc_u32x4& v) {
 }
 
 // Eight elements of a row as loaded.  Global accesses of 16 bytes need no alignment beyond the element's on gfx950 (the unaligned access mode that HSA code objects
-// run in).  shift(): drops the first k elements and fills up at the end.
+// run in).  load_some(): the first n one by one, in a loop of few instructions (a short call's time goes by the code it has to fetch, too); shift(): drops the
+// first k elements and fills up at the end.
 template <typename T>
 struct Packed;
 template <>
@@ -35,10 +36,11 @@ struct Packed<float> {
         b = lc_load16<NT>(p + 4);
     }
     __device__ __forceinline__ void load_some(const float* p, int n, uint32_t fill) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            a[j] = j < n ? __float_as_uint(p[j]) : fill;
-            b[j] = j + 4 < n ? __float_as_uint(p[j + 4]) : fill;
+        a = b = lc_u32x4{fill, fill, fill, fill};
+#pragma unroll 1
+        for (int j = min(n, 8) - 1; j >= 0; --j) {
+            b = lc_u32x4{a[3], b[0], b[1], b[2]};
+            a = lc_u32x4{__float_as_uint(p[j]), a[0], a[1], a[2]};
         }
     }
     __device__ __forceinline__ void shift(int k, uint32_t fill) {
@@ -65,9 +67,12 @@ struct Packed<uint16_t> {
     template <bool NT = false>
     __device__ __forceinline__ void load(const uint16_t* p) { a = lc_load16<NT>(p); }
     __device__ __forceinline__ void load_some(const uint16_t* p, int n, uint32_t fill) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            a[j] = (2 * j < n ? (uint32_t)p[2 * j] : fill) | (2 * j + 1 < n ? (uint32_t)p[2 * j + 1] : fill) << 16;
+        const uint32_t f = fill | fill << 16;
+        a = lc_u32x4{f, f, f, f};
+#pragma unroll 1
+        for (int j = min(n, 8) - 1; j >= 0; --j)
+            a = lc_u32x4{a[0] << 16 | p[j], __builtin_amdgcn_alignbit(a[1], a[0], 16), __builtin_amdgcn_alignbit(a[2], a[1], 16),
+                         __builtin_amdgcn_alignbit(a[3], a[2], 16)};
     }
     __device__ __forceinline__ void shift(int k, uint32_t fill) {
         const uint32_t f = fill | fill << 16;
@@ -116,29 +121,35 @@ __device__ __forceinline__ void lc_load8(Packed<T>& to, const T* row, int col, i
     to = one[0];
 }
 
-// Eight results, rounded once.
+// The first n of eight results (none for n <= 0), rounded once.
 template <bool NT = false>
 __device__ __forceinline__ void lc_store8(float* p, const float* v, int n) {
+    lc_u32x4 a = {__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+    lc_u32x4 b = {__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])};
     if (n >= 8) {
-        const lc_u32x4 a = {__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
-        const lc_u32x4 b = {__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])};
         lc_store16<NT>(p, a);
         lc_store16<NT>(p + 4, b);
     } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (j < n) p[j] = v[j];
+#pragma unroll 1
+        for (int j = 0; j < n; ++j) {
+            p[j] = __uint_as_float(a[0]);
+            a = lc_u32x4{a[1], a[2], a[3], b[0]};
+            b = lc_u32x4{b[1], b[2], b[3], 0u};
+        }
     }
 }
 template <bool NT = false>
 __device__ __forceinline__ void lc_store8(uint16_t* p, const float* v, int n) {
+    lc_u32x4 a = {lc_bf16x2_rne(v[0], v[1]), lc_bf16x2_rne(v[2], v[3]), lc_bf16x2_rne(v[4], v[5]), lc_bf16x2_rne(v[6], v[7])};
     if (n >= 8) {
-        const lc_u32x4 a = {lc_bf16x2_rne(v[0], v[1]), lc_bf16x2_rne(v[2], v[3]), lc_bf16x2_rne(v[4], v[5]), lc_bf16x2_rne(v[6], v[7])};
         lc_store16<NT>(p, a);
     } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (j < n) p[j] = lc_bf16_rne(v[j]);
+#pragma unroll 1
+        for (int j = 0; j < n; ++j) {
+            p[j] = (uint16_t)a[0];
+            a = lc_u32x4{__builtin_amdgcn_alignbit(a[1], a[0], 16), __builtin_amdgcn_alignbit(a[2], a[1], 16), __builtin_amdgcn_alignbit(a[3], a[2], 16),
+                         a[3] >> 16};
+        }
     }
 }
 
@@ -170,6 +181,17 @@ __device__ __forceinline__ float lc_wave_sum(float x) {
 }
 __device__ __forceinline__ float lc_wave_max(float x) {
     return lc_wave_join(x, -INFINITY, [](float a, float b) { return fmaxf(a, b); });
+}
+__device__ __forceinline__ uint32_t lc_wave_umax(uint32_t x) {
+    // (a float's operations would lose unsigned numbers that are no floats')
+    const auto step = [](uint32_t a, uint32_t b) { return a > b ? a : b; };
+    x = step(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xB1, 0xf, 0xf, false));
+    x = step(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x4E, 0xf, 0xf, false));
+    x = step(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x141, 0xf, 0xf, false));
+    x = step(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x140, 0xf, 0xf, false));
+    x = step(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xa, 0xf, false));
+    x = step(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, false));
+    return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
 }
 // Over a block of WAVES waves, every thread with the result; `red` (WAVES floats) must not be in use by an earlier call that a slower wave may still read.
 template <int WAVES>

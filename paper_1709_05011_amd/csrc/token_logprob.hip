@@ -21,6 +21,7 @@
 namespace {
 
 constexpr int kMostTop = 32;
+constexpr int kMostWaves = 4;               // of a block
 constexpr int kCandidates = 256;            // keys that a wave's LDS has room for
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kFar = -150.f;              // 2^-150 is 0 in fp32: distances are no longer than this where 0 * infinity would be formed
@@ -35,10 +36,10 @@ struct TokenArgs {
     float* lse;              // or null
     int32_t* top_tokens;
     float* top_logprobs;
-    float* stats;            // [rows][slices][4]: m, S, T (T in units of log 2, as the slices' own exponentials)
-    Key* keys;               // [rows][slices][top], falling; 0 where a slice has fewer
+    float4* stats;           // [rows][blocks]: m, S, T (T in units of log 2, as the exponentials' own arguments)
+    Key* keys;               // [rows][blocks][top], falling; 0 where a block has fewer
     long long rows, ld;
-    int vocab, top, slices, slice;      // slice: values of one, a multiple of 8
+    int vocab, top, blocks, slice;      // blocks of a row; values of a block, a multiple of 8
 };
 
 // order-preserving map of floats to unsigned; both zeros alike
@@ -60,18 +61,26 @@ struct Row {
     float m, log_s;          // maximum (0 where there is none) and log S
 };
 
-// What a row gives but for its alternatives, from its m, S and T; a whole wave with the same values, lane 0 writes.
+struct Target {              // a row's token and its logit, asked for before the row's sums are known
+    bool counts;
+    float z;
+};
 template <typename T>
-__device__ __forceinline__ Row finish_row(const TokenArgs& p, long long row, float m, float s, float t) {
+__device__ __forceinline__ Target target_of(const TokenArgs& p, long long row) {
     const int token = p.tokens[row];
-    const bool counts = token >= 0 && token < p.vocab, empty = s == 0.f;
-    const float z = counts ? as_float<T>(static_cast<const T*>(p.z)[row * p.ld + token]) : 0.f;
+    const bool counts = token >= 0 && token < p.vocab;
+    return {counts, counts ? as_float<T>(static_cast<const T*>(p.z)[row * p.ld + token]) : 0.f};
+}
+
+// What a row gives but for its alternatives, from its m, S and T; a whole wave with the same values, lane 0 writes.
+__device__ __forceinline__ Row finish_row(const TokenArgs& p, long long row, const Target& target, float3 w) {
+    const bool empty = w.y == 0.f;
     Row r;
-    r.m = m == -INFINITY ? 0.f : m;
-    r.log_s = logf(s);
+    r.m = w.x == -INFINITY ? 0.f : w.x;
+    r.log_s = logf(w.y);
     if ((threadIdx.x & 63) == 0) {
-        p.logprob[row] = !counts ? 0.f : empty ? -INFINITY : (z - r.m) - r.log_s;
-        if (p.entropy) p.entropy[row] = empty ? 0.f : r.log_s - kLn2 * (t / s);
+        p.logprob[row] = !target.counts ? 0.f : empty ? -INFINITY : (target.z - r.m) - r.log_s;
+        if (p.entropy) p.entropy[row] = empty ? 0.f : r.log_s - kLn2 * (w.z / w.y);
         if (p.lse) p.lse[row] = empty ? -INFINITY : r.m + r.log_s;
     }
     return r;
@@ -84,15 +93,15 @@ __device__ __forceinline__ void put_alternative(const TokenArgs& p, long long ro
 
 // Order of a value that at least `need` lanes of the wave reach with theirs, and few more; the least of all values where fewer lanes hold one.
 __device__ __forceinline__ uint32_t lanes_bound(uint32_t mine, bool holds, int need) {
-    uint32_t lo = 0x00800000u;                        // order of the lowest finite float
-    if (__popcll(__ballot(holds)) < need) return lo;
-    uint32_t hi = 0xff800001u;                        // above the order of infinity
-    while (hi - lo > 1) {
+    const int holders = __popcll(__ballot(holds));
+    if (holders < need) return 0x00800000u;           // order of the lowest finite float
+    uint32_t lo = ~lc_wave_umax(holds ? ~mine : 0u), hi = lc_wave_umax(holds ? mine : 0u) + 1;      // every holder reaches lo, none hi
+    for (int n = holders; n > need + need / 4 && hi - lo > 1;) {
         const uint32_t mid = lo + ((hi - lo) >> 1);
-        const int n = __popcll(__ballot(holds && mine >= mid));
-        if (n >= need) {
+        const int c = __popcll(__ballot(holds && mine >= mid));
+        if (c >= need) {
             lo = mid;
-            if (n <= need + need / 4) break;
+            n = c;
         } else {
             hi = mid;
         }
@@ -122,19 +131,86 @@ __device__ __forceinline__ void rank_keys(const Key* keys, int count, int top, F
     for (int i = count + lane; i < top; i += 64) emit(i, (Key)0);
 }
 
-// The sums of one slice or row by a wave, from memory and from the distances themselves: where they cannot be had from products with log2 e.
+// (m, S, T) of n parts, by a wave.
+__device__ __forceinline__ float3 join_sums(const float4* stats, int n) {
+    const int lane = threadIdx.x & 63;
+    const float4 own = lane < n ? stats[lane] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+    float m = own.x;
+    for (int i = lane + 64; i < n; i += 64) m = fmaxf(m, stats[i].x);
+    m = lc_wave_max(m);
+    float s = 0.f, t = 0.f;
+    for (int i = lane; i < n; i += 64) {
+        const float4 a = i == lane ? own : stats[i];
+        const float shift = a.x == -INFINITY ? 0.f : (a.x - m) * kLog2e;      // (a part without a value keeps its sums: 0, or NaN)
+        const float f = __builtin_amdgcn_exp2f(shift);
+        s = fmaf(f, a.y, s);
+        t = fmaf(f, fmaf(fmaxf(shift, kFar), a.y, a.z), t);
+    }
+    return make_float3(m, lc_wave_sum(s), lc_wave_sum(t));
+}
+
+// The `top` largest keys of n falling lists of `top`, by a wave; `keys`: kCandidates in LDS.  A lane answers for k keys no smaller than its own: the k-th of
+// its list, or the first of the largest of its lists; then every list is walked from its head while its keys reach the bound that follows.
+template <typename F>
+__device__ __forceinline__ void join_lists(const Key* lists, int n, int top, Key* keys, F&& emit) {
+    constexpr int kHead = 4;
+    const int lane = threadIdx.x & 63, lanes = min(n, 64), k = (top + lanes - 1) / lanes;
+    Key head[kHead], own = 0;
+#pragma unroll
+    for (int j = 0; j < kHead; ++j) head[j] = lane < n && j < top ? lists[(long long)lane * top + j] : 0;
+    for (int i = lane; i < n; i += 64) own = max(own, i == lane && k == 1 ? head[0] : lists[(long long)i * top + k - 1]);
+    Key least = max((Key)lanes_bound((uint32_t)(own >> 32), own != 0, (top + k - 1) / k) << 32, (Key)1);
+    int held = 0;
+    const auto gather = [&]() __attribute__((always_inline)) {
+        held = 0;
+        for (int base = 0; base < n; base += 64) {
+            const Key* list = lists + (long long)(base + lane) * top;
+            int j = 0;
+            if (base == 0) {
+#pragma unroll
+                for (; j < kHead; ++j) held = append(keys, held, head[j] >= least, head[j]);
+            }
+            for (; j < top; ++j) {
+                const Key key = base + lane < n ? list[j] : 0;
+                if (!__ballot(key >= least)) break;
+                held = append(keys, held, key >= least, key);
+            }
+        }
+    };
+    gather();
+    if (held > kCandidates) {
+        const long long all = (long long)n * top;
+        Key hi = ~(Key)0;                           // fewer than `top` keys reach hi, more than there is room for reach least
+        while (hi - least > 1) {
+            const Key mid = least + ((hi - least) >> 1);
+            int c = 0;
+            for (long long base = 0; base < all; base += 64) c += __popcll(__ballot(base + lane < all && lists[base + lane] >= mid));
+            if (c >= top) least = mid;
+            else hi = mid;
+            if (c >= top && c <= kCandidates) break;
+        }
+        gather();
+    }
+    __builtin_amdgcn_wave_barrier();
+    rank_keys(keys, min(held, kCandidates), top, emit);
+}
+
+// The sums by a wave of columns [first, first + span) of each `stride` up to `end`, from memory and from the distances themselves: where they cannot be had from
+// products with log2 e.
 template <typename T>
-__device__ __attribute__((noinline)) float3 sums_by_distances(const T* z, int first, int end) {
+__device__ __attribute__((noinline)) float3 sums_by_distances(const T* z, int first, int span, int stride, int end) {
     const int lane = threadIdx.x & 63;
     float m = -INFINITY, s = 0.f, t = 0.f;
-    for (int i = first + lane; i < end; i += 64) m = fmaxf(m, as_float(z[i]));
+    for (int at = first; at < end; at += stride)
+        for (int i = at + lane; i < min(at + span, end); i += 64) m = fmaxf(m, as_float(z[i]));
     m = lc_wave_max(m);
     const float from = m == -INFINITY ? 0.f : m;
-    for (int i = first + lane; i < end; i += 64) {
-        const float d = (as_float(z[i]) - from) * kLog2e, e = __builtin_amdgcn_exp2f(d);
-        s += e;
-        t = fmaf(e, fmaxf(d, kFar), t);
-    }
+    for (int at = first; at < end; at += stride)
+        for (int i = at + lane; i < min(at + span, end); i += 64) {
+            const float d = (as_float(z[i]) - from) * kLog2e, e = __builtin_amdgcn_exp2f(d);
+            s += e;
+            t = fmaf(e, fmaxf(d, kFar), t);
+        }
     return make_float3(m, lc_wave_sum(s), lc_wave_sum(t));
 }
 constexpr float kProductsEnd = 2.3e38f;      // largest magnitude whose product with log2 e is finite
@@ -189,9 +265,9 @@ struct LaneSums {
 
     // The wave's m, S and T about m itself.
     template <typename T>
-    __device__ __forceinline__ float3 join(const T* z, int first, int end) const {
+    __device__ __forceinline__ float3 join(const T* z, int first, int span, int stride, int end) const {
         const float all = lc_wave_max(m);
-        if (fabsf(all) > kProductsEnd && fabsf(all) < INFINITY) return sums_by_distances(z, first, end);
+        if (fabsf(all) > kProductsEnd && fabsf(all) < INFINITY) return sums_by_distances(z, first, span, stride, end);
         const float most = all * kLog2e, less = all == -INFINITY ? 0.f : -most;
         const bool none = ref == -INFINITY;             // (a lane without a value keeps its sums: 0, or NaN)
         const float shift = none ? 0.f : fmaxf(ref + less, kFar), f = none ? 1.f : __builtin_amdgcn_exp2f(ref + less);
@@ -202,23 +278,53 @@ struct LaneSums {
     }
 };
 
-// A wave a slice, in rounds of 512 * CH values, the next round's loads under way while one is summed.
-template <typename T, int CH, bool ENT>
-__global__ void __launch_bounds__(64) token_sums_kernel(const TokenArgs p) {
+// What a block of the forward pass has joined goes to the results, or, of a row in several blocks, to the workspace.
+template <bool TOP>
+__device__ __forceinline__ void leave(const TokenArgs& p, long long row, const Target& target, float3 w, const Key* lists, int n, Key* keys, bool ranked) {
+    const long long unit = row * p.blocks + blockIdx.x;
+    const int lane = threadIdx.x & 63;
+    Row r;
+    if (p.blocks == 1) r = finish_row(p, row, target, w);
+    else if (lane == 0) p.stats[unit] = make_float4(w.x, w.y, w.z, 0.f);
+    if constexpr (TOP) {
+        const auto emit = [&](int place, Key k) {
+            if (p.blocks == 1) put_alternative(p, row, place, k, r);
+            else p.keys[unit * p.top + place] = k;
+        };
+        if (ranked) join_lists(lists, n, p.top, keys, emit);
+        else rank_keys(keys, n, p.top, emit);
+    }
+}
+
+// A slice of a row by a block of up to kMostWaves waves, whose first joins what the others leave in LDS.  Rounds of 512 * CH values go to the waves in turn, so that a
+// block reads one stretch at a time; a wave's next round is under way while one is summed.  ENT: with the entropy.  TOP: with the alternatives: the slice is read a second time, from
+// the caches, for what reaches the bound that its lanes' maxima give; LDS: kCandidates keys a wave and its list of `top`.
+template <typename T, int CH, bool ENT, bool TOP>
+__global__ void __launch_bounds__(kMostWaves * 64) token_sums_kernel(const TokenArgs p) {
+    __shared__ float4 stats[kMostWaves];
+    extern __shared__ __align__(16) char lds[];
     constexpr uint32_t kMaskedBits = sizeof(T) == 2 ? 0xff80u : 0xff800000u;
     constexpr int kRound = 512 * CH;
-    const int lane = threadIdx.x, part = blockIdx.x;
-    const int first = part * p.slice, end = min(p.vocab - first, p.slice) + first;
+    const int lane = threadIdx.x & 63, waves = blockDim.x >> 6, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int part = (int)blockIdx.x * p.slice, end = min(p.vocab - part, p.slice) + part;
+    const int first = min(part + wave * kRound, end), stride = waves * kRound;
+    Key* keys = TOP ? reinterpret_cast<Key*>(lds) + wave * kCandidates : nullptr;
+    Key* lists = TOP ? reinterpret_cast<Key*>(lds) + waves * kCandidates : nullptr;
     for (long long row = blockIdx.y; row < p.rows; row += gridDim.y) {
         const T* z = static_cast<const T*>(p.z) + row * p.ld;
+        Target target;
+        if (wave == 0 && p.blocks == 1) target = target_of<T>(p, row);
         LaneSums<ENT> sums;
-        Packed<T> a[CH], b[CH];
+        Packed<T> now[CH], next[CH];
+        const auto column = [&](int at) __attribute__((always_inline)) { return [at, lane](int i) { return at + (i * 64 + lane) * 8; }; };
         const auto issue = [&](Packed<T>(&to)[CH], int at) __attribute__((always_inline)) {
-            if (at < end) lc_issue8(to, z, [&](int i) { return at + (i * 64 + lane) * 8; }, p.vocab, at + kRound <= end, kMaskedBits);
+            if (at < end) lc_issue8(to, z, column(at), p.vocab, at + kRound <= end, kMaskedBits);
+        };
+        const auto settle = [&](Packed<T>(&of)[CH], int at) __attribute__((always_inline)) {
+            lc_settle8(of, column(at), p.vocab, end, at + kRound <= end, kMaskedBits);
         };
         const auto add = [&](Packed<T>(&from)[CH], int at) __attribute__((always_inline)) {
-            if (at >= end) return;
-            lc_settle8(from, [&](int i) { return at + (i * 64 + lane) * 8; }, p.vocab, end, at + kRound <= end, kMaskedBits);
+            settle(from, at);
             float v[CH * 8];
 #pragma unroll
             for (int i = 0; i < CH; ++i)
@@ -226,136 +332,80 @@ __global__ void __launch_bounds__(64) token_sums_kernel(const TokenArgs p) {
                 for (int j = 0; j < 8; ++j) v[8 * i + j] = from[i].get(j);
             sums.add(v);
         };
-        issue(a, first);
-        for (int at = first; at < end; at += 2 * kRound) {
-            issue(b, at + kRound);
-            add(a, at);
-            issue(a, at + 2 * kRound);
-            add(b, at + kRound);
+        issue(now, first);
+        for (int at = first; at < end; at += 2 * stride) {
+            issue(next, at + stride);
+            add(now, at);
+            issue(now, at + 2 * stride);
+            if (at + stride < end) add(next, at + stride);
         }
-        const float3 w = sums.join(z, first, end);
-        if (p.slices == 1) finish_row<T>(p, row, w.x, w.y, w.z);
-        else if (lane == 0) *reinterpret_cast<float4*>(p.stats + (row * p.slices + part) * 4) = make_float4(w.x, w.y, w.z, 0.f);
-    }
-}
-
-// The same with the slice's alternatives, which its values stay in registers for: 512 * CH of them.
-template <typename T, int CH>
-__global__ void __launch_bounds__(64) token_top_kernel(const TokenArgs p) {
-    __shared__ Key keys[kCandidates];
-    constexpr uint32_t kMaskedBits = sizeof(T) == 2 ? 0xff80u : 0xff800000u;
-    const int lane = threadIdx.x, part = blockIdx.x;
-    const int first = part * p.slice, end = min(p.vocab - first, p.slice) + first;
-    for (long long row = blockIdx.y; row < p.rows; row += gridDim.y) {
-        const long long unit = row * p.slices + part;
-        const T* z = static_cast<const T*>(p.z) + row * p.ld;
-        Packed<T> packed[CH];
-        const auto column = [&](int i) { return first + (i * 64 + lane) * 8; };
-        const bool full = end - first == 512 * CH;
-        lc_issue8(packed, z, column, p.vocab, full, kMaskedBits);
-        lc_settle8(packed, column, p.vocab, end, full, kMaskedBits);
-        float v[CH * 8], most = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < CH; ++i)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                v[8 * i + j] = packed[i].get(j);
-                most = fmaxf(most, v[8 * i + j]);
-            }
-        LaneSums<true> sums;
-        sums.add(v);
-        const float3 w = sums.join(z, first, end);
-        Row r;
-        if (p.slices == 1) r = finish_row<T>(p, row, w.x, w.y, w.z);
-        else if (lane == 0) *reinterpret_cast<float4*>(p.stats + unit * 4) = make_float4(w.x, w.y, w.z, 0.f);
-
-        auto each = [&](auto&& f) __attribute__((always_inline)) {
-#pragma unroll
-            for (int i = 0; i < CH; ++i)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) f(v[8 * i + j], first + (i * 64 + lane) * 8 + j);
-        };
-        const float bound = value_of(lanes_bound(order_of(most), listable(most), p.top));
+        float3 w = sums.join(z, first, kRound, stride, end);
         int held = 0;
-        each([&](float x, int at) {
-            if (__ballot(x >= bound)) held = append(keys, held, x >= bound, key_of(x, at));
-        });
-        if (held > kCandidates) {
-            Key least = (Key)order_of(bound) << 32, hi = ~(Key)0;        // fewer than `top` keys reach hi, more than there is room for reach least
-            while (hi - least > 1) {
-                const Key mid = least + ((hi - least) >> 1);
-                int n = 0;
-                each([&](float x, int at) { n += __popcll(__ballot(listable(x) && key_of(x, at) >= mid)); });
-                if (n >= p.top) least = mid;
-                else hi = mid;
-                if (n >= p.top && n <= kCandidates) break;
-            }
-            held = 0;
-            each([&](float x, int at) { held = append(keys, held, listable(x) && key_of(x, at) >= least, key_of(x, at)); });
-        }
-        __syncthreads();
-        const int count = min(held, kCandidates);
-        if (p.slices == 1) rank_keys(keys, count, p.top, [&](int place, Key k) { put_alternative(p, row, place, k, r); });
-        else rank_keys(keys, count, p.top, [&](int place, Key k) { p.keys[unit * p.top + place] = k; });
-        __syncthreads();
-    }
-}
-
-// Joins a row's slices: one wave a row.
-template <typename T>
-__global__ void __launch_bounds__(64) token_join_kernel(const TokenArgs p) {
-    __shared__ Key keys[kCandidates];
-    const int lane = threadIdx.x;
-    for (long long row = blockIdx.x; row < p.rows; row += gridDim.x) {
-        const float4* stats = reinterpret_cast<const float4*>(p.stats) + row * p.slices;
-        float m = -INFINITY;
-        for (int i = lane; i < p.slices; i += 64) m = fmaxf(m, stats[i].x);
-        m = lc_wave_max(m);
-        float s = 0.f, t = 0.f;
-        for (int i = lane; i < p.slices; i += 64) {
-            const float4 a = stats[i];
-            const float shift = a.x == -INFINITY ? 0.f : (a.x - m) * kLog2e;      // (a slice without a value keeps its sums: 0, or NaN)
-            const float f = __builtin_amdgcn_exp2f(shift);
-            s = fmaf(f, a.y, s);
-            t = fmaf(f, fmaf(fmaxf(shift, kFar), a.y, a.z), t);
-        }
-        s = lc_wave_sum(s);
-        t = lc_wave_sum(t);
-        const Row r = finish_row<T>(p, row, m, s, t);
-        if (p.top) {
-            const Key* lists = p.keys + row * p.slices * p.top;
-            const long long all = (long long)p.slices * p.top;
-            // every lane answers for k keys no smaller than its own: the k-th of a list, or the first of the largest of its lists
-            const int lanes = min(p.slices, 64), k = (p.top + lanes - 1) / lanes;
-            Key own = 0;
-            for (int i = lane; i < p.slices; i += 64) own = max(own, lists[(long long)i * p.top + k - 1]);
-            const uint32_t bound = lanes_bound((uint32_t)(own >> 32), own != 0, (p.top + k - 1) / k);
-            Key least = max((Key)bound << 32, (Key)1);
-            int held = 0;
-            auto gather = [&]() __attribute__((always_inline)) {
-                held = 0;
-                for (long long base = 0; base < all; base += 64) {
-                    const Key key = base + lane < all ? lists[base + lane] : 0;
-                    if (__ballot(key >= least)) held = append(keys, held, key >= least, key);
+        if constexpr (TOP) {
+            const uint32_t order = lanes_bound(order_of(sums.m), listable(sums.m), p.top);
+            const float bound = value_of(order);
+            const auto look = [&](Packed<T>& from, int col) __attribute__((always_inline)) {
+                float most = from.get(0);
+#pragma unroll
+                for (int j = 1; j < 7; j += 2) most = max3(from.get(j), from.get(j + 1), most);
+                if (!__ballot(most >= bound || from.get(7) >= bound)) return;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float x = from.get(j);
+                    if (__ballot(x >= bound)) held = append(keys, held, x >= bound, key_of(x, col + j));
                 }
             };
-            gather();
+            for (int at = first; at < end; at += stride) {
+                issue(now, at);
+                settle(now, at);
+#pragma unroll
+                for (int i = 0; i < CH; ++i) look(now[i], column(at)(i));
+            }
             if (held > kCandidates) {
-                Key hi = ~(Key)0;
+                Key least = (Key)order << 32, hi = ~(Key)0;        // fewer than `top` keys reach hi, more than there is room for reach least
+                const auto each = [&](auto&& f) __attribute__((always_inline)) {
+                    for (int at = first; at < end; at += stride)
+                        for (int i = at + lane; i < at + kRound; i += 64) {
+                            const float x = i < end ? as_float(z[i]) : -INFINITY;
+                            f(listable(x), key_of(x, i));
+                        }
+                };
                 while (hi - least > 1) {
                     const Key mid = least + ((hi - least) >> 1);
                     int n = 0;
-                    for (long long base = 0; base < all; base += 64) n += __popcll(__ballot(base + lane < all && lists[base + lane] >= mid));
+                    each([&](bool is, Key k) { n += __popcll(__ballot(is && k >= mid)); });
                     if (n >= p.top) least = mid;
                     else hi = mid;
                     if (n >= p.top && n <= kCandidates) break;
                 }
-                gather();
+                held = 0;
+                each([&](bool is, Key k) { held = append(keys, held, is && k >= least, k); });
             }
-            __syncthreads();
-            rank_keys(keys, min(held, kCandidates), p.top, [&](int place, Key key) { put_alternative(p, row, place, key, r); });
-            __syncthreads();
+            held = min(held, kCandidates);
+            __builtin_amdgcn_wave_barrier();
         }
+        if (waves == 1) {
+            leave<TOP>(p, row, target, w, nullptr, held, keys, false);
+            if (TOP) __syncthreads();
+            continue;
+        }
+        if constexpr (TOP) rank_keys(keys, held, p.top, [&](int place, Key k) { lists[wave * p.top + place] = k; });
+        if (lane == 0) stats[wave] = make_float4(w.x, w.y, w.z, 0.f);
+        __syncthreads();
+        if (wave == 0) leave<TOP>(p, row, target, join_sums(stats, waves), lists, waves, keys, true);
+        __syncthreads();
+    }
+}
+
+// Joins the blocks of a row: a wave a row.
+template <typename T>
+__global__ void __launch_bounds__(64) token_join_kernel(const TokenArgs p) {
+    __shared__ Key keys[kCandidates];
+    for (long long row = blockIdx.x; row < p.rows; row += gridDim.x) {
+        const Target target = target_of<T>(p, row);
+        const Row r = finish_row(p, row, target, join_sums(p.stats + row * p.blocks, p.blocks));
+        if (p.top) join_lists(p.keys + row * p.blocks * p.top, p.blocks, p.top, keys, [&](int place, Key k) { put_alternative(p, row, place, k, r); });
+        __syncthreads();
     }
 }
 
@@ -396,7 +446,7 @@ __global__ void __launch_bounds__(64) token_bwd_kernel(const TokenBwdArgs p) {
         const float ent = p.dentropy ? p.entropy[row] : 0.f;
         float from = lse, log_s = 0.f;
         if (fabsf(lse) > kLseEnd<T> && !empty) {
-            const float3 w = sums_by_distances(z, 0, p.vocab);
+            const float3 w = sums_by_distances(z, 0, p.vocab, p.vocab, p.vocab);
             from = w.x;
             log_s = logf(w.y);
         }
@@ -439,7 +489,7 @@ __global__ void __launch_bounds__(64) token_bwd_kernel(const TokenBwdArgs p) {
 }
 
 constexpr int kMostWidth = 1 << 30;
-constexpr long long kMostBlocks = 1 << 25;          // of a wave (a launch holds fewer than 2^32 threads); rows beyond are dealt round
+constexpr long long kMostThreads = 1ll << 31;       // of a launch, which has to hold fewer than 2^32
 
 lc_status check_desc(const lc_token_desc* d) {
     if (!d) return LC_ERR_NULL;
@@ -453,53 +503,40 @@ lc_status check_desc(const lc_token_desc* d) {
 }
 
 struct TokenPlan {
-    int chunks, slices, slice;
-    size_t stats, keys, total;
+    int chunks, waves, blocks, slice;      // chunks: of 512 values, of a wave's round; waves of a block, blocks of a row, values of a block
+    size_t keys, total;
 };
 
-constexpr long long kUnits = 8192;                  // slices that fill the chip: rows are cut no finer than that takes
+constexpr long long kFillWaves = 16384, kFillTop = 2048;      // waves that rows are cut into
 
-// Even slices of whole rounds.
 TokenPlan plan_of(const lc_token_desc* d) {
     TokenPlan p;
-    p.chunks = d->vocab <= 512 ? 1 : d->vocab <= 1024 ? 2 : 4;
+    p.chunks = d->vocab <= 512 ? 1 : 2;
     const int round = 512 * p.chunks, rounds = (d->vocab + round - 1) / round;
-    int most = 1;                                   // rounds of a slice
-    if (d->top == 0)
-        while (most < rounds && d->rows * ((rounds + 2 * most - 1) / (2 * most)) >= kUnits) most *= 2;
-    p.slices = (rounds + most - 1) / most;
-    p.slice = ((d->vocab + p.slices - 1) / p.slices + 7) & ~7;
-    p.slices = (d->vocab + p.slice - 1) / p.slice;
-    const size_t units = (size_t)d->rows * p.slices;
-    p.stats = 0;
-    p.keys = p.slices == 1 ? 0 : (units * 16 + 255) & ~(size_t)255;
-    p.total = p.slices == 1 ? 0 : p.keys + ((units * d->top * sizeof(Key) + 255) & ~(size_t)255);
+    int most = 1;                                      // rounds of a wave
+    while (most < rounds && d->rows * ((rounds + 2 * most - 1) / (2 * most)) >= (d->top ? kFillTop : kFillWaves)) most *= 2;
+    const int waves = (rounds + most - 1) / most;      // of a row
+    p.blocks = waves > kMostWaves ? waves : 1;
+    p.waves = (waves + p.blocks - 1) / p.blocks;
+    p.slice = ((d->vocab + p.blocks - 1) / p.blocks + 7) & ~7;
+    const size_t units = (size_t)d->rows * p.blocks;
+    p.keys = p.blocks == 1 ? 0 : (units * sizeof(float4) + 255) & ~(size_t)255;
+    p.total = p.blocks == 1 ? 0 : p.keys + ((units * d->top * sizeof(Key) + 255) & ~(size_t)255);
     return p;
 }
 
-// A block for every part of every row; as many rows as a grid's second dimension and kMostBlocks take, the others dealt round.
-dim3 grid_of(int parts, long long rows) {
-    return dim3((unsigned)parts, (unsigned)std::max(1ll, std::min<long long>({rows, 65535, kMostBlocks / parts})));
+// A block for every part of every row; as many rows as a grid's second dimension and kMostThreads take, the others dealt round.
+dim3 grid_of(int parts, long long rows, int threads) {
+    return dim3((unsigned)parts, (unsigned)std::max(1ll, std::min<long long>({rows, 65535, kMostThreads / threads / parts})));
 }
 
-template <typename T, bool ENT>
-void launch_sums(const TokenArgs& a, int chunks, dim3 grid, hipStream_t stream) {
-    if (chunks == 1) hipLaunchKernelGGL((token_sums_kernel<T, 1, ENT>), grid, dim3(64), 0, stream, a);
-    else if (chunks == 2) hipLaunchKernelGGL((token_sums_kernel<T, 2, ENT>), grid, dim3(64), 0, stream, a);
-    else hipLaunchKernelGGL((token_sums_kernel<T, 4, ENT>), grid, dim3(64), 0, stream, a);
-}
-
-template <typename T>
-void launch_fwd(const TokenArgs& a, int chunks, hipStream_t stream) {
-    const dim3 grid = grid_of(a.slices, a.rows), block(64);
-    if (a.top) {
-        if (chunks == 1) hipLaunchKernelGGL((token_top_kernel<T, 1>), grid, block, 0, stream, a);
-        else if (chunks == 2) hipLaunchKernelGGL((token_top_kernel<T, 2>), grid, block, 0, stream, a);
-        else hipLaunchKernelGGL((token_top_kernel<T, 4>), grid, block, 0, stream, a);
-    } else {
-        a.entropy ? launch_sums<T, true>(a, chunks, grid, stream) : launch_sums<T, false>(a, chunks, grid, stream);
-    }
-    if (a.slices > 1) hipLaunchKernelGGL((token_join_kernel<T>), dim3((unsigned)std::min(a.rows, kMostBlocks)), dim3(64), 0, stream, a);
+template <typename T, int CH>
+void launch_fwd(const TokenArgs& a, int waves, hipStream_t stream) {
+    const dim3 grid = grid_of(a.blocks, a.rows, waves * 64), block(waves * 64);
+    if (a.top) hipLaunchKernelGGL((token_sums_kernel<T, CH, true, true>), grid, block, waves * (kCandidates + a.top) * sizeof(Key), stream, a);
+    else if (a.entropy) hipLaunchKernelGGL((token_sums_kernel<T, CH, true, false>), grid, block, 0, stream, a);
+    else hipLaunchKernelGGL((token_sums_kernel<T, CH, false, false>), grid, block, 0, stream, a);
+    if (a.blocks > 1) hipLaunchKernelGGL((token_join_kernel<T>), dim3((unsigned)std::min(a.rows, kMostThreads / 64)), dim3(64), 0, stream, a);
 }
 
 }  // namespace
@@ -524,12 +561,13 @@ extern "C" lc_status token_logprob_fwd(const lc_token_desc* desc, const void* lo
     const TokenPlan plan = plan_of(desc);
     if (plan.total && (!workspace || (((uintptr_t)workspace) & 255) || workspace_bytes < plan.total)) return LC_ERR_WORKSPACE;
     char* base = static_cast<char*>(workspace);
-    TokenArgs a{logits, tokens, logprob, entropy, lse, top_tokens, top_logprobs, plan.total ? reinterpret_cast<float*>(base + plan.stats) : nullptr,
+    TokenArgs a{logits, tokens, logprob, entropy, lse, top_tokens, top_logprobs, plan.total ? reinterpret_cast<float4*>(base) : nullptr,
                 plan.total ? reinterpret_cast<Key*>(base + plan.keys) : nullptr, desc->rows, desc->ld ? desc->ld : desc->vocab, desc->vocab, desc->top,
-                plan.slices, plan.slice};
+                plan.blocks, plan.slice};
     lc_begin_call();
-    if (desc->dtype == LC_BF16) launch_fwd<uint16_t>(a, plan.chunks, static_cast<hipStream_t>(hip_stream));
-    else launch_fwd<float>(a, plan.chunks, static_cast<hipStream_t>(hip_stream));
+    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    if (desc->dtype == LC_BF16) plan.chunks == 1 ? launch_fwd<uint16_t, 1>(a, plan.waves, stream) : launch_fwd<uint16_t, 2>(a, plan.waves, stream);
+    else plan.chunks == 1 ? launch_fwd<float, 1>(a, plan.waves, stream) : launch_fwd<float, 2>(a, plan.waves, stream);
     return lc_end_call();
 }
 
@@ -549,7 +587,7 @@ extern "C" lc_status token_logprob_bwd(const lc_token_desc* desc, const void* lo
         return LC_ERR_ALIGN;
     TokenBwdArgs a{logits, tokens, lse, entropy, dlogprob, dentropy, dlogits, desc->rows, desc->ld ? desc->ld : desc->vocab,
                    dlogits_ld ? dlogits_ld : desc->vocab, desc->vocab};
-    const dim3 grid = grid_of((desc->vocab + 1023) / 1024, a.rows);
+    const dim3 grid = grid_of((desc->vocab + 1023) / 1024, a.rows, 64);
     lc_begin_call();
     if (desc->dtype == LC_BF16) hipLaunchKernelGGL((token_bwd_kernel<uint16_t, 2>), grid, dim3(64), 0, static_cast<hipStream_t>(hip_stream), a);
     else hipLaunchKernelGGL((token_bwd_kernel<float, 2>), grid, dim3(64), 0, static_cast<hipStream_t>(hip_stream), a);

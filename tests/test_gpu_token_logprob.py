@@ -156,6 +156,39 @@ def test_backward(kind, rows, vocab, parts):
     assert np.all(np.abs(dz - want) <= half * (1 + half) * np.abs(want) + (1 + half) * bound)
 
 
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab", [7, 700, 9001])
+def test_rows_far_from_zero_and_rows_of_the_lowest_value(kind, vocab):
+    """Where products with log2 e overflow (the type's lowest and highest value) and where lse as stored says little (|lse| of 3e4 to 3e38): log p stays
+    what the differences of the logits give.  On such rows p is exp(d - log S) with d exact or rounded once, so that the gradient is within tol + 4|d| u of it,
+    and half a unit of lse's own size where it is formed from lse: 2^-24 * 256 in fp32, 2^-24 * 16384 in bf16."""
+    dtype, t, half = TYPES[kind]
+    low, high = float(torch.finfo(t).min), float(torch.finfo(t).max)
+    place = np.arange(vocab, dtype=np.float64)
+    z = np.stack([np.full(vocab, low), np.where(place % 3 == 0, low, place % 5), np.where(place == 2, high, low), -3e4 - place % 7, 250.0 + place % 4, 7e3 + place % 4,
+                  np.where(place < 3, -np.inf, low)])
+    z = torch.from_numpy(z).to(t).to(gu.DEV)
+    rows = z.shape[0]
+    t64 = np.array([vocab // 2] * rows)
+    tokens = gu.dev(t64.astype(np.int32))
+    d, (lp, ent, lse), ids, lps = run(dtype, z, tokens, vocab, 3)
+    in_range = lambda a: np.where(np.abs(a) > np.finfo(np.float32).max, np.copysign(np.inf, a), a)      # (the highest above the lowest: beyond fp32)
+    check_forward(vocab, (d, (lp, ent, lse), ids, lps), [in_range(a) for a in ops.token_logprob(f64(z), t64, 3)], 3)
+    d, (lp2, ent2, lse2), _, _ = run(dtype, z, tokens, vocab)
+    check_forward(vocab, (d, (lp2, ent2, lse2), None, None), [in_range(a) for a in ops.token_logprob(f64(z), t64, 0)], 0)
+    dz, one = torch.empty_like(z), torch.ones(rows, device=gu.DEV)
+    lc.token_logprob_bwd(d, z, tokens, lse, ent, one, 0.5 * one, dz)
+    torch.cuda.synchronize()
+    w64, e64, _, _, _ = ops.token_logprob(f64(z), t64)
+    m = np.max(f64(z), axis=1, keepdims=True)
+    logp = (f64(z) - m) - np.log(np.sum(np.exp(f64(z) - m), axis=1, keepdims=True))
+    p, fine = np.exp(logp), np.where(np.exp(logp) > 0, logp, 0.0)
+    want = (place == vocab // 2) - p - 0.5 * p * (fine + e64[:, None])
+    rel = tol(vocab) * (2 + e64[:, None]) + U * (4 * np.abs(fine) + (16384 if kind == "bf16" else 256))
+    bound = p * (1.5 + np.abs(fine) + e64[:, None]) * rel + 2 * U
+    assert np.all(np.abs(f64(dz) - want) <= half * (1 + half) * np.abs(want) + (1 + half) * bound)
+
+
 def test_the_gradient_against_differences():
     """Central differences of the float64 sum over the kernel's own forward outputs, fp32: a step of 2^-6 keeps its rounding under 1e-3."""
     z = synth.normal((2, 50), 6)
