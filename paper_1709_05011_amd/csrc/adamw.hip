@@ -16,11 +16,9 @@
 
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kWavePart = 256;                                   // elements of a wave
-constexpr int kChunk = kWavePart * (kThreads / 64);
+constexpr int kPart = 256;                                       // elements of a wave, four a lane
 constexpr int kTable = 176;                                      // descriptors per launch (13.4 KB of launch arguments)
-static_assert(kWavePart == ADAMW_Q8_BLOCK, "a wave makes a block's scale by itself");
+static_assert(kPart == ADAMW_Q8_BLOCK, "a wave makes a block's scale by itself");
 
 struct AdamTensor {
     float* w;
@@ -67,8 +65,75 @@ __device__ __forceinline__ uint32_t e5m2_dithered(float x, uint32_t r) {
 
 __device__ __forceinline__ float finite_size(float x) { return fabsf(x) < INFINITY ? fabsf(x) : 0.f; }
 
-template <typename G, bool Q8>
-__global__ void __launch_bounds__(kThreads) adamw_kernel(const AdamArgs p) {
+// Four neighbouring elements at any element's alignment, the first n of them (none for n <= 0; what is not read is 0).
+template <bool NT>
+__device__ __forceinline__ void load4(float* to, const float* p, int n) {
+    lc_u32x4 x = {};
+    if (n >= 4) x = lc_load16<NT>(p);
+    else
+        for (int j = 0; j < 4; ++j)
+            if (j < n) x[j] = __float_as_uint(p[j]);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) to[j] = __uint_as_float(x[j]);
+}
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef u32x2 u32x2_any __attribute__((aligned(2)));
+typedef uint32_t u32_any __attribute__((aligned(1)));
+template <bool NT>
+__device__ __forceinline__ void load4(float* to, const uint16_t* p, int n) {
+    u32x2 x = {};
+    if (n >= 4) {
+        if constexpr (NT) x = __builtin_nontemporal_load(reinterpret_cast<const u32x2_any*>(p));
+        else x = *reinterpret_cast<const u32x2_any*>(p);
+    } else {
+        for (int j = 0; j < 4; ++j)
+            if (j < n) x[j >> 1] |= (uint32_t)p[j] << (16 * (j & 1));
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) to[j] = __uint_as_float(j & 1 ? x[j >> 1] & 0xffff0000u : x[j >> 1] << 16);
+}
+template <bool NT>
+__device__ __forceinline__ uint32_t load4(const uint8_t* p, int n) {
+    uint32_t x = 0;
+    if (n >= 4) {
+        if constexpr (NT) return __builtin_nontemporal_load(reinterpret_cast<const u32_any*>(p));
+        else return *reinterpret_cast<const u32_any*>(p);
+    }
+    for (int j = 0; j < 4; ++j)
+        if (j < n) x |= (uint32_t)p[j] << (8 * j);
+    return x;
+}
+template <bool NT>
+__device__ __forceinline__ void store4(float* p, const float* v, int n) {
+    const lc_u32x4 x = {__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+    if (n >= 4) lc_store16<NT>(p, x);
+    else
+        for (int j = 0; j < 4; ++j)
+            if (j < n) p[j] = v[j];
+}
+__device__ __forceinline__ void store4(uint16_t* p, const float* v, int n) {       // (read by the next step's products: an ordinary store)
+    const u32x2 x = {lc_bf16x2_rne(v[0], v[1]), lc_bf16x2_rne(v[2], v[3])};
+    if (n >= 4) *reinterpret_cast<u32x2_any*>(p) = x;
+    else
+        for (int j = 0; j < 4; ++j)
+            if (j < n) p[j] = (uint16_t)(x[j >> 1] >> (16 * (j & 1)));
+}
+template <bool NT>
+__device__ __forceinline__ void store4(uint8_t* p, uint32_t x, int n) {
+    if (n >= 4) {
+        if constexpr (NT) __builtin_nontemporal_store(x, reinterpret_cast<u32_any*>(p));
+        else *reinterpret_cast<u32_any*>(p) = x;
+    } else {
+        for (int j = 0; j < 4; ++j)
+            if (j < n) p[j] = (uint8_t)(x >> (8 * j));
+    }
+}
+
+// One vector a thread, so that the chip works on one narrow stretch of each array at a time.  NT: accesses past the caches' usual keeping, for lists that the
+// caches do not hold.  Blocks of one wave; of four where a tensor's arrays do not start on whole lines of 128 bytes: a line that two waves fill is then
+// mostly filled within one unit's cache and not by two dies' (201 million parameters with 8-bit states 4 bytes off a line, us: waves by themselves 737, four 617; on it 540 and 580).
+template <typename G, bool Q8, bool NT, int WAVES>
+__global__ void __launch_bounds__(WAVES * 64) adamw_kernel(const AdamArgs p) {
 #pragma clang fp contract(off)
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const float gs = p.grad_scale ? *p.grad_scale : 1.f;
@@ -79,53 +144,17 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const AdamArgs p) {
             const int at = i + lane;
             owner += __popcll(__ballot(at < p.count && p.start[at < kTable ? at : 0] <= chunk));
         }
-        const AdamTensor& t = p.t[__builtin_amdgcn_readfirstlane(owner)];
-        const long long block = (long long)(chunk - p.start[__builtin_amdgcn_readfirstlane(owner)]) * (kThreads / 64) + wave;
-        const long long first = block * kWavePart, at = first + lane * 4;
-        if (first >= t.numel) continue;
-        const long long left = t.numel - at;
+        owner = __builtin_amdgcn_readfirstlane(owner);
+        const AdamTensor& t = p.t[owner];
+        const long long block = (long long)(chunk - p.start[owner]) * WAVES + wave;
+        if (block * kPart >= t.numel) continue;
+        const long long at = block * kPart + lane * 4, left = t.numel - at;
         const int n = left < 4 ? (int)left : 4;                       // this lane's elements; none or fewer than none past the end
         float w[4], g[4], m[4], v[4];
-        const float* tw = t.w + at;
-        const G* tg = static_cast<const G*>(t.g) + at;
-        if (n == 4) {
-            lc_u32x4 x;
-            __builtin_memcpy(&x, tw, 16);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) w[j] = __uint_as_float(x[j]);
-            if constexpr (sizeof(G) == 2) {
-                uint32_t h[2];
-                __builtin_memcpy(h, tg, 8);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) g[j] = __uint_as_float(j & 1 ? h[j >> 1] & 0xffff0000u : h[j >> 1] << 16);
-            } else {
-                __builtin_memcpy(&x, tg, 16);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) g[j] = __uint_as_float(x[j]);
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                w[j] = j < n ? tw[j] : 0.f;
-                if constexpr (sizeof(G) == 2) g[j] = j < n ? __uint_as_float((uint32_t)tg[j] << 16) : 0.f;
-                else g[j] = j < n ? tg[j] : 0.f;
-            }
-        }
+        load4<NT>(w, t.w + at, n);
+        load4<NT>(g, static_cast<const G*>(t.g) + at, n);
         if constexpr (Q8) {
-            const uint8_t* tm = static_cast<const uint8_t*>(t.m) + at;
-            const uint8_t* tv = static_cast<const uint8_t*>(t.v) + at;
-            uint32_t cm = 0, cv = 0;
-            if (n == 4) {
-                __builtin_memcpy(&cm, tm, 4);
-                __builtin_memcpy(&cv, tv, 4);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (j < n) {
-                        cm |= (uint32_t)tm[j] << (8 * j);
-                        cv |= (uint32_t)tv[j] << (8 * j);
-                    }
-            }
+            const uint32_t cm = load4<NT>(static_cast<const uint8_t*>(t.m) + at, n), cv = load4<NT>(static_cast<const uint8_t*>(t.v) + at, n);
             const float ms = t.m_scale[block], vs = t.v_scale[block];
             m[0] = __builtin_amdgcn_cvt_f32_fp8((int)cm, 0) * ms;
             m[1] = __builtin_amdgcn_cvt_f32_fp8((int)cm, 1) * ms;
@@ -136,50 +165,21 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const AdamArgs p) {
             v[2] = __builtin_amdgcn_cvt_f32_bf8((int)cv, 2) * vs;
             v[3] = __builtin_amdgcn_cvt_f32_bf8((int)cv, 3) * vs;
         } else {
-            const float* tm = static_cast<const float*>(t.m) + at;
-            const float* tv = static_cast<const float*>(t.v) + at;
-            if (n == 4) {
-                lc_u32x4 x, y;
-                __builtin_memcpy(&x, tm, 16);
-                __builtin_memcpy(&y, tv, 16);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    m[j] = __uint_as_float(x[j]);
-                    v[j] = __uint_as_float(y[j]);
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    m[j] = j < n ? tm[j] : 0.f;
-                    v[j] = j < n ? tv[j] : 0.f;
-                }
-            }
+            load4<NT>(m, static_cast<const float*>(t.m) + at, n);
+            load4<NT>(v, static_cast<const float*>(t.v) + at, n);
         }
+        // m and v by separately rounded products and sums (their bits are defined so); the update by the instructions for roots and reciprocals, one unit in the
+        // last place each
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const float x = g[j] * gs;
             m[j] = p.b1 * m[j] + p.one_b1 * x;
             v[j] = p.b2 * v[j] + p.one_b2 * (x * x);
-            const float root = sqrtf(v[j]) * p.inv_root_c2 + p.eps;
-            w[j] = w[j] - t.lr_decay * w[j] - p.step_size * (m[j] / root);
+            const float root = fmaf(__builtin_amdgcn_sqrtf(v[j]), p.inv_root_c2, p.eps);
+            w[j] = fmaf(-p.step_size, m[j] * __builtin_amdgcn_rcpf(root), fmaf(-t.lr_decay, w[j], w[j]));
         }
-        float* ow = t.w + at;
-        uint16_t* ol = t.w_lowp ? t.w_lowp + at : nullptr;
-        if (n == 4) {
-            const lc_u32x4 x = {__float_as_uint(w[0]), __float_as_uint(w[1]), __float_as_uint(w[2]), __float_as_uint(w[3])};
-            __builtin_memcpy(ow, &x, 16);
-            if (ol) {
-                const uint32_t h[2] = {lc_bf16x2_rne(w[0], w[1]), lc_bf16x2_rne(w[2], w[3])};
-                __builtin_memcpy(ol, h, 8);
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (j < n) {
-                    ow[j] = w[j];
-                    if (ol) ol[j] = lc_bf16_rne(w[j]);
-                }
-        }
+        store4<NT>(t.w + at, w, n);
+        if (t.w_lowp) store4(t.w_lowp + at, w, n);
         if constexpr (Q8) {
             float am = 0.f, av = 0.f;
 #pragma unroll
@@ -204,40 +204,16 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const AdamArgs p) {
                 const uint32_t code = x < INFINITY ? e5m2_dithered(x, dither21(number + j)) : 0x7fu;
                 cv |= code << (8 * j);
             }
-            uint8_t* om = static_cast<uint8_t*>(t.m) + at;
-            uint8_t* ov = static_cast<uint8_t*>(t.v) + at;
-            if (n == 4) {
-                __builtin_memcpy(om, &cm, 4);
-                __builtin_memcpy(ov, &cv, 4);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (j < n) {
-                        om[j] = (uint8_t)((uint32_t)cm >> (8 * j));
-                        ov[j] = (uint8_t)(cv >> (8 * j));
-                    }
-            }
+            store4<NT>(static_cast<uint8_t*>(t.m) + at, (uint32_t)cm, n);
+            store4<NT>(static_cast<uint8_t*>(t.v) + at, cv, n);
         } else {
-            float* om = static_cast<float*>(t.m) + at;
-            float* ov = static_cast<float*>(t.v) + at;
-            if (n == 4) {
-                const lc_u32x4 x = {__float_as_uint(m[0]), __float_as_uint(m[1]), __float_as_uint(m[2]), __float_as_uint(m[3])};
-                const lc_u32x4 y = {__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
-                __builtin_memcpy(om, &x, 16);
-                __builtin_memcpy(ov, &y, 16);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (j < n) {
-                        om[j] = m[j];
-                        ov[j] = v[j];
-                    }
-            }
+            store4<NT>(static_cast<float*>(t.m) + at, m, n);
+            store4<NT>(static_cast<float*>(t.v) + at, v, n);
         }
     }
 }
 
-constexpr int kMostBlocks = 1 << 23;      // of 256 threads: a launch holds fewer than 2^32
+constexpr int kMostBlocks = 1 << 24;      // of a wave: a launch holds fewer than 2^32 threads
 
 struct AdamList {                          // what both entry points take
     int n;
@@ -259,7 +235,7 @@ struct AdamList {                          // what both entry points take
     void* const* w_lowp;
 };
 
-long long chunks_of(int64_t numel) { return numel / kChunk + (numel % kChunk != 0); }
+long long chunks_of(int64_t numel, int waves) { return numel / (kPart * waves) + (numel % (kPart * waves) != 0); }
 
 lc_status check_list(const AdamList& a, bool q8) {
     if (a.n < 0) return LC_ERR_SHAPE;
@@ -269,7 +245,7 @@ lc_status check_list(const AdamList& a, bool q8) {
     if (!a.w || !a.g || !a.m || !a.v || !a.numel || (q8 && (!a.m_scale || !a.v_scale))) return LC_ERR_NULL;
     if (lc_off_element(a.grad_scale, 4)) return LC_ERR_ALIGN;
     for (int l = 0; l < a.n; ++l) {
-        if (a.numel[l] < 0 || a.numel[l] > (int64_t)1 << 40) return LC_ERR_SHAPE;
+        if (a.numel[l] < 0 || a.numel[l] > (int64_t)1 << 38) return LC_ERR_SHAPE;
         if (a.numel[l] == 0) continue;
         if (!a.w[l] || !a.g[l] || !a.m[l] || !a.v[l] || (q8 && (!a.m_scale[l] || !a.v_scale[l]))) return LC_ERR_NULL;
         if (lc_off_element(a.w[l], 4) || lc_off_element(a.g[l], a.g_dtype == LC_BF16 ? 2 : 4) || (a.w_lowp && lc_off_element(a.w_lowp[l], 2))) return LC_ERR_ALIGN;
@@ -277,6 +253,22 @@ lc_status check_list(const AdamList& a, bool q8) {
     }
     return LC_OK;
 }
+
+template <typename G, bool Q8>
+void launch(const AdamArgs& args, int waves, bool past, hipStream_t stream) {
+    const dim3 grid((unsigned)std::min(args.chunks, kMostBlocks)), block(waves * 64);
+    if (waves == 1) {
+        if (past) hipLaunchKernelGGL((adamw_kernel<G, Q8, true, 1>), grid, block, 0, stream, args);
+        else hipLaunchKernelGGL((adamw_kernel<G, Q8, false, 1>), grid, block, 0, stream, args);
+    } else {
+        if (past) hipLaunchKernelGGL((adamw_kernel<G, Q8, true, 4>), grid, block, 0, stream, args);
+        else hipLaunchKernelGGL((adamw_kernel<G, Q8, false, 4>), grid, block, 0, stream, args);
+    }
+}
+
+// What a step reads and writes from which it goes past the caches.  Three lists in turn, us, ordinary / past: fp32 states, 5.9 million parameters (166 MB) 28.9 / 29.4, 7.1 (198 MB)
+// 35.1 / 34.5, 9.6 (270 MB) 52.4 / 45.9; 8 bits, 6.3 million (101 MB) 20.1 / 20.7, 9.8 (157 MB) 30.3 / 29.6, 14.2 (226 MB) 44.6 / 41.2.
+constexpr long long kStreamBytes = 160 << 20;
 
 lc_status run_list(const AdamList& a, bool q8, void* hip_stream) {
     const lc_status st = check_list(a, q8);
@@ -292,13 +284,22 @@ lc_status run_list(const AdamList& a, bool q8, void* hip_stream) {
     args.inv_root_c2 = (float)(1.0 / std::sqrt(1.0 - std::pow(a.beta2, (double)a.step)));
     args.eps = a.eps;
     args.dither = a.seed * 0x9E3779B1u + 0x7F4A7C15u;
+    double all = 0.0;
+    uintptr_t starts = 0;
+    for (int l = 0; l < a.n; ++l) {
+        if (a.numel[l] == 0) continue;
+        all += (double)a.numel[l];
+        starts |= (uintptr_t)a.w[l] | (uintptr_t)a.m[l] | (uintptr_t)a.v[l];
+    }
+    const bool past = all * ((q8 ? 12 : 24) + (a.g_dtype == LC_BF16 ? 2 : 4)) >= (double)kStreamBytes;
+    const int waves = (starts & 127) == 0 ? 1 : 4;
     lc_begin_call();
     for (int l = 0; l < a.n;) {
         long long chunks = 0;
         int count = 0;
         for (; l < a.n && count < kTable; ++l) {
             if (a.numel[l] == 0) continue;
-            const long long more = chunks_of(a.numel[l]);
+            const long long more = chunks_of(a.numel[l], waves);
             if (chunks + more > 0x7f000000ll) break;                   // a chunk's number and the grid beyond it stay in 31 bits (one tensor has 2^30 at most)
             AdamTensor& t = args.t[count];
             t.w = a.w[l];
@@ -316,14 +317,8 @@ lc_status run_list(const AdamList& a, bool q8, void* hip_stream) {
         if (count == 0) break;                                         // only empty tensors were left
         args.count = count;
         args.chunks = (int)chunks;
-        const dim3 grid((unsigned)std::min<long long>(chunks, kMostBlocks));
-        if (a.g_dtype == LC_BF16) {
-            if (q8) hipLaunchKernelGGL((adamw_kernel<uint16_t, true>), grid, dim3(kThreads), 0, stream, args);
-            else hipLaunchKernelGGL((adamw_kernel<uint16_t, false>), grid, dim3(kThreads), 0, stream, args);
-        } else {
-            if (q8) hipLaunchKernelGGL((adamw_kernel<float, true>), grid, dim3(kThreads), 0, stream, args);
-            else hipLaunchKernelGGL((adamw_kernel<float, false>), grid, dim3(kThreads), 0, stream, args);
-        }
+        if (a.g_dtype == LC_BF16) q8 ? launch<uint16_t, true>(args, waves, past, stream) : launch<uint16_t, false>(args, waves, past, stream);
+        else q8 ? launch<float, true>(args, waves, past, stream) : launch<float, false>(args, waves, past, stream);
     }
     return lc_end_call();
 }
