@@ -5,6 +5,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "internal.h"
 
 namespace {
@@ -161,37 +163,37 @@ __device__ __forceinline__ float lc_as_stored(float x) {
 }
 
 // Sum and maximum over a wave, every lane with the result: five exchanges inside the vector unit (neighbours, pairs, halves of 8 and of 16 lanes, a row's last lane to the
-// next row, the first two rows' to the last two) and one lane read back as a scalar, where a shuffle through LDS takes some 100 cycles for each of six.
+// next row, the first two rows' to the last two) and one lane read back as a scalar, where a shuffle through LDS takes some 100 cycles for each of six.  What a lane
+// outside an exchange meets is the operation's neutral element: 0, or its own value.
 template <int CTRL, int ROWS = 0xf>
-__device__ __forceinline__ float lc_dpp(float other, float x) {
-    return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(other), __float_as_int(x), CTRL, ROWS, 0xf, false));
+__device__ __forceinline__ uint32_t lc_dpp(uint32_t other, uint32_t x) {
+    return (uint32_t)__builtin_amdgcn_update_dpp((int)other, (int)x, CTRL, ROWS, 0xf, false);
 }
 template <typename F>
-__device__ __forceinline__ float lc_wave_join(float x, float neutral, F&& f) {
-    x = f(x, lc_dpp<0xB1>(neutral, x));              // quad_perm 1 0 3 2
-    x = f(x, lc_dpp<0x4E>(neutral, x));              // quad_perm 2 3 0 1
-    x = f(x, lc_dpp<0x141>(neutral, x));             // row_half_mirror
-    x = f(x, lc_dpp<0x140>(neutral, x));             // row_mirror
-    x = f(x, lc_dpp<0x142, 0xa>(neutral, x));        // row_bcast:15 into rows 1 and 3
-    x = f(x, lc_dpp<0x143, 0xc>(neutral, x));        // row_bcast:31 into rows 2 and 3
-    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
+__device__ __forceinline__ uint32_t lc_wave_join(uint32_t x, F&& step) {
+    x = step(x, std::integral_constant<int, 0xB1>{}, std::integral_constant<int, 0xf>{});        // quad_perm 1 0 3 2
+    x = step(x, std::integral_constant<int, 0x4E>{}, std::integral_constant<int, 0xf>{});        // quad_perm 2 3 0 1
+    x = step(x, std::integral_constant<int, 0x141>{}, std::integral_constant<int, 0xf>{});       // row_half_mirror
+    x = step(x, std::integral_constant<int, 0x140>{}, std::integral_constant<int, 0xf>{});       // row_mirror
+    x = step(x, std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});       // row_bcast:15 into rows 1 and 3
+    x = step(x, std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});       // row_bcast:31 into rows 2 and 3
+    return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
 }
 __device__ __forceinline__ float lc_wave_sum(float x) {
-    return lc_wave_join(x, 0.f, [](float a, float b) { return a + b; });
+    return __uint_as_float(lc_wave_join(__float_as_uint(x), [](uint32_t a, auto ctrl, auto rows) {
+        return __float_as_uint(__uint_as_float(a) + __uint_as_float(lc_dpp<decltype(ctrl)::value, decltype(rows)::value>(0u, a)));
+    }));
 }
 __device__ __forceinline__ float lc_wave_max(float x) {
-    return lc_wave_join(x, -INFINITY, [](float a, float b) { return fmaxf(a, b); });
+    return __uint_as_float(lc_wave_join(__float_as_uint(x), [](uint32_t a, auto ctrl, auto rows) {
+        return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(lc_dpp<decltype(ctrl)::value, decltype(rows)::value>(a, a))));
+    }));
 }
 __device__ __forceinline__ uint32_t lc_wave_umax(uint32_t x) {
-    // (a float's operations would lose unsigned numbers that are no floats')
-    const auto step = [](uint32_t a, uint32_t b) { return a > b ? a : b; };
-    x = step(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xB1, 0xf, 0xf, false));
-    x = step(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x4E, 0xf, 0xf, false));
-    x = step(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x141, 0xf, 0xf, false));
-    x = step(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x140, 0xf, 0xf, false));
-    x = step(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xa, 0xf, false));
-    x = step(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, false));
-    return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
+    return lc_wave_join(x, [](uint32_t a, auto ctrl, auto rows) {
+        const uint32_t b = lc_dpp<decltype(ctrl)::value, decltype(rows)::value>(0u, a);
+        return a > b ? a : b;
+    });
 }
 // Over a block of WAVES waves, every thread with the result; `red` (WAVES floats) must not be in use by an earlier call that a slower wave may still read.
 template <int WAVES>
