@@ -88,19 +88,32 @@ struct Packed<uint16_t> {
     __device__ __forceinline__ float get(int j) const { return __uint_as_float(j & 1 ? a[j >> 1] & 0xffff0000u : a[j >> 1] << 16); }
 };
 
-// Columns col(i) .. col(i) + 7 of a row of c for i < CH in two steps, so that all of a thread's loads are under way before the first is looked at: lc_issue8()
-// loads the row's last eight columns in place of what would pass its end (no branch, nothing outside the row), lc_settle8() moves those to their places and
-// puts `fill` (the type's own bits) where a column lies at `end` or past it; end is c, or a multiple of 8 before it.  Rows under eight columns, one
-// thread's at most, are read one by one.  full (the same for a wave): every column asked for lies before `end`; the plain addresses are a quarter of the
-// instructions of the others.
+// How a row's columns meet the threads that own eight of them each: kWhole: every thread's lie in the row; kEights: a thread's lie in it or past it, all of them; kAny.
+enum Ends { kWhole, kEights, kAny };
+
+// Columns col(i) .. col(i) + 7 of a row of c >= 8 for i < CH in two steps, so that all of a thread's loads are under way before the first is looked at:
+// lc_issue8() loads the row's last eight columns in place of what would pass its end (no branch, nothing outside the row), lc_settle8() moves those to
+// their places and puts `fill` (the type's own bits) where a column lies at `end` or past it; end is c, or a multiple of 8 before it.
+template <Ends ENDS, bool NT = false, int CH, typename T, typename F>
+__device__ __forceinline__ void lc_issue8(Packed<T> (&to)[CH], const T* row, F&& col, int c) {
+#pragma unroll
+    for (int i = 0; i < CH; ++i) to[i].template load<NT>(row + (ENDS == kWhole ? col(i) : min(col(i), c - 8)));
+}
+template <Ends ENDS, int CH, typename T, typename F>
+__device__ __forceinline__ void lc_settle8(Packed<T> (&to)[CH], F&& col, int end, uint32_t fill = 0) {
+    if constexpr (ENDS == kWhole) return;
+#pragma unroll
+    for (int i = 0; i < CH; ++i)
+        if (end - col(i) < 8) to[i].shift(ENDS == kEights ? 8 : min(8 - (end - col(i)), 8), fill);
+}
+// The same where it depends on the place (full: the same for a wave; every column asked for lies before `end`), and for rows under eight columns, one thread's at
+// most, which are read one by one.
 template <bool NT = false, int CH, typename T, typename F>
 __device__ __forceinline__ void lc_issue8(Packed<T> (&to)[CH], const T* row, F&& col, int c, bool full, uint32_t fill = 0) {
     if (full) {
-#pragma unroll
-        for (int i = 0; i < CH; ++i) to[i].template load<NT>(row + col(i));
+        lc_issue8<kWhole, NT>(to, row, col, c);
     } else if (c >= 8) {
-#pragma unroll
-        for (int i = 0; i < CH; ++i) to[i].template load<NT>(row + min(col(i), c - 8));
+        lc_issue8<kAny, NT>(to, row, col, c);
     } else {
         to[0].load_some(row + col(0), c - col(0), fill);
 #pragma unroll
@@ -109,10 +122,7 @@ __device__ __forceinline__ void lc_issue8(Packed<T> (&to)[CH], const T* row, F&&
 }
 template <int CH, typename T, typename F>
 __device__ __forceinline__ void lc_settle8(Packed<T> (&to)[CH], F&& col, int c, int end, bool full, uint32_t fill = 0) {
-    if (full || c < 8) return;
-#pragma unroll
-    for (int i = 0; i < CH; ++i)
-        if (end - col(i) < 8) to[i].shift(min(8 - (end - col(i)), 8), fill);
+    if (!full && c >= 8) lc_settle8<kAny>(to, col, end, fill);
 }
 template <bool NT = false, typename T>
 __device__ __forceinline__ void lc_load8(Packed<T>& to, const T* row, int col, int c) {
