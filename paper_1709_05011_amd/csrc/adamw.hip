@@ -17,10 +17,8 @@
 namespace {
 
 constexpr int kPart = 256;                                       // elements of a wave, four a lane
-constexpr int kTable = 176;                                      // descriptors per launch (13.4 KB of launch arguments)
+constexpr int kTable = 176, kSmallTable = 24;                    // descriptors per launch: 13.4 KB of launch arguments, which a short list's call need not copy (4.4 us a call, so 3.3)
 static_assert(kPart == ADAMW_Q8_BLOCK, "a wave makes a block's scale by itself");
-
-constexpr int kStarts = (kTable + 63) / 64 * 64;
 
 struct AdamTensor {
     float* w;
@@ -34,13 +32,19 @@ struct AdamTensor {
     float lr_decay;
 };
 
-struct AdamArgs {
-    AdamTensor t[kTable];
-    int start[kStarts];    // first chunk of each, ascending; past the last the largest int
+struct AdamScalars {
     int chunks;
     const float* grad_scale;
     float b1, one_b1, b2, one_b2, step_size, inv_root_c2, eps;
     uint32_t dither;
+};
+
+template <int TABLE>
+struct AdamArgs {
+    static constexpr int kStarts = (TABLE + 63) / 64 * 64;
+    AdamTensor t[TABLE];
+    int start[kStarts];    // first chunk of each, ascending; past the last the largest int
+    AdamScalars s;
 };
 
 // 21 bits from an element's number: two rounds of shift and odd product (the golden ratio's and root two's bits) modulo 2^32.
@@ -137,7 +141,7 @@ __device__ __forceinline__ void store4(uint8_t* p, uint32_t x, int n) {
 
 // What a wave does to its 256 elements, number `block` of the tensor; FULL: all of them lie within it (left: how many do).
 template <typename G, bool Q8, int PAST, bool FULL>
-__device__ __forceinline__ void adamw_part(const AdamArgs& p, const AdamTensor& t, long long block, long long left_in_block) {
+__device__ __forceinline__ void adamw_part(const AdamScalars& p, const AdamTensor& t, long long block, long long left_in_block) {
 #pragma clang fp contract(off)
     constexpr bool NT = PAST > 0;
     const int lane = threadIdx.x & 63, own = lane * 4;
@@ -227,18 +231,20 @@ __device__ __forceinline__ void adamw_part(const AdamArgs& p, const AdamTensor& 
 // One vector a thread, so that the chip works on one narrow stretch of each array at a time.  PAST: accesses past the caches' usual keeping, for lists that the
 // caches do not hold; 1: but for the bf16 copies, 2: all.  Blocks of one wave; of four where a tensor's arrays do not start on whole lines of 128 bytes: a line that two waves fill is then
 // mostly filled within one unit's cache and not by two dies' (201 million parameters with 8-bit states 4 bytes off a line, us: waves by themselves 737, four 617; on it 540 and 580).
-template <typename G, bool Q8, int PAST, int WAVES>
-__global__ void __launch_bounds__(WAVES * 64) adamw_kernel(const AdamArgs p) {
+template <typename G, bool Q8, int PAST, int WAVES, int TABLE>
+__global__ void __launch_bounds__(WAVES * 64) adamw_kernel(const AdamArgs<TABLE> args) {
+    constexpr int kStarts = AdamArgs<TABLE>::kStarts;
+    const AdamScalars& p = args.s;
     const int lane = threadIdx.x & 63, wave = WAVES == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     for (int chunk = blockIdx.x; chunk < p.chunks; chunk += gridDim.x) {
         int first[kStarts / 64], owner = -1;
 #pragma unroll
-        for (int i = 0; i < kStarts / 64; ++i) first[i] = p.start[64 * i + lane];
+        for (int i = 0; i < kStarts / 64; ++i) first[i] = args.start[64 * i + lane];
 #pragma unroll
         for (int i = 0; i < kStarts / 64; ++i) owner += __popcll(__ballot(first[i] <= chunk));
         owner = __builtin_amdgcn_readfirstlane(owner);
-        const AdamTensor t = p.t[owner];
-        const long long block = (long long)(chunk - p.start[owner]) * WAVES + wave, left = t.numel - block * kPart;
+        const AdamTensor t = args.t[owner];
+        const long long block = (long long)(chunk - args.start[owner]) * WAVES + wave, left = t.numel - block * kPart;
         if (left >= kPart) adamw_part<G, Q8, PAST, true>(p, t, block, kPart);
         else if (left > 0) adamw_part<G, Q8, PAST, false>(p, t, block, left);
     }
@@ -285,17 +291,27 @@ lc_status check_list(const AdamList& a, bool q8) {
     return LC_OK;
 }
 
-template <typename G, bool Q8, int PAST>
-void launch(const AdamArgs& args, int waves, hipStream_t stream) {
-    const dim3 grid((unsigned)std::min(args.chunks, kMostBlocks));
-    if (waves == 1) hipLaunchKernelGGL((adamw_kernel<G, Q8, PAST, 1>), grid, dim3(64), 0, stream, args);
-    else hipLaunchKernelGGL((adamw_kernel<G, Q8, PAST, 4>), grid, dim3(256), 0, stream, args);
+template <typename G, bool Q8, int PAST, int TABLE>
+void launch(const AdamArgs<TABLE>& args, int waves, hipStream_t stream) {
+    const dim3 grid((unsigned)std::min(args.s.chunks, kMostBlocks));
+    if (waves == 1) hipLaunchKernelGGL((adamw_kernel<G, Q8, PAST, 1, TABLE>), grid, dim3(64), 0, stream, args);
+    else hipLaunchKernelGGL((adamw_kernel<G, Q8, PAST, 4, TABLE>), grid, dim3(256), 0, stream, args);
 }
 template <typename G, bool Q8>
-void launch(const AdamArgs& args, int waves, int past, hipStream_t stream) {
-    if (past == 0) launch<G, Q8, 0>(args, waves, stream);
-    else if (past == 1) launch<G, Q8, 1>(args, waves, stream);
-    else launch<G, Q8, 2>(args, waves, stream);
+void launch(const AdamArgs<kTable>& args, int count, int waves, int past, hipStream_t stream) {
+    if (past == 0 && count <= kSmallTable) {
+        AdamArgs<kSmallTable> few;
+        std::copy(args.t, args.t + kSmallTable, few.t);
+        std::copy(args.start, args.start + few.kStarts, few.start);
+        few.s = args.s;
+        launch<G, Q8, 0>(few, waves, stream);
+    } else if (past == 0) {
+        launch<G, Q8, 0>(args, waves, stream);
+    } else if (past == 1) {
+        launch<G, Q8, 1>(args, waves, stream);
+    } else {
+        launch<G, Q8, 2>(args, waves, stream);
+    }
 }
 
 // What a step reads and writes from which it goes past the caches.  Three lists in turn, us, ordinary / past: fp32 states, 5.9 million parameters (166 MB) 28.9 / 29.4, 7.1 (198 MB)
@@ -306,16 +322,17 @@ lc_status run_list(const AdamList& a, bool q8, void* hip_stream) {
     const lc_status st = check_list(a, q8);
     if (st != LC_OK || a.n == 0 || std::all_of(a.numel, a.numel + a.n, [](int64_t n) { return n == 0; })) return st;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    AdamArgs args;
-    args.grad_scale = a.grad_scale;
-    args.b1 = (float)a.beta1;
-    args.one_b1 = (float)(1.0 - a.beta1);
-    args.b2 = (float)a.beta2;
-    args.one_b2 = (float)(1.0 - a.beta2);
-    args.step_size = (float)((double)a.lr / (1.0 - std::pow(a.beta1, (double)a.step)));
-    args.inv_root_c2 = (float)(1.0 / std::sqrt(1.0 - std::pow(a.beta2, (double)a.step)));
-    args.eps = a.eps;
-    args.dither = a.seed * 0x9E3779B1u + 0x7F4A7C15u;
+    AdamArgs<kTable> args;
+    AdamScalars& p = args.s;
+    p.grad_scale = a.grad_scale;
+    p.b1 = (float)a.beta1;
+    p.one_b1 = (float)(1.0 - a.beta1);
+    p.b2 = (float)a.beta2;
+    p.one_b2 = (float)(1.0 - a.beta2);
+    p.step_size = (float)((double)a.lr / (1.0 - std::pow(a.beta1, (double)a.step)));
+    p.inv_root_c2 = (float)(1.0 / std::sqrt(1.0 - std::pow(a.beta2, (double)a.step)));
+    p.eps = a.eps;
+    p.dither = a.seed * 0x9E3779B1u + 0x7F4A7C15u;
     double all = 0.0;
     uintptr_t starts = 0;
     for (int l = 0; l < a.n; ++l) {
@@ -348,10 +365,10 @@ lc_status run_list(const AdamList& a, bool q8, void* hip_stream) {
             chunks += more;
         }
         if (count == 0) break;                                         // only empty tensors were left
-        std::fill(args.start + count, args.start + kStarts, 0x7fffffff);
-        args.chunks = (int)chunks;
-        if (a.g_dtype == LC_BF16) q8 ? launch<uint16_t, true>(args, waves, past, stream) : launch<uint16_t, false>(args, waves, past, stream);
-        else q8 ? launch<float, true>(args, waves, past, stream) : launch<float, false>(args, waves, past, stream);
+        std::fill(args.start + count, args.start + args.kStarts, 0x7fffffff);
+        p.chunks = (int)chunks;
+        if (a.g_dtype == LC_BF16) q8 ? launch<uint16_t, true>(args, count, waves, past, stream) : launch<uint16_t, false>(args, count, waves, past, stream);
+        else q8 ? launch<float, true>(args, count, waves, past, stream) : launch<float, false>(args, count, waves, past, stream);
     }
     return lc_end_call();
 }

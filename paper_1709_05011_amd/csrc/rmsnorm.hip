@@ -254,13 +254,26 @@ __global__ void __launch_bounds__(kMostWaves * 64) rmsnorm_bwd_kernel(const Norm
     float acc[CH][8] = {};
     lc_issue8<ENDS>(pg, p.gamma, column, c);
     lc_settle8<ENDS>(pg, column, c);
+    // the next row's loads are under way while this one is summed and written
+    Packed<T> ph[CH], pd[CH], pt[CH], nh[CH], nd[CH], nt[CH];
+    float rstd = 0.f, next_rstd = 0.f;
+    const auto issue = [&](long long row) __attribute__((always_inline)) {
+        lc_issue8<ENDS, NT>(nh, static_cast<const T*>(p.h) + row * p.h_ld, column, c);
+        lc_issue8<ENDS, NT>(nd, static_cast<const T*>(p.dy) + row * (long long)c, column, c);
+        if (p.dh) lc_issue8<ENDS, NT>(nt, static_cast<const T*>(p.dh) + row * (long long)c, column, c);
+        next_rstd = p.rstd[row];
+    };
     int parity = 0;
+    if (blockIdx.x < p.rows) issue(blockIdx.x);
     for (long long row = blockIdx.x; row < p.rows; row += gridDim.x, parity ^= 1) {
-        Packed<T> ph[CH], pd[CH], pt[CH];
-        lc_issue8<ENDS, NT>(ph, static_cast<const T*>(p.h) + row * p.h_ld, column, c);
-        lc_issue8<ENDS, NT>(pd, static_cast<const T*>(p.dy) + row * (long long)c, column, c);
-        if (p.dh) lc_issue8<ENDS, NT>(pt, static_cast<const T*>(p.dh) + row * (long long)c, column, c);
-        const float rstd = p.rstd[row];
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            ph[i] = nh[i];
+            pd[i] = nd[i];
+            pt[i] = nt[i];
+        }
+        rstd = next_rstd;
+        if (row + gridDim.x < p.rows) issue(row + gridDim.x);
         float s = 0.f;
         lc_settle8<ENDS>(ph, column, c);
         lc_settle8<ENDS>(pd, column, c);

@@ -230,9 +230,10 @@ def lib() -> ctypes.CDLL:
 def _ptr(obj) -> Optional[int]:
     if obj is None:
         return None
-    if hasattr(obj, "data_ptr"):
+    try:
         return obj.data_ptr() or None
-    return int(obj) or None
+    except AttributeError:
+        return int(obj) or None
 
 
 def _nbytes(ws) -> int:
@@ -241,13 +242,23 @@ def _nbytes(ws) -> int:
     return ws.numel() * ws.element_size()
 
 
+_current_stream = None
+
+
+def _first_current_stream() -> Optional[int]:
+    """torch's current stream; once its runtime is up, later calls ask for the handle alone (0.1 us, where the stream object that holds it takes 2.9)."""
+    global _current_stream
+    import torch
+    if torch.cuda.is_initialized():
+        raw, device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+        _current_stream = lambda: raw(device()) or None
+        return _current_stream()
+    return torch.cuda.current_stream().cuda_stream or None
+
+
 def _stream(stream) -> Optional[int]:
     if stream is None:
-        import torch
-        if torch.cuda.is_initialized():
-            # the handle alone: 0.1 us a call, where building the stream object that holds it takes 2.9
-            return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()) or None
-        return torch.cuda.current_stream().cuda_stream or None
+        return _current_stream() if _current_stream else _first_current_stream()
     if hasattr(stream, "cuda_stream"):
         return stream.cuda_stream or None
     return int(stream) or None
@@ -586,8 +597,14 @@ def batchnorm_fwd_pre(dtype: int, x, gamma, beta, residual, y, save_mean, save_i
 # ---- the output side of a token model: RMS norm with the residual's addition ----
 
 def _c(desc):
-    """The C structure of a descriptor dataclass (or the structure itself)."""
-    return ctypes.byref(desc.c_struct() if hasattr(desc, "c_struct") else desc)
+    """The C structure of a descriptor (made once for each: descriptors do not change), or of a structure as it is."""
+    if isinstance(desc, ctypes.Structure):
+        return ctypes.byref(desc)
+    made = desc.__dict__.get("_c_ref")
+    if made is None:
+        made = ctypes.byref(desc.c_struct())
+        object.__setattr__(desc, "_c_ref", made)
+    return made
 
 
 def rmsnorm_fwd(desc, x, residual, gamma, total, y, save_rstd=None, stream=None) -> None:
