@@ -365,33 +365,37 @@ __global__ void __launch_bounds__(1024) rmsnorm_bwd_wide_kernel(const NormBwdArg
     }
 }
 
-// dgamma[k] = the blocks' shares added in a fixed order: 64 columns a block, a wave takes every 16th share, eight of them under way at a time.
+// dgamma[k] = the blocks' shares added in a fixed order: COLS columns a block, whose 1024 / COLS groups of threads take every so many shares, eight of them under way at a
+// time.  16 columns a block where 64 would leave most of the chip without one (16384 x 256, forward and backward, 29.6 us,
+// so 25.9; from 1537 columns on 64 are as fast or faster).
+constexpr int kNarrow = 1024;
+template <int COLS>
 __global__ void __launch_bounds__(1024) rmsnorm_dgamma_kernel(const float* __restrict__ part, float* __restrict__ dgamma, int parts, int c) {
-    constexpr int U = 8;
-    __shared__ float sum[16][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const long long k = (long long)blockIdx.x * 64 + lane;
+    constexpr int U = 8, kGroups = 1024 / COLS;
+    __shared__ float sum[kGroups][COLS];
+    const int column = threadIdx.x & (COLS - 1), group = threadIdx.x / COLS;
+    const long long k = (long long)blockIdx.x * COLS + column;
     float s[U] = {};
     if (k < c) {
-        int i = wave;
-        for (; i + 16 * (U - 1) < parts; i += 16 * U) {
+        int i = group;
+        for (; i + kGroups * (U - 1) < parts; i += kGroups * U) {
             float v[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) v[u] = part[(long long)(i + 16 * u) * c + k];
+            for (int u = 0; u < U; ++u) v[u] = part[(long long)(i + kGroups * u) * c + k];
 #pragma unroll
             for (int u = 0; u < U; ++u) s[u] += v[u];
         }
 #pragma unroll
         for (int u = 0; u < U - 1; ++u)
-            if (i + 16 * u < parts) s[u] += part[(long long)(i + 16 * u) * c + k];
+            if (i + kGroups * u < parts) s[u] += part[(long long)(i + kGroups * u) * c + k];
     }
-    sum[wave][lane] = ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
+    sum[group][column] = ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
     __syncthreads();
-    if (wave == 0 && k < c) {
-        float t = 0.f;
+    if (group == 0 && k < c) {
+        float t[4] = {};
 #pragma unroll
-        for (int w = 0; w < 16; ++w) t += sum[w][lane];
-        dgamma[k] = t;
+        for (int w = 0; w < kGroups; ++w) t[w & 3] += sum[w][column];
+        dgamma[k] = (t[0] + t[1]) + (t[2] + t[3]);
     }
 }
 
@@ -537,6 +541,8 @@ extern "C" lc_status rmsnorm_bwd(const lc_rmsnorm_desc* desc, const void* total,
     lc_begin_call();
     if (desc->dtype == LC_BF16) launch_bwd<uint16_t>(a, blocks, stream);
     else launch_bwd<float>(a, blocks, stream);
-    hipLaunchKernelGGL(rmsnorm_dgamma_kernel, dim3((unsigned)(((long long)desc->c + 63) / 64)), dim3(1024), 0, stream, a.part, dgamma, blocks, desc->c);
+    const long long c = desc->c;
+    if (c <= kNarrow) hipLaunchKernelGGL((rmsnorm_dgamma_kernel<16>), dim3((unsigned)((c + 15) / 16)), dim3(1024), 0, stream, a.part, dgamma, blocks, desc->c);
+    else hipLaunchKernelGGL((rmsnorm_dgamma_kernel<64>), dim3((unsigned)((c + 63) / 64)), dim3(1024), 0, stream, a.part, dgamma, blocks, desc->c);
     return lc_end_call();
 }
