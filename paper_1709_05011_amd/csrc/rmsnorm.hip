@@ -432,11 +432,14 @@ void launch_fwd(const NormArgs& a, hipStream_t stream) {
     const dim3 grid((unsigned)std::min(a.rows, kMostBlocks)), block((a.c + 512 * CH - 1) / (512 * CH) * 64);
     if (a.c % (512 * CH) == 0) hipLaunchKernelGGL((rmsnorm_fwd_kernel<T, CH, Q8, NT, kWhole>), grid, block, 0, stream, a);
     else if (a.c % 8 == 0) hipLaunchKernelGGL((rmsnorm_fwd_kernel<T, CH, Q8, NT, kEights>), grid, block, 0, stream, a);
-    else hipLaunchKernelGGL((rmsnorm_fwd_kernel<T, CH, Q8, NT, kAny>), grid, block, 0, stream, a);
+    else if constexpr (CH * sizeof(T) < 8) hipLaunchKernelGGL((rmsnorm_fwd_kernel<T, CH, Q8, NT, kAny>), grid, block, 0, stream, a);
 }
+// Rows that go by in passes: what a block's registers do not hold (of fp32 rows that end within a thread's columns 16 a thread neither), and under eight columns.
+bool in_passes(const lc_dtype dtype, int c) { return c < 8 || c > kMostColumns || (dtype == LC_F32 && c % 8 && c > 512 * kMostWaves); }
+
 template <typename T, bool Q8>
 void launch_fwd(const NormArgs& a, hipStream_t stream) {
-    if (a.c < 8 || a.c > kMostColumns) {
+    if (in_passes(sizeof(T) == 2 ? LC_BF16 : LC_F32, a.c)) {
         hipLaunchKernelGGL((rmsnorm_fwd_wide_kernel<T, Q8>), dim3((unsigned)std::min(a.rows, kMostBlocks)), dim3(1024), 0, stream, a);
         return;
     }
@@ -472,7 +475,7 @@ lc_status run_fwd(const lc_rmsnorm_desc* d, const void* x, const void* residual,
 // backward with 256, 512, 1024 blocks 110, 96.6, 104; 16384 x 1024 97, 70, 58; 2048 x 16384 105, 114, 128; 512 x 4096 14.8, 16.0, 16.0.
 int bwd_chunks(int c) { return c <= 512 * kMostWaves ? 1 : 2; }
 long long bwd_blocks(const lc_rmsnorm_desc* d) {
-    if (d->c < 8 || d->c > kMostColumns) return std::min<long long>(d->rows, 64);
+    if (in_passes(d->dtype, d->c)) return std::min<long long>(d->rows, 64);
     const int columns = 512 * bwd_chunks(d->c), waves = (d->c + columns - 1) / columns;
     return std::min<long long>(d->rows, std::max<long long>(256, std::min<long long>(4096 / waves, d->rows / 4)));
 }
@@ -482,11 +485,11 @@ void launch_bwd(const NormBwdArgs& a, int blocks, hipStream_t stream) {
     const dim3 grid((unsigned)blocks), block((a.c + 512 * CH - 1) / (512 * CH) * 64);
     if (a.c % (512 * CH) == 0) hipLaunchKernelGGL((rmsnorm_bwd_kernel<T, CH, NT, kWhole>), grid, block, 0, stream, a);
     else if (a.c % 8 == 0) hipLaunchKernelGGL((rmsnorm_bwd_kernel<T, CH, NT, kEights>), grid, block, 0, stream, a);
-    else hipLaunchKernelGGL((rmsnorm_bwd_kernel<T, CH, NT, kAny>), grid, block, 0, stream, a);
+    else if constexpr (CH * sizeof(T) < 8) hipLaunchKernelGGL((rmsnorm_bwd_kernel<T, CH, NT, kAny>), grid, block, 0, stream, a);
 }
 template <typename T>
 void launch_bwd(const NormBwdArgs& a, int blocks, hipStream_t stream) {
-    if (a.c < 8 || a.c > kMostColumns) {
+    if (in_passes(sizeof(T) == 2 ? LC_BF16 : LC_F32, a.c)) {
         hipLaunchKernelGGL((rmsnorm_dgamma_wide_kernel<T>), dim3((unsigned)(((long long)a.c + 2047) / 2048), (unsigned)blocks), dim3(256), 0, stream, a);
         hipLaunchKernelGGL((rmsnorm_bwd_wide_kernel<T>), dim3((unsigned)std::min(a.rows, kMostBlocks)), dim3(1024), 0, stream, a);
         return;

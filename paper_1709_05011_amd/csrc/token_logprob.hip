@@ -153,18 +153,19 @@ __device__ __forceinline__ float3 join_sums(const float4* stats, int n) {
 // its list, or the first of the largest of its lists; then every list is walked from its head while its keys reach the bound that follows.
 template <typename F>
 __device__ __forceinline__ void join_lists(const Key* lists, int n, int top, Key* keys, F&& emit) {
-    constexpr int kHead = 4, kGroups = 2;           // what is asked for at once: the heads of as many lists as a row of 131072 has, of four keys
-    const int lane = threadIdx.x & 63, lanes = min(n, 64), k = (top + lanes - 1) / lanes;
-    Key head[kGroups][kHead], own = 0;
+    constexpr int kHead = 8;                        // keys of a lane that are asked for at once: of its list, or half of them of each of two lists
+    const int lane = threadIdx.x & 63, lanes = min(n, 64), k = (top + lanes - 1) / lanes, each = n > 64 ? kHead / 2 : kHead;
+    Key head[kHead], own = 0;
 #pragma unroll
-    for (int g = 0; g < kGroups; ++g)
-#pragma unroll
-        for (int j = 0; j < kHead; ++j) head[g][j] = 64 * g + lane < n && j < top ? lists[(long long)(64 * g + lane) * top + j] : 0;
+    for (int j = 0; j < kHead; ++j) {
+        const int list = j < each ? lane : lane + 64, at = j < each ? j : j - each;
+        head[j] = list < n && at < top ? lists[(long long)list * top + at] : 0;
+    }
     if (k > 1) {
         if (lane < n) own = lists[(long long)lane * top + k - 1];
     } else {
-        own = max(head[0][0], head[1][0]);
-        for (int i = lane + 64 * kGroups; i < n; i += 64) own = max(own, lists[(long long)i * top]);
+        own = each < kHead ? max(head[0], head[kHead / 2]) : head[0];
+        for (int i = lane + 128; i < n; i += 64) own = max(own, lists[(long long)i * top]);
     }
     Key least = max((Key)lanes_bound((uint32_t)(own >> 32), own != 0, (top + k - 1) / k) << 32, (Key)1);
     int held = 0;
@@ -177,18 +178,19 @@ __device__ __forceinline__ void join_lists(const Key* lists, int n, int top, Key
     };
     const auto gather = [&]() __attribute__((always_inline)) {
         held = 0;
+        bool more = true;
 #pragma unroll
-        for (int g = 0; g < kGroups; ++g) {
-            if (64 * g >= n) break;
-            bool more = true;
-#pragma unroll
-            for (int j = 0; j < kHead; ++j) {
-                more = __ballot(head[g][j] >= least) != 0;
-                if (more) held = append(keys, held, head[g][j] >= least, head[g][j]);
+        for (int j = 0; j < kHead; ++j) {
+            if (j == kHead / 2 && each < kHead) {
+                if (more) walk(lists + (long long)lane * top, lane < n, each);
+                more = true;
             }
-            if (more) walk(lists + (long long)(64 * g + lane) * top, 64 * g + lane < n, kHead);
+            if (more) more = __ballot(head[j] >= least) != 0;
+            if (more) held = append(keys, held, head[j] >= least, head[j]);
         }
-        for (int base = 64 * kGroups; base < n; base += 64) walk(lists + (long long)(base + lane) * top, base + lane < n, 0);
+        const int last = each < kHead ? 64 : 0;
+        if (more) walk(lists + (long long)(last + lane) * top, last + lane < n, each);
+        for (int base = 128; base < n; base += 64) walk(lists + (long long)(base + lane) * top, base + lane < n, 0);
     };
     gather();
     if (held > kCandidates) {
