@@ -23,6 +23,7 @@ namespace {
 constexpr int kMostTop = 32;
 constexpr int kMostWaves = 4;               // of a block
 constexpr int kCandidates = 256;            // keys that a wave's LDS has room for
+constexpr int kChunks = 128, kRounds = 32;  // places of a lane's values of a round, and rounds, that it has room for
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kFar = -150.f;              // 2^-150 is 0 in fp32: distances are no longer than this where 0 * infinity would be formed
 
@@ -40,6 +41,12 @@ struct TokenArgs {
     Key* keys;               // [rows][blocks][top], falling; 0 where a block has fewer
     long long rows, ld;
     int vocab, top, blocks, slice;      // blocks of a row; values of a block, a multiple of 8
+};
+
+struct WaveTop {
+    Key keys[kCandidates];
+    uint16_t marks[kRounds][64];
+    uint16_t chunks[kChunks];
 };
 
 // order-preserving map of floats to unsigned; both zeros alike
@@ -245,13 +252,14 @@ template <bool ENT>
 struct LaneSums {
     float m = -INFINITY, ref = -INFINITY, s = 0.f, t = 0.f;      // (t only with ENT)
 
+    // Returns the largest of the values (at least `floor`).
     template <int N>
-    __device__ __forceinline__ void add(const float (&v)[N]) {
+    __device__ __forceinline__ float add(const float (&v)[N], float floor) {
         static_assert(N % 2 == 0, "in pairs");
-        float most = m;
+        float most = floor;
 #pragma unroll
         for (int j = 0; j < N; j += 2) most = max3(v[j], v[j + 1], most);
-        m = most;
+        m = fmaxf(m, most);
         const float now = fmaxf(ref, most * kLog2e), less = now == -INFINITY ? 0.f : -now;
         const float shift = fmaxf(ref + less, kFar), f = __builtin_amdgcn_exp2f(ref + less);
         if (ENT) t = f * fmaf(shift, s, t);
@@ -276,6 +284,7 @@ struct LaneSums {
         }
         s += ds;
         t += dt;
+        return most;
     }
 
     // The wave's m, S and T about m itself.
@@ -312,10 +321,11 @@ __device__ __forceinline__ void leave(const TokenArgs& p, long long row, const T
 }
 
 // A slice of a row by a block of up to kMostWaves waves, whose first joins what the others leave in LDS.  Rounds of 512 * CH values go to the waves in turn, so that a
-// block reads one stretch at a time; a wave's next round is under way while one is summed.  ENT: with the entropy.  TOP: with the alternatives: the slice is read a second time, from
-// the caches, for what reaches the bound that its lanes' maxima give; LDS: kCandidates keys a wave and its list of `top`.
+// block reads one stretch at a time; a wave's next round is under way while one is summed.  ENT: with the entropy.  TOP: with the alternatives: a lane marks in LDS how
+// large the largest of its values of each round is (the upper half of its order); of those that may reach the bound, a few more than N as a rule, one each a
+// lane reads the values again.  LDS: WaveTop a wave and its list of `top`.
 template <typename T, int CH, bool ENT, bool TOP>
-__global__ void __launch_bounds__(kMostWaves * 64) token_sums_kernel(const TokenArgs p) {
+__global__ void __launch_bounds__(kMostWaves * 64, 4) token_sums_kernel(const TokenArgs p) {
     __shared__ float4 stats[kMostWaves];
     extern __shared__ __align__(16) char lds[];
     constexpr uint32_t kMaskedBits = sizeof(T) == 2 ? 0xff80u : 0xff800000u;
@@ -323,8 +333,9 @@ __global__ void __launch_bounds__(kMostWaves * 64) token_sums_kernel(const Token
     const int lane = threadIdx.x & 63, waves = blockDim.x >> 6, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int part = (int)blockIdx.x * p.slice, end = min(p.vocab - part, p.slice) + part;
     const int first = min(part + wave * kRound, end), stride = waves * kRound;
-    Key* keys = TOP ? reinterpret_cast<Key*>(lds) + wave * kCandidates : nullptr;
-    Key* lists = TOP ? reinterpret_cast<Key*>(lds) + waves * kCandidates : nullptr;
+    WaveTop* top = TOP ? reinterpret_cast<WaveTop*>(lds) + wave : nullptr;
+    Key* keys = TOP ? top->keys : nullptr;
+    Key* lists = TOP ? reinterpret_cast<Key*>(reinterpret_cast<WaveTop*>(lds) + waves) : nullptr;
     for (long long row = blockIdx.y; row < p.rows; row += gridDim.y) {
         const T* z = static_cast<const T*>(p.z) + row * p.ld;
         Target target;
@@ -338,6 +349,8 @@ __global__ void __launch_bounds__(kMostWaves * 64) token_sums_kernel(const Token
         const auto settle = [&](Packed<T>(&of)[CH], int at) __attribute__((always_inline)) {
             lc_settle8(of, column(at), p.vocab, end, at + kRound <= end, kMaskedBits);
         };
+        const bool single = first + stride >= end;              // one round, or none
+        int round = 0;
         const auto add = [&](Packed<T>(&from)[CH], int at) __attribute__((always_inline)) {
             settle(from, at);
             float v[CH * 8];
@@ -345,7 +358,8 @@ __global__ void __launch_bounds__(kMostWaves * 64) token_sums_kernel(const Token
             for (int i = 0; i < CH; ++i)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[8 * i + j] = from[i].get(j);
-            sums.add(v);
+            if (TOP && !single) top->marks[round++][lane] = (uint16_t)(order_of(sums.add(v, -INFINITY)) >> 16);
+            else sums.add(v, sums.m);
         };
         issue(now, first);
         for (int at = first; at < end; at += 2 * stride) {
@@ -359,22 +373,39 @@ __global__ void __launch_bounds__(kMostWaves * 64) token_sums_kernel(const Token
         if constexpr (TOP) {
             const uint32_t order = lanes_bound(order_of(sums.m), listable(sums.m), p.top);
             const float bound = value_of(order);
-            const auto look = [&](Packed<T>& from, int col) __attribute__((always_inline)) {
-                float most = from.get(0);
+            const auto look = [&](bool there, auto&& column_of) __attribute__((always_inline)) {
 #pragma unroll
-                for (int j = 1; j < 7; j += 2) most = max3(from.get(j), from.get(j + 1), most);
-                if (!__ballot(most >= bound || from.get(7) >= bound)) return;
+                for (int i = 0; i < CH; ++i)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float x = from.get(j);
-                    if (__ballot(x >= bound)) held = append(keys, held, x >= bound, key_of(x, col + j));
-                }
+                    for (int j = 0; j < 8; ++j) {
+                        const float x = now[i].get(j);
+                        const bool is = there && x >= bound;
+                        if (__ballot(is)) held = append(keys, held, is, key_of(x, column_of(i) + j));
+                    }
             };
-            for (int at = first; at < end; at += stride) {
-                issue(now, at);
-                settle(now, at);
-#pragma unroll
-                for (int i = 0; i < CH; ++i) look(now[i], column(at)(i));
+            if (single) {                                       // (the values are still there)
+                if (first < end) look(true, column(first));
+            } else {
+                int chunks = 0;
+                for (int r = 0; r < round; ++r) {
+                    const bool may = top->marks[r][lane] >= (uint16_t)(order >> 16);
+                    const unsigned long long mask = __ballot(may);
+                    if (!mask) continue;
+                    const int place = chunks + __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+                    if (may && place < kChunks) top->chunks[place] = (uint16_t)(r * 64 + lane);
+                    chunks += __popcll(mask);
+                }
+                __builtin_amdgcn_wave_barrier();
+                for (int base = 0; base < chunks && chunks <= kChunks; base += 64) {
+                    const bool there = base + lane < chunks;
+                    const int chunk = there ? top->chunks[base + lane] : 0;
+                    const int at = there ? first + (chunk >> 6) * stride : end, of = chunk & 63;
+                    const auto where = [&](int i) { return at + (i * 64 + of) * 8; };
+                    lc_issue8(now, z, where, p.vocab, false, kMaskedBits);
+                    lc_settle8(now, where, p.vocab, there ? end : 0, false, kMaskedBits);
+                    look(there, where);
+                }
+                if (chunks > kChunks) held = kCandidates + 1;
             }
             if (held > kCandidates) {
                 Key least = (Key)order << 32, hi = ~(Key)0;        // fewer than `top` keys reach hi, more than there is room for reach least
@@ -529,7 +560,7 @@ TokenPlan plan_of(const lc_token_desc* d) {
     p.chunks = d->vocab <= 512 ? 1 : 2;
     const int round = 512 * p.chunks, rounds = (d->vocab + round - 1) / round;
     int most = 1;                                      // rounds of a wave
-    while (most < rounds && d->rows * ((rounds + 2 * most - 1) / (2 * most)) >= (d->top ? kFillTop : kFillWaves)) most *= 2;
+    while (most < rounds && (!d->top || 2 * most <= kRounds) && d->rows * ((rounds + 2 * most - 1) / (2 * most)) >= (d->top ? kFillTop : kFillWaves)) most *= 2;
     const int waves = (rounds + most - 1) / most;      // of a row
     p.blocks = waves > kMostWaves ? waves : 1;
     p.waves = (waves + p.blocks - 1) / p.blocks;
@@ -548,7 +579,7 @@ dim3 grid_of(int parts, long long rows, int threads) {
 template <typename T, int CH>
 void launch_fwd(const TokenArgs& a, int waves, hipStream_t stream) {
     const dim3 grid = grid_of(a.blocks, a.rows, waves * 64), block(waves * 64);
-    if (a.top) hipLaunchKernelGGL((token_sums_kernel<T, CH, true, true>), grid, block, waves * (kCandidates + a.top) * sizeof(Key), stream, a);
+    if (a.top) hipLaunchKernelGGL((token_sums_kernel<T, CH, true, true>), grid, block, waves * (sizeof(WaveTop) + a.top * sizeof(Key)), stream, a);
     else if (a.entropy) hipLaunchKernelGGL((token_sums_kernel<T, CH, true, false>), grid, block, 0, stream, a);
     else hipLaunchKernelGGL((token_sums_kernel<T, CH, false, false>), grid, block, 0, stream, a);
     if (a.blocks > 1) hipLaunchKernelGGL((token_join_kernel<T>), dim3((unsigned)std::min(a.rows, kMostThreads / 64)), dim3(64), 0, stream, a);
