@@ -325,7 +325,7 @@ __device__ __forceinline__ void leave(const TokenArgs& p, long long row, const T
 // large the largest of its values of each round is (the upper half of its order); of those that may reach the bound, a few more than N as a rule, one each a
 // lane reads the values again.  LDS: WaveTop a wave and its list of `top`.
 template <typename T, int CH, bool ENT, bool TOP>
-__global__ void __launch_bounds__(kMostWaves * 64, 4) token_sums_kernel(const TokenArgs p) {
+__global__ void __launch_bounds__(kMostWaves * 64, TOP && sizeof(T) * CH == 8 ? 3 : 4) token_sums_kernel(const TokenArgs p) {
     __shared__ float4 stats[kMostWaves];
     extern __shared__ __align__(16) char lds[];
     constexpr uint32_t kMaskedBits = sizeof(T) == 2 ? 0xff80u : 0xff800000u;
@@ -557,7 +557,10 @@ constexpr long long kFillWaves = 16384, kFillTop = 2048;      // waves that rows
 
 TokenPlan plan_of(const lc_token_desc* d) {
     TokenPlan p;
-    p.chunks = d->vocab <= 512 ? 1 : 2;
+    // 16 values a lane of a round; eight of fp32 logits with alternatives, whose registers a SIMD then has for four waves, where there are rows enough for them (1000 rows
+    // of 32000 39 us, so 31; one row of 128000 10.2, so 11.9)
+    const bool eight = d->top && d->dtype == LC_F32 && d->rows * ((d->vocab + 1023) / 1024) >= 2 * kFillTop;
+    p.chunks = d->vocab <= 512 || eight ? 1 : 2;
     const int round = 512 * p.chunks, rounds = (d->vocab + round - 1) / round;
     int most = 1;                                      // rounds of a wave
     while (most < rounds && (!d->top || 2 * most <= kRounds) && d->rows * ((rounds + 2 * most - 1) / (2 * most)) >= (d->top ? kFillTop : kFillWaves)) most *= 2;
