@@ -25,6 +25,7 @@ struct NormArgs {
     long long rows, x_ld, r_ld;
     int c, group;
     float eps;
+    double inv_c;            // 1 / c
 };
 
 constexpr int kMostWaves = 16;
@@ -44,26 +45,71 @@ __device__ __forceinline__ float block_join(float x, int waves, float* red, W&& 
 
 constexpr float kE4m3Max = 448.f, kLeastScale = 0x1p-126f;
 
-// eight e4m3 codes of v * inv, nearest even (the conversion instruction's own rounding; NaN keeps the code of NaN)
-__device__ __forceinline__ void store8_e4m3(uint8_t* p, const float* v, float inv, int n) {
+// 1/sqrt(sum / c + eps) to more than fp32's places: the instruction's estimate and one step of Newton's method in double.
+__device__ __forceinline__ double rstd_of(const NormArgs& p, float sum) {
+    const double x = fma((double)sum, p.inv_c, (double)p.eps);
+    const double r = (double)__builtin_amdgcn_rsqf((float)x);
+    const double better = r * fma(-0.5 * x * r, r, 1.5);
+    return fabs(better) < INFINITY ? better : r;         // (x = 0 or infinite: the estimate is the value)
+}
+
+// rstd as a power of two and the rest, in [0.5, 1): a total times the power is near its normalised value, so that its product with gamma leaves fp32's range only where the
+// output does.  (The power is 1 for zero, infinity and NaN; it is exact otherwise, and so is a product with it.)
+struct Split {
+    float power;
+    double rest;
+};
+__device__ __forceinline__ Split split_of(double rstd) {
+    const int e = __builtin_amdgcn_frexp_exp(rstd);
+    return {ldexpf(1.f, e), ldexp(rstd, -e)};
+}
+
+// A group's scale from its largest |g|, g = total * power * gamma, and the rest of rstd, and what takes g to codes: rest / scale as the sum of two floats.
+struct Scale {
+    float scale, hi, lo;
+};
+__device__ __forceinline__ Scale scale_of(float amax, double rest) {
+    Scale s;
+    s.scale = fmaxf((float)((double)amax * rest * (1.0 / kE4m3Max)), kLeastScale);
+    const double r = (double)__builtin_amdgcn_rcpf(s.scale), k = rest * (r * fma(-(double)s.scale, r, 2.0));
+    s.hi = (float)k;
+    s.lo = (float)(k - (double)s.hi);
+    return s;
+}
+
+// Eight e4m3 codes of g[j] * rest / scale, to nearest even; `low` holds what the rounding of g[j] left.  The quotient is right to nearly all of fp32's places, so that a code is
+// off the exact value's only next to a border; with y * (1 / scale) in fp32 more of them were (4099 rows of 5120 with groups of 128: 28.0 us instead of 28.9).  NaN keeps the code of NaN.
+__device__ __forceinline__ void store8_e4m3(uint8_t* p, const float* g, const float* low, const Scale& s, double rest, int n) {
+    float q[8];
+    if (s.scale > kLeastScale) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float a = g[j] * s.hi;
+            q[j] = a + fmaf(g[j], s.lo, fmaf(low[j], s.hi, fmaf(g[j], s.hi, -a)));
+        }
+    } else {                                            // (rest / scale may be beyond fp32)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) q[j] = (float)((double)g[j] * rest) * (1.f / kLeastScale);
+    }
     uint32_t w[2];
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
         int u = 0;
-        u = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * k] * inv, v[4 * k + 1] * inv, u, false);
-        u = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * k + 2] * inv, v[4 * k + 3] * inv, u, true);
+        u = __builtin_amdgcn_cvt_pk_fp8_f32(q[4 * k], q[4 * k + 1], u, false);
+        u = __builtin_amdgcn_cvt_pk_fp8_f32(q[4 * k + 2], q[4 * k + 3], u, true);
         w[k] = (uint32_t)u;
     }
     if (n >= 8) {
         __builtin_memcpy(p, w, 8);
     } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (j < n) p[j] = (uint8_t)(w[j >> 2] >> (8 * (j & 3)));
+#pragma unroll 1
+        for (int j = 0; j < n; ++j) {
+            p[j] = (uint8_t)w[0];
+            w[0] = __builtin_amdgcn_alignbit(w[1], w[0], 8);
+            w[1] >>= 8;
+        }
     }
 }
-
-__device__ __forceinline__ float scale_of(float amax) { return fmaxf(amax / kE4m3Max, kLeastScale); }
 
 // A block per row (rows dealt round the grid), its waves as many as the row has 512 * CH columns.
 template <typename T, int CH, bool Q8, bool NT, Ends ENDS>
@@ -106,34 +152,41 @@ __global__ void __launch_bounds__(kMostWaves * 64) rmsnorm_fwd_kernel(const Norm
             for (int i = 0; i < CH; ++i) lc_store8<NT>(t + column(i), h[i], inside(i));
         }
         ss = block_join(ss, waves, red[parity][0], [](float a) { return lc_wave_sum(a); }, [](float a, float b) { return a + b; });
-        const float rstd = 1.f / sqrtf(ss / (float)c + p.eps);
-        if (p.rstd && tid == 0) p.rstd[row] = rstd;
-#pragma unroll
-        for (int i = 0; i < CH; ++i)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) h[i][j] = h[i][j] * rstd * pg[i].get(j);
+        const double rstd = rstd_of(p, ss);
+        if (p.rstd && tid == 0) p.rstd[row] = (float)rstd;
         if constexpr (!Q8) {
+            const float r = (float)rstd;
             T* y = static_cast<T*>(p.y) + row * (long long)c;
 #pragma unroll
-            for (int i = 0; i < CH; ++i) lc_store8<NT>(y + column(i), h[i], inside(i));
+            for (int i = 0; i < CH; ++i) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) h[i][j] = h[i][j] * r * pg[i].get(j);
+                lc_store8<NT>(y + column(i), h[i], inside(i));
+            }
         } else {
             uint8_t* y = static_cast<uint8_t*>(p.y) + row * (long long)c;
-            float amax[CH];
+            const Split split = split_of(rstd);
+            float low[CH][8], amax[CH];
 #pragma unroll
             for (int i = 0; i < CH; ++i) {
                 amax[i] = 0.f;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) amax[i] = fmaxf(amax[i], fabsf(h[i][j]));
+                for (int j = 0; j < 8; ++j) {
+                    const float n = h[i][j] * split.power, g = n * pg[i].get(j);
+                    low[i][j] = fmaf(n, pg[i].get(j), -g);
+                    h[i][j] = g;
+                    amax[i] = fmaxf(amax[i], fabsf(g));
+                }
             }
             if (p.group == 0) {
                 float m = amax[0];
 #pragma unroll
                 for (int i = 1; i < CH; ++i) m = fmaxf(m, amax[i]);
-                const float scale = scale_of(block_join(m, waves, red[parity][1], [](float a) { return lc_wave_max(a); }, [](float a, float b) { return fmaxf(a, b); }));
-                if (tid == 0) p.scales[row] = scale;
-                const float inv = 1.f / scale;
+                m = block_join(m, waves, red[parity][1], [](float a) { return lc_wave_max(a); }, [](float a, float b) { return fmaxf(a, b); });
+                const Scale scale = scale_of(m, split.rest);
+                if (tid == 0) p.scales[row] = scale.scale;
 #pragma unroll
-                for (int i = 0; i < CH; ++i) store8_e4m3(y + column(i), h[i], inv, inside(i));
+                for (int i = 0; i < CH; ++i) store8_e4m3(y + column(i), h[i], low[i], scale, split.rest, inside(i));
             } else {
                 const int lanes = p.group >> 3, shift = __builtin_ctz(p.group);
                 const long long groups = (c + p.group - 1) >> shift;
@@ -141,9 +194,9 @@ __global__ void __launch_bounds__(kMostWaves * 64) rmsnorm_fwd_kernel(const Norm
                 for (int i = 0; i < CH; ++i) {
                     float m = amax[i];
                     for (int off = 1; off < lanes; off <<= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
-                    const float scale = scale_of(m);
-                    if (column(i) < c && (tid & (lanes - 1)) == 0) p.scales[row * groups + (column(i) >> shift)] = scale;
-                    store8_e4m3(y + column(i), h[i], 1.f / scale, inside(i));
+                    const Scale scale = scale_of(m, split.rest);
+                    if (column(i) < c && (tid & (lanes - 1)) == 0) p.scales[row * groups + (column(i) >> shift)] = scale.scale;
+                    store8_e4m3(y + column(i), h[i], low[i], scale, split.rest, inside(i));
                 }
             }
         }
@@ -184,48 +237,55 @@ __global__ void __launch_bounds__(1024) rmsnorm_fwd_wide_kernel(const NormArgs p
             if (t) lc_store8(t + col, h, c - col);
         }
         ss = lc_block_sum<WAVES>(ss, red[parity][0]);
-        const float rstd = 1.f / sqrtf(ss / (float)c + p.eps);
-        if (p.rstd && tid == 0) p.rstd[row] = rstd;
-        auto normed = [&](int col, float* y) __attribute__((always_inline)) {
-            Packed<float> g;
-            lc_load8(g, p.gamma, col, c);
-            value(col, y, false);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) y[j] = y[j] * rstd * g.get(j);
-        };
+        const double rstd = rstd_of(p, ss);
+        if (p.rstd && tid == 0) p.rstd[row] = (float)rstd;
         if constexpr (!Q8) {
+            const float r = (float)rstd;
             for (long long at = tid * 8; at < c; at += kSpan) {
-                normed((int)at, h);
+                Packed<float> g;
+                lc_load8(g, p.gamma, (int)at, c);
+                value((int)at, h, false);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) h[j] = h[j] * r * g.get(j);
                 lc_store8(static_cast<T*>(p.y) + row * (long long)c + at, h, c - (int)at);
             }
         } else {
             uint8_t* y = static_cast<uint8_t*>(p.y) + row * (long long)c;
             const int lanes = p.group >> 3;
             const long long groups = p.group ? (c + p.group - 1) / p.group : 1;
-            float scale = 0.f;
+            const Split split = split_of(rstd);
+            float low[8];
+            const auto scaled = [&](int col) __attribute__((always_inline)) {        // g of the above; returns the largest magnitude
+                Packed<float> g;
+                lc_load8(g, p.gamma, col, c);
+                value(col, h, false);
+                float m = 0.f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float n = h[j] * split.power, a = n * g.get(j);
+                    low[j] = fmaf(n, g.get(j), -a);
+                    h[j] = a;
+                    m = fmaxf(m, fabsf(a));
+                }
+                return m;
+            };
+            Scale scale;
             if (p.group == 0) {
                 float m = 0.f;
-                for (long long at = tid * 8; at < c; at += kSpan) {
-                    normed((int)at, h);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) m = fmaxf(m, fabsf(h[j]));
-                }
-                scale = scale_of(lc_block_max<WAVES>(m, red[parity][1]));
-                if (tid == 0) p.scales[row] = scale;
+                for (long long at = tid * 8; at < c; at += kSpan) m = fmaxf(m, scaled((int)at));
+                scale = scale_of(lc_block_max<WAVES>(m, red[parity][1]), split.rest);
+                if (tid == 0) p.scales[row] = scale.scale;
             }
             for (long long base = 0; base < c; base += kSpan) {     // every lane of a group takes part in its maximum
                 const long long at = base + tid * 8;
                 const int col = at < c ? (int)at : c;
-                normed(col, h);
+                float m = scaled(col);
                 if (p.group) {
-                    float m = 0.f;
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) m = fmaxf(m, fabsf(h[j]));
                     for (int off = 1; off < lanes; off <<= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
-                    scale = scale_of(m);
-                    if (col < c && (tid & (lanes - 1)) == 0) p.scales[row * groups + col / p.group] = scale;
+                    scale = scale_of(m, split.rest);
+                    if (col < c && (tid & (lanes - 1)) == 0) p.scales[row * groups + col / p.group] = scale.scale;
                 }
-                store8_e4m3(y + col, h, 1.f / scale, c - col);
+                store8_e4m3(y + col, h, low, scale, split.rest, c - col);
             }
         }
     }
@@ -463,7 +523,7 @@ lc_status run_fwd(const lc_rmsnorm_desc* d, const void* x, const void* residual,
         lc_off_element(gamma, 4) || lc_off_element(scales, 4) || lc_off_element(save_rstd, 4))
         return LC_ERR_ALIGN;
     NormArgs a{x, residual, gamma, total, y, scales, save_rstd, d->rows, d->x_ld ? d->x_ld : d->c, d->residual_ld ? d->residual_ld : d->c,
-               d->c, group, d->eps};
+               d->c, group, d->eps, 1.0 / d->c};
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     lc_begin_call();
     if (d->dtype == LC_BF16) q8 ? launch_fwd<uint16_t, true>(a, stream) : launch_fwd<uint16_t, false>(a, stream);

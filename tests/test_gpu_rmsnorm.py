@@ -199,3 +199,22 @@ def test_another_stream_and_bit_identical_reruns():
         torch.cuda.synchronize()
         got.append((y, rstd, dx, dg))
     assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("c", [96, 2048, 17000])
+@pytest.mark.parametrize("group", [0, 32])
+@pytest.mark.parametrize("up,gain", [(50, 90), (-50, -80)])
+def test_powers_of_two_move_the_scales_and_not_the_codes(kind, c, group, up, gain):
+    """Every step scales exactly by powers of two without eps, also where total * gamma itself (2^140, 2^-130) is out of fp32's range."""
+    dtype, t, _ = TYPES[kind]
+    x, _ = rows_of(3, c, 19, t)
+    gamma = gu.dev(1 + synth.normal((c,), 20, std=0.3))
+    groups = -(-c // group) if group else 1
+    out = []
+    for a, b in [(0, 0), (up, gain)]:
+        y, s = torch.empty((3, c), dtype=torch.float8_e4m3fn, device=gu.DEV), torch.empty((3, groups), device=gu.DEV)
+        lc.rmsnorm_fwd_q8(lc.RmsNormDesc(3, c, eps=0.0, dtype=dtype), x * 2.0 ** a, None, gamma * 2.0 ** b, None, y, s, group)
+        torch.cuda.synchronize()
+        out.append((y.view(torch.uint8), s))
+    assert torch.equal(out[0][0], out[1][0]) and torch.equal(out[0][1] * 2.0 ** gain, out[1][1])
