@@ -21,7 +21,7 @@
 namespace {
 
 constexpr int kMostTop = 32;
-constexpr int kMostWaves = 4;               // of a block
+constexpr int kMostWaves = 16, kMostListing = 8;      // of a block; with alternatives, for which a wave needs 6.5 KB of LDS
 constexpr int kCandidates = 256;            // keys that a wave's LDS has room for
 constexpr int kChunks = 128, kRounds = 32;  // places of a lane's values of a round, and rounds, that it has room for
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -320,12 +320,12 @@ __device__ __forceinline__ void leave(const TokenArgs& p, long long row, const T
     }
 }
 
-// A slice of a row by a block of up to kMostWaves waves, whose first joins what the others leave in LDS.  Rounds of 512 * CH values go to the waves in turn, so that a
+// A slice of a row by a block of one wave or several, whose first joins what the others leave in LDS.  Rounds of 512 * CH values go to the waves in turn, so that a
 // block reads one stretch at a time; a wave's next round is under way while one is summed.  ENT: with the entropy.  TOP: with the alternatives: a lane marks in LDS how
 // large the largest of its values of each round is (the upper half of its order); of those that may reach the bound, a few more than N as a rule, one each a
 // lane reads the values again.  LDS: WaveTop a wave and its list of `top`.
 template <typename T, int CH, bool ENT, bool TOP>
-__global__ void __launch_bounds__(kMostWaves * 64, TOP && sizeof(T) * CH == 8 ? 3 : 4) token_sums_kernel(const TokenArgs p) {
+__global__ void __launch_bounds__((TOP ? kMostListing : kMostWaves) * 64, TOP && sizeof(T) * CH == 8 ? 3 : 4) token_sums_kernel(const TokenArgs p) {
     __shared__ float4 stats[kMostWaves];
     extern __shared__ __align__(16) char lds[];
     constexpr uint32_t kMaskedBits = sizeof(T) == 2 ? 0xff80u : 0xff800000u;
@@ -553,21 +553,55 @@ struct TokenPlan {
     size_t keys, total;
 };
 
-constexpr long long kFillWaves = 16384, kFillTop = 2048;      // waves that rows are cut into
+constexpr int kResident = 4096;      // waves that the chip holds at a time, 16 a compute unit
 
+// Waves of a row.  As a rule they are one block, which joins them itself: a second launch costs 3 us or more.  Too few leave the chip idle, and with more than it holds at
+// once the last of them are too few.  us for bf16 rows by waves a row, or waves of a block x blocks:
+//   without alternatives           16 waves   8 waves   4 waves   1 wave    in blocks of one
+//     64 rows of 131072              10.7       12.3        -       57         9.0 (32)
+//     128 rows of 131072             11.1       12.6        -       57        11.5 (32)
+//     256 rows of 32000               6.1        6.1       7.2      17         9.3 (8)
+//     1024 rows of 32000             18         15.0      14.0      18.5      17.7 (4)
+//     4096 rows of 32000             68         51.2      51.6      53.8      53.4 (8)
+//     4096 rows of 131072           188.5 (12) 175.6     193       198       189.2 (8)
+//     6000 rows of 16000              -         47.5      40.0      47.3      43.6 (4)
+//   with 20 alternatives                       8 waves   4 waves   2 waves   1 wave      in blocks of one
+//     1 row of 32000                            12.0      12.8       -        22           11.0 (32)
+//     64 rows of 131072                         22.5       -         -         -           16.0 (64), 16.5 (32)
+//     400 rows of 16000                         16.2      12.9      16.1      16.8         17.4 (4)
+//     400 rows of 131072                        33.2      37.6       -         -           36.8 (16)
+//     700 rows of 131072                        54.3      46.9       -         -           50.5 (4)
+//     2048 rows of 32000                        59.2      41.7      36.9      39.9         41.6 (2)
+//     3000 rows of 32000                        82.5      59.4      58.3      47.9         61.1 (2)
 TokenPlan plan_of(const lc_token_desc* d) {
     TokenPlan p;
-    // 16 values a lane of a round; eight of fp32 logits with alternatives, whose registers a SIMD then has for four waves, where there are rows enough for them (1000 rows
-    // of 32000 39 us, so 31; one row of 128000 10.2, so 11.9)
-    const bool eight = d->top && d->dtype == LC_F32 && d->rows * ((d->vocab + 1023) / 1024) >= 2 * kFillTop;
+    // 16 values a lane of a round; eight of fp32 logits with alternatives where that fills the chip, whose registers then do for four waves a SIMD instead of three (us:
+    // 300 rows of 32000 22.7, so 15.5; 1000 37.3, so 31; one row of 128000 10.2, so 11.9)
+    const int thousands = (d->vocab + 1023) / 1024;
+    const bool eight = d->top && d->dtype == LC_F32 && d->rows * thousands >= kResident;
     p.chunks = d->vocab <= 512 || eight ? 1 : 2;
     const int round = 512 * p.chunks, rounds = (d->vocab + round - 1) / round;
-    int most = 1;                                      // rounds of a wave
-    while (most < rounds && (!d->top || 2 * most <= kRounds) && d->rows * ((rounds + 2 * most - 1) / (2 * most)) >= (d->top ? kFillTop : kFillWaves)) most *= 2;
-    const int waves = (rounds + most - 1) / most;      // of a row
-    p.blocks = waves > kMostWaves ? waves : 1;
+    const int fit = (int)(kResident / std::clamp<long long>(d->rows, 1, kResident));      // waves a row that the chip holds at once
+    bool apart;                                        // every wave a block
+    int waves;
+    if (!d->top) {
+        apart = rounds > 96 && d->rows <= 128;
+        if (apart) waves = std::min(rounds, fit);
+        else waves = d->rows < 256 ? std::min(rounds, kMostWaves) : std::clamp(rounds / 4, 1, 8);
+    } else {
+        // (a wave's own list takes as long as several rounds; of three, five, six or seven waves fewer fit: 700 rows of 70000 by four 28.7 us, by five 40)
+        apart = (thousands >= 32 && d->rows <= 64) || (thousands >= 48 && d->rows <= 128);
+        const int kilobytes = thousands * (d->dtype == LC_BF16 ? 2 : 4), least = (rounds + kRounds - 1) / kRounds;
+        if (apart) waves = std::max(least, std::min(rounds, fit / 2));
+        else waves = kilobytes >= 128 && fit >= 8 ? 8 : kilobytes >= 32 && fit >= 4 ? 4 : kilobytes >= 64 && fit >= 2 ? 2 : 1;
+        if (waves < least) waves = std::max(least, 4);
+    }
+    const int most = apart ? 1 : d->top ? kMostListing : kMostWaves;
+    p.blocks = (waves + most - 1) / most;
     p.waves = (waves + p.blocks - 1) / p.blocks;
-    p.slice = ((d->vocab + p.blocks - 1) / p.blocks + 7) & ~7;
+    const int each = (rounds + p.blocks - 1) / p.blocks;                // rounds of a block
+    p.blocks = (rounds + each - 1) / each;
+    p.slice = each * round;
     const size_t units = (size_t)d->rows * p.blocks;
     p.keys = p.blocks == 1 ? 0 : (units * sizeof(float4) + 255) & ~(size_t)255;
     p.total = p.blocks == 1 ? 0 : p.keys + ((units * d->top * sizeof(Key) + 255) & ~(size_t)255);
