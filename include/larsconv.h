@@ -418,7 +418,7 @@ lc_status token_logprob_fwd(const lc_token_desc* desc, const void* logits, const
  *     dlogits_j = dlogprob * ([j = token] - p_j) - dentropy * p_j * (log p_j + entropy).
  * lse and entropy: what the forward pass gave (entropy may be NULL without dentropy).  dlogprob has no effect where the token does not
  * count; masked logits, and rows that are masked entirely, get 0.  p_j is formed from lse as stored (relative error about |lse| 2^-24)
- * while |lse| is at most 256 (fp32 logits) or 16384 (bf16); rows beyond are summed again by every 1024 columns of theirs (right, and slow).  dlogits_ld: elements from row to row (0: vocab; otherwise >= vocab; the pad is
+ * while |lse| is at most 256 (fp32 logits) or 16384 (bf16); rows beyond are summed again, by one wave each (right, and slow).  dlogits_ld: elements from row to row (0: vocab; otherwise >= vocab; the pad is
  * not written).  dlogits may be the logits' own buffer if its ld is theirs; otherwise they must not overlap. */
 lc_status token_logprob_bwd(const lc_token_desc* desc, const void* logits, const int32_t* tokens, const float* lse, const float* entropy,
                             const float* dlogprob, const float* dentropy, void* dlogits, int64_t dlogits_ld, void* hip_stream);

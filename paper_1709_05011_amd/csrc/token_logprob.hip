@@ -468,9 +468,27 @@ struct TokenBwdArgs {
     int vocab;
 };
 
-// Beyond these magnitudes the rounding of lse (2^-24 of it) shows in p: such a row's sums are made again by every wave of it.
+// Beyond these magnitudes the rounding of lse (2^-24 of it) shows in p, and products with log2 e may overflow.
 template <typename T>
 constexpr float kLseEnd = sizeof(T) == 2 ? 16384.f : 256.f;
+
+// Such a row's gradient, by one wave: its sums again, then all of it (dz may be the logits' own buffer: no other wave writes to the row).
+template <typename T>
+__device__ __attribute__((noinline)) void far_row(const T* z, T* out, int vocab, int token, float a, float b, float ent) {
+    const float3 w = sums_by_distances(z, 0, vocab, vocab, vocab);
+    const float log_s = logf(w.y);
+    for (int col = threadIdx.x * 8; col < vocab; col += 512) {
+        Packed<T> v;
+        lc_load8(v, z, col, vocab);
+        float o[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float d = (v.get(j) - w.x) - log_s;
+            o[j] = (col + j == token ? a : 0.f) - __builtin_amdgcn_exp2f(d * kLog2e) * (a + b * (fmaxf(d, kFar) + ent));
+        }
+        lc_store8(out + col, o, vocab - col);
+    }
+}
 
 // One wave a block, CH times eight columns a lane.  With d = (z - lse) log2 e the result is 2^d (A + B d): a fused multiply-add, an exponential, another multiply-add and
 // a product a value, the token's own term apart.  Bound by memory: 4096 rows of 32000 bf16 85 us, 6.2 TB/s of what it must read and write.  The results go past the caches (forward
@@ -483,6 +501,7 @@ __global__ void __launch_bounds__(64) token_bwd_kernel(const TokenBwdArgs p) {
     const bool full = first + 512 * CH <= p.vocab;
     for (long long row = blockIdx.y; row < p.rows; row += gridDim.y) {
         const T* z = static_cast<const T*>(p.z) + row * p.ld;
+        T* out = static_cast<T*>(p.dz) + row * p.dld;
         Packed<T> v[CH];
         lc_issue8(v, z, column, p.vocab, full);
         const float lse = p.lse[row];
@@ -491,17 +510,13 @@ __global__ void __launch_bounds__(64) token_bwd_kernel(const TokenBwdArgs p) {
         const float a = p.dlogprob && counts && !empty ? p.dlogprob[row] : 0.f;
         const float b = p.dentropy && !empty ? p.dentropy[row] : 0.f;
         const float ent = p.dentropy ? p.entropy[row] : 0.f;
-        float from = lse, log_s = 0.f;
         if (fabsf(lse) > kLseEnd<T> && !empty) {
-            const float3 w = sums_by_distances(z, 0, p.vocab, p.vocab, p.vocab);
-            from = w.x;
-            log_s = logf(w.y);
+            if (blockIdx.x == 0) far_row(z, out, p.vocab, token, a, b, ent);
+            continue;
         }
         lc_settle8(v, column, p.vocab, p.vocab, full);
-        T* out = static_cast<T*>(p.dz) + row * p.dld;
-        // (as in the forward pass: every exponent is off by what rounding the product takes; with the row's log S it goes into the factors)
-        const bool far = fabsf(from) > kProductsEnd;
-        const float less = -from * kLog2e, off = far ? 0.f : fmaf(from, kLog2e, less) + log_s * kLog2e, scale = -__builtin_amdgcn_exp2f(-off);
+        // (as in the forward pass: every exponent is off by what rounding the product takes, which goes into the factors)
+        const float less = -lse * kLog2e, off = fmaf(lse, kLog2e, less), scale = -__builtin_amdgcn_exp2f(-off);
         const float A = scale * (a + b * (ent - off * kLn2)), B = scale * (b * kLn2);
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
@@ -510,12 +525,6 @@ __global__ void __launch_bounds__(64) token_bwd_kernel(const TokenBwdArgs p) {
             if (empty) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) o[j] = 0.f;
-            } else if (far) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float d = (v[i].get(j) - from) - log_s;
-                    o[j] = -__builtin_amdgcn_exp2f(d * kLog2e) * (a + b * (fmaxf(d, kFar) + ent));
-                }
             } else if (b != 0.f) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {

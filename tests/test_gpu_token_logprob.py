@@ -226,3 +226,21 @@ def test_many_rows_of_one_element_and_bit_identical_reruns():
     _, tokens = tokens_of(3000, 9000, 10)
     first, again = run(lc.LC_BF16, z, tokens, 9000, 8), run(lc.LC_BF16, z, tokens, 9000, 8)
     assert all(torch.equal(x, y) for x, y in zip(first[1], again[1])) and np.array_equal(first[2], again[2]) and np.array_equal(first[3], again[3])
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab", [700, 9001, 60000])
+def test_gradient_of_rows_far_from_zero_in_the_logits_own_buffer(kind, vocab):
+    """Rows whose sums the gradient makes again (see the lowest value and |lse| above): no part of them may be written before they are read."""
+    dtype, t, _ = TYPES[kind]
+    rows = 24
+    place = np.arange(vocab, dtype=np.float64)
+    z = np.stack([3e4 * (1 + r) + (place * (r + 3)) % 11 if r % 3 else np.where(place % 7 == r % 7, float(torch.finfo(t).max), float(torch.finfo(t).min)) for r in range(rows)])
+    z = torch.from_numpy(z).to(t).to(gu.DEV)
+    _, tokens = tokens_of(rows, vocab, 11)
+    d, (lp, ent, lse), _, _ = run(dtype, z, tokens, vocab)
+    one, dz = torch.ones(rows, device=gu.DEV), torch.empty_like(z)
+    lc.token_logprob_bwd(d, z, tokens, lse, ent, one, one, dz)
+    lc.token_logprob_bwd(d, z, tokens, lse, ent, one, one, z)
+    torch.cuda.synchronize()
+    assert torch.equal(z, dz)
