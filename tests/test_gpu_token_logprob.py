@@ -244,3 +244,17 @@ def test_gradient_of_rows_far_from_zero_in_the_logits_own_buffer(kind, vocab):
     lc.token_logprob_bwd(d, z, tokens, lse, ent, one, one, z)
     torch.cuda.synchronize()
     assert torch.equal(z, dz)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,vocab", [(70, 34001), (130, 66005), (270, 9001), (300, 33000), (1100, 16003), (4200, 1500), (2, 270001)])
+@pytest.mark.parametrize("top", [0, 5])
+def test_forward_with_rows_divided_in_every_way(kind, rows, vocab, top):
+    """Rows by one wave, by two to sixteen of a block, and by blocks of one; one round a wave and several; by a third of the rows with masked logits."""
+    dtype, t, _ = TYPES[kind]
+    z, _ = logits_of(rows, vocab, 12, t, pad=vocab % 8)
+    z[::3, vocab // 7: vocab // 2] = -float("inf")
+    z64 = f64(z)
+    t64, tokens = tokens_of(rows, vocab, 13)
+    d, got, ids, lps = run(dtype, z, tokens, vocab, top)
+    check_forward(vocab, (d, got, ids, lps), ops.token_logprob(z64, t64, top), top)

@@ -6,7 +6,7 @@ import pytest
 from paper_1709_05011_amd import larsconv as lc
 
 FAKE = 0x10000000  # never dereferenced: every call below fails validation first, or has no work
-ONE, MANY, TOP = lc.TokenDesc(4, 100), lc.TokenDesc(4, 50000), lc.TokenDesc(4, 50000, top=5)
+ONE, MANY, TOP = lc.TokenDesc(4, 100), lc.TokenDesc(4, 131072), lc.TokenDesc(4, 131072, top=5)
 
 
 def status(fn, *args, **kw):
