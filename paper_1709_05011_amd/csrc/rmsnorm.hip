@@ -43,6 +43,23 @@ __device__ __forceinline__ float block_join(float x, int waves, float* red, W&& 
     return s;
 }
 
+// How a block's threads share rows: all of them one row (LANES 0), or LANES neighbouring lanes of a wave each a row (of a block of kNarrowThreads).
+constexpr int kNarrowThreads = 256;
+template <int LANES>
+struct Rows {
+    static constexpr int kEach = LANES ? kNarrowThreads / LANES : 1;     // rows of a block
+    const int tid = LANES ? threadIdx.x & (LANES - 1) : threadIdx.x, threads = LANES ? LANES : blockDim.x;
+    const long long first = (long long)blockIdx.x * kEach + (LANES ? threadIdx.x / (kNarrowThreads / kEach) : 0), step = (long long)gridDim.x * kEach;
+
+    template <typename W, typename F>
+    __device__ __forceinline__ float join(float v, float* red, W&& wave, F&& f) const {
+        if constexpr (LANES == 0) return block_join(v, threads >> 6, red, wave, f);
+#pragma unroll
+        for (int off = 1; off < LANES; off <<= 1) v = f(v, __shfl_xor(v, off, 64));
+        return v;
+    }
+};
+
 constexpr float kE4m3Max = 448.f, kLeastScale = 0x1p-126f;
 
 // 1/sqrt(sum / c + eps) to more than fp32's places: the instruction's estimate and one step of Newton's method in double.
@@ -114,14 +131,15 @@ __device__ __forceinline__ void store8_e4m3(uint8_t* p, const float* g, const fl
 // A block per row (rows dealt round the grid), its waves as many as the row has 512 * CH columns: all of a row's loads are under way at once and it is read once.  What bounds it is
 // memory: 8192 rows of 4096 bf16 with the residual, its sum and the output 45.5 us, 5.9 TB/s of the 268 MB that must move; 4099 rows of 5120 with residual and sum to 8 bits with a scale per 128
 // 28.9 us, 5.1 TB/s; one row 2.6 us, a launch.  NT: past the caches.  ENDS: what may lie past a row's end, so that rows of whole waves carry no comparisons.
-template <typename T, int CH, bool Q8, bool NT, Ends ENDS>
-__global__ void __launch_bounds__(kMostWaves * 64) rmsnorm_fwd_kernel(const NormArgs p) {
+template <typename T, int CH, bool Q8, bool NT, Ends ENDS, int LANES = 0>
+__global__ void __launch_bounds__(LANES ? kNarrowThreads : kMostWaves * 64) rmsnorm_fwd_kernel(const NormArgs p) {
     __shared__ float red[2][2][kMostWaves];
-    const int tid = threadIdx.x, c = p.c, waves = blockDim.x >> 6, threads = blockDim.x;
+    const Rows<LANES> rows;
+    const int tid = rows.tid, c = p.c, threads = rows.threads;
     const auto column = [tid, threads](int i) { return (i * threads + tid) * 8; };
     const auto inside = [&](int i) { return ENDS == kWhole ? 8 : ENDS == kEights ? (column(i) < c ? 8 : 0) : c - column(i); };
     int parity = 0;
-    for (long long row = blockIdx.x; row < p.rows; row += gridDim.x, parity ^= 1) {
+    for (long long row = rows.first; row < p.rows; row += rows.step, parity ^= 1) {
         const T* x = static_cast<const T*>(p.x) + row * p.x_ld;
         Packed<T> px[CH], pr[CH];
         Packed<float> pg[CH];
@@ -153,7 +171,7 @@ __global__ void __launch_bounds__(kMostWaves * 64) rmsnorm_fwd_kernel(const Norm
 #pragma unroll
             for (int i = 0; i < CH; ++i) lc_store8<NT>(t + column(i), h[i], inside(i));
         }
-        ss = block_join(ss, waves, red[parity][0], [](float a) { return lc_wave_sum(a); }, [](float a, float b) { return a + b; });
+        ss = rows.join(ss, red[parity][0], [](float a) { return lc_wave_sum(a); }, [](float a, float b) { return a + b; });
         const double rstd = rstd_of(p, ss);
         if (p.rstd && tid == 0) p.rstd[row] = (float)rstd;
         if constexpr (!Q8) {
@@ -184,13 +202,13 @@ __global__ void __launch_bounds__(kMostWaves * 64) rmsnorm_fwd_kernel(const Norm
                 float m = amax[0];
 #pragma unroll
                 for (int i = 1; i < CH; ++i) m = fmaxf(m, amax[i]);
-                m = block_join(m, waves, red[parity][1], [](float a) { return lc_wave_max(a); }, [](float a, float b) { return fmaxf(a, b); });
+                m = rows.join(m, red[parity][1], [](float a) { return lc_wave_max(a); }, [](float a, float b) { return fmaxf(a, b); });
                 const Scale scale = scale_of(m, split.rest);
                 if (tid == 0) p.scales[row] = scale.scale;
 #pragma unroll
                 for (int i = 0; i < CH; ++i) store8_e4m3(y + column(i), h[i], low[i], scale, split.rest, inside(i));
             } else {
-                const int lanes = p.group >> 3, shift = __builtin_ctz(p.group);
+                const int lanes = LANES ? min(p.group >> 3, LANES) : p.group >> 3, shift = __builtin_ctz(p.group);
                 const long long groups = (c + p.group - 1) >> shift;
 #pragma unroll
                 for (int i = 0; i < CH; ++i) {
@@ -308,10 +326,11 @@ struct NormBwdArgs {
 // A block walks rows blockIdx, blockIdx + gridDim, ...; a thread's columns stay the same, so that its share of dgamma stays in registers and no atomics are needed, and the next row's loads
 // are under way while one is summed.  Bound by memory: 8192 rows of 4096 bf16 with three inputs and dx 43 us, 6.2 TB/s; 1003 rows of 1537 fp32 7 us, of which the launch and the
 // latency of four rows one after another are most.
-template <typename T, int CH, bool NT, Ends ENDS>
-__global__ void __launch_bounds__(kMostWaves * 64) rmsnorm_bwd_kernel(const NormBwdArgs p) {
+template <typename T, int CH, bool NT, Ends ENDS, int LANES = 0>
+__global__ void __launch_bounds__(LANES ? kNarrowThreads : kMostWaves * 64) rmsnorm_bwd_kernel(const NormBwdArgs p) {
     __shared__ float red[2][kMostWaves];
-    const int tid = threadIdx.x, c = p.c, waves = blockDim.x >> 6, threads = blockDim.x;
+    const Rows<LANES> rows;
+    const int tid = rows.tid, c = p.c, threads = rows.threads;
     const auto column = [tid, threads](int i) { return (i * threads + tid) * 8; };
     const auto inside = [&](int i) { return ENDS == kWhole ? 8 : ENDS == kEights ? (column(i) < c ? 8 : 0) : c - column(i); };
     Packed<float> pg[CH];
@@ -328,8 +347,8 @@ __global__ void __launch_bounds__(kMostWaves * 64) rmsnorm_bwd_kernel(const Norm
         next_rstd = p.rstd[row];
     };
     int parity = 0;
-    if (blockIdx.x < p.rows) issue(blockIdx.x);
-    for (long long row = blockIdx.x; row < p.rows; row += gridDim.x, parity ^= 1) {
+    if (rows.first < p.rows) issue(rows.first);
+    for (long long row = rows.first; row < p.rows; row += rows.step, parity ^= 1) {
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
             ph[i] = nh[i];
@@ -337,7 +356,7 @@ __global__ void __launch_bounds__(kMostWaves * 64) rmsnorm_bwd_kernel(const Norm
             pt[i] = nt[i];
         }
         rstd = next_rstd;
-        if (row + gridDim.x < p.rows) issue(row + gridDim.x);
+        if (row + rows.step < p.rows) issue(row + rows.step);
         float s = 0.f;
         lc_settle8<ENDS>(ph, column, c);
         lc_settle8<ENDS>(pd, column, c);
@@ -350,7 +369,7 @@ __global__ void __launch_bounds__(kMostWaves * 64) rmsnorm_bwd_kernel(const Norm
                 s = fmaf(d * pg[i].get(j), n, s);
                 acc[i][j] = fmaf(d, n, acc[i][j]);
             }
-        const float mean = block_join(s, waves, red[parity], [](float a) { return lc_wave_sum(a); }, [](float a, float b) { return a + b; }) / (float)c;
+        const float mean = rows.join(s, red[parity], [](float a) { return lc_wave_sum(a); }, [](float a, float b) { return a + b; }) / (float)c;
         T* dx = static_cast<T*>(p.dx) + row * (long long)c;
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
@@ -368,8 +387,19 @@ __global__ void __launch_bounds__(kMostWaves * 64) rmsnorm_bwd_kernel(const Norm
         }
     }
     float* part = p.part + (long long)blockIdx.x * c;
+    if constexpr (LANES == 0) {
 #pragma unroll
-    for (int i = 0; i < CH; ++i) lc_store8(part + column(i), acc[i], inside(i));
+        for (int i = 0; i < CH; ++i) lc_store8(part + column(i), acc[i], inside(i));
+    } else {                                    // the block's rows in a fixed order: those of a wave, then the waves
+        __shared__ float share[kNarrowThreads / 64][LANES * 8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            for (int off = LANES; off < 64; off <<= 1) acc[0][j] += __shfl_xor(acc[0][j], off, 64);
+            if ((threadIdx.x & 63) < LANES) share[threadIdx.x >> 6][tid * 8 + j] = acc[0][j];
+        }
+        __syncthreads();
+        if (threadIdx.x < c) part[threadIdx.x] = (share[0][threadIdx.x] + share[1][threadIdx.x]) + (share[2][threadIdx.x] + share[3][threadIdx.x]);
+    }
 }
 
 // Wide rows: dgamma's shares by column tiles and ranges of rows (blockIdx.y), and dx in two passes over a row.
@@ -498,6 +528,22 @@ void launch_fwd(const NormArgs& a, hipStream_t stream) {
     else if (a.c % 8 == 0) hipLaunchKernelGGL((rmsnorm_fwd_kernel<T, CH, Q8, NT, kEights>), grid, block, 0, stream, a);
     else if constexpr (CH * sizeof(T) < 8) hipLaunchKernelGGL((rmsnorm_fwd_kernel<T, CH, Q8, NT, kAny>), grid, block, 0, stream, a);
 }
+// Lanes of a row where a wave takes several, from what a wave of its own per row takes, us, 2^25 elements in all: bf16 forward with c = 64, 128, 256 125, 69, 39, so 26;
+// to 8 bits 216, 119, 65, so 42; forward and backward 250, 140, 88, so 66; fp32 forward 143, 82, 51, so 49.
+constexpr int kMostNarrow = 256;             // columns
+int lanes_of(int c) { return c <= 64 ? 8 : c <= 128 ? 16 : 32; }
+template <typename T, bool Q8, bool NT, int LANES>
+void launch_fwd_narrow(const NormArgs& a, hipStream_t stream) {
+    const dim3 grid((unsigned)std::min((a.rows + Rows<LANES>::kEach - 1) / Rows<LANES>::kEach, kMostBlocks)), block(kNarrowThreads);
+    if (a.c % 8 == 0) hipLaunchKernelGGL((rmsnorm_fwd_kernel<T, 1, Q8, NT, kEights, LANES>), grid, block, 0, stream, a);
+    else hipLaunchKernelGGL((rmsnorm_fwd_kernel<T, 1, Q8, NT, kAny, LANES>), grid, block, 0, stream, a);
+}
+template <typename T, bool Q8, bool NT>
+void launch_fwd_narrow(const NormArgs& a, hipStream_t stream) {
+    const int lanes = lanes_of(a.c);
+    lanes == 8 ? launch_fwd_narrow<T, Q8, NT, 8>(a, stream) : lanes == 16 ? launch_fwd_narrow<T, Q8, NT, 16>(a, stream) : launch_fwd_narrow<T, Q8, NT, 32>(a, stream);
+}
+
 // Rows that go by in passes: what a block's registers do not hold (of fp32 rows that end within a thread's columns 16 a thread neither: 3000 x 9001, forward and backward, 317 us, in
 // passes 275), and under eight columns.
 bool in_passes(const lc_dtype dtype, int c) { return c < 8 || c > kMostColumns || (dtype == LC_F32 && c % 8 && c > 512 * kMostWaves); }
@@ -510,8 +556,10 @@ void launch_fwd(const NormArgs& a, hipStream_t stream) {
     }
     if constexpr (sizeof(T) == 2) {
         const long long bytes = a.rows * a.c * (2 + (a.r ? 2 : 0) + (a.total ? 2 : 0) + (Q8 ? 1 : 2));
+        if (bytes >= kStreamBytes && a.c <= kMostNarrow) return launch_fwd_narrow<T, Q8, true>(a, stream);
         if (bytes >= kStreamBytes) return chunks_of<T>(a.c) == 1 ? launch_fwd<T, 1, Q8, true>(a, stream) : launch_fwd<T, 2, Q8, true>(a, stream);
     }
+    if (a.c <= kMostNarrow) return launch_fwd_narrow<T, Q8, false>(a, stream);
     chunks_of<T>(a.c) == 1 ? launch_fwd<T, 1, Q8, false>(a, stream) : launch_fwd<T, 2, Q8, false>(a, stream);
 }
 
@@ -537,10 +585,15 @@ lc_status run_fwd(const lc_rmsnorm_desc* d, const void* x, const void* residual,
 }
 
 // Blocks of the backward pass, each with a share of dgamma: 16 waves a compute unit, with four rows a block or more as long as every unit has one.  us, 8192 x 4096 bf16 forward and
-// backward with 256, 512, 1024 blocks 110, 96.6, 104; 16384 x 1024 97, 70, 58; 2048 x 16384 105, 114, 128; 512 x 4096 14.8, 16.0, 16.0.
+// backward with 256, 512, 1024 blocks 110, 96.6, 104; 16384 x 1024 97, 70, 58; 2048 x 16384 105, 114, 128; 512 x 4096 14.8, 16.0, 16.0.  Narrow rows: the same with a wave's several rows
+// for one (2^20 rows of 32 with 512, 1024, 2048 blocks of four waves 97, 83, 88).
 int bwd_chunks(int c) { return c <= 512 * kMostWaves ? 1 : 2; }
 long long bwd_blocks(const lc_rmsnorm_desc* d) {
     if (in_passes(d->dtype, d->c)) return std::min<long long>(d->rows, 64);
+    if (d->c <= kMostNarrow) {
+        const long long each = kNarrowThreads / lanes_of(d->c), all = (d->rows + each - 1) / each;
+        return std::min(all, std::max<long long>(256, std::min<long long>(1024, all / 4)));
+    }
     const int columns = 512 * bwd_chunks(d->c), waves = (d->c + columns - 1) / columns;
     return std::min<long long>(d->rows, std::max<long long>(256, std::min<long long>(4096 / waves, d->rows / 4)));
 }
@@ -552,6 +605,16 @@ void launch_bwd(const NormBwdArgs& a, int blocks, hipStream_t stream) {
     else if (a.c % 8 == 0) hipLaunchKernelGGL((rmsnorm_bwd_kernel<T, CH, NT, kEights>), grid, block, 0, stream, a);
     else if constexpr (CH * sizeof(T) < 8) hipLaunchKernelGGL((rmsnorm_bwd_kernel<T, CH, NT, kAny>), grid, block, 0, stream, a);
 }
+template <typename T, bool NT, int LANES>
+void launch_bwd_narrow(const NormBwdArgs& a, int blocks, hipStream_t stream) {
+    if (a.c % 8 == 0) hipLaunchKernelGGL((rmsnorm_bwd_kernel<T, 1, NT, kEights, LANES>), dim3((unsigned)blocks), dim3(kNarrowThreads), 0, stream, a);
+    else hipLaunchKernelGGL((rmsnorm_bwd_kernel<T, 1, NT, kAny, LANES>), dim3((unsigned)blocks), dim3(kNarrowThreads), 0, stream, a);
+}
+template <typename T, bool NT>
+void launch_bwd_narrow(const NormBwdArgs& a, int blocks, hipStream_t stream) {
+    const int lanes = lanes_of(a.c);
+    lanes == 8 ? launch_bwd_narrow<T, NT, 8>(a, blocks, stream) : lanes == 16 ? launch_bwd_narrow<T, NT, 16>(a, blocks, stream) : launch_bwd_narrow<T, NT, 32>(a, blocks, stream);
+}
 template <typename T>
 void launch_bwd(const NormBwdArgs& a, int blocks, hipStream_t stream) {
     if (in_passes(sizeof(T) == 2 ? LC_BF16 : LC_F32, a.c)) {
@@ -560,8 +623,10 @@ void launch_bwd(const NormBwdArgs& a, int blocks, hipStream_t stream) {
         return;
     }
     if constexpr (sizeof(T) == 2) {
+        if (a.rows * a.c * (a.dh ? 8 : 6) >= kStreamBytes && a.c <= kMostNarrow) return launch_bwd_narrow<T, true>(a, blocks, stream);
         if (a.rows * a.c * (a.dh ? 8 : 6) >= kStreamBytes) return bwd_chunks(a.c) == 1 ? launch_bwd<T, 1, true>(a, blocks, stream) : launch_bwd<T, 2, true>(a, blocks, stream);
     }
+    if (a.c <= kMostNarrow) return launch_bwd_narrow<T, false>(a, blocks, stream);
     bwd_chunks(a.c) == 1 ? launch_bwd<T, 1, false>(a, blocks, stream) : launch_bwd<T, 2, false>(a, blocks, stream);
 }
 

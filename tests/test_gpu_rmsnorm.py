@@ -218,3 +218,15 @@ def test_powers_of_two_move_the_scales_and_not_the_codes(kind, c, group, up, gai
         torch.cuda.synchronize()
         out.append((y.view(torch.uint8), s))
     assert torch.equal(out[0][0], out[1][0]) and torch.equal(out[0][1] * 2.0 ** gain, out[1][1])
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,c", [(1, 16), (33, 64), (70, 72), (17, 128), (700, 128), (9, 129), (301, 200), (500, 256), (5000, 64), (40000, 40)])
+def test_narrow_rows(kind, rows, c):
+    """Several rows of a wave: blocks that end within their rows, rows that end within a lane's columns, groups as wide as a row and wider."""
+    for residual, pad, offset in [(True, 0, 0), (False, 5, 1)]:
+        test_forward(kind, rows, c, residual, pad, offset)
+    for group in (0, 32, 512):
+        test_forward_in_8_bits(kind, rows, c, group)
+    for joined, pad in [(True, 0), (False, 3)]:
+        test_backward(kind, rows, c, joined, pad)
