@@ -48,12 +48,13 @@ constexpr int kNarrowThreads = 256;
 template <int LANES>
 struct Rows {
     static constexpr int kEach = LANES ? kNarrowThreads / LANES : 1;     // rows of a block
-    const int tid = LANES ? threadIdx.x & (LANES - 1) : threadIdx.x, threads = LANES ? LANES : blockDim.x;
-    const long long first = (long long)blockIdx.x * kEach + (LANES ? threadIdx.x / (kNarrowThreads / kEach) : 0), step = (long long)gridDim.x * kEach;
+    static __device__ __forceinline__ int tid() { return LANES ? threadIdx.x & (LANES - 1) : threadIdx.x; }
+    static __device__ __forceinline__ long long first() { return LANES ? (long long)blockIdx.x * kEach + threadIdx.x / (kNarrowThreads / kEach) : blockIdx.x; }
+    static __device__ __forceinline__ long long step() { return LANES ? (long long)gridDim.x * kEach : gridDim.x; }
 
     template <typename W, typename F>
-    __device__ __forceinline__ float join(float v, float* red, W&& wave, F&& f) const {
-        if constexpr (LANES == 0) return block_join(v, threads >> 6, red, wave, f);
+    static __device__ __forceinline__ float join(float v, int waves, float* red, W&& wave, F&& f) {
+        if constexpr (LANES == 0) return block_join(v, waves, red, wave, f);
 #pragma unroll
         for (int off = 1; off < LANES; off <<= 1) v = f(v, __shfl_xor(v, off, 64));
         return v;
@@ -134,12 +135,12 @@ __device__ __forceinline__ void store8_e4m3(uint8_t* p, const float* g, const fl
 template <typename T, int CH, bool Q8, bool NT, Ends ENDS, int LANES = 0>
 __global__ void __launch_bounds__(LANES ? kNarrowThreads : kMostWaves * 64) rmsnorm_fwd_kernel(const NormArgs p) {
     __shared__ float red[2][2][kMostWaves];
-    const Rows<LANES> rows;
-    const int tid = rows.tid, c = p.c, threads = rows.threads;
-    const auto column = [tid, threads](int i) { return (i * threads + tid) * 8; };
+    using Of = Rows<LANES>;
+    const int tid = Of::tid(), c = p.c, waves = blockDim.x >> 6, threads = LANES ? LANES : blockDim.x;
+    const auto column = [=](int i) { return (i * threads + tid) * 8; };
     const auto inside = [&](int i) { return ENDS == kWhole ? 8 : ENDS == kEights ? (column(i) < c ? 8 : 0) : c - column(i); };
     int parity = 0;
-    for (long long row = rows.first; row < p.rows; row += rows.step, parity ^= 1) {
+    for (long long row = Of::first(); row < p.rows; row += Of::step(), parity ^= 1) {
         const T* x = static_cast<const T*>(p.x) + row * p.x_ld;
         Packed<T> px[CH], pr[CH];
         Packed<float> pg[CH];
@@ -171,7 +172,7 @@ __global__ void __launch_bounds__(LANES ? kNarrowThreads : kMostWaves * 64) rmsn
 #pragma unroll
             for (int i = 0; i < CH; ++i) lc_store8<NT>(t + column(i), h[i], inside(i));
         }
-        ss = rows.join(ss, red[parity][0], [](float a) { return lc_wave_sum(a); }, [](float a, float b) { return a + b; });
+        ss = Of::join(ss, waves, red[parity][0], [](float a) { return lc_wave_sum(a); }, [](float a, float b) { return a + b; });
         const double rstd = rstd_of(p, ss);
         if (p.rstd && tid == 0) p.rstd[row] = (float)rstd;
         if constexpr (!Q8) {
@@ -202,7 +203,7 @@ __global__ void __launch_bounds__(LANES ? kNarrowThreads : kMostWaves * 64) rmsn
                 float m = amax[0];
 #pragma unroll
                 for (int i = 1; i < CH; ++i) m = fmaxf(m, amax[i]);
-                m = rows.join(m, red[parity][1], [](float a) { return lc_wave_max(a); }, [](float a, float b) { return fmaxf(a, b); });
+                m = Of::join(m, waves, red[parity][1], [](float a) { return lc_wave_max(a); }, [](float a, float b) { return fmaxf(a, b); });
                 const Scale scale = scale_of(m, split.rest);
                 if (tid == 0) p.scales[row] = scale.scale;
 #pragma unroll
@@ -329,9 +330,9 @@ struct NormBwdArgs {
 template <typename T, int CH, bool NT, Ends ENDS, int LANES = 0>
 __global__ void __launch_bounds__(LANES ? kNarrowThreads : kMostWaves * 64) rmsnorm_bwd_kernel(const NormBwdArgs p) {
     __shared__ float red[2][kMostWaves];
-    const Rows<LANES> rows;
-    const int tid = rows.tid, c = p.c, threads = rows.threads;
-    const auto column = [tid, threads](int i) { return (i * threads + tid) * 8; };
+    using Of = Rows<LANES>;
+    const int tid = Of::tid(), c = p.c, waves = blockDim.x >> 6, threads = LANES ? LANES : blockDim.x;
+    const auto column = [=](int i) { return (i * threads + tid) * 8; };
     const auto inside = [&](int i) { return ENDS == kWhole ? 8 : ENDS == kEights ? (column(i) < c ? 8 : 0) : c - column(i); };
     Packed<float> pg[CH];
     float acc[CH][8] = {};
@@ -347,8 +348,8 @@ __global__ void __launch_bounds__(LANES ? kNarrowThreads : kMostWaves * 64) rmsn
         next_rstd = p.rstd[row];
     };
     int parity = 0;
-    if (rows.first < p.rows) issue(rows.first);
-    for (long long row = rows.first; row < p.rows; row += rows.step, parity ^= 1) {
+    if (Of::first() < p.rows) issue(Of::first());
+    for (long long row = Of::first(); row < p.rows; row += Of::step(), parity ^= 1) {
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
             ph[i] = nh[i];
@@ -356,7 +357,7 @@ __global__ void __launch_bounds__(LANES ? kNarrowThreads : kMostWaves * 64) rmsn
             pt[i] = nt[i];
         }
         rstd = next_rstd;
-        if (row + rows.step < p.rows) issue(row + rows.step);
+        if (row + Of::step() < p.rows) issue(row + Of::step());
         float s = 0.f;
         lc_settle8<ENDS>(ph, column, c);
         lc_settle8<ENDS>(pd, column, c);
@@ -369,7 +370,7 @@ __global__ void __launch_bounds__(LANES ? kNarrowThreads : kMostWaves * 64) rmsn
                 s = fmaf(d * pg[i].get(j), n, s);
                 acc[i][j] = fmaf(d, n, acc[i][j]);
             }
-        const float mean = rows.join(s, red[parity], [](float a) { return lc_wave_sum(a); }, [](float a, float b) { return a + b; }) / (float)c;
+        const float mean = Of::join(s, waves, red[parity], [](float a) { return lc_wave_sum(a); }, [](float a, float b) { return a + b; }) / (float)c;
         T* dx = static_cast<T*>(p.dx) + row * (long long)c;
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
