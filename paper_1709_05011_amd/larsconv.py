@@ -658,6 +658,9 @@ class AdamWArgs:
                  w_lowp: Optional[Sequence] = None, g_dtype: int = LC_F32):
         if numel is None:
             numel = [t.numel() for t in w]
+        for t in g:
+            if str(getattr(t, "dtype", "")) not in ("", "torch.bfloat16" if g_dtype == LC_BF16 else "torch.float32"):
+                raise ValueError(f"gradients of type {t.dtype} with g_dtype {g_dtype}")
         self.n, self.numel, self.g_dtype = len(w), list(numel), g_dtype
         self.w, self.g, self.m, self.v = _ptr_array(w), _ptr_array(g), _ptr_array(m), _ptr_array(v)
         self.numel_arr = _i64_array(self.numel)

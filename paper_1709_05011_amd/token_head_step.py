@@ -53,6 +53,15 @@ class TokenHeadStep:
         if self.w_lowp is not None:
             self.w_lowp.copy_(self.params["w"])
 
+    def _check(self, rows: int, **tensors: Optional[torch.Tensor]) -> None:
+        """The entry points take pointers: what a call hands over has to be contiguous, of its type and of `rows` rows."""
+        for name, t in tensors.items():
+            if t is None:
+                continue
+            shape, dtype = ((rows, self.width), self.type) if name in ("x", "residual", "dtotal") else ((rows,), torch.int32 if name == "tokens" else torch.float32)
+            if tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous():
+                raise ValueError(f"{name}: a contiguous {dtype} tensor of shape {shape} is needed, got {t.dtype} {tuple(t.shape)} with strides {t.stride()}")
+
     def _buffers(self, rows: int, top: int) -> dict:
         """What a call over `rows` tokens works in, made once for each (rows, top)."""
         if (rows, top) not in self._rows:
@@ -77,6 +86,7 @@ class TokenHeadStep:
     def score(self, x, residual, tokens, top: int = 0):
         """Log probability and entropy of each row's token (int32; outside the vocabulary: does not count), and the `top` likeliest tokens with
         theirs.  The tensors returned are this object's buffers: the next call over as many rows writes them again."""
+        self._check(x.shape[0], x=x, residual=residual, tokens=tokens)
         b = self._buffers(x.shape[0], top)
         self._forward(b, x, residual, tokens)
         return b["logprob"], b["entropy"], b["ids"], b["top"]
@@ -84,7 +94,9 @@ class TokenHeadStep:
     def step(self, x, residual, tokens, dlogprob, dentropy=None, dtotal=None, grad_scale=None):
         """Forward, backward and update.  dlogprob, dentropy: gradient of the loss with respect to each row's log probability and entropy (a mean
         cross-entropy: -1/rows); dtotal: gradient that reaches x + residual by another way; grad_scale: one float on the device, multiplies the
-        parameters' gradients.  Returns the rows' log probabilities and entropies and the gradient with respect to x (and to residual)."""
+        parameters' gradients.  Returns the rows' log probabilities and entropies and the gradient with respect to x (and to residual),
+        in this object's buffers."""
+        self._check(x.shape[0], x=x, residual=residual, tokens=tokens, dlogprob=dlogprob, dentropy=dentropy, dtotal=dtotal)
         b = self._buffers(x.shape[0], 0)
         if "dlogits" not in b:
             b["dlogits"] = torch.zeros_like(b["logits"])          # the pad stays zero
@@ -107,6 +119,7 @@ class TokenHeadStep:
     def packed(self, x, residual, group: int = 128):
         """x + residual and its norm as e4m3 codes with a scale for every `group` columns (0: one a row)."""
         rows = x.shape[0]
+        self._check(rows, x=x, residual=residual)
         total = torch.empty((rows, self.width), dtype=self.type, device=self.dev) if residual is not None else None
         codes = torch.empty((rows, self.width), dtype=torch.float8_e4m3fn, device=self.dev)
         scales = torch.empty((rows, -(-self.width // group) if group else 1), device=self.dev)

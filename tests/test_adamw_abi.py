@@ -61,3 +61,13 @@ def test_nothing_to_do():
     lc.adamw_step_q8(lc.AdamWQ8Args([], [], [], [], [], []), 0.1, 0.9, 0.9, 1e-8, 0.0, 1, 1, stream=0)
     none = [None, None]
     lc.adamw_step(lc.AdamWArgs(none, none, none, none, [0, 0]), 0.1, 0.9, 0.9, 1e-8, 0.0, 1, stream=0)
+
+
+def test_gradients_of_another_type_than_said():
+    import torch
+    f, h = torch.zeros(4), torch.zeros(4, dtype=torch.bfloat16)
+    for g, kind in ((h, lc.LC_F32), (f, lc.LC_BF16), (f.double(), lc.LC_F32)):
+        with pytest.raises(ValueError):
+            lc.AdamWArgs([f], [g], [f], [f], g_dtype=kind)
+    lc.AdamWArgs([f], [f], [f], [f])
+    lc.AdamWArgs([f], [h], [f], [f], g_dtype=lc.LC_BF16)
