@@ -532,6 +532,7 @@ void launch_fwd(const NormArgs& a, hipStream_t stream) {
 // Lanes of a row where a wave takes several, from what a wave of its own per row takes, us, 2^25 elements in all: bf16 forward with c = 64, 128, 256 125, 69, 39, so 26;
 // to 8 bits 216, 119, 65, so 42; forward and backward 250, 140, 88, so 66; fp32 forward 143, 82, 51, so 49.
 constexpr int kMostNarrow = 256;             // columns
+bool narrow(long long rows, int c) { return c <= kMostNarrow && rows > 256; }        // (fewer have a compute unit each; the same to 4096 rows, where a launch is what they take)
 int lanes_of(int c) { return c <= 64 ? 8 : c <= 128 ? 16 : 32; }
 template <typename T, bool Q8, bool NT, int LANES>
 void launch_fwd_narrow(const NormArgs& a, hipStream_t stream) {
@@ -557,10 +558,10 @@ void launch_fwd(const NormArgs& a, hipStream_t stream) {
     }
     if constexpr (sizeof(T) == 2) {
         const long long bytes = a.rows * a.c * (2 + (a.r ? 2 : 0) + (a.total ? 2 : 0) + (Q8 ? 1 : 2));
-        if (bytes >= kStreamBytes && a.c <= kMostNarrow) return launch_fwd_narrow<T, Q8, true>(a, stream);
+        if (bytes >= kStreamBytes && narrow(a.rows, a.c)) return launch_fwd_narrow<T, Q8, true>(a, stream);
         if (bytes >= kStreamBytes) return chunks_of<T>(a.c) == 1 ? launch_fwd<T, 1, Q8, true>(a, stream) : launch_fwd<T, 2, Q8, true>(a, stream);
     }
-    if (a.c <= kMostNarrow) return launch_fwd_narrow<T, Q8, false>(a, stream);
+    if (narrow(a.rows, a.c)) return launch_fwd_narrow<T, Q8, false>(a, stream);
     chunks_of<T>(a.c) == 1 ? launch_fwd<T, 1, Q8, false>(a, stream) : launch_fwd<T, 2, Q8, false>(a, stream);
 }
 
@@ -591,7 +592,7 @@ lc_status run_fwd(const lc_rmsnorm_desc* d, const void* x, const void* residual,
 int bwd_chunks(int c) { return c <= 512 * kMostWaves ? 1 : 2; }
 long long bwd_blocks(const lc_rmsnorm_desc* d) {
     if (in_passes(d->dtype, d->c)) return std::min<long long>(d->rows, 64);
-    if (d->c <= kMostNarrow) {
+    if (narrow(d->rows, d->c)) {
         const long long each = kNarrowThreads / lanes_of(d->c), all = (d->rows + each - 1) / each;
         return std::min(all, std::max<long long>(256, std::min<long long>(1024, all / 4)));
     }
@@ -624,10 +625,10 @@ void launch_bwd(const NormBwdArgs& a, int blocks, hipStream_t stream) {
         return;
     }
     if constexpr (sizeof(T) == 2) {
-        if (a.rows * a.c * (a.dh ? 8 : 6) >= kStreamBytes && a.c <= kMostNarrow) return launch_bwd_narrow<T, true>(a, blocks, stream);
+        if (a.rows * a.c * (a.dh ? 8 : 6) >= kStreamBytes && narrow(a.rows, a.c)) return launch_bwd_narrow<T, true>(a, blocks, stream);
         if (a.rows * a.c * (a.dh ? 8 : 6) >= kStreamBytes) return bwd_chunks(a.c) == 1 ? launch_bwd<T, 1, true>(a, blocks, stream) : launch_bwd<T, 2, true>(a, blocks, stream);
     }
-    if (a.c <= kMostNarrow) return launch_bwd_narrow<T, false>(a, blocks, stream);
+    if (narrow(a.rows, a.c)) return launch_bwd_narrow<T, false>(a, blocks, stream);
     bwd_chunks(a.c) == 1 ? launch_bwd<T, 1, false>(a, blocks, stream) : launch_bwd<T, 2, false>(a, blocks, stream);
 }
 
