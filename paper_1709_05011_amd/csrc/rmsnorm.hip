@@ -90,8 +90,8 @@ __device__ __forceinline__ Scale scale_of(float amax, double rest) {
     Scale s;
     s.scale = fmaxf((float)((double)amax * rest * (1.0 / kE4m3Max)), kLeastScale);
     const double r = (double)__builtin_amdgcn_rcpf(s.scale), k = rest * (r * fma(-(double)s.scale, r, 2.0));
-    s.hi = (float)k;
-    s.lo = (float)(k - (double)s.hi);
+    s.hi = s.scale < INFINITY ? (float)k : 0.f;
+    s.lo = s.scale < INFINITY ? (float)(k - (double)s.hi) : 0.f;
     return s;
 }
 

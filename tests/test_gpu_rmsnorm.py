@@ -230,3 +230,26 @@ def test_narrow_rows(kind, rows, c):
         test_forward_in_8_bits(kind, rows, c, group)
     for joined, pad in [(True, 0), (False, 3)]:
         test_backward(kind, rows, c, joined, pad)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,c", [(3, 130), (300, 130), (3, 3000), (3, 17000)])
+@pytest.mark.parametrize("group", [0, 128])
+def test_an_infinite_factor_stays_in_its_group(kind, rows, c, group):
+    """The group's scale is infinite: the column itself has no number for a code, its neighbours' quotient is 0, other groups are as without it."""
+    dtype, t, _ = TYPES[kind]
+    x, _ = rows_of(rows, c, 21, t)
+    gamma = gu.dev(1 + synth.normal((c,), 22, std=0.3))
+    groups = -(-c // group) if group else 1
+    out = []
+    for _ in range(2):
+        y, s = torch.empty((rows, c), dtype=torch.float8_e4m3fn, device=gu.DEV), torch.empty((rows, groups), device=gu.DEV)
+        lc.rmsnorm_fwd_q8(lc.RmsNormDesc(rows, c, dtype=dtype), x, None, gamma, None, y, s, group)
+        torch.cuda.synchronize()
+        out.append((y.float(), s))
+        gamma[5] = float("inf")
+    (y0, s0), (y1, s1) = out
+    end = group or c
+    assert torch.all(s1[:, 0].isinf()) and torch.all(y1[:, 5].isnan())
+    assert not y1[:, :5].any() and not y1[:, 6:end].any()
+    assert torch.equal(y1[:, end:], y0[:, end:]) and torch.equal(s1[:, 1:], s0[:, 1:])
