@@ -258,3 +258,20 @@ def test_forward_with_rows_divided_in_every_way(kind, rows, vocab, top):
     t64, tokens = tokens_of(rows, vocab, 13)
     d, got, ids, lps = run(dtype, z, tokens, vocab, top)
     check_forward(vocab, (d, got, ids, lps), ops.token_logprob(z64, t64, top), top)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("top", [0, 3])
+def test_more_rows_than_a_grid_takes_at_once(kind, top):
+    rows, vocab = 70001, 17
+    dtype, t, half = TYPES[kind]
+    z, z64 = logits_of(rows, vocab, 14, t, masked=0.2)
+    t64, tokens = tokens_of(rows, vocab, 15)
+    d, (lp, ent, lse), ids, lps = run(dtype, z, tokens, vocab, top)
+    want = ops.token_logprob(z64, t64, top)
+    check_forward(vocab, (d, (lp, ent, lse), ids, lps), want, top)
+    one, dz = torch.ones(rows, device=gu.DEV), torch.empty_like(z)
+    lc.token_logprob_bwd(d, z, tokens, lse, None, one, None, dz)
+    torch.cuda.synchronize()
+    exact = ops.token_logprob_bwd(z64, t64, np.ones(rows), np.zeros(rows))
+    assert np.all(np.abs(f64(dz) - exact) <= half * (1 + half) * np.abs(exact) + (1 + half) * (tol(vocab) + 16 * U))
