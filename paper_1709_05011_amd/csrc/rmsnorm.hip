@@ -470,34 +470,37 @@ __global__ void __launch_bounds__(1024) rmsnorm_dgamma_kernel(const float* __res
     constexpr int U = 8, kGroups = 1024 / COLS;
     __shared__ float sum[kGroups][COLS];
     const int column = threadIdx.x & (COLS - 1), group = threadIdx.x / COLS;
-    const long long k = (long long)blockIdx.x * COLS + column;
-    float s[U] = {};
-    if (k < c) {
-        int i = group;
-        for (; i + kGroups * (U - 1) < parts; i += kGroups * U) {
-            float v[U];
+    for (long long at = (long long)blockIdx.x * COLS; at < c; at += (long long)gridDim.x * COLS) {
+        const long long k = at + column;
+        float s[U] = {};
+        if (k < c) {
+            int i = group;
+            for (; i + kGroups * (U - 1) < parts; i += kGroups * U) {
+                float v[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) v[u] = part[(long long)(i + kGroups * u) * c + k];
+                for (int u = 0; u < U; ++u) v[u] = part[(long long)(i + kGroups * u) * c + k];
 #pragma unroll
-            for (int u = 0; u < U; ++u) s[u] += v[u];
+                for (int u = 0; u < U; ++u) s[u] += v[u];
+            }
+#pragma unroll
+            for (int u = 0; u < U - 1; ++u)
+                if (i + kGroups * u < parts) s[u] += part[(long long)(i + kGroups * u) * c + k];
         }
+        sum[group][column] = ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
+        __syncthreads();
+        if (group == 0 && k < c) {
+            float t[4] = {};
 #pragma unroll
-        for (int u = 0; u < U - 1; ++u)
-            if (i + kGroups * u < parts) s[u] += part[(long long)(i + kGroups * u) * c + k];
-    }
-    sum[group][column] = ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
-    __syncthreads();
-    if (group == 0 && k < c) {
-        float t[4] = {};
-#pragma unroll
-        for (int w = 0; w < kGroups; ++w) t[w & 3] += sum[w][column];
-        dgamma[k] = (t[0] + t[1]) + (t[2] + t[3]);
+            for (int w = 0; w < kGroups; ++w) t[w & 3] += sum[w][column];
+            dgamma[k] = (t[0] + t[1]) + (t[2] + t[3]);
+        }
+        __syncthreads();
     }
 }
 
 constexpr int kMostColumns = 16384;          // what a block's registers hold of a row
 constexpr int kMostWidth = 1 << 30;          // columns are counted in 32 bits, eight past the end among them
-constexpr long long kMostBlocks = 1 << 20;   // rows beyond are dealt round
+constexpr long long kMostBlocks = 1 << 20;   // rows, or column tiles, beyond are dealt round
 
 lc_status check_desc(const lc_rmsnorm_desc* d) {
     if (!d) return LC_ERR_NULL;
@@ -677,8 +680,8 @@ extern "C" lc_status rmsnorm_bwd(const lc_rmsnorm_desc* desc, const void* total,
     lc_begin_call();
     if (desc->dtype == LC_BF16) launch_bwd<uint16_t>(a, blocks, stream);
     else launch_bwd<float>(a, blocks, stream);
-    const long long c = desc->c;
-    if (c <= kNarrow) hipLaunchKernelGGL((rmsnorm_dgamma_kernel<16>), dim3((unsigned)((c + 15) / 16)), dim3(1024), 0, stream, a.part, dgamma, blocks, desc->c);
-    else hipLaunchKernelGGL((rmsnorm_dgamma_kernel<64>), dim3((unsigned)((c + 63) / 64)), dim3(1024), 0, stream, a.part, dgamma, blocks, desc->c);
+    const long long c = desc->c, tiles = std::min(c <= kNarrow ? (c + 15) / 16 : (c + 63) / 64, kMostBlocks);      // (a launch holds fewer than 2^32 threads)
+    if (c <= kNarrow) hipLaunchKernelGGL((rmsnorm_dgamma_kernel<16>), dim3((unsigned)tiles), dim3(1024), 0, stream, a.part, dgamma, blocks, desc->c);
+    else hipLaunchKernelGGL((rmsnorm_dgamma_kernel<64>), dim3((unsigned)tiles), dim3(1024), 0, stream, a.part, dgamma, blocks, desc->c);
     return lc_end_call();
 }

@@ -253,3 +253,19 @@ def test_an_infinite_factor_stays_in_its_group(kind, rows, c, group):
     assert torch.all(s1[:, 0].isinf()) and torch.all(y1[:, 5].isnan())
     assert not y1[:, :5].any() and not y1[:, 6:end].any()
     assert torch.equal(y1[:, end:], y0[:, end:]) and torch.equal(s1[:, 1:], s0[:, 1:])
+
+
+def test_gradient_of_more_columns_than_a_launch_has_threads_for():
+    """dgamma's sum takes 1024 threads for 64 columns: 2^32 of them from 2^28 columns on.  One row in three, so that a wrong tile of columns shows."""
+    rows, c = 3, (1 << 28) + 37
+    gen = torch.Generator(device=gu.DEV).manual_seed(3)
+    h, dy = (torch.randn((rows, c), generator=gen, device=gu.DEV, dtype=torch.bfloat16) for _ in range(2))
+    gamma, dx, dg = torch.ones(c, device=gu.DEV), torch.empty_like(h), torch.full((c,), float("nan"), device=gu.DEV)
+    rstd = torch.tensor([1.0, 0.5, 2.0], device=gu.DEV)
+    d = lc.RmsNormDesc(rows, c, dtype=lc.LC_BF16)
+    lc.rmsnorm_bwd(d, h, dy, None, gamma, rstd, dx, dg, gu.workspace(lc.rmsnorm_bwd_workspace_bytes(d)))
+    torch.cuda.synchronize()
+    for at in range(0, c, 1 << 26):                  # rstd a power of two and products of two bf16 values: three exact terms, two roundings
+        terms = h[:, at:at + (1 << 26)].float() * rstd[:, None] * dy[:, at:at + (1 << 26)].float()
+        off = (dg[at:at + (1 << 26)] - terms.double().sum(0)).abs()
+        assert bool((off <= 3 * U * terms.abs().double().sum(0)).all()), at
