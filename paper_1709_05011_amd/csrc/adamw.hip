@@ -251,7 +251,7 @@ __global__ void __launch_bounds__(WAVES * 64) adamw_kernel(const AdamArgs<TABLE>
     }
 }
 
-constexpr int kMostBlocks = 1 << 24;      // of a wave: a launch holds fewer than 2^32 threads
+constexpr int kMostWaves = 1 << 24;       // of a launch, which holds fewer than 2^32 threads; chunks beyond are dealt round
 
 struct AdamList {                          // what both entry points take
     int n;
@@ -294,7 +294,7 @@ lc_status check_list(const AdamList& a, bool q8) {
 
 template <typename G, bool Q8, int PAST, int TABLE>
 void launch(const AdamArgs<TABLE>& args, int waves, hipStream_t stream) {
-    const dim3 grid((unsigned)std::min(args.s.chunks, kMostBlocks));
+    const dim3 grid((unsigned)std::min(args.s.chunks, kMostWaves / waves));
     if (waves == 1) hipLaunchKernelGGL((adamw_kernel<G, Q8, PAST, 1, TABLE>), grid, dim3(64), 0, stream, args);
     else hipLaunchKernelGGL((adamw_kernel<G, Q8, PAST, 4, TABLE>), grid, dim3(256), 0, stream, args);
 }

@@ -179,3 +179,20 @@ def test_another_stream(q8):
         torch.cuda.synchronize()
         got.append((w, m, v))
     assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+@pytest.mark.parametrize("offset", [0, 1])
+def test_more_elements_than_a_launch_has_threads_for(offset):
+    """Two thousand million elements more than 2^34 in one launch, off a line of 128 bytes in blocks of four waves.  The list names the same tensors again and again: with
+    betas of zero and no learning rate every one of them writes the same values."""
+    n, times = 1 << 27, 145
+    g, w = torch.randn(n + offset, device=gu.DEV, dtype=torch.bfloat16)[offset:], torch.randn(n + offset, device=gu.DEV)[offset:]
+    m, v = (torch.zeros(n + offset, dtype=torch.uint8, device=gu.DEV)[offset:] for _ in range(2))
+    sm, sv = (torch.zeros(n // 256, device=gu.DEV) for _ in range(2))
+    one = [t.clone() for t in (w, m, v, sm, sv)]
+    step = lambda k, w, m, v, sm, sv: lc.adamw_step_q8(lc.AdamWQ8Args([w] * k, [g] * k, [m] * k, [sm] * k, [v] * k, [sv] * k, g_dtype=lc.LC_BF16), 0.0, 0.0, 0.0,
+                                                       EPS, 0.0, 1, 77)
+    step(1, *one)
+    step(times, w, m, v, sm, sv)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(one, (w, m, v, sm, sv))) and bool((sm > 0).all())
