@@ -37,6 +37,7 @@ struct AdamScalars {
     int chunks;
     const float* grad_scale;
     float b1, one_b1, b2, one_b2, step_size, inv_root_c2, eps;
+    bool small_eps;
     uint32_t dither;
 };
 
@@ -140,6 +141,16 @@ __device__ __forceinline__ void store4(uint8_t* p, uint32_t x, int n) {
     }
 }
 
+// m / (sqrt(v) / root c2 + eps) by the instructions for roots and reciprocals, one unit in the last place each.  They take a number under 2^-126 for zero, which a root of 2^-63 beside an eps
+// shows where eps is less than 2^25 of them (SMALL): scaled by powers of two then.
+template <bool SMALL>
+__device__ __forceinline__ float update_of(const AdamScalars& p, float m, float v) {
+    if constexpr (!SMALL) return m * __builtin_amdgcn_rcpf(fmaf(__builtin_amdgcn_sqrtf(v), p.inv_root_c2, p.eps));
+    const bool low = v < 0x1p-96f;
+    const float root = fmaf(__builtin_amdgcn_sqrtf(low ? v * 0x1p64f : v) * (low ? 0x1p-32f : 1.f), p.inv_root_c2, p.eps);
+    return root < 0x1p-64f ? m * __builtin_amdgcn_rcpf(root * 0x1p64f) * 0x1p64f : m * __builtin_amdgcn_rcpf(root);
+}
+
 // What a wave does to its 256 elements, number `block` of the tensor; FULL: all of them lie within it (left: how many do).
 template <typename G, bool Q8, int PAST, bool FULL>
 __device__ __forceinline__ void adamw_part(const AdamScalars& p, const AdamTensor& t, long long block, long long left_in_block) {
@@ -170,16 +181,21 @@ __device__ __forceinline__ void adamw_part(const AdamScalars& p, const AdamTenso
         load4<NT, FULL>(m, static_cast<const float*>(t.m) + first + own, n);
         load4<NT, FULL>(v, static_cast<const float*>(t.v) + first + own, n);
     }
-    // m and v by separately rounded products and sums (their bits are defined so); the update by the instructions for roots and reciprocals, one unit in the
-    // last place each
+    // m and v by separately rounded products and sums (their bits are defined so)
+    float update[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const float x = g[j] * gs;
         m[j] = p.b1 * m[j] + p.one_b1 * x;
         v[j] = p.b2 * v[j] + p.one_b2 * (x * x);
-        const float root = fmaf(__builtin_amdgcn_sqrtf(v[j]), p.inv_root_c2, p.eps);
-        w[j] = fmaf(-p.step_size, m[j] * __builtin_amdgcn_rcpf(root), fmaf(-t.lr_decay, w[j], w[j]));
+        update[j] = update_of<false>(p, m[j], v[j]);
     }
+    if (p.small_eps) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) update[j] = update_of<true>(p, m[j], v[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = fmaf(-p.step_size, update[j], fmaf(-t.lr_decay, w[j], w[j]));
     store4<NT, FULL>(t.w + first + own, w, n);
     if (t.w_lowp) store4<(PAST > 1), FULL>(t.w_lowp + first + own, w, n);
     if constexpr (!Q8) {
@@ -333,6 +349,7 @@ lc_status run_list(const AdamList& a, bool q8, void* hip_stream) {
     p.step_size = (float)((double)a.lr / (1.0 - std::pow(a.beta1, (double)a.step)));
     p.inv_root_c2 = (float)(1.0 / std::sqrt(1.0 - std::pow(a.beta2, (double)a.step)));
     p.eps = a.eps;
+    p.small_eps = a.eps < 0x1p-38f * p.inv_root_c2;
     p.dither = a.seed * 0x9E3779B1u + 0x7F4A7C15u;
     double all = 0.0;
     uintptr_t starts = 0;

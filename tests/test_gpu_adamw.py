@@ -196,3 +196,23 @@ def test_more_elements_than_a_launch_has_threads_for(offset):
     step(times, w, m, v, sm, sv)
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(one, (w, m, v, sm, sv))) and bool((sm > 0).all())
+
+
+@pytest.mark.parametrize("q8", [False, True])
+@pytest.mark.parametrize("eps", [1e-12, 1e-20, 1e-30, 1e-39, 1e-44])
+def test_an_eps_beside_roots_of_the_smallest_numbers(q8, eps):
+    """Second moments under fp32's normal range (gradients of 1e-18 and less) and none at all, with an eps that does not hide their roots.  w as the rule gives it in float64
+    from the moments as defined in fp32; three roundings of coefficients and ten of the instructions beside those of w."""
+    g = np.float32([1e-15, 1e-17, 3e-18, 1e-18, 4e-19, 1e-19, 3e-20, 1e-21, 0.0, -2e-18, -1e-19, 1.0] * 40)
+    n = g.size
+    w = gu.dev(np.full(n, 0.5, np.float32))
+    m, v = (torch.zeros(n, dtype=torch.uint8 if q8 else torch.float32, device=gu.DEV) for _ in range(2))
+    sm, sv = (torch.ones(2, device=gu.DEV) for _ in range(2))
+    if q8:
+        lc.adamw_step_q8(lc.AdamWQ8Args([w], [gu.dev(g)], [m], [sm], [v], [sv]), LR, B1, B2, eps, 0.0, 1, 3)
+    else:
+        lc.adamw_step(lc.AdamWArgs([w], [gu.dev(g)], [m], [v]), LR, B1, B2, eps, 0.0, 1)
+    torch.cuda.synchronize()
+    wm, wv = (a.astype(np.float64) for a in ops.adam_states_as_rounded(g, 0 * g, 0 * g, B1, B2))
+    update = f32(LR) * (wm / (1 - B1)) / (np.sqrt(wv / (1 - B2)) + float(np.float32(eps)))
+    assert np.all(np.abs(w.double().cpu().numpy() - (0.5 - update)) <= U * (0.5 + np.abs(0.5 - update)) + 16 * U * np.abs(update))
