@@ -371,6 +371,7 @@ typedef struct {
  * The statistics are those of total as stored.  total ([rows][c], contiguous) may be NULL (not stored) and must be NULL without a
  * residual (LC_ERR_UNSUPPORTED); it may be the residual's or x's own buffer where that is contiguous, otherwise buffers must not
  * overlap.  save_rstd: rows floats for the backward pass, or NULL.  y: [rows][c], contiguous.
+ * Squares are summed in fp32; where their sum leaves its range on either side (and eps does not hide it), they are summed again scaled by a power of two.
  * A row that holds an infinity or a NaN gets NaN where the formula gives it. */
 lc_status rmsnorm_fwd(const lc_rmsnorm_desc* desc, const void* x, const void* residual, const float* gamma, void* total, void* y,
                       float* save_rstd, void* hip_stream);

@@ -71,6 +71,17 @@ __device__ __forceinline__ double rstd_of(const NormArgs& p, float sum) {
     return fabs(better) < INFINITY ? better : r;         // (x = 0 or infinite: the estimate is the value)
 }
 
+// Whether squares summed as they are say enough: their sum is finite, and either eps hides what they lose under fp32's normal range or none does (2^30 of them lose 2^-120
+// at most).  Other rows are summed again as totals / 2^e with 2^e above the largest.
+__device__ __forceinline__ bool sum_serves(const NormArgs& p, float sum) { return sum < INFINITY && (p.eps >= 0x1p-120f || sum >= 0x1p-90f); }
+__device__ __forceinline__ double rstd_of_scaled(const NormArgs& p, float sum, int e) {
+    const double x = ldexp((double)sum * p.inv_c, 2 * e) + (double)p.eps;
+    const int half = __builtin_amdgcn_frexp_exp(x) >> 1;
+    const double near = ldexp(x, -2 * half), r = (double)__builtin_amdgcn_rsqf((float)near);
+    const double better = r * fma(-0.5 * near * r, r, 1.5);
+    return ldexp(fabs(better) < INFINITY ? better : r, -half);
+}
+
 // rstd as a power of two and the rest, in [0.5, 1): a total times the power is near its normalised value, so that its product with gamma leaves fp32's range only where the
 // output does.  (The power is 1 for zero, infinity and NaN; it is exact otherwise, and so is a product with it.)
 struct Split {
@@ -135,7 +146,7 @@ __device__ __forceinline__ void store8_e4m3(uint8_t* p, const float* g, const fl
 // of a wave instead (2^18 rows of 128 bf16 26 us, 5.1 TB/s).
 template <typename T, int CH, bool Q8, bool NT, Ends ENDS, int LANES = 0>
 __global__ void __launch_bounds__(LANES ? kNarrowThreads : kMostWaves * 64) rmsnorm_fwd_kernel(const NormArgs p) {
-    __shared__ float red[2][2][kMostWaves];
+    __shared__ float red[2][4][kMostWaves];
     using Of = Rows<LANES>;
     const int tid = Of::tid(), c = p.c, waves = blockDim.x >> 6, threads = LANES ? LANES : blockDim.x;
     const auto column = [=](int i) { return (i * threads + tid) * 8; };
@@ -174,7 +185,27 @@ __global__ void __launch_bounds__(LANES ? kNarrowThreads : kMostWaves * 64) rmsn
             for (int i = 0; i < CH; ++i) lc_store8<NT>(t + column(i), h[i], inside(i));
         }
         ss = Of::join(ss, waves, red[parity][0], [](float a) { return lc_wave_sum(a); }, [](float a, float b) { return a + b; });
-        const double rstd = rstd_of(p, ss);
+        double rstd;
+        if (sum_serves(p, ss)) {
+            rstd = rstd_of(p, ss);
+        } else {
+            float most = 0.f;
+#pragma unroll
+            for (int i = 0; i < CH; ++i)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf(h[i][j]));
+            most = Of::join(most, waves, red[parity][2], [](float a) { return lc_wave_max(a); }, [](float a, float b) { return fmaxf(a, b); });
+            const int e = __builtin_amdgcn_frexp_expf(most);         // (0 for zero and infinity)
+            float s = 0.f;
+#pragma unroll
+            for (int i = 0; i < CH; ++i)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float n = ldexpf(h[i][j], -e);
+                    s = fmaf(n, n, s);
+                }
+            rstd = rstd_of_scaled(p, Of::join(s, waves, red[parity][3], [](float a) { return lc_wave_sum(a); }, [](float a, float b) { return a + b; }), e);
+        }
         if (p.rstd && tid == 0) p.rstd[row] = (float)rstd;
         if constexpr (!Q8) {
             const float r = (float)rstd;
@@ -229,7 +260,7 @@ __global__ void __launch_bounds__(LANES ? kNarrowThreads : kMostWaves * 64) rmsn
 template <typename T, bool Q8>
 __global__ void __launch_bounds__(1024) rmsnorm_fwd_wide_kernel(const NormArgs p) {
     constexpr int WAVES = 16, kSpan = WAVES * 64 * 8;
-    __shared__ float red[2][2][WAVES];
+    __shared__ float red[2][4][WAVES];
     const int tid = threadIdx.x, c = p.c;
     int parity = 0;
     for (long long row = blockIdx.x; row < p.rows; row += gridDim.x, parity ^= 1) {
@@ -259,7 +290,26 @@ __global__ void __launch_bounds__(1024) rmsnorm_fwd_wide_kernel(const NormArgs p
             if (t) lc_store8(t + col, h, c - col);
         }
         ss = lc_block_sum<WAVES>(ss, red[parity][0]);
-        const double rstd = rstd_of(p, ss);
+        double rstd;
+        if (sum_serves(p, ss)) {
+            rstd = rstd_of(p, ss);
+        } else {
+            const auto over = [&](auto&& f) __attribute__((always_inline)) {
+                for (long long at = tid * 8; at < c; at += kSpan) {
+                    value((int)at, h, false);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) f(h[j]);
+                }
+            };
+            float most = 0.f, s = 0.f;
+            over([&](float x) { most = fmaxf(most, fabsf(x)); });
+            const int e = __builtin_amdgcn_frexp_expf(lc_block_max<WAVES>(most, red[parity][2]));
+            over([&](float x) {
+                const float n = ldexpf(x, -e);
+                s = fmaf(n, n, s);
+            });
+            rstd = rstd_of_scaled(p, lc_block_sum<WAVES>(s, red[parity][3]), e);
+        }
         if (p.rstd && tid == 0) p.rstd[row] = (float)rstd;
         if constexpr (!Q8) {
             const float r = (float)rstd;

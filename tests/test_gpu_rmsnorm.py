@@ -269,3 +269,32 @@ def test_gradient_of_more_columns_than_a_launch_has_threads_for():
         terms = h[:, at:at + (1 << 26)].float() * rstd[:, None] * dy[:, at:at + (1 << 26)].float()
         off = (dg[at:at + (1 << 26)] - terms.double().sum(0)).abs()
         assert bool((off <= 3 * U * terms.abs().double().sum(0)).all()), at
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,c", [(9, 1), (9, 24), (700, 100), (9, 512), (9, 5000), (9, 8200), (9, 16384), (9, 17000), (9, 9001)])
+@pytest.mark.parametrize("eps", [0.0, 1e-40, 1e-33, 1e-5])
+def test_rows_whose_squares_leave_fp32(kind, rows, c, eps):
+    """Ordinary rows beside rows of 1e-36 to 1e37: sums of squares under the normal range or beyond the largest number, with an eps that hides the small ones and with one that
+    does not.  The result is the definition's; the tolerances are those of the forward pass, and eight more roundings of an rstd under 2^-126 (which holds 2^-149 or 2^-21 of
+    1e-37's neighbours)."""
+    dtype, t, half = TYPES[kind]
+    sizes = np.array([1.0, 1e-36, 1e-25, 1e-20, 1e-19, 1e18, 1e19, 1e30, 2e37])
+    x = synth.normal((rows, c), 23).astype(np.float64) * sizes[np.arange(rows) % 9][:, None]
+    x = torch.from_numpy(x).to(t).to(gu.DEV)
+    gamma, d = gu.dev(1 + synth.normal((c,), 24, std=0.3)), lc.RmsNormDesc(rows, c, eps=eps, dtype=dtype)
+    y, rstd = torch.empty((rows, c), dtype=t, device=gu.DEV), torch.empty(rows, device=gu.DEV)
+    y8, s = torch.empty((rows, c), dtype=torch.float8_e4m3fn, device=gu.DEV), torch.empty((rows, -(-c // 32)), device=gu.DEV)
+    lc.rmsnorm_fwd(d, x, None, gamma, None, y, rstd)
+    lc.rmsnorm_fwd_q8(d, x, None, gamma, None, y8, s, 32)
+    torch.cuda.synchronize()
+    _, want_rstd, want = ops.rmsnorm(f64(x), None, f64(gamma), float(np.float32(eps)))
+    small = 8 * U * (want_rstd < 2.0 ** -120)[:, None]
+    assert np.all(np.abs(f64(rstd) - want_rstd) <= (k_of(c) + small[:, 0]) * want_rstd)
+    low = 2.0 ** -130                                  # (an eps beside rows of 1e-36 takes their y under the normal range)
+    assert np.all(np.abs(f64(y) - want) <= (half * (1 + half) + k_of(c) + small) * np.abs(want) + low)
+    want_s = ops.quantise_rows(want, 32)[1]
+    assert np.all(np.abs(f64(s) - want_s) <= k_of(c) * want_s)
+    wide = np.repeat(f64(s), 32, axis=1)[:, :c]
+    got = y8.float().double().cpu().numpy() * wide
+    assert np.all(np.abs(got - want) <= np.maximum(2.0 ** -4 * np.abs(want), 2.0 ** -10 * wide) + k_of(c) * np.abs(want))
