@@ -7,6 +7,9 @@ norm's scale.  Every operator is a call into the C library; this module only own
     logprob, entropy, ids, top = head.score(x, residual, tokens, top=5) # one token or many, nothing is updated
     total, codes, scales = head.packed(x, residual)                     # the norm's output in 8 bits, for a product or a wire that takes it so
 
+Calls share one set of buffers, for as many rows as any of them has had; results are kept apart for the last eight of (rows, top).  What a captured call
+works in stays with the object.
+
 The vocabulary is padded to a multiple of 8 rows of the classifier (what the bf16 products take without copies); the pad's logits are never read and their
 gradient stays zero.
 """
@@ -17,6 +20,9 @@ from typing import Dict, Optional, Tuple
 import torch
 
 from . import larsconv as lc
+
+
+KEPT_SETS = 8
 
 
 class TokenHeadStep:
@@ -43,7 +49,9 @@ class TokenHeadStep:
         else:
             self.m, self.v = ([torch.zeros(n, **f32) for n in sizes] for _ in range(2))
             self._adam = lc.AdamWArgs(*lists, self.m, self.v, w_lowp=lowp)
-        self._rows: Dict[Tuple[int, int], dict] = {}
+        self._room: Optional[dict] = None                                   # what calls work in, for room["rows"] rows
+        self._sets: Dict[Tuple[int, int], dict] = {}                        # views of it and results for (rows, top), the one used last at the end
+        self._of_graphs: Dict[Tuple[int, int], dict] = {}                   # sets made while a graph recorded, which graphs alone use
 
     def load(self, w: torch.Tensor, gamma: torch.Tensor) -> None:
         """Sets the classifier ([vocab][width]) and the norm's scale."""
@@ -62,20 +70,60 @@ class TokenHeadStep:
             if tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous():
                 raise ValueError(f"{name}: a contiguous {dtype} tensor of shape {shape} is needed, got {t.dtype} {tuple(t.shape)} with strides {t.stride()}")
 
-    def _buffers(self, rows: int, top: int) -> dict:
-        """What a call over `rows` tokens works in, made once for each (rows, top)."""
-        if (rows, top) not in self._rows:
-            e = lambda *shape, dtype=torch.float32: torch.empty(shape, dtype=dtype, device=self.dev)
-            norm = lc.RmsNormDesc(rows, self.width, eps=self.eps, dtype=self.dtype)
-            token = lc.TokenDesc(rows, self.vocab, ld=self.padded, dtype=self.dtype, top=top)
-            product = lc.ConvDesc(rows, self.width, 1, 1, self.padded, 1, 1, dtype=self.dtype)
-            need = max([lc.rmsnorm_bwd_workspace_bytes(norm), lc.token_logprob_workspace_bytes(token), 256] +
-                       [lc.conv2d_workspace_bytes(product, p) for p in (lc.LC_PASS_FWD, lc.LC_PASS_BWD_DATA, lc.LC_PASS_BWD_WEIGHT)])
-            self._rows[rows, top] = dict(
-                norm=norm, token=token, product=product, ws=e(need, dtype=torch.uint8), total=e(rows, self.width, dtype=self.type),
-                y=e(rows, self.width, dtype=self.type), rstd=e(rows), logits=e(rows, self.padded, dtype=self.type), logprob=e(rows), entropy=e(rows),
-                lse=e(rows), ids=e(rows, top, dtype=torch.int32) if top else None, top=e(rows, top) if top else None)
-        return self._rows[rows, top]
+    def _capturing(self) -> bool:
+        return self.params["w"].is_cuda and torch.cuda.is_current_stream_capturing()
+
+    def _make_set(self, rows: int, top: int, of_graphs: bool) -> dict:
+        e = lambda *shape, dtype=torch.float32: torch.empty(shape, dtype=dtype, device=self.dev)
+        norm = lc.RmsNormDesc(rows, self.width, eps=self.eps, dtype=self.dtype)
+        token = lc.TokenDesc(rows, self.vocab, ld=self.padded, dtype=self.dtype, top=top)
+        product = lc.ConvDesc(rows, self.width, 1, 1, self.padded, 1, 1, dtype=self.dtype)
+        need = max([lc.rmsnorm_bwd_workspace_bytes(norm), lc.token_logprob_workspace_bytes(token), 256] +
+                   [lc.conv2d_workspace_bytes(product, p) for p in (lc.LC_PASS_FWD, lc.LC_PASS_BWD_DATA, lc.LC_PASS_BWD_WEIGHT)])
+        room = None if of_graphs else self._room
+        if room is None or room["rows"] < rows or room["ws"].numel() < need:
+            most = rows
+            if room is not None:                                            # (freed before its successor is made, but for what graphs use)
+                most, need = max(rows, room["rows"]), max(need, room["ws"].numel())
+                room = self._room = None
+                self._sets = {k: b for k, b in self._sets.items() if b["in_graph"]}
+            room = dict(rows=most, ws=e(need, dtype=torch.uint8), total=e(most, self.width, dtype=self.type), y=e(most, self.width, dtype=self.type),
+                        rstd=e(most), logits=e(most, self.padded, dtype=self.type), lse=e(most))
+            if not of_graphs:
+                self._room = room
+        b = dict(norm=norm, token=token, product=product, room=room, in_graph=of_graphs, ws=room["ws"], logprob=e(rows), entropy=e(rows),
+                 ids=e(rows, top, dtype=torch.int32) if top else None, top=e(rows, top) if top else None)
+        for name in ("total", "y", "rstd", "logits", "lse"):
+            b[name] = room[name][:rows]
+        return b
+
+    def _buffers(self, rows: int, top: int, training: bool = False) -> dict:
+        """What a call over `rows` tokens works in.  A set that a graph records is kept, with the room it is in; one that has to be made while a graph records is for graphs
+        alone, as nothing of it is filled before one runs."""
+        key, recording = (rows, top), self.params["w"].is_cuda and torch.cuda.is_current_stream_capturing()
+        b = self._sets.get(key)
+        of_graphs = recording and (b is None or (training and "dlogits" not in b))
+        if of_graphs:
+            b = self._of_graphs.get(key) or self._make_set(rows, top, True)
+            self._of_graphs[key] = b
+        elif b is None:
+            b = self._make_set(rows, top, False)
+            spare = [k for k, s in self._sets.items() if not s["in_graph"]]
+            if len(spare) >= KEPT_SETS:
+                del self._sets[spare[0]]
+            self._sets[key] = b
+        else:
+            self._sets[key] = self._sets.pop(key)
+            b["in_graph"] |= recording
+        if training:
+            if "dlogits" not in b["room"]:
+                b["room"]["dlogits"] = (torch.empty_like if of_graphs else torch.zeros_like)(b["room"]["logits"])      # the pad stays zero
+                b["room"]["dy"] = torch.empty_like(b["room"]["y"])
+            if "dlogits" not in b:
+                b["dlogits"], b["dy"], b["dx"] = b["room"]["dlogits"][:rows], b["room"]["dy"][:rows], torch.empty_like(b["y"])
+            if of_graphs:
+                b["dlogits"][:, self.vocab:].zero_()
+        return b
 
     def _forward(self, b: dict, x: torch.Tensor, residual: Optional[torch.Tensor], tokens: torch.Tensor) -> None:
         w = self.params["w"] if self.w_lowp is None else self.w_lowp
@@ -97,10 +145,7 @@ class TokenHeadStep:
         parameters' gradients.  Returns the rows' log probabilities and entropies and the gradient with respect to x (and to residual),
         in this object's buffers."""
         self._check(x.shape[0], x=x, residual=residual, tokens=tokens, dlogprob=dlogprob, dentropy=dentropy, dtotal=dtotal)
-        b = self._buffers(x.shape[0], 0)
-        if "dlogits" not in b:
-            b["dlogits"] = torch.zeros_like(b["logits"])          # the pad stays zero
-            b["dy"], b["dx"] = torch.empty_like(b["y"]), torch.empty_like(b["y"])
+        b = self._buffers(x.shape[0], 0, training=True)
         self._forward(b, x, residual, tokens)
         lc.token_logprob_bwd(b["token"], b["logits"], tokens, b["lse"], b["entropy"], dlogprob, dentropy, b["dlogits"], self.padded)
         w = self.params["w"] if self.w_lowp is None else self.w_lowp

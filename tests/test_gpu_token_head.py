@@ -122,3 +122,50 @@ def test_the_step_in_a_graph(states_in_8_bits):
         graph.replay()
         assert all(torch.equal(g, w) for g, w in zip(results(), want))
         del junk
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_ragged_calls_in_shared_room(kind):
+    """Calls of many sizes, rising and falling, with steps between: each gives the bits that an object of its own gives."""
+    rows, width, vocab = 40, 64, 1003
+    head, x, r, _, tokens = setup(kind, rows, width, vocab, lr=0.0)
+    alone = lambda: setup(kind, rows, width, vocab, lr=0.0)[0]
+    a = torch.full((rows,), -1.0 / rows, device=gu.DEV)
+    for n, top in [(3, 0), (17, 5), (1, 5), (40, 0), (2, 20), (39, 0), (5, 1), (6, 1), (7, 1), (8, 1), (9, 1), (3, 0), (40, 3)]:
+        got = [None if t is None else t.clone() for t in head.score(x[:n], r[:n], tokens[:n], top=top)]
+        want = alone().score(x[:n], r[:n], tokens[:n], top=top)
+        assert all(p is q or torch.equal(p, q) for p, q in zip(got, want)), (n, top)
+        other = alone()
+        got = [t.clone() for t in head.step(x[:n], r[:n], tokens[:n], a[:n])] + [g.clone() for g in head.grads.values()]
+        want = list(other.step(x[:n], r[:n], tokens[:n], a[:n])) + list(other.grads.values())
+        assert all(torch.equal(p, q) for p, q in zip(got, want)), n
+
+
+@pytest.mark.parametrize("warm", [True, False])
+def test_a_graph_keeps_what_it_works_in(warm):
+    """A step recorded with or without an eager call of its size before; later calls of other sizes, the larger ones in a new room, take nothing from it."""
+    rows, width, vocab = 16, 64, 1003
+    head, x, r, _, tokens = setup("bf16", 50, width, vocab, lr=0.0)
+    a = torch.full((50,), -1.0 / rows, device=gu.DEV)
+    call = lambda n: head.step(x[:n], r[:n], tokens[:n], a[:n])
+    want = [t.clone() for t in call(rows)] + [g.clone() for g in head.grads.values()]
+    if not warm:
+        head, _, _, _, _ = setup("bf16", 50, width, vocab, lr=0.0)
+        torch.cuda.synchronize()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        out = call(rows)
+        again = call(rows)
+    assert all(p is q for p, q in zip(out, again))
+    for n in (50, 1, 3, 7, 20, 50, 9, 11, 13, 21, 2, 16):
+        call(n)
+        head.score(x[:n], r[:n], tokens[:n], top=3)
+        junk = [torch.full((k,), float("nan"), device=gu.DEV) for k in (1 << 14, 1 << 16, 1 << 18, 1 << 20)]      # what an eager call freed is written by others
+        for t in (*out, *head.grads.values()):
+            t.fill_(float("nan"))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip([*out, *head.grads.values()], want)), n
+        del junk

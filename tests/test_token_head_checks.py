@@ -23,3 +23,38 @@ def test_refusals(bad):
             head.packed(a["x"], a["residual"])
         with pytest.raises(ValueError):
             head.score(a["x"], a["residual"], a["tokens"])
+
+
+def held_bytes(head):
+    """Bytes of every tensor storage that the object holds beside its parameters, states and gradients."""
+    seen, todo = {}, [v for k, v in vars(head).items() if k not in ("params", "grads", "w_lowp", "m", "v", "m_scale", "v_scale", "_adam")]
+    while todo:
+        o = todo.pop()
+        if isinstance(o, torch.Tensor):
+            seen[o.untyped_storage().data_ptr()] = o.untyped_storage().nbytes()
+        elif isinstance(o, dict):
+            todo += o.values()
+        elif isinstance(o, (list, tuple)):
+            todo += o
+    return sum(seen.values())
+
+
+def test_ragged_calls_hold_what_the_largest_needs():
+    """Every number of rows in turn, with and without alternatives, for training too: one room for the largest (logits and their gradient above all) and a few calls' results."""
+    width, vocab, most = 32, 1000, 150
+    head = TokenHeadStep(width, vocab, lc.LC_F32, device="cpu")
+    for rows in list(range(1, most + 1)) + list(range(most, 0, -7)):
+        for top in (0, 1, 20):
+            head._buffers(rows, top)
+        head._buffers(rows, 0, training=True)
+    room = most * 4 * (2 * head.padded + 3 * width + 2) + 4 * lc.rmsnorm_bwd_workspace_bytes(lc.RmsNormDesc(most, width)) + (1 << 20)
+    assert held_bytes(head) < room + 9 * most * 4 * (2 + 40 + width)
+
+
+def test_results_of_another_number_of_rows_stay():
+    head = TokenHeadStep(16, 40, lc.LC_F32, device="cpu")
+    a, b = head._buffers(8, 0), head._buffers(3, 5)
+    assert a["logprob"].data_ptr() != b["logprob"].data_ptr() and a["logits"].data_ptr() == b["logits"].data_ptr()
+    assert head._buffers(8, 0) is a and head._buffers(3, 5) is b and tuple(b["logits"].shape) == (3, 40) and tuple(b["ids"].shape) == (3, 5)
+    c = head._buffers(9, 0, training=True)                     # the room grows
+    assert head._buffers(9, 0, training=True) is c and not c["dlogits"].any() and c["room"]["rows"] == 9
