@@ -62,16 +62,15 @@ class TokenHeadStep:
             self.w_lowp.copy_(self.params["w"])
 
     def _check(self, rows: int, **tensors: Optional[torch.Tensor]) -> None:
-        """The entry points take pointers: what a call hands over has to be contiguous, of its type and of `rows` rows."""
+        """The entry points take pointers: what a call hands over has to be contiguous, of its type and of `rows` rows (grad_scale: one float), on this object's device."""
         for name, t in tensors.items():
             if t is None:
                 continue
             shape, dtype = ((rows, self.width), self.type) if name in ("x", "residual", "dtotal") else ((rows,), torch.int32 if name == "tokens" else torch.float32)
-            if tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous():
-                raise ValueError(f"{name}: a contiguous {dtype} tensor of shape {shape} is needed, got {t.dtype} {tuple(t.shape)} with strides {t.stride()}")
-
-    def _capturing(self) -> bool:
-        return self.params["w"].is_cuda and torch.cuda.is_current_stream_capturing()
+            if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != self.params["w"].device or not t.is_contiguous() or \
+                    (t.numel() != 1 if name == "grad_scale" else tuple(t.shape) != shape):
+                raise ValueError(f"{name}: a contiguous {dtype} tensor of {'one element' if name == 'grad_scale' else f'shape {shape}'} on {self.params['w'].device} is needed, got " +
+                                 (f"{t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}" if isinstance(t, torch.Tensor) else f"{t!r}"))
 
     def _make_set(self, rows: int, top: int, of_graphs: bool) -> dict:
         e = lambda *shape, dtype=torch.float32: torch.empty(shape, dtype=dtype, device=self.dev)
@@ -144,7 +143,8 @@ class TokenHeadStep:
         cross-entropy: -1/rows); dtotal: gradient that reaches x + residual by another way; grad_scale: one float on the device, multiplies the
         parameters' gradients.  Returns the rows' log probabilities and entropies and the gradient with respect to x (and to residual),
         in this object's buffers."""
-        self._check(x.shape[0], x=x, residual=residual, tokens=tokens, dlogprob=dlogprob, dentropy=dentropy, dtotal=dtotal)
+        self._check(x.shape[0], x=x, residual=residual, tokens=tokens, dlogprob=dlogprob, dentropy=dentropy, dtotal=dtotal,
+                    grad_scale=grad_scale)
         b = self._buffers(x.shape[0], 0, training=True)
         self._forward(b, x, residual, tokens)
         lc.token_logprob_bwd(b["token"], b["logits"], tokens, b["lse"], b["entropy"], dlogprob, dentropy, b["dlogits"], self.padded)

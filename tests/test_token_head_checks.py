@@ -58,3 +58,28 @@ def test_results_of_another_number_of_rows_stay():
     assert head._buffers(8, 0) is a and head._buffers(3, 5) is b and tuple(b["logits"].shape) == (3, 40) and tuple(b["ids"].shape) == (3, 5)
     c = head._buffers(9, 0, training=True)                     # the room grows
     assert head._buffers(9, 0, training=True) is c and not c["dlogits"].any() and c["room"]["rows"] == 9
+
+
+@pytest.mark.parametrize("name", ["x", "residual", "tokens", "dlogprob", "dentropy", "dtotal", "grad_scale"])
+def test_tensors_of_another_device(name):
+    """Checked before any launch, and without a GPU: another device than the parameters'."""
+    head = TokenHeadStep(WIDTH, 40, lc.LC_F32, device="cpu")
+    x, row = torch.zeros(ROWS, WIDTH), torch.zeros(ROWS)
+    a = dict(x=x, residual=x, tokens=row.int(), dlogprob=row, dentropy=row, dtotal=x, grad_scale=torch.ones(1))
+    a[name] = a[name].to("meta")
+    with pytest.raises(ValueError, match=name):
+        head.step(**a)
+    if name in ("x", "residual"):
+        with pytest.raises(ValueError, match=name):
+            head.packed(a["x"], a["residual"])
+    if name in ("x", "residual", "tokens"):
+        with pytest.raises(ValueError, match=name):
+            head.score(a["x"], a["residual"], a["tokens"])
+
+
+@pytest.mark.parametrize("bad", [0.37, 1, torch.ones(2), torch.ones(1, dtype=torch.float64), torch.ones(1, dtype=torch.bfloat16)])
+def test_gradient_scales_that_are_not_one_float_on_the_device(bad):
+    head = TokenHeadStep(WIDTH, 40, lc.LC_F32, device="cpu")
+    x = torch.zeros(ROWS, WIDTH)
+    with pytest.raises(ValueError, match="grad_scale"):
+        head.step(x, x, torch.zeros(ROWS, dtype=torch.int32), torch.zeros(ROWS), grad_scale=bad)
