@@ -7,6 +7,7 @@ computed here, and there is no fallback: if the HIP library has not been built, 
 from __future__ import annotations
 
 import ctypes
+import operator
 import os
 from dataclasses import dataclass
 from typing import Optional, Sequence
@@ -233,7 +234,7 @@ def _ptr(obj) -> Optional[int]:
     try:
         return obj.data_ptr() or None
     except AttributeError:
-        return int(obj) or None
+        return operator.index(obj) or None            # (a whole number: a float is a value that was meant as one, not an address)
 
 
 def _nbytes(ws) -> int:

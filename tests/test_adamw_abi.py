@@ -71,3 +71,12 @@ def test_gradients_of_another_type_than_said():
             lc.AdamWArgs([f], [g], [f], [f], g_dtype=kind)
     lc.AdamWArgs([f], [f], [f], [f])
     lc.AdamWArgs([f], [h], [f], [f], g_dtype=lc.LC_BF16)
+
+
+@pytest.mark.parametrize("scale", [0.37, 1.0, 2.5, 0.0])
+def test_a_number_in_place_of_a_pointer(scale):
+    """grad_scale is a pointer to one float on the device; a Python float would have become address 0 (no scale at all), 1 or 2."""
+    with pytest.raises(TypeError):
+        lc.adamw_step(args(), 1e-3, 0.9, 0.99, 1e-8, 0.1, 1, grad_scale=scale, stream=0)
+    with pytest.raises(TypeError):
+        lc.adamw_step_q8(args(True), 1e-3, 0.9, 0.99, 1e-8, 0.1, 1, 7, grad_scale=scale, stream=0)
