@@ -653,28 +653,50 @@ ADAMW_Q8_BLOCK = 256
 
 
 class AdamWArgs:
-    """Host-side pointer and size arrays of one parameter list (fp32 states), marshalled once and reusable."""
+    """Host-side pointer and size arrays of one parameter list (fp32 states), marshalled once and reusable.  The entry points take addresses: lists of tensors are checked here (as
+    many of each, their types, contiguous, as many elements as the list says, one device); plain addresses are taken as they are."""
+    _state = ("torch.float32",)
 
     def __init__(self, w: Sequence, g: Sequence, m: Sequence, v: Sequence, numel: Optional[Sequence[int]] = None,
                  w_lowp: Optional[Sequence] = None, g_dtype: int = LC_F32):
         if numel is None:
             numel = [t.numel() for t in w]
-        for t in g:
-            if str(getattr(t, "dtype", "")) not in ("", "torch.bfloat16" if g_dtype == LC_BF16 else "torch.float32"):
-                raise ValueError(f"gradients of type {t.dtype} with g_dtype {g_dtype}")
         self.n, self.numel, self.g_dtype = len(w), list(numel), g_dtype
+        if len(self.numel) != self.n:
+            raise ValueError(f"{len(self.numel)} sizes for {self.n} tensors")
+        self._check("w", w, ("torch.float32",))
+        self._check("g", g, ("torch.bfloat16" if g_dtype == LC_BF16 else "torch.float32",))
+        self._check("m", m, self._state)
+        self._check("v", v, self._state)
+        if w_lowp is not None:
+            self._check("w_lowp", w_lowp, ("torch.bfloat16",))
         self.w, self.g, self.m, self.v = _ptr_array(w), _ptr_array(g), _ptr_array(m), _ptr_array(v)
         self.numel_arr = _i64_array(self.numel)
         self.w_lowp = _ptr_array(w_lowp) if w_lowp is not None else None
         self._keep = [list(a) for a in (w, g, m, v, w_lowp or [])]
 
+    def _check(self, name: str, tensors: Sequence, types: Sequence[str], per: int = 1) -> None:
+        if len(tensors) != self.n:
+            raise ValueError(f"{name}: {len(tensors)} tensors for {self.n} of w")
+        for i, t in enumerate(tensors):
+            if not hasattr(t, "data_ptr"):
+                continue
+            need = -(-self.numel[i] // per)
+            self._device = getattr(self, "_device", t.device)
+            if str(t.dtype) not in types or not t.is_contiguous() or t.numel() < need or t.device != self._device:
+                raise ValueError(f"{name}[{i}]: a contiguous tensor of {' or '.join(types)} with {need} elements on {self._device} is needed, got {t.dtype} {tuple(t.shape)} "
+                                 f"with strides {t.stride()} on {t.device}")
+
 
 class AdamWQ8Args(AdamWArgs):
     """The same with the states in 8 bits (bytes) and a scale for every ADAMW_Q8_BLOCK elements."""
+    _state = ("torch.uint8", "torch.float8_e4m3fn", "torch.float8_e5m2")
 
     def __init__(self, w: Sequence, g: Sequence, m: Sequence, m_scale: Sequence, v: Sequence, v_scale: Sequence,
                  numel: Optional[Sequence[int]] = None, w_lowp: Optional[Sequence] = None, g_dtype: int = LC_F32):
         super().__init__(w, g, m, v, numel, w_lowp, g_dtype)
+        self._check("m_scale", m_scale, ("torch.float32",), ADAMW_Q8_BLOCK)
+        self._check("v_scale", v_scale, ("torch.float32",), ADAMW_Q8_BLOCK)
         self.m_scale, self.v_scale = _ptr_array(m_scale), _ptr_array(v_scale)
         self._keep += [list(m_scale), list(v_scale)]
 
@@ -687,14 +709,20 @@ def _decays(args: AdamWArgs, weight_decay_per_tensor):
     return (ctypes.c_float * max(args.n, 1))(*[float(x) for x in weight_decay_per_tensor])
 
 
+def _one_float(grad_scale):
+    if hasattr(grad_scale, "data_ptr") and not (grad_scale.numel() == 1 and grad_scale.element_size() == 4 and grad_scale.is_floating_point()):
+        raise ValueError(f"grad_scale: one float is needed, got {grad_scale.dtype} {tuple(grad_scale.shape)}")
+    return _ptr(grad_scale)
+
+
 def adamw_step(args: AdamWArgs, lr: float, beta1: float, beta2: float, eps: float, weight_decay: float, step: int,
                weight_decay_per_tensor=None, grad_scale=None, stream=None) -> None:
     _check(lib().adamw_step(args.n, args.w, args.g, args.g_dtype, args.m, args.v, args.numel_arr, lr, beta1, beta2, eps, weight_decay, step,
-                            _decays(args, weight_decay_per_tensor), _ptr(grad_scale), args.w_lowp, _stream(stream)), "adamw_step")
+                            _decays(args, weight_decay_per_tensor), _one_float(grad_scale), args.w_lowp, _stream(stream)), "adamw_step")
 
 
 def adamw_step_q8(args: AdamWQ8Args, lr: float, beta1: float, beta2: float, eps: float, weight_decay: float, step: int, seed: int,
                   weight_decay_per_tensor=None, grad_scale=None, stream=None) -> None:
     _check(lib().adamw_step_q8(args.n, args.w, args.g, args.g_dtype, args.m, args.m_scale, args.v, args.v_scale, args.numel_arr, lr, beta1, beta2,
-                               eps, weight_decay, step, seed & 0xFFFFFFFF, _decays(args, weight_decay_per_tensor), _ptr(grad_scale), args.w_lowp,
+                               eps, weight_decay, step, seed & 0xFFFFFFFF, _decays(args, weight_decay_per_tensor), _one_float(grad_scale), args.w_lowp,
                                _stream(stream)), "adamw_step_q8")

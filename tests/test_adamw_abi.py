@@ -80,3 +80,42 @@ def test_a_number_in_place_of_a_pointer(scale):
         lc.adamw_step(args(), 1e-3, 0.9, 0.99, 1e-8, 0.1, 1, grad_scale=scale, stream=0)
     with pytest.raises(TypeError):
         lc.adamw_step_q8(args(True), 1e-3, 0.9, 0.99, 1e-8, 0.1, 1, 7, grad_scale=scale, stream=0)
+
+
+@pytest.mark.parametrize("q8", [False, True])
+def test_lists_that_pointers_would_misread(q8):
+    """Lengths, types, strides, sizes and devices of what the arrays of addresses are made from."""
+    import torch
+    n = 600
+    f32, byte = torch.zeros(n), torch.zeros(n, dtype=torch.uint8)
+    state, scale = (byte if q8 else f32), torch.zeros(3)
+
+    def make(**swap):
+        a = dict(w=[f32, f32], g=[f32, f32], m=[state, state], v=[state, state], numel=None, w_lowp=[None, torch.zeros(n, dtype=torch.bfloat16)], m_scale=[scale, scale],
+                 v_scale=[scale, scale]) | swap
+        if q8:
+            return lc.AdamWQ8Args(a["w"], a["g"], a["m"], a["m_scale"], a["v"], a["v_scale"], a["numel"], a["w_lowp"])
+        return lc.AdamWArgs(a["w"], a["g"], a["m"], a["v"], a["numel"], a["w_lowp"])
+
+    make()
+    make(w=[f32, FAKE], numel=[n, n], m=[state, FAKE], w_lowp=None)
+    if q8:
+        make(m=[byte.view(torch.float8_e4m3fn)] * 2, v=[byte.view(torch.float8_e5m2)] * 2)
+    names = ("w", "g", "m", "v", "w_lowp") + (("m_scale", "v_scale") if q8 else ())
+    for name in names:
+        good = scale if "scale" in name else torch.zeros(n, dtype=torch.bfloat16) if name == "w_lowp" else state if name in "mv" else f32
+        fewer = good.clone()[:-1]
+        for bad in ([good], [good, good, good], [good, good.double()], [good, torch.zeros(2 * good.numel(), dtype=good.dtype)[::2]], [good, good.to("meta")]) + \
+                (() if name == "w" else ([good, fewer],)):
+            with pytest.raises(ValueError):
+                make(**{name: bad})
+    with pytest.raises(ValueError):
+        make(numel=[n])
+    with pytest.raises(ValueError, match="w"):
+        make(numel=[n, n + 1])
+    with pytest.raises(ValueError):                              # states of the other width
+        make(m=[f32 if q8 else byte] * 2)
+    for bad in (torch.ones(2), torch.ones(1, dtype=torch.float64)):
+        with pytest.raises(ValueError, match="grad_scale"):
+            (lc.adamw_step_q8(make(), 1e-3, 0.9, 0.99, 1e-8, 0.1, 1, 7, grad_scale=bad, stream=0) if q8 else
+             lc.adamw_step(make(), 1e-3, 0.9, 0.99, 1e-8, 0.1, 1, grad_scale=bad, stream=0))
