@@ -74,8 +74,15 @@ class lc_rmsnorm_desc(ctypes.Structure):
                 ("eps", ctypes.c_float), ("dtype", ctypes.c_int)]
 
 
+class _Kept:
+    """A descriptor that keeps its C structure (see _c): what copies and pickles of it leave out."""
+
+    def __getstate__(self):
+        return {k: v for k, v in self.__dict__.items() if k != "_c_ref"}
+
+
 @dataclass(frozen=True)
-class RmsNormDesc:
+class RmsNormDesc(_Kept):
     rows: int
     c: int
     x_ld: int = 0
@@ -92,7 +99,7 @@ class lc_token_desc(ctypes.Structure):
 
 
 @dataclass(frozen=True)
-class TokenDesc:
+class TokenDesc(_Kept):
     rows: int
     vocab: int
     ld: int = 0
