@@ -8,7 +8,8 @@ norm's scale.  Every operator is a call into the C library; this module only own
     total, codes, scales = head.packed(x, residual)                     # the norm's output in 8 bits, for a product or a wire that takes it so
 
 Calls share one set of buffers, for as many rows as any of them has had; results are kept apart for the last eight of (rows, top).  What a captured call
-works in stays with the object.
+works in stays with the object.  Calls of one object follow one another: one on another stream than the last waits for it there (a graph's replays and
+other threads have to see to that themselves).
 
 The vocabulary is padded to a multiple of 8 rows of the classifier (what the bf16 products take without copies); the pad's logits are never read and their
 gradient stays zero.
@@ -49,12 +50,14 @@ class TokenHeadStep:
         else:
             self.m, self.v = ([torch.zeros(n, **f32) for n in sizes] for _ in range(2))
             self._adam = lc.AdamWArgs(*lists, self.m, self.v, w_lowp=lowp)
+        self._stream = torch.cuda.current_stream() if self.params["w"].is_cuda else None      # the last call's
         self._room: Optional[dict] = None                                   # what calls work in, for room["rows"] rows
         self._sets: Dict[Tuple[int, int], dict] = {}                        # views of it and results for (rows, top), the one used last at the end
         self._of_graphs: Dict[Tuple[int, int], dict] = {}                   # sets made while a graph recorded, which graphs alone use
 
     def load(self, w: torch.Tensor, gamma: torch.Tensor) -> None:
         """Sets the classifier ([vocab][width]) and the norm's scale."""
+        self._follow()
         self.params["w"].zero_()
         self.params["w"][:self.vocab].copy_(w)
         self.params["gamma"].copy_(gamma)
@@ -72,6 +75,21 @@ class TokenHeadStep:
                 raise ValueError(f"{name}: a contiguous {dtype} tensor of {'one element' if name == 'grad_scale' else f'shape {shape}'} on {self.params['w'].device} is needed, got " +
                                  (f"{t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}" if isinstance(t, torch.Tensor) else f"{t!r}"))
 
+    def _follow(self) -> None:
+        """Parameters, states and room are shared: the call that begins waits for the last one where that was on another stream (not while a graph records, which runs nothing)."""
+        if self._stream is None or (lc._stream(None) or 0) == self._stream.cuda_stream or torch.cuda.is_current_stream_capturing():
+            return
+        stream = torch.cuda.current_stream()
+        stream.wait_stream(self._stream)
+        self._stream = stream
+
+    def _let_go(self, b: dict) -> None:
+        """Before a set is dropped: its memory is another's only when the last call's stream is done with it."""
+        if self._stream is not None:
+            for t in (*b.values(), *b["room"].values()):
+                if isinstance(t, torch.Tensor):
+                    t.record_stream(self._stream)
+
     def _make_set(self, rows: int, top: int, of_graphs: bool) -> dict:
         e = lambda *shape, dtype=torch.float32: torch.empty(shape, dtype=dtype, device=self.dev)
         norm = lc.RmsNormDesc(rows, self.width, eps=self.eps, dtype=self.dtype)
@@ -84,7 +102,9 @@ class TokenHeadStep:
             most = rows
             if room is not None:                                            # (freed before its successor is made, but for what graphs use)
                 most, need = max(rows, room["rows"]), max(need, room["ws"].numel())
-                room = self._room = None
+                for b in self._sets.values():
+                    self._let_go(b)
+                room = self._room = b = None
                 self._sets = {k: b for k, b in self._sets.items() if b["in_graph"]}
             room = dict(rows=most, ws=e(need, dtype=torch.uint8), total=e(most, self.width, dtype=self.type), y=e(most, self.width, dtype=self.type),
                         rstd=e(most), logits=e(most, self.padded, dtype=self.type), lse=e(most))
@@ -109,7 +129,7 @@ class TokenHeadStep:
             b = self._make_set(rows, top, False)
             spare = [k for k, s in self._sets.items() if not s["in_graph"]]
             if len(spare) >= KEPT_SETS:
-                del self._sets[spare[0]]
+                self._let_go(self._sets.pop(spare[0]))
             self._sets[key] = b
         else:
             self._sets[key] = self._sets.pop(key)
@@ -134,6 +154,7 @@ class TokenHeadStep:
         """Log probability and entropy of each row's token (int32; outside the vocabulary: does not count), and the `top` likeliest tokens with
         theirs.  The tensors returned are this object's buffers: the next call over as many rows writes them again."""
         self._check(x.shape[0], x=x, residual=residual, tokens=tokens)
+        self._follow()
         b = self._buffers(x.shape[0], top)
         self._forward(b, x, residual, tokens)
         return b["logprob"], b["entropy"], b["ids"], b["top"]
@@ -145,6 +166,7 @@ class TokenHeadStep:
         in this object's buffers."""
         self._check(x.shape[0], x=x, residual=residual, tokens=tokens, dlogprob=dlogprob, dentropy=dentropy, dtotal=dtotal,
                     grad_scale=grad_scale)
+        self._follow()
         b = self._buffers(x.shape[0], 0, training=True)
         self._forward(b, x, residual, tokens)
         lc.token_logprob_bwd(b["token"], b["logits"], tokens, b["lse"], b["entropy"], dlogprob, dentropy, b["dlogits"], self.padded)
@@ -165,6 +187,7 @@ class TokenHeadStep:
         """x + residual and its norm as e4m3 codes with a scale for every `group` columns (0: one a row)."""
         rows = x.shape[0]
         self._check(rows, x=x, residual=residual)
+        self._follow()
         total = torch.empty((rows, self.width), dtype=self.type, device=self.dev) if residual is not None else None
         codes = torch.empty((rows, self.width), dtype=torch.float8_e4m3fn, device=self.dev)
         scales = torch.empty((rows, -(-self.width // group) if group else 1), device=self.dev)

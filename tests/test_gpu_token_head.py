@@ -169,3 +169,31 @@ def test_a_graph_keeps_what_it_works_in(warm):
         torch.cuda.synchronize()
         assert all(torch.equal(p, q) for p, q in zip([*out, *head.grads.values()], want)), n
         del junk
+
+
+def test_calls_on_streams_in_turn():
+    """A step behind long work on one stream, a score and a step on two others, with nothing between them: each sees what the one before it has left."""
+    rows, width, vocab = 30, 64, 1003
+    a = torch.full((rows,), -1.0 / rows, device=gu.DEV)
+
+    def run(streams, busy):
+        head, x, r, _, tokens = setup("bf16", rows, width, vocab, lr=0.01)
+        out = []
+        torch.cuda.synchronize()
+        for i, stream in enumerate(streams):
+            with torch.cuda.stream(stream):
+                for _ in range(busy):
+                    torch.mm(big, big)
+                if i % 2:
+                    out += [t.clone() for t in head.score(x[:rows - i], r[:rows - i], tokens[:rows - i], top=i)]
+                else:
+                    out += [t.clone() for t in head.step(x, r, tokens, a)]
+            busy = max(busy - 10, 0)
+        torch.cuda.synchronize()
+        return out + [p.clone() for p in head.params.values()]
+
+    big = torch.randn(4096, 4096, device=gu.DEV)
+    side = [torch.cuda.Stream() for _ in range(2)]
+    want = run([torch.cuda.current_stream()] * 9, 0)
+    got = run([side[0], torch.cuda.current_stream(), side[1], side[0], torch.cuda.current_stream(), side[1], side[1], side[0], torch.cuda.current_stream()], 30)
+    assert all(torch.equal(p, q) for p, q in zip(got, want))
