@@ -145,6 +145,8 @@ class TokenHeadStep:
         return b
 
     def _forward(self, b: dict, x: torch.Tensor, residual: Optional[torch.Tensor], tokens: torch.Tensor) -> None:
+        if x.shape[0] == 0:                                       # (the product takes no empty batch)
+            return
         w = self.params["w"] if self.w_lowp is None else self.w_lowp
         lc.rmsnorm_fwd(b["norm"], x, residual, self.params["gamma"], b["total"] if residual is not None else None, b["y"], b["rstd"])
         lc.conv2d_fwd(b["product"], b["y"], w, b["logits"], b["ws"])
@@ -169,12 +171,16 @@ class TokenHeadStep:
         self._follow()
         b = self._buffers(x.shape[0], 0, training=True)
         self._forward(b, x, residual, tokens)
-        lc.token_logprob_bwd(b["token"], b["logits"], tokens, b["lse"], b["entropy"], dlogprob, dentropy, b["dlogits"], self.padded)
-        w = self.params["w"] if self.w_lowp is None else self.w_lowp
-        lc.conv2d_bwd_data(b["product"], b["dlogits"], w, b["dy"], b["ws"])
-        lc.conv2d_bwd_weight(b["product"], b["y"], b["dlogits"], self.grads["w"], b["ws"])
-        lc.rmsnorm_bwd(b["norm"], b["total"] if residual is not None else x, b["dy"], dtotal, self.params["gamma"], b["rstd"], b["dx"],
-                       self.grads["gamma"], b["ws"])
+        if x.shape[0]:
+            lc.token_logprob_bwd(b["token"], b["logits"], tokens, b["lse"], b["entropy"], dlogprob, dentropy, b["dlogits"], self.padded)
+            w = self.params["w"] if self.w_lowp is None else self.w_lowp
+            lc.conv2d_bwd_data(b["product"], b["dlogits"], w, b["dy"], b["ws"])
+            lc.conv2d_bwd_weight(b["product"], b["y"], b["dlogits"], self.grads["w"], b["ws"])
+            lc.rmsnorm_bwd(b["norm"], b["total"] if residual is not None else x, b["dy"], dtotal, self.params["gamma"], b["rstd"], b["dx"],
+                           self.grads["gamma"], b["ws"])
+        else:                                                     # gradients are sums over no rows
+            for g in self.grads.values():
+                g.zero_()
         self.steps += 1
         decays = [self.weight_decay, 0.0]                         # the norm's scale is not decayed
         if self.states_in_8_bits:
@@ -191,5 +197,6 @@ class TokenHeadStep:
         total = torch.empty((rows, self.width), dtype=self.type, device=self.dev) if residual is not None else None
         codes = torch.empty((rows, self.width), dtype=torch.float8_e4m3fn, device=self.dev)
         scales = torch.empty((rows, -(-self.width // group) if group else 1), device=self.dev)
-        lc.rmsnorm_fwd_q8(lc.RmsNormDesc(rows, self.width, eps=self.eps, dtype=self.dtype), x, residual, self.params["gamma"], total, codes, scales, group)
+        if rows:
+            lc.rmsnorm_fwd_q8(lc.RmsNormDesc(rows, self.width, eps=self.eps, dtype=self.dtype), x, residual, self.params["gamma"], total, codes, scales, group)
         return total, codes, scales

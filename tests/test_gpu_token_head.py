@@ -197,3 +197,20 @@ def test_calls_on_streams_in_turn():
     want = run([torch.cuda.current_stream()] * 9, 0)
     got = run([side[0], torch.cuda.current_stream(), side[1], side[0], torch.cuda.current_stream(), side[1], side[1], side[0], torch.cuda.current_stream()], 30)
     assert all(torch.equal(p, q) for p, q in zip(got, want))
+
+
+@pytest.mark.parametrize("states_in_8_bits", [False, True])
+def test_a_step_over_no_rows(states_in_8_bits):
+    """Gradients are zero: the classifier decays, the norm's scale stays, and a step over rows after it is the second step."""
+    head, x, r, _, tokens = setup("bf16", 20, 64, 40, states_in_8_bits=states_in_8_bits, lr=0.25)
+    a = torch.full((20,), -0.05, device=gu.DEV)
+    before = {k: p.clone() for k, p in head.params.items()}
+    lp, ent, dx = head.step(x[:0], r[:0], tokens[:0], a[:0])
+    torch.cuda.synchronize()
+    assert lp.shape == ent.shape == (0,) and dx.shape == (0, 64) and head.steps == 1
+    assert torch.equal(head.params["gamma"], before["gamma"]) and not any(g.any() for g in head.grads.values())
+    want = before["w"].double() * (1 - float(np.float32(0.25 * 0.1)))
+    assert bool(((head.params["w"].double() - want).abs() <= 2.0 ** -24 * want.abs()).all()) and torch.equal(head.w_lowp, head.params["w"].bfloat16())
+    head.step(x, r, tokens, a)
+    torch.cuda.synchronize()
+    assert head.steps == 2 and all(p.isfinite().all() for p in head.params.values()) and head.grads["w"].any()

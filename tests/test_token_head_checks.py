@@ -83,3 +83,14 @@ def test_gradient_scales_that_are_not_one_float_on_the_device(bad):
     x = torch.zeros(ROWS, WIDTH)
     with pytest.raises(ValueError, match="grad_scale"):
         head.step(x, x, torch.zeros(ROWS, dtype=torch.int32), torch.zeros(ROWS), grad_scale=bad)
+
+
+@pytest.mark.parametrize("residual", [True, False])
+def test_no_rows(residual):
+    """An empty batch is scored and packed without a launch."""
+    head = TokenHeadStep(WIDTH, 40, lc.LC_F32, device="cpu")
+    x, tokens = torch.zeros(0, WIDTH), torch.zeros(0, dtype=torch.int32)
+    lp, ent, ids, top = head.score(x, x if residual else None, tokens, top=3)
+    assert lp.shape == ent.shape == (0,) and ids.shape == top.shape == (0, 3)
+    total, codes, scales = head.packed(x, x if residual else None, group=0)
+    assert codes.shape == (0, WIDTH) and scales.shape == (0, 1) and (total is None) == (not residual)
