@@ -275,3 +275,19 @@ def test_more_rows_than_a_grid_takes_at_once(kind, top):
     torch.cuda.synchronize()
     exact = ops.token_logprob_bwd(z64, t64, np.ones(rows), np.zeros(rows))
     assert np.all(np.abs(f64(dz) - exact) <= half * (1 + half) * np.abs(exact) + (1 + half) * (tol(vocab) + 16 * U))
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab", [40000, 70000, 140000, 300000])
+@pytest.mark.parametrize("top", [20, 32])
+@pytest.mark.parametrize("case", ["equal", "two_values", "falling", "rising", "few_steps", "one_block"])
+def test_alternatives_joined_from_many_lists(kind, vocab, top, case):
+    """Rows in 40 to 293 blocks whose lists together hold more equal or near-equal keys than there is room for at once (256), one list a lane and several."""
+    dtype, t, _ = TYPES[kind]
+    place = np.arange(vocab, dtype=np.float64)
+    z = {"equal": np.full(vocab, 1.5), "two_values": np.where(place % 3 == 1, 2.0, -1.0), "falling": -np.floor(place / 64) / 64, "rising": np.floor(place / 64) / 64,
+         "few_steps": np.floor(place / vocab * 7), "one_block": np.where((place >= 2048) & (place < 3072), 2.0, 1.0)}[case]
+    z = torch.from_numpy(np.stack([z, z[::-1]])).to(t).to(gu.DEV).contiguous()
+    t64 = np.array([0, vocab - 1])
+    got = run(dtype, z, gu.dev(t64.astype(np.int32)), vocab, top)
+    check_forward(vocab, got, ops.token_logprob(f64(z), t64, top), top)
