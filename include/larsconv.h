@@ -410,8 +410,8 @@ typedef struct {
  * (0 where the token does not count).  A row with a NaN or +infinity has NaN in lse, entropy and log probabilities (a NaN is never listed).
  * A finite mask (-1e9, the type's lowest value) is a logit like any other: probability 0 beside ordinary ones.
  * logprob, entropy, lse: rows floats each; entropy may be NULL, and lse where no backward pass follows.  Sums are
- * fp32; logprob is formed from the difference to the row's maximum, so that large logits do not cancel in it.  Rows whose largest finite logit is beyond 5.8e6 on
- * either side (all of it such a mask, for one) are read again by one wave each: right, and slower. */
+ * fp32; logprob is formed from the difference to the row's maximum, so that large logits do not cancel in it.  Parts of a row (a wave's) whose
+ * largest finite logit is beyond 1.48e9 on either side are read again: right, and slower. */
 size_t token_logprob_workspace_bytes(const lc_token_desc* desc);
 lc_status token_logprob_fwd(const lc_token_desc* desc, const void* logits, const int32_t* tokens, float* logprob, float* entropy, float* lse,
                             int32_t* top_tokens, float* top_logprobs, void* workspace, size_t workspace_bytes, void* hip_stream);

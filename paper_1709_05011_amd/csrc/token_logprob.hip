@@ -80,42 +80,8 @@ __device__ __forceinline__ Target target_of(const TokenArgs& p, long long row) {
     return {counts, counts ? as_float<T>(static_cast<const T*>(p.z)[row * p.ld + token]) : 0.f};
 }
 
-// The sums of a row of c columns by one wave, from memory and from the distances themselves: for rows whose maximum is further from zero than products with log2 e carry
-// (see LaneSums).  KNOWN: m is its maximum already.
-template <bool KNOWN, typename T>
-__device__ __forceinline__ float3 sums_by_distances(const T* z, int c, float m = -INFINITY) {
-    constexpr uint32_t kMaskedBits = sizeof(T) == 2 ? 0xff80u : 0xff800000u;
-    const int lane = threadIdx.x & 63;
-    const auto over = [&](auto&& f) __attribute__((always_inline)) {
-        for (int at = 0; at < c; at += 512) {
-            const auto column = [&](int) { return at + lane * 8; };
-            Packed<T> v[1];
-            lc_issue8(v, z, column, c, at + 512 <= c, kMaskedBits);
-            lc_settle8(v, column, c, c, at + 512 <= c, kMaskedBits);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) f(v[0].get(j));
-        }
-    };
-    if constexpr (!KNOWN) {
-        over([&](float x) { m = fmaxf(m, x); });
-        m = lc_wave_max(m);
-    }
-    const float from = m == -INFINITY ? 0.f : m;
-    float s = 0.f, t = 0.f;
-    over([&](float x) {
-        const float d = (x - from) * kLog2e, e = __builtin_amdgcn_exp2f(d);
-        s += e;
-        t = fmaf(e, fmaxf(d, kFar), t);
-    });
-    return make_float3(m, lc_wave_sum(s), lc_wave_sum(t));
-}
-constexpr float kProductsFloor = -8388608.f;     // -2^23: from here to 2^23 rounding a product to 24 bits takes 1/4 at most
-constexpr float kProductsEnd = 5.8e6f;           // largest magnitude whose product with log2 e stays within that
-
 // What a row gives but for its alternatives, from its m, S and T; a whole wave with the same values, lane 0 writes.
-template <typename T>
 __device__ __forceinline__ Row finish_row(const TokenArgs& p, long long row, const Target& target, float3 w) {
-    if (fabsf(w.x) > kProductsEnd && fabsf(w.x) < INFINITY) w = sums_by_distances<true>(static_cast<const T*>(p.z) + row * p.ld, p.vocab, w.x);
     const bool empty = w.y == 0.f;
     Row r;
     r.m = w.x == -INFINITY ? 0.f : w.x;
@@ -252,6 +218,39 @@ __device__ __forceinline__ void join_lists(const Key* lists, int n, int top, Key
     rank_keys(keys, min(held, kCandidates), top, emit);
 }
 
+// The sums by one wave of columns [first, first + SPAN) of each `stride` up to `end`, of a row of c, from memory and from the distances themselves: where its maximum is further from
+// zero than products with log2 e carry (see LaneSums).  KNOWN: m is the maximum already.
+template <int SPAN, bool KNOWN, typename T>
+__device__ __forceinline__ float3 sums_by_distances(const T* z, int c, int first, int stride, int end, float m = -INFINITY) {
+    constexpr uint32_t kMaskedBits = sizeof(T) == 2 ? 0xff80u : 0xff800000u;
+    const int lane = threadIdx.x & 63;
+    const auto over = [&](auto&& f) __attribute__((always_inline)) {
+        for (int start = first; start < end; start += stride)
+            for (int at = start; at < start + SPAN; at += 512) {
+                const auto column = [&](int) { return at + lane * 8; };
+                Packed<T> v[1];
+                lc_issue8(v, z, column, c, at + 512 <= end, kMaskedBits);
+                lc_settle8(v, column, c, end, at + 512 <= end, kMaskedBits);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) f(v[0].get(j));
+            }
+    };
+    if constexpr (!KNOWN) {
+        over([&](float x) { m = fmaxf(m, x); });
+        m = lc_wave_max(m);
+    }
+    const float from = m == -INFINITY ? 0.f : m;
+    float s = 0.f, t = 0.f;
+    over([&](float x) {
+        const float d = (x - from) * kLog2e, e = __builtin_amdgcn_exp2f(d);
+        s += e;
+        t = fmaf(e, fmaxf(d, kFar), t);
+    });
+    return make_float3(m, lc_wave_sum(s), lc_wave_sum(t));
+}
+constexpr float kProductsFloor = -0x1p31f;       // from here to 2^31 rounding a product to 24 bits takes 64 at most
+constexpr float kProductsEnd = 1.48e9f;          // largest magnitude whose product with log2 e stays within that
+
 // Larger of three, a NaN ignored: without the instruction that the compiler puts before fmaxf() for each operand from memory, against signalling NaN
 // (one of those may cost a lane its maximum here; its row is NaN either way).
 __device__ __forceinline__ float max3(float a, float b, float c) {
@@ -261,10 +260,10 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 }
 
 // What a lane has summed: S and T = sum e d over e = 2^d, d = z log2 e - ref, with ref the product m log2 e as rounded for the largest m so far.  One fused
-// multiply-add a value, exact to its rounding because ref is.  What rounding takes from the product shifts every d alike: 1/4 at most within 2^23 of zero, hundreds from 2^31 on (a
-// mask of -1e10 in all of a lane's values: 2^440).  So ref is -2^23 at least: what lies further down adds 0 beside any maximum that does not, and a row whose maximum lies beyond
-// that on either side is summed again when its maximum is known (finish_row; what the waves have summed of it is not used).  A masked value makes T 0 * infinity: the sum
-// is then made again with the distance bounded (NaN and infinity among the logits come out NaN either way).
+// multiply-add a value, exact to its rounding because ref is.  What rounding takes from the product shifts every d alike, to be put right at the wave's end: by 64 at most within 2^31 of
+// zero, where 2^64 for each of 2^30 values and its product with d are in range, and by hundreds beyond (a mask of -1e10 in all of a lane's values: 2^440).  So ref is -2^31 at
+// least: what lies further down adds 0 beside any maximum that does not, and a wave whose maximum lies beyond that on either side sums its part again, now that it knows the
+// maximum.  A masked value makes T 0 * infinity: the sum is then made again with the distance bounded (NaN and infinity among the logits come out NaN either way).
 template <bool ENT>
 struct LaneSums {
     float m = -INFINITY, ref = kProductsFloor, s = 0.f, t = 0.f;      // (t only with ENT)
@@ -304,24 +303,26 @@ struct LaneSums {
         return most;
     }
 
-    // The wave's m, S and T about m itself.
-    __device__ __forceinline__ float3 join() const {
-        const float all = lc_wave_max(m), product = all * kLog2e, less = -fmaxf(product, kProductsFloor);
+    // The wave's m, S and T about m itself; z to end: its part of the row, for sums_by_distances().
+    template <int SPAN, typename T>
+    __device__ __forceinline__ float3 join(const T* z, int c, int first, int stride, int end) const {
+        const float all = lc_wave_max(m), less = -fmaxf(all * kLog2e, kProductsFloor);
+        if (fabsf(all) > kProductsEnd && fabsf(all) < INFINITY) return sums_by_distances<SPAN, true>(z, c, first, stride, end, all);
         const float shift = fmaxf(ref + less, kFar), f = __builtin_amdgcn_exp2f(ref + less);      // (a lane whose sums are NaN keeps them so)
         const float ws = lc_wave_sum(f * s), wt = lc_wave_sum(f * fmaf(shift, s, t));
-        // every exponent is off by what rounding the product took (of a wave that lies below the floor nothing counts)
-        const float off = product < kProductsFloor ? 0.f : fmaf(all, kLog2e, less), back = __builtin_amdgcn_exp2f(-off);
+        // every exponent is off by what rounding the product took
+        const float off = all == -INFINITY ? 0.f : fmaf(all, kLog2e, less), back = __builtin_amdgcn_exp2f(-off);
         return make_float3(all, ws * back, fmaf(-off, ws, wt) * back);
     }
 };
 
 // What a block of the forward pass has joined goes to the results, or, of a row in several blocks, to the workspace.
-template <typename T, bool TOP>
+template <bool TOP>
 __device__ __forceinline__ void leave(const TokenArgs& p, long long row, const Target& target, float3 w, const Key* lists, int n, Key* keys, bool ranked) {
     const long long unit = row * p.blocks + blockIdx.x;
     const int lane = threadIdx.x & 63;
     Row r;
-    if (p.blocks == 1) r = finish_row<T>(p, row, target, w);
+    if (p.blocks == 1) r = finish_row(p, row, target, w);
     else if (lane == 0) p.stats[unit] = make_float4(w.x, w.y, w.z, 0.f);
     if constexpr (TOP) {
         const auto emit = [&](int place, Key k) {
@@ -381,7 +382,7 @@ __global__ void __launch_bounds__((TOP ? kMostListing : kMostWaves) * 64, TOP &&
             issue(now, at + 2 * stride);
             if (at + stride < end) add(next, at + stride);
         }
-        const float3 w = sums.join();
+        const float3 w = sums.template join<kRound>(z, p.vocab, first, stride, end);
         int held = 0;
         if constexpr (TOP) {
             const uint32_t order = lanes_bound(order_of(sums.m), listable(sums.m), p.top);
@@ -444,14 +445,14 @@ __global__ void __launch_bounds__((TOP ? kMostListing : kMostWaves) * 64, TOP &&
             __builtin_amdgcn_wave_barrier();
         }
         if (waves == 1) {
-            leave<T, TOP>(p, row, target, w, nullptr, held, keys, false);
+            leave<TOP>(p, row, target, w, nullptr, held, keys, false);
             if (TOP) __syncthreads();
             continue;
         }
         if constexpr (TOP) rank_keys(keys, held, p.top, [&](int place, Key k) { lists[wave * p.top + place] = k; });
         if (lane == 0) stats[wave] = make_float4(w.x, w.y, w.z, 0.f);
         __syncthreads();
-        if (wave == 0) leave<T, TOP>(p, row, target, join_sums(stats, waves), lists, waves, keys, true);
+        if (wave == 0) leave<TOP>(p, row, target, join_sums(stats, waves), lists, waves, keys, true);
         __syncthreads();
     }
 }
@@ -462,7 +463,7 @@ __global__ void __launch_bounds__(64) token_join_kernel(const TokenArgs p) {
     __shared__ Key keys[kCandidates];
     for (long long row = blockIdx.x; row < p.rows; row += gridDim.x) {
         const Target target = target_of<T>(p, row);
-        const Row r = finish_row<T>(p, row, target, join_sums(p.stats + row * p.blocks, p.blocks));
+        const Row r = finish_row(p, row, target, join_sums(p.stats + row * p.blocks, p.blocks));
         if (p.top) join_lists(p.keys + row * p.blocks * p.top, p.blocks, p.top, keys, [&](int place, Key k) { put_alternative(p, row, place, k, r); });
         __syncthreads();
     }
@@ -487,7 +488,7 @@ constexpr float kLseEnd = sizeof(T) == 2 ? 16384.f : 256.f;
 // Such a row's gradient, by one wave: its sums again, then all of it (dz may be the logits' own buffer: no other wave writes to the row).
 template <typename T>
 __device__ __attribute__((noinline)) void far_row(const T* z, T* out, int vocab, int token, float a, float b, float ent) {
-    const float3 w = sums_by_distances<false>(z, vocab);
+    const float3 w = sums_by_distances<512, false>(z, vocab, 0, 512, vocab);
     const float log_s = logf(w.y);
     for (int col = threadIdx.x * 8; col < vocab; col += 512) {
         Packed<T> v;
