@@ -158,11 +158,12 @@ __device__ __forceinline__ float3 join_sums(const float4* stats, int n) {
 }
 
 // The `top` largest keys of n falling lists of `top`, by a wave; `keys`: kCandidates in LDS.  A lane answers for k keys no smaller than its own: the k-th of
-// its list, or the first of the largest of its lists; then every list is walked from its head while its keys reach the bound that follows.
+// its list, or the first of the largest of its lists; then every list is walked from its head while its keys reach the bound that follows.  Where there are more keys than room, k is such that half of the
+// lists answer for `top` of them: were it nearly all (25 lists, 20 keys), the bound would be their least, and more keys than there is room for would reach it (64 rows of 50021 27 us, so 14).
 template <typename F>
 __device__ __forceinline__ void join_lists(const Key* lists, int n, int top, Key* keys, F&& emit) {
     constexpr int kHead = 8;                        // keys of a lane that are asked for at once: of its list, or half of them of each of two lists
-    const int lane = threadIdx.x & 63, lanes = min(n, 64), k = (top + lanes - 1) / lanes, each = n > 64 ? kHead / 2 : kHead;
+    const int lane = threadIdx.x & 63, lanes = min(n, 64), k = ((n * top > kCandidates ? 2 * top : top) + lanes - 1) / lanes, each = n > 64 ? kHead / 2 : kHead;
     Key head[kHead], own = 0;
 #pragma unroll
     for (int j = 0; j < kHead; ++j) {

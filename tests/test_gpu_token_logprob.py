@@ -291,3 +291,17 @@ def test_alternatives_joined_from_many_lists(kind, vocab, top, case):
     t64 = np.array([0, vocab - 1])
     got = run(dtype, z, gu.dev(t64.astype(np.int32)), vocab, top)
     check_forward(vocab, got, ops.token_logprob(f64(z), t64, top), top)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,vocab", [(64, 40000), (64, 50021), (96, 98304), (16, 33000)])
+@pytest.mark.parametrize("top", [17, 20, 32])
+def test_alternatives_joined_from_few_more_lists_than_places(kind, rows, vocab, top):
+    """20 to 33 lists: nearly as many as places, where a bound that every list has to reach would be the least of all; a third of the rows with one list's worth of logits, so that most
+    lists hold less than they answer for."""
+    dtype, t, _ = TYPES[kind]
+    z, _ = logits_of(rows, vocab, 16, t, masked=0.1)
+    z[::3] = torch.where(torch.arange(vocab, device=gu.DEV) % 2003 < 2, z[::3], torch.tensor(-float("inf"), dtype=t, device=gu.DEV))
+    z[1::6, 5000:9000] = 2.5
+    t64, tokens = tokens_of(rows, vocab, 17)
+    check_forward(vocab, run(dtype, z, tokens, vocab, top), ops.token_logprob(f64(z), t64, top), top)
