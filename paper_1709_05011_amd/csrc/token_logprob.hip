@@ -1,7 +1,7 @@
 // Log probabilities of given tokens over a vocabulary, with entropy and the likeliest alternatives, and the gradient, for gfx950.
 //
 // Per row of logits z: m = max z, S = sum e^(z-m), T = sum e^(z-m) (z-m); lse = m + log S, log p = z - m - log S, entropy = log S - T/S.
-// Bound by memory: the logits are read once, 16 bytes a lane at any alignment; 4096 rows of 32000 bf16 take 51 us, 5.1 TB/s (a value's four or five instructions and its
+// Bound by memory: the logits are read once, 16 bytes a lane at any alignment; 4096 rows of 32768 bf16 take 51 us, 5.2 TB/s (a value's four or five instructions and its
 // exponential, at a quarter of their rate, are 30 us by themselves).  A wave takes 1024 values a round into registers, so that a round's maximum is known before its first
 // exponential and the running maximum rescales once a round; the waves of a row are one block, whose first joins what the others leave, or, of few long rows, blocks that a second
 // launch joins.  Few rows are bound by latency: one row of 131072 with 20 alternatives takes 5.7 us and 4.5 us for the join, of which 2.5 each are a launch.
@@ -10,7 +10,7 @@
 // lower: equal values by rising place), all different.  A lower bound on the N-th largest of a slice comes from the lanes' own maxima -- N lanes
 // have one at least as large -- found by halving over their order with a ballot a step; what reaches it, a few more than N as a
 // rule, is gathered in LDS and ranked.  More than LDS has room for (many equal values): the bound is raised by halving over
-// the keys themselves, which ends, as no two are equal.
+// the keys themselves, which ends, as no two are equal, and takes many looks (2048 rows of 32000 equal logits with 5 alternatives 5.7 ms instead of 31 us, one of 131072 225 instead of 9).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -488,24 +488,28 @@ constexpr float kLseEnd = sizeof(T) == 2 ? 16384.f : 256.f;
 
 // Such a row's gradient, by one wave: its sums again, then all of it (dz may be the logits' own buffer: no other wave writes to the row).
 template <typename T>
-__device__ __attribute__((noinline)) void far_row(const T* z, T* out, int vocab, int token, float a, float b, float ent) {
-    const float3 w = sums_by_distances<512, false>(z, vocab, 0, 512, vocab);
+__device__ __forceinline__ void far_row(const TokenBwdArgs& p, long long row) {
+    const T* z = static_cast<const T*>(p.z) + row * p.ld;
+    T* out = static_cast<T*>(p.dz) + row * p.dld;
+    const int token = p.tokens[row];
+    const float a = p.dlogprob && token >= 0 && token < p.vocab ? p.dlogprob[row] : 0.f, b = p.dentropy ? p.dentropy[row] : 0.f, ent = p.dentropy ? p.entropy[row] : 0.f;
+    const float3 w = sums_by_distances<512, false>(z, p.vocab, 0, 512, p.vocab);
     const float log_s = logf(w.y);
-    for (int col = threadIdx.x * 8; col < vocab; col += 512) {
+    for (int col = threadIdx.x * 8; col < p.vocab; col += 512) {
         Packed<T> v;
-        lc_load8(v, z, col, vocab);
+        lc_load8(v, z, col, p.vocab);
         float o[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const float d = (v.get(j) - w.x) - log_s;
             o[j] = (col + j == token ? a : 0.f) - __builtin_amdgcn_exp2f(d * kLog2e) * (a + b * (fmaxf(d, kFar) + ent));
         }
-        lc_store8(out + col, o, vocab - col);
+        lc_store8(out + col, o, p.vocab - col);
     }
 }
 
 // One wave a block, CH times eight columns a lane.  With d = (z - lse) log2 e the result is 2^d (A + B d): a fused multiply-add, an exponential, another multiply-add and
-// a product a value, the token's own term apart.  Bound by memory: 4096 rows of 32000 bf16 85 us, 6.2 TB/s of what it must read and write.  The results go past the caches (forward
+// a product a value, the token's own term apart.  Bound by memory: 4096 rows of 32768 bf16 85 us, 6.4 TB/s of what it must read and write.  The results go past the caches (forward
 // and backward together 135 us, with ordinary stores 152); 16 columns a lane (8: 1 % slower there, 3 % at 256 rows, 5 % faster at 1024).  Rows from the last to the first, as the
 // memory-side cache would hold those the forward pass has just read, are no better: 3000 rows of 32000 fp32 218 us instead of 205, 2048 of 50000 227 instead of 241.
 template <typename T, int CH>
@@ -513,21 +517,21 @@ __global__ void __launch_bounds__(64) token_bwd_kernel(const TokenBwdArgs p) {
     const int lane = threadIdx.x, first = blockIdx.x * 512 * CH;
     const auto column = [&](int i) { return first + (i * 64 + lane) * 8; };
     const bool full = first + 512 * CH <= p.vocab;
+    const auto is_far = [](float lse) { return fabsf(lse) > kLseEnd<T> && lse != -INFINITY; };
+    bool far = false;
     for (long long row = blockIdx.y; row < p.rows; row += gridDim.y) {
         const T* z = static_cast<const T*>(p.z) + row * p.ld;
         T* out = static_cast<T*>(p.dz) + row * p.dld;
         Packed<T> v[CH];
         lc_issue8(v, z, column, p.vocab, full);
-        const float lse = p.lse[row];
+        const float lse = p.lse[row], da = p.dlogprob ? p.dlogprob[row] : 0.f, db = p.dentropy ? p.dentropy[row] : 0.f, ent = p.dentropy ? p.entropy[row] : 0.f;
         const int token = p.tokens[row];
-        const bool empty = lse == -INFINITY, counts = token >= 0 && token < p.vocab;
-        const float a = p.dlogprob && counts && !empty ? p.dlogprob[row] : 0.f;
-        const float b = p.dentropy && !empty ? p.dentropy[row] : 0.f;
-        const float ent = p.dentropy ? p.entropy[row] : 0.f;
-        if (fabsf(lse) > kLseEnd<T> && !empty) {
-            if (blockIdx.x == 0) far_row(z, out, p.vocab, token, a, b, ent);
+        if (is_far(lse)) {
+            far = true;
             continue;
         }
+        const bool empty = lse == -INFINITY, counts = token >= 0 && token < p.vocab;
+        const float a = counts && !empty ? da : 0.f, b = empty ? 0.f : db;
         lc_settle8(v, column, p.vocab, p.vocab, full);
         // (as in the forward pass: every exponent is off by what rounding the product takes, which goes into the factors)
         const float less = -lse * kLog2e, off = fmaf(lse, kLog2e, less), scale = -__builtin_amdgcn_exp2f(-off);
@@ -556,6 +560,9 @@ __global__ void __launch_bounds__(64) token_bwd_kernel(const TokenBwdArgs p) {
             lc_store8<true>(out + col, o, full ? 8 : p.vocab - col);
         }
     }
+    if (far && blockIdx.x == 0)                  // (behind the others: their loop has more registers so, and waits for nothing but what it has asked for at once)
+        for (long long row = blockIdx.y; row < p.rows; row += gridDim.y)
+            if (is_far(p.lse[row])) far_row<T>(p, row);
 }
 
 constexpr int kMostWidth = 1 << 30;
@@ -566,7 +573,7 @@ lc_status check_desc(const lc_token_desc* d) {
     if (d->dtype != LC_F32 && d->dtype != LC_BF16) return LC_ERR_UNSUPPORTED;
     if (d->rows < 0 || d->vocab <= 0 || d->vocab > kMostWidth || (d->ld && d->ld < d->vocab)) return LC_ERR_SHAPE;
     if (d->top < 0 || d->top > kMostTop) return LC_ERR_UNSUPPORTED;
-    long long bytes;          // every offset in bytes, the workspace's (at most 260 for 512 logits) among them, fits 63 bits
+    long long bytes;          // every offset in bytes, the workspace's (at most 272 for 512 logits) among them, fits 63 bits
     if (__builtin_mul_overflow((long long)d->rows, std::max<long long>({d->ld, d->vocab, 512}), &bytes) || __builtin_mul_overflow(bytes, 8ll, &bytes))
         return LC_ERR_SHAPE;
     return LC_OK;
@@ -580,10 +587,15 @@ struct TokenPlan {
 constexpr int kResident = 4096;      // waves that the chip holds at a time, 16 a compute unit
 
 // Waves of a row.  As a rule they are one block, which joins them itself: a second launch costs 3 us or more.  Too few leave the chip idle, and with more than it holds at
-// once the last of them are too few.  us for bf16 rows by waves a row, or waves of a block x blocks:
+// once the last of them are too few.  us for bf16 rows by waves a row, or waves of a block x blocks (where both sides are within a tenth the rule takes one for all types and numbers of
+// alternatives: 8 waves for 1024 rows of 32000, as longer rows and more of them have; with alternatives blocks from 48 thousand columns on up to 128 rows):
 //   without alternatives           16 waves   8 waves   4 waves   1 wave    in blocks of one
 //     64 rows of 131072              10.7       12.3        -       57         9.0 (32)
-//     128 rows of 131072             11.1       12.6        -       57        11.5 (32)
+//     96 rows of 131072              11.1        -          -       -         10.4 (42)
+//     128 rows of 131072             11.6       12.8        -       57        12.4 (32)
+//     112 rows of 200000             16.0        -          -       -         14.5 (36)
+//     128 rows of 200000             16.0        -          -       -         16.4 (32)
+//     256 rows of 131072             14.4       13.9        -       -         17.7 (32)
 //     256 rows of 32000               6.1        6.1       7.2      17         9.3 (8)
 //     1024 rows of 32000             18         15.0      14.0      18.5      17.7 (4)
 //     4096 rows of 32000             68         51.2      51.6      53.8      53.4 (8)
@@ -592,6 +604,11 @@ constexpr int kResident = 4096;      // waves that the chip holds at a time, 16 
 //   with 20 alternatives                       8 waves   4 waves   2 waves   1 wave      in blocks of one
 //     1 row of 32000                            12.0      12.8       -        22           11.0 (32)
 //     64 rows of 131072                         22.5       -         -         -           16.0 (64), 16.5 (32)
+//     64 rows of 50000                          16.1      18         -         -           14.4 (25)         (with 5 alternatives 13.0, in blocks 13.8)
+//     96 rows of 50000                          16.4       -         -         -           15.9 (17)         (with 5 13.1 and 14.6, fp32 14.7 and 14.0)
+//     128 rows of 65536                         17.5       -         -         -           16.7 (16)         (with 5 14.7 and 15.7)
+//     128 rows of 98304                         18.6       -         -         -           18.0 (14)
+//     160 rows of 131072                        25.1      32.8       -         -           22.2 (16), 26.0 (32)
 //     400 rows of 16000                         16.2      12.9      16.1      16.8         17.4 (4)
 //     400 rows of 131072                        33.2      37.6       -         -           36.8 (16)
 //     700 rows of 131072                        54.3      46.9       -         -           50.5 (4)
