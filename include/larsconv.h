@@ -406,7 +406,7 @@ typedef struct {
  * tokens: DEVICE, rows int32 values; a token outside [0, vocab) marks a position that does not count: logprob 0.
  * top_tokens, top_logprobs: [rows][top], the top largest logits in falling order, equal ones by rising token, with their log
  * probabilities; both NULL if and only if top is 0.  Masked logits are -infinity: probability 0, no part in the entropy, never listed
- * (places left over hold token -1 and -infinity).  A row whose logits are all masked has lse -infinity, entropy 0, logprob -infinity
+ * (places left over hold token -1 and -infinity).  Rows with more than 256 equal logits where the list ends are right and slow (131072 of them 225 us instead of 9).  A row whose logits are all masked has lse -infinity, entropy 0, logprob -infinity
  * (0 where the token does not count).  A row with a NaN or +infinity has NaN in lse, entropy and log probabilities (a NaN is never listed).
  * A finite mask (-1e9, the type's lowest value) is a logit like any other: probability 0 beside ordinary ones.
  * logprob, entropy, lse: rows floats each; entropy may be NULL, and lse where no backward pass follows.  Sums are
@@ -435,7 +435,7 @@ lc_status token_logprob_bwd(const lc_token_desc* desc, const void* logits, const
  * is rounded by itself (no fused multiply-add), so that any fp32 program gets their bits.  The betas are double because 1 - beta is what matters: in
  * [0, 1); eps > 0; step >= 1 -- LC_ERR_UNSUPPORTED otherwise.  n_tensors = 0 is a no-op.  No workspace; results do not depend on the other
  * tensors of the list.  Host arrays are read during the call and travel as launch arguments, lr and step with them: a captured graph
- * replays the step of the capture. */
+ * replays the step of the capture (and, below, its seed: each replay rounds an element's v by the same bits, so that its mean is not kept over replays). */
 lc_status adamw_step(int n_tensors, float* const* w, const void* const* g, lc_dtype g_dtype, float* const* m, float* const* v,
                      const int64_t* numel, float lr, double beta1, double beta2, float eps, float weight_decay, int64_t step,
                      const float* weight_decay_per_tensor, const float* grad_scale, void* const* w_lowp_out, void* hip_stream);

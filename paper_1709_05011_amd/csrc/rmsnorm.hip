@@ -142,7 +142,7 @@ __device__ __forceinline__ void store8_e4m3(uint8_t* p, const float* g, const fl
 
 // A block per row (rows dealt round the grid), its waves as many as the row has 512 * CH columns: all of a row's loads are under way at once and it is read once.  What bounds it is
 // memory: 8192 rows of 4096 bf16 with the residual, its sum and the output 45.5 us, 5.9 TB/s of the 268 MB that must move; 4099 rows of 5120 with residual and sum to 8 bits with a scale per 128
-// 28.9 us, 5.1 TB/s; one row 2.6 us, a launch.  NT: past the caches.  ENDS: what may lie past a row's end, so that rows of whole waves carry no comparisons.  LANES: several narrow rows
+// 28.9 us, 5.1 TB/s; one row 2.8 us, a launch.  NT: past the caches.  ENDS: what may lie past a row's end, so that rows of whole waves carry no comparisons.  LANES: several narrow rows
 // of a wave instead (2^18 rows of 128 bf16 26 us, 5.1 TB/s).
 template <typename T, int CH, bool Q8, bool NT, Ends ENDS, int LANES = 0>
 __global__ void __launch_bounds__(LANES ? kNarrowThreads : kMostWaves * 64) rmsnorm_fwd_kernel(const NormArgs p) {
@@ -376,7 +376,7 @@ struct NormBwdArgs {
 };
 
 // A block walks rows blockIdx, blockIdx + gridDim, ...; a thread's columns stay the same, so that its share of dgamma stays in registers and no atomics are needed, and the next row's loads
-// are under way while one is summed.  Bound by memory: 8192 rows of 4096 bf16 with three inputs and dx 43 us, 6.2 TB/s; 1003 rows of 1537 fp32 7 us, of which the launch and the
+// are under way while one is summed.  Bound by memory: 8192 rows of 4096 bf16 with three inputs and dx 43 us, 6.2 TB/s; 1003 rows of 1537 fp32 7 to 8 us, of which the launch and the
 // latency of four rows one after another are most.
 template <typename T, int CH, bool NT, Ends ENDS, int LANES = 0>
 __global__ void __launch_bounds__(LANES ? kNarrowThreads : kMostWaves * 64) rmsnorm_bwd_kernel(const NormBwdArgs p) {

@@ -509,7 +509,7 @@ __device__ __forceinline__ void far_row(const TokenBwdArgs& p, long long row) {
 }
 
 // One wave a block, CH times eight columns a lane.  With d = (z - lse) log2 e the result is 2^d (A + B d): a fused multiply-add, an exponential, another multiply-add and
-// a product a value, the token's own term apart.  Bound by memory: 4096 rows of 32768 bf16 85 us, 6.4 TB/s of what it must read and write.  The results go past the caches (forward
+// a product a value, the token's own term apart.  Bound by memory: 4096 rows of 32768 bf16 85 us, 6.3 TB/s of what it must read and write.  The results go past the caches (forward
 // and backward together 135 us, with ordinary stores 152); 16 columns a lane (8: 1 % slower there, 3 % at 256 rows, 5 % faster at 1024).  Rows from the last to the first, as the
 // memory-side cache would hold those the forward pass has just read, are no better: 3000 rows of 32000 fp32 218 us instead of 205, 2048 of 50000 227 instead of 241.
 template <typename T, int CH>

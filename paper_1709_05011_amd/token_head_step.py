@@ -154,7 +154,8 @@ class TokenHeadStep:
 
     def score(self, x, residual, tokens, top: int = 0):
         """Log probability and entropy of each row's token (int32; outside the vocabulary: does not count), and the `top` likeliest tokens with
-        theirs.  The tensors returned are this object's buffers: the next call over as many rows writes them again."""
+        theirs.  The tensors returned are this object's buffers: the next call over as many rows writes them again.  (Before load() all logits
+        are equal, and listing alternatives among them is slow.)"""
         self._check(x.shape[0], x=x, residual=residual, tokens=tokens)
         self._follow()
         b = self._buffers(x.shape[0], top)
@@ -165,7 +166,7 @@ class TokenHeadStep:
         """Forward, backward and update.  dlogprob, dentropy: gradient of the loss with respect to each row's log probability and entropy (a mean
         cross-entropy: -1/rows); dtotal: gradient that reaches x + residual by another way; grad_scale: one float on the device, multiplies the
         parameters' gradients.  Returns the rows' log probabilities and entropies and the gradient with respect to x (and to residual),
-        in this object's buffers."""
+        in this object's buffers.  A graph replays the step number of its recording, and with states in 8 bits the rounding of that step."""
         self._check(x.shape[0], x=x, residual=residual, tokens=tokens, dlogprob=dlogprob, dentropy=dentropy, dtotal=dtotal,
                     grad_scale=grad_scale)
         self._follow()
