@@ -392,6 +392,31 @@ size_t rmsnorm_bwd_workspace_bytes(const lc_rmsnorm_desc* desc);
 lc_status rmsnorm_bwd(const lc_rmsnorm_desc* desc, const void* total, int64_t h_ld, const void* dy, const void* dtotal, const float* gamma,
                       const float* save_rstd, void* dx, float* dgamma, void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/* rows x c values; x_ld and residual_ld: elements from one row of x / residual to the next (0: c; otherwise >= c). */
+typedef struct {
+    int64_t rows;
+    int c;            /* at most 2^30 */
+    int64_t x_ld, residual_ld;
+    float eps;        /* >= 0, inside the root */
+    lc_dtype dtype;   /* type of x, residual, total, y and of the gradients dy, dtotal, dx; everything else is fp32 */
+} lc_layernorm_desc;
+
+/* Layer norm with the residual's addition: total = x + residual (rounded to dtype; x where residual is NULL); with the row's mean and its (biased) variance,
+ *     rstd = 1/sqrt(variance + eps),   y = ((total - mean) * rstd) * gamma + beta.
+ * beta may be NULL (no shift).  total, the buffers it may share, and rows that leave fp32's range or hold an infinity or a NaN: as rmsnorm_fwd.  save_mean, save_rstd: rows floats
+ * each for the backward pass, or NULL.  y: [rows][c], contiguous.  Deviations are taken from the mean to more than fp32's places: a mean far from zero costs y none. */
+lc_status layernorm_fwd(const lc_layernorm_desc* desc, const void* x, const void* residual, const float* gamma, const float* beta, void* total,
+                        void* y, float* save_mean, float* save_rstd, void* hip_stream);
+
+/* Gradient: with a = dy * gamma and n = (total - mean) * rstd (total: what the forward pass stored, or its x where there was no residual; h_ld elements from row to row, 0: c),
+ *     dx = rstd * (a - mean of a - n * mean of (a * n)) + dtotal,   dgamma = sum over the rows of dy * n,   dbeta = sum over the rows of dy.
+ * dtotal as in rmsnorm_bwd, or NULL; dbeta may be NULL.  dy, dtotal, dx: [rows][c], contiguous.  n is formed from save_mean as stored (an error of |mean| * rstd * 2^-24).
+ * x_ld and residual_ld of desc are not used.  Buffers must not overlap. */
+size_t layernorm_bwd_workspace_bytes(const lc_layernorm_desc* desc);
+lc_status layernorm_bwd(const lc_layernorm_desc* desc, const void* total, int64_t h_ld, const void* dy, const void* dtotal, const float* gamma,
+                        const float* save_mean, const float* save_rstd, void* dx, float* dgamma, float* dbeta, void* workspace,
+                        size_t workspace_bytes, void* hip_stream);
+
 /* rows x vocab logits, `ld` elements from one row to the next (0: vocab; otherwise >= vocab: a padded vocabulary's pad is not read). */
 typedef struct {
     int64_t rows;

@@ -10,6 +10,7 @@
 #include <algorithm>
 
 #include "internal.h"
+#include "norm_common.h"
 #include "token_common.h"
 
 namespace {
@@ -26,39 +27,6 @@ struct NormArgs {
     int c, group;
     float eps;
     double inv_c;            // 1 / c
-};
-
-constexpr int kMostWaves = 16;
-
-// A value of each wave's own making, joined over a block of `waves` waves, every thread with the result; `red` (a float a wave) must not be in use by an
-// earlier call that a slower wave may still read.
-template <typename W, typename F>
-__device__ __forceinline__ float block_join(float x, int waves, float* red, W&& in_wave, F&& f) {
-    x = in_wave(x);
-    if (waves == 1) return x;
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
-    __syncthreads();
-    float s = red[0];
-    for (int w = 1; w < waves; ++w) s = f(s, red[w]);
-    return s;
-}
-
-// How a block's threads share rows: all of them one row (LANES 0), or LANES neighbouring lanes of a wave each a row (of a block of kNarrowThreads).
-constexpr int kNarrowThreads = 256;
-template <int LANES>
-struct Rows {
-    static constexpr int kEach = LANES ? kNarrowThreads / LANES : 1;     // rows of a block
-    static __device__ __forceinline__ int tid() { return LANES ? threadIdx.x & (LANES - 1) : threadIdx.x; }
-    static __device__ __forceinline__ long long first() { return LANES ? (long long)blockIdx.x * kEach + threadIdx.x / (kNarrowThreads / kEach) : blockIdx.x; }
-    static __device__ __forceinline__ long long step() { return LANES ? (long long)gridDim.x * kEach : gridDim.x; }
-
-    template <typename W, typename F>
-    static __device__ __forceinline__ float join(float v, int waves, float* red, W&& wave, F&& f) {
-        if constexpr (LANES == 0) return block_join(v, waves, red, wave, f);
-#pragma unroll
-        for (int off = 1; off < LANES; off <<= 1) v = f(v, __shfl_xor(v, off, 64));
-        return v;
-    }
 };
 
 constexpr float kE4m3Max = 448.f, kLeastScale = 0x1p-126f;
@@ -511,47 +479,6 @@ __global__ void __launch_bounds__(1024) rmsnorm_bwd_wide_kernel(const NormBwdArg
     }
 }
 
-// dgamma[k] = the blocks' shares added in a fixed order: COLS columns a block, whose 1024 / COLS groups of threads take every so many shares, eight of them under way at a
-// time.  16 columns a block where 64 would leave most of the chip without one (16384 x 256, forward and backward, 29.6 us,
-// so 25.9; from 1537 columns on 64 are as fast or faster).
-constexpr int kNarrow = 1024;
-template <int COLS>
-__global__ void __launch_bounds__(1024) rmsnorm_dgamma_kernel(const float* __restrict__ part, float* __restrict__ dgamma, int parts, int c) {
-    constexpr int U = 8, kGroups = 1024 / COLS;
-    __shared__ float sum[kGroups][COLS];
-    const int column = threadIdx.x & (COLS - 1), group = threadIdx.x / COLS;
-    for (long long at = (long long)blockIdx.x * COLS; at < c; at += (long long)gridDim.x * COLS) {
-        const long long k = at + column;
-        float s[U] = {};
-        if (k < c) {
-            int i = group;
-            for (; i + kGroups * (U - 1) < parts; i += kGroups * U) {
-                float v[U];
-#pragma unroll
-                for (int u = 0; u < U; ++u) v[u] = part[(long long)(i + kGroups * u) * c + k];
-#pragma unroll
-                for (int u = 0; u < U; ++u) s[u] += v[u];
-            }
-#pragma unroll
-            for (int u = 0; u < U - 1; ++u)
-                if (i + kGroups * u < parts) s[u] += part[(long long)(i + kGroups * u) * c + k];
-        }
-        sum[group][column] = ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
-        __syncthreads();
-        if (group == 0 && k < c) {
-            float t[4] = {};
-#pragma unroll
-            for (int w = 0; w < kGroups; ++w) t[w & 3] += sum[w][column];
-            dgamma[k] = (t[0] + t[1]) + (t[2] + t[3]);
-        }
-        __syncthreads();
-    }
-}
-
-constexpr int kMostColumns = 16384;          // what a block's registers hold of a row
-constexpr int kMostWidth = 1 << 30;          // columns are counted in 32 bits, eight past the end among them
-constexpr long long kMostBlocks = 1 << 20;   // rows, or column tiles, beyond are dealt round
-
 lc_status check_desc(const lc_rmsnorm_desc* d) {
     if (!d) return LC_ERR_NULL;
     if (d->dtype != LC_F32 && d->dtype != LC_BF16) return LC_ERR_UNSUPPORTED;
@@ -564,18 +491,6 @@ lc_status check_desc(const lc_rmsnorm_desc* d) {
     return LC_OK;
 }
 
-// Bytes that a call reads and writes from which it goes past the caches, where the row's accesses take whole lines of 128 bytes (bf16; fp32's two halves of
-// eight columns do not: 8192 x 4096 94 us, past the caches 105).  Three sets in turn, us, ordinary / past, c = 4096: 2048 rows (67 MB) 11.8 / 13.7, 3000 (98 MB) 19.9 / 18.9,
-// 4096 (134 MB) 26.2 / 24.2, 8192 47.8 / 45.4.
-constexpr long long kStreamBytes = 96 << 20;
-
-// Columns of a wave by what a thread has in registers: 16 for bf16 (rows under 512 columns 8: 16384 x 256 7.7 us, with 16 9.2; 4099 x 5120 to 8 bits 36.0, with 16 32.2, with 32 34.7), 8 for
-// fp32 (8192 x 4096 94 us, with 16 97), 16 where 16 waves would not do.
-template <typename T>
-int chunks_of(int c) {
-    return sizeof(T) == 2 ? (c <= 512 ? 1 : 2) : (c <= 512 * kMostWaves ? 1 : 2);
-}
-
 template <typename T, int CH, bool Q8, bool NT>
 void launch_fwd(const NormArgs& a, hipStream_t stream) {
     const dim3 grid((unsigned)std::min(a.rows, kMostBlocks)), block((a.c + 512 * CH - 1) / (512 * CH) * 64);
@@ -583,11 +498,6 @@ void launch_fwd(const NormArgs& a, hipStream_t stream) {
     else if (a.c % 8 == 0) hipLaunchKernelGGL((rmsnorm_fwd_kernel<T, CH, Q8, NT, kEights>), grid, block, 0, stream, a);
     else if constexpr (CH * sizeof(T) < 8) hipLaunchKernelGGL((rmsnorm_fwd_kernel<T, CH, Q8, NT, kAny>), grid, block, 0, stream, a);
 }
-// Lanes of a row where a wave takes several, from what a wave of its own per row takes, us, 2^25 elements in all: bf16 forward with c = 64, 128, 256 125, 69, 39, so 26;
-// to 8 bits 216, 119, 65, so 42; forward and backward 250, 140, 88, so 66; fp32 forward 143, 82, 51, so 49.
-constexpr int kMostNarrow = 256;             // columns
-bool narrow(long long rows, int c) { return c <= kMostNarrow && rows > 256; }        // (fewer have a compute unit each; the same to 4096 rows, where a launch is what they take)
-int lanes_of(int c) { return c <= 64 ? 8 : c <= 128 ? 16 : 32; }
 template <typename T, bool Q8, bool NT, int LANES>
 void launch_fwd_narrow(const NormArgs& a, hipStream_t stream) {
     const dim3 grid((unsigned)std::min((a.rows + Rows<LANES>::kEach - 1) / Rows<LANES>::kEach, kMostBlocks)), block(kNarrowThreads);
@@ -599,10 +509,6 @@ void launch_fwd_narrow(const NormArgs& a, hipStream_t stream) {
     const int lanes = lanes_of(a.c);
     lanes == 8 ? launch_fwd_narrow<T, Q8, NT, 8>(a, stream) : lanes == 16 ? launch_fwd_narrow<T, Q8, NT, 16>(a, stream) : launch_fwd_narrow<T, Q8, NT, 32>(a, stream);
 }
-
-// Rows that go by in passes: what a block's registers do not hold (of fp32 rows that end within a thread's columns 16 a thread neither: 3000 x 9001, forward and backward, 317 us, in
-// passes 275), and under eight columns.
-bool in_passes(const lc_dtype dtype, int c) { return c < 8 || c > kMostColumns || (dtype == LC_F32 && c % 8 && c > 512 * kMostWaves); }
 
 template <typename T, bool Q8>
 void launch_fwd(const NormArgs& a, hipStream_t stream) {
@@ -638,20 +544,6 @@ lc_status run_fwd(const lc_rmsnorm_desc* d, const void* x, const void* residual,
     if (d->dtype == LC_BF16) q8 ? launch_fwd<uint16_t, true>(a, stream) : launch_fwd<uint16_t, false>(a, stream);
     else q8 ? launch_fwd<float, true>(a, stream) : launch_fwd<float, false>(a, stream);
     return lc_end_call();
-}
-
-// Blocks of the backward pass, each with a share of dgamma: 16 waves a compute unit, with four rows a block or more as long as every unit has one.  us, 8192 x 4096 bf16 forward and
-// backward with 256, 512, 1024 blocks 110, 96.6, 104; 16384 x 1024 97, 70, 58; 2048 x 16384 105, 114, 128; 512 x 4096 14.8, 16.0, 16.0.  Narrow rows: the same with a wave's several rows
-// for one (2^20 rows of 32 with 512, 1024, 2048 blocks of four waves 97, 83, 88).
-int bwd_chunks(int c) { return c <= 512 * kMostWaves ? 1 : 2; }
-long long bwd_blocks(const lc_rmsnorm_desc* d) {
-    if (in_passes(d->dtype, d->c)) return std::min<long long>(d->rows, 64);
-    if (narrow(d->rows, d->c)) {
-        const long long each = kNarrowThreads / lanes_of(d->c), all = (d->rows + each - 1) / each;
-        return std::min(all, std::max<long long>(256, std::min<long long>(1024, all / 4)));
-    }
-    const int columns = 512 * bwd_chunks(d->c), waves = (d->c + columns - 1) / columns;
-    return std::min<long long>(d->rows, std::max<long long>(256, std::min<long long>(4096 / waves, d->rows / 4)));
 }
 
 template <typename T, int CH, bool NT>
@@ -700,7 +592,7 @@ extern "C" lc_status rmsnorm_fwd_q8(const lc_rmsnorm_desc* desc, const void* x, 
 
 extern "C" size_t rmsnorm_bwd_workspace_bytes(const lc_rmsnorm_desc* desc) {
     if (check_desc(desc) != LC_OK) return 0;
-    return ((size_t)bwd_blocks(desc) * desc->c * sizeof(float) + 255) & ~(size_t)255;
+    return ((size_t)bwd_blocks(desc->dtype, desc->rows, desc->c) * desc->c * sizeof(float) + 255) & ~(size_t)255;
 }
 
 extern "C" lc_status rmsnorm_bwd(const lc_rmsnorm_desc* desc, const void* total, int64_t h_ld, const void* dy, const void* dtotal,
@@ -725,13 +617,11 @@ extern "C" lc_status rmsnorm_bwd(const lc_rmsnorm_desc* desc, const void* total,
         lc_off_element(save_rstd, 4))
         return LC_ERR_ALIGN;
     if (!workspace || (((uintptr_t)workspace) & 255) || workspace_bytes < rmsnorm_bwd_workspace_bytes(desc)) return LC_ERR_WORKSPACE;
-    const int blocks = (int)bwd_blocks(desc);
+    const int blocks = (int)bwd_blocks(desc->dtype, desc->rows, desc->c);
     NormBwdArgs a{total, dy, dtotal, gamma, save_rstd, dx, static_cast<float*>(workspace), desc->rows, h_ld ? h_ld : desc->c, desc->c};
     lc_begin_call();
     if (desc->dtype == LC_BF16) launch_bwd<uint16_t>(a, blocks, stream);
     else launch_bwd<float>(a, blocks, stream);
-    const long long c = desc->c, tiles = std::min(c <= kNarrow ? (c + 15) / 16 : (c + 63) / 64, kMostBlocks);      // (a launch holds fewer than 2^32 threads)
-    if (c <= kNarrow) hipLaunchKernelGGL((rmsnorm_dgamma_kernel<16>), dim3((unsigned)tiles), dim3(1024), 0, stream, a.part, dgamma, blocks, desc->c);
-    else hipLaunchKernelGGL((rmsnorm_dgamma_kernel<64>), dim3((unsigned)tiles), dim3(1024), 0, stream, a.part, dgamma, blocks, desc->c);
+    sum_parts(a.part, dgamma, nullptr, blocks, desc->c, stream);
     return lc_end_call();
 }

@@ -30,6 +30,7 @@ EXPORTS = ["conv2d_out_shape", "conv2d_workspace_bytes", "conv2d_fwd", "conv2d_b
            "global_avgpool_bwd_t", "relu_add_bwd_bnsums_t", "relu_add_bwd_bnsums_grid_t", "batchnorm_bwd_presummed_t",
            "conv2d_fwd_stats_count", "conv2d_fwd_stats", "batchnorm_fwd_pre", "batchnorm_fwd_pair_t",
            "rmsnorm_fwd", "rmsnorm_fwd_q8", "rmsnorm_bwd_workspace_bytes", "rmsnorm_bwd",
+           "layernorm_fwd", "layernorm_bwd_workspace_bytes", "layernorm_bwd",
            "token_logprob_workspace_bytes", "token_logprob_fwd", "token_logprob_bwd",
            "adamw_step", "adamw_step_q8",
            "lc_status_string", "lc_last_error_detail"]
@@ -92,6 +93,23 @@ class RmsNormDesc(_Kept):
 
     def c_struct(self) -> lc_rmsnorm_desc:
         return lc_rmsnorm_desc(self.rows, self.c, self.x_ld, self.residual_ld, self.eps, self.dtype)
+
+
+class lc_layernorm_desc(ctypes.Structure):
+    _fields_ = lc_rmsnorm_desc._fields_
+
+
+@dataclass(frozen=True)
+class LayerNormDesc(_Kept):
+    rows: int
+    c: int
+    x_ld: int = 0
+    residual_ld: int = 0
+    eps: float = 1e-5
+    dtype: int = LC_F32
+
+    def c_struct(self) -> lc_layernorm_desc:
+        return lc_layernorm_desc(self.rows, self.c, self.x_ld, self.residual_ld, self.eps, self.dtype)
 
 
 class lc_token_desc(ctypes.Structure):
@@ -215,6 +233,13 @@ def lib() -> ctypes.CDLL:
         L.rmsnorm_bwd_workspace_bytes.argtypes = [rp]
         L.rmsnorm_bwd.restype = i32
         L.rmsnorm_bwd.argtypes = [rp, vp, ctypes.c_int64, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        np_ = ctypes.POINTER(lc_layernorm_desc)
+        L.layernorm_fwd.restype = i32
+        L.layernorm_fwd.argtypes = [np_, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+        L.layernorm_bwd_workspace_bytes.restype = sz
+        L.layernorm_bwd_workspace_bytes.argtypes = [np_]
+        L.layernorm_bwd.restype = i32
+        L.layernorm_bwd.argtypes = [np_, vp, ctypes.c_int64, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         tp = ctypes.POINTER(lc_token_desc)
         L.token_logprob_workspace_bytes.restype = sz
         L.token_logprob_workspace_bytes.argtypes = [tp]
@@ -634,6 +659,24 @@ def rmsnorm_bwd(desc, total, dy, dtotal, gamma, save_rstd, dx, dgamma, workspace
     nb = _nbytes(workspace) if workspace_bytes is None else workspace_bytes
     _check(lib().rmsnorm_bwd(_c(desc), _ptr(total), h_ld, _ptr(dy), _ptr(dtotal), _ptr(gamma), _ptr(save_rstd), _ptr(dx),
                              _ptr(dgamma), _ptr(workspace), nb, _stream(stream)), "rmsnorm_bwd")
+
+
+# ---- layer norm with the residual's addition ----
+
+def layernorm_fwd(desc, x, residual, gamma, beta, total, y, save_mean=None, save_rstd=None, stream=None) -> None:
+    _check(lib().layernorm_fwd(_c(desc), _ptr(x), _ptr(residual), _ptr(gamma), _ptr(beta), _ptr(total), _ptr(y), _ptr(save_mean), _ptr(save_rstd),
+                               _stream(stream)), "layernorm_fwd")
+
+
+def layernorm_bwd_workspace_bytes(desc) -> int:
+    return int(lib().layernorm_bwd_workspace_bytes(_c(desc)))
+
+
+def layernorm_bwd(desc, total, dy, dtotal, gamma, save_mean, save_rstd, dx, dgamma, dbeta=None, workspace=None, h_ld: int = 0, stream=None,
+                  workspace_bytes: Optional[int] = None) -> None:
+    nb = _nbytes(workspace) if workspace_bytes is None else workspace_bytes
+    _check(lib().layernorm_bwd(_c(desc), _ptr(total), h_ld, _ptr(dy), _ptr(dtotal), _ptr(gamma), _ptr(save_mean), _ptr(save_rstd), _ptr(dx),
+                               _ptr(dgamma), _ptr(dbeta), _ptr(workspace), nb, _stream(stream)), "layernorm_bwd")
 
 
 # ---- log probabilities of given tokens, entropy, likeliest alternatives ----
