@@ -480,6 +480,39 @@ lc_status adamw_step_q8(int n_tensors, float* const* w, const void* const* g, lc
                         float weight_decay, int64_t step, uint32_t seed, const float* weight_decay_per_tensor, const float* grad_scale,
                         void* const* w_lowp_out, void* hip_stream);
 
+/* ---- Orthogonalised updates ----
+ * Newton-Schulz steps on a matrix X of rows x cols: X <- X / (|X| + eps) with the root of the sum of its squares, then `iterations` (1 to 64) times
+ *     A = X X^T,   X <- 3.4445 X + (-4.7750 A + 2.0315 A A) X
+ * on its shorter side: singular values s go through 3.4445 s - 4.7750 s^3 + 2.0315 s^5 and come, but for the smallest, to between 0.68 and 1.14 after five.  Values between the products
+ * are pairs of fp16 (22 bits) and sums fp32: results are as near as with fp32 products.  A matrix of zeros stays zero; one that holds an infinity or a NaN becomes NaN.  Values under 2^-36 of
+ * the normalised matrix are lost.  Sums run in a fixed order.  Sides are at most 65536.  The host prepares lists of matrices in memory of its own during the call (LC_ERR_SHAPE where that does not fit). */
+typedef struct {
+    int batch;        /* matrices, one after another: of x every rows * ld elements, of y every rows * cols */
+    int rows, cols;
+    int64_t ld;       /* elements from one row of x to the next (0: cols; otherwise >= cols) */
+    int iterations;
+    float eps;        /* >= 0 */
+    lc_dtype dtype;   /* type of x and y */
+} lc_newton_schulz_desc;
+
+/* y = the steps' result for each matrix of x.  y: contiguous; it may be x's own buffer where that is contiguous.  Alignment: one element. */
+size_t newton_schulz_workspace_bytes(const lc_newton_schulz_desc* desc);
+lc_status newton_schulz(const lc_newton_schulz_desc* desc, const void* x, void* y, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* One optimizer step over a list of matrices: with g' = grad_scale * g,
+ *     m <- momentum m + g',   u = g' + momentum m (nesterov) or m,   w <- w - lr * decay * w - lr * scale * O(u),
+ * O(u) the steps' result above.  w, m: HOST arrays of n_tensors DEVICE pointers to fp32 data of rows[i] x cols[i] (HOST arrays; contiguous), updated in place; g: pointers to gradients of
+ * type g_dtype, read only.  A filter of a convolution is a matrix of k rows and c*r*s columns.  scale_per_tensor: HOST array, or NULL for sqrt(max(1, rows / cols)).
+ * weight_decay_per_tensor, grad_scale, w_lowp_out: as adamw_step.  momentum in [0, 1), eps >= 0, iterations 1 to 64 -- LC_ERR_UNSUPPORTED otherwise.  A side of 0 is an empty tensor, n_tensors = 0 a
+ * no-op.  Tensors must not overlap.  Host arrays are read during the call and travel as launch arguments.  Results do not depend on the other tensors of the list.
+ * Matrices go through the steps in groups that share the workspace: at most 64 and, but for a single larger one, 2 GiB at a time (12 bytes for each value, 8 for each of the
+ * square of the shorter side, sides counted in multiples of 32). */
+size_t muon_workspace_bytes(int n_tensors, const int* rows, const int* cols);
+lc_status muon_step(int n_tensors, float* const* w, const void* const* g, lc_dtype g_dtype, float* const* m, const int* rows, const int* cols, float lr,
+                    float momentum, int nesterov, float weight_decay, int iterations, float eps, const float* scale_per_tensor,
+                    const float* weight_decay_per_tensor, const float* grad_scale, void* const* w_lowp_out, void* workspace, size_t workspace_bytes,
+                    void* hip_stream);
+
 /* Static, human-readable name of a status code. */
 const char* lc_status_string(lc_status status);
 

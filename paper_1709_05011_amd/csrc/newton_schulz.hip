@@ -1,0 +1,631 @@
+// Newton-Schulz steps that orthogonalise matrices, and the optimizer's step around them (momentum, orthogonalised update, decay), for gfx950.
+//
+// X = u / (|u| + eps), then `iterations` times X <- a X + (b A + c A A) X with A = X X^T on the shorter side: the singular values go through a x + b x^3 + c x^5, which takes all but the
+// smallest near 1.  Three products a step, A and B = b A + c A A symmetric: of those only tiles on and below the diagonal are made and written twice.
+//
+// Values are pairs of fp16, hi = x rounded, lo = (x - hi) rounded, 22 bits, scaled by 2^12: singular values stay below 1.21, hence every value of X below 1.21, of A below 1.46 and of B below 2.81,
+// and fp16's range leaves room for five times that; a product is three matrix instructions, lo hi + hi lo + hi hi, summed in fp32.  One fp16 (or bf16) value each, a third of the instructions, was simulated in 64 bits and
+// left: small singular values grow by up to 3.4445 a step, and the first rounding with them: errors of 1.4e-3 (bf16 1.3e-2) on a random matrix and 1.4e-2 (0.11) on one of rank 8 and noise, pairs 3e-7 to 3e-6, fp32 products
+// 1e-6 to 6e-5.
+//
+// In memory a matrix is [row][32 columns: 32 hi, 32 lo], sides filled up with zeros to multiples of 32: a k-step of 32 is 128 bytes of a row, a whole line, and LDS holds it as the bf16 products of conv_dma.h do.  X is
+// kept both ways round, so that all three products read rows along their sum.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <cmath>
+#include <type_traits>
+#include <vector>
+
+#include "dma_common.h"
+#include "internal.h"
+#include "token_common.h"
+
+namespace {
+
+constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
+constexpr float kScale = 4096.f, kInvScale = 1.f / 4096.f;
+constexpr int kPad = 32;                           // sides in memory are multiples of it
+constexpr int kMostParts = 1024;                   // sums of squares of a matrix
+constexpr int kTable = 64, kSmallTable = 8;        // matrices of a launch
+
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+struct Mat {
+    const void* in;          // gradient, or the matrix itself
+    float* m;                // momentum; null: no optimizer's step
+    float* w;
+    void* out;               // bf16 copy of w or null; the result
+    long long ld;            // of in
+    int rows, cols;
+    int M, N;                // sides in memory, M <= N
+    int tall;                // rows > cols: X is the transpose
+    int chunk;               // vectors of four that a block sums the squares of
+    unsigned char* base;     // its part of the workspace
+    float step, lr_decay;    // lr * scale, lr * decay
+    __host__ __device__ long long side() const { return (long long)M * N * 4; }
+    __host__ __device__ unsigned char* x() const { return base + kMostParts * 8; }
+    __host__ __device__ unsigned char* xt(int which) const { return x() + (1 + which) * side(); }
+    __host__ __device__ unsigned char* a() const { return x() + 3 * side(); }
+    __host__ __device__ unsigned char* b() const { return a() + (long long)M * M * 4; }
+};
+
+struct Scalars {
+    int count;
+    const float* grad_scale;
+    float momentum, eps;
+    int nesterov;
+    int which;               // of the two transposes, the one that is read
+};
+
+template <int TABLE>
+struct Args {
+    Mat t[TABLE];
+    int start[(TABLE + 63) / 64 * 64];   // first block of each, past the last the largest int
+    Scalars s;
+};
+
+// The matrix that a block belongs to (the same for the block) and the block's number within it.
+template <int TABLE>
+__device__ __forceinline__ int owner_of(const Args<TABLE>& args, int bid, int* local) {
+    const int lane = threadIdx.x & 63;
+    const int owner = __builtin_amdgcn_readfirstlane(__popcll(__ballot(args.start[lane] <= bid)) - 1);
+    *local = bid - args.start[owner];
+    return owner;
+}
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef u32x2 u32x2_any __attribute__((aligned(2)));
+__device__ __forceinline__ void load4(float* to, const float* p, int n) {
+    if (n >= 4) {
+        const lc_u32x4 x = lc_load16(p);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) to[j] = __uint_as_float(x[j]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) to[j] = j < n ? p[j] : 0.f;
+    }
+}
+__device__ __forceinline__ void load4(float* to, const uint16_t* p, int n) {
+    u32x2 x = {0u, 0u};
+    if (n >= 4) {
+        x = *reinterpret_cast<const u32x2_any*>(p);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (j < n) x[j >> 1] |= (uint32_t)p[j] << (16 * (j & 1));
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) to[j] = __uint_as_float(j & 1 ? x[j >> 1] & 0xffff0000u : x[j >> 1] << 16);
+}
+
+// The momentum's update and the sum of squares, in double, of what is orthogonalised: one block a chunk.
+template <typename T, bool MUON, int TABLE>
+__global__ void __launch_bounds__(256) ns_squares_kernel(const Args<TABLE> args) {
+    __shared__ double red[4];
+    int part;
+    const Mat& t = args.t[owner_of(args, blockIdx.x, &part)];
+    const unsigned per_row = MUON ? 0u : (unsigned)((t.cols + 3) / 4);
+    const long long all = MUON ? ((long long)t.rows * t.cols + 3) / 4 : (long long)t.rows * per_row;
+    const long long end = std::min(all, (long long)(part + 1) * t.chunk);
+    const float gs = args.s.grad_scale ? *args.s.grad_scale : 1.f, mu = args.s.momentum;
+    double sum = 0.0;
+    for (long long v = (long long)part * t.chunk + threadIdx.x; v < end; v += 256) {
+        float u[4];
+        if constexpr (MUON) {
+            float m[4];
+            const long long at = v * 4, left = (long long)t.rows * t.cols - at;
+            const int n = (int)std::min(left, 4ll);
+            load4(u, static_cast<const T*>(t.in) + at, n);
+            load4(m, t.m + at, n);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float g = u[j] * gs;
+                m[j] = fmaf(mu, m[j], g);
+                u[j] = args.s.nesterov ? fmaf(mu, m[j], g) : m[j];
+            }
+            if (n == 4) {
+                lc_store16(t.m + at, lc_u32x4{__float_as_uint(m[0]), __float_as_uint(m[1]), __float_as_uint(m[2]), __float_as_uint(m[3])});
+            } else {
+                for (int j = 0; j < 4; ++j)
+                    if (j < n) t.m[at + j] = m[j];
+            }
+        } else {
+            const unsigned row = (unsigned)v / per_row, col = ((unsigned)v - row * per_row) * 4;
+            load4(u, static_cast<const T*>(t.in) + (long long)row * t.ld + col, t.cols - (int)col);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sum = fma((double)u[j], (double)u[j], sum);
+    }
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) reinterpret_cast<double*>(t.base)[part] = (red[0] + red[1]) + (red[2] + red[3]);
+}
+
+// Eight scaled values as pairs: hi in the first 16 bytes' place, lo 64 bytes behind.
+__device__ __forceinline__ void store_pairs(unsigned char* p, const float* v) {
+    f16x8 hi, lo;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        hi[j] = (_Float16)v[j];
+        lo[j] = (_Float16)(v[j] - (float)hi[j]);
+    }
+    *reinterpret_cast<f16x8*>(p) = hi;
+    *reinterpret_cast<f16x8*>(p + 64) = lo;
+}
+__device__ __forceinline__ void load_pairs(float* v, const unsigned char* p) {
+    const f16x8 hi = *reinterpret_cast<const f16x8*>(p), lo = *reinterpret_cast<const f16x8*>(p + 64);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = (float)hi[j] + (float)lo[j];
+}
+// Byte of element (row, col) of a matrix with `k` columns in memory, col a multiple of 8.
+__device__ __forceinline__ long long pair_at(long long row, int col, int k) { return row * k * 4 + (col >> 5) * 128 + (col & 31) * 2; }
+
+// u / (|u| + eps) as pairs, both ways round: a block 64 x 64 values.
+template <typename T, bool MUON, int TABLE>
+__global__ void __launch_bounds__(256) ns_split_kernel(const Args<TABLE> args) {
+    __shared__ double red[4];
+    __shared__ float tile[64][65];
+    int local;
+    const Mat& t = args.t[owner_of(args, blockIdx.x, &local)];
+    const int tid = threadIdx.x;
+    const int prows = t.tall ? t.N : t.M, pcols = t.tall ? t.M : t.N;           // sides in memory as the matrix lies
+    const int across = (pcols + 63) / 64, r0 = local / across * 64, c0 = local % across * 64;
+    const float gs = args.s.grad_scale ? *args.s.grad_scale : 1.f, mu = args.s.momentum;
+    float u[4][4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int row = r0 + (tid >> 4) + 16 * k, col = c0 + 4 * (tid & 15);
+        const int n = row < t.rows ? t.cols - col : 0;
+        load4(u[k], static_cast<const T*>(t.in) + (n > 0 ? (long long)row * t.ld + col : 0), n);
+        if constexpr (MUON) {
+            float m[4];
+            load4(m, t.m + (n > 0 ? (long long)row * t.cols + col : 0), n);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) u[k][j] = args.s.nesterov ? fmaf(mu, m[j], u[k][j] * gs) : m[j];
+        }
+    }
+    const long long vectors = MUON ? ((long long)t.rows * t.cols + 3) / 4 : (long long)t.rows * ((t.cols + 3) / 4);
+    const int parts = (int)((vectors + t.chunk - 1) / t.chunk);
+    double sum = 0.0;
+    for (int i = tid; i < parts; i += 256) sum += reinterpret_cast<const double*>(t.base)[i];
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
+    if ((tid & 63) == 0) red[tid >> 6] = sum;
+    __syncthreads();
+    sum = (red[0] + red[1]) + (red[2] + red[3]);
+    const double norm = sqrt(sum) + (double)args.s.eps, inv = sum == 0.0 ? 0.0 : (double)kScale / norm;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) tile[(tid >> 4) + 16 * k][4 * (tid & 15) + j] = (float)((double)u[k][j] * inv);
+    __syncthreads();
+    unsigned char* const along = t.tall ? t.xt(0) : t.x();
+    unsigned char* const turned = t.tall ? t.x() : t.xt(0);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int line = (tid >> 3) + 32 * k, run = (tid & 7) * 8;
+        float v[8];
+        if (r0 + line < prows && c0 + run < pcols) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = tile[line][run + j];
+            store_pairs(along + pair_at(r0 + line, c0 + run, pcols), v);
+        }
+        if (c0 + line < pcols && r0 + run < prows) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = tile[run + j][line];
+            store_pairs(turned + pair_at(c0 + line, r0 + run, prows), v);
+        }
+    }
+}
+
+// What a product makes: A = X X^T; B = b A + c A A; X <- a X + B X, both ways round; the same as the result.
+enum Product { kGram, kSquare, kNext, kLast };
+
+template <Product KIND>
+__host__ __device__ inline int tiles_of(const Mat& t, int BM, int BN) {
+    const int nm = (t.M + BM - 1) / BM, nn = (t.N + BN - 1) / BN;
+    return KIND <= kSquare ? nm * (nm + 1) / 2 : nm * nn;
+}
+
+__device__ __forceinline__ f32x4 multiply(const f16x8& a, const f16x8& b, const f32x4& c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+
+// Rows P[i] times rows Q[j] along their sum.  A block has WM x WN waves of 16 TM x 16 TN values each; NS stages of LDS, the next ones arriving while one is multiplied.
+template <Product KIND, bool MUON, typename T, int TM, int TN, int WM, int WN, int NS, int TABLE>
+__global__ void __launch_bounds__(WM * WN * 64, 2) ns_product_kernel(const Args<TABLE> args) {
+    constexpr int BM = 16 * TM * WM, BN = 16 * TN * WN, NW = WM * WN;
+    constexpr int LP = BM / 8 / NW, LQ = BN / 8 / NW;              // loads of a wave a stage
+    constexpr int STAGE = (BM + BN) * 128;
+    constexpr int kPitch = TN * 16 + 4;                           // floats
+    static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && NW % 2 == 0, "tile shape");
+    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave / WN, wn = wave % WN;
+    int local;
+    const Mat& t = args.t[owner_of(args, xcd_tile(blockIdx.x, gridDim.x), &local)];
+    const int M = t.M, N = t.N;
+    int ti, tj;
+    if constexpr (KIND <= kSquare) {
+        ti = (int)((sqrtf(8.f * (float)local + 1.f) - 1.f) * 0.5f);
+        while ((ti + 1) * (ti + 2) / 2 <= local) ++ti;
+        while (ti * (ti + 1) / 2 > local) --ti;
+        tj = local - ti * (ti + 1) / 2;
+    } else {
+        const int across = (N + BN - 1) / BN;
+        ti = local / across;
+        tj = local - ti * across;
+    }
+    ti = __builtin_amdgcn_readfirstlane(ti);
+    tj = __builtin_amdgcn_readfirstlane(tj);
+    const int i0 = ti * BM, j0 = tj * BN;
+    const int K = KIND == kGram ? N : M, rowsQ = KIND <= kSquare ? M : N;
+    const unsigned pitch = (unsigned)K * 4u;
+    const unsigned char* const P = KIND == kGram ? t.x() : KIND == kSquare ? t.a() : t.b();
+    const unsigned char* const Q = KIND == kGram ? t.x() : KIND == kSquare ? t.a() : t.xt(args.s.which);
+    // rows past the matrix lie past the end of the buffer: zeros
+    const u32x4 p_rsrc = buffer_words(P + (long long)i0 * pitch, (unsigned)std::min(BM, M - i0) * pitch);
+    const u32x4 q_rsrc = buffer_words(Q + (long long)j0 * pitch, (unsigned)std::min(BN, rowsQ - j0) * pitch);
+    const int lrow = lane >> 3, piece = (lane & 7) ^ (((wave & 1) * 4 + (lrow >> 1)) & 7);
+    const unsigned voff = (unsigned)(wave * 8 + lrow) * pitch + piece * 16;
+    const unsigned lds0 = lds_address(smem);
+    const int steps = K / 32;
+    const auto load = [&](int k, int stage) __attribute__((always_inline)) {
+        const unsigned past = k < steps ? 0u : kBufferBytes;       // (behind the last step the loads fetch nothing, and their number stays the same)
+#pragma unroll
+        for (int l = 0; l < LP; ++l) load_to_lds(p_rsrc, (voff + (unsigned)(l * NW * 8) * pitch) | past, k * 128, lds0 + stage * STAGE + (l * NW + wave) * 1024);
+#pragma unroll
+        for (int l = 0; l < LQ; ++l) load_to_lds(q_rsrc, (voff + (unsigned)(l * NW * 8) * pitch) | past, k * 128, lds0 + stage * STAGE + BM * 128 + (l * NW + wave) * 1024);
+    };
+    f32x4 acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int sw = (lane & 15) >> 1, fp = lane >> 4;
+    const int hi = ((fp ^ sw) & 7) * 16, lo = (((4 + fp) ^ sw) & 7) * 16;
+    const unsigned char* const p_lane = smem + (wm * TM * 16 + (lane & 15)) * 128;
+    const unsigned char* const q_lane = smem + BM * 128 + (wn * TN * 16 + (lane & 15)) * 128;
+#pragma unroll
+    for (int s = 0; s < NS - 1; ++s) load(s, s);
+    int stage = 0, next = NS - 1;
+    for (int k = 0; k < steps; ++k) {
+        wait_loads_and_barrier<(NS - 2) * (LP + LQ)>();             // this stage has arrived, and all waves have read the one before
+        load(k + NS - 1, next);
+        next = stage;
+        const int at = stage * STAGE;
+        f16x8 ph[TM], pl[TM], qh[TN], ql[TN];
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            ph[i] = *reinterpret_cast<const f16x8*>(p_lane + at + hi + i * 2048);
+            pl[i] = *reinterpret_cast<const f16x8*>(p_lane + at + lo + i * 2048);
+        }
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+            qh[j] = *reinterpret_cast<const f16x8*>(q_lane + at + hi + j * 2048);
+            ql[j] = *reinterpret_cast<const f16x8*>(q_lane + at + lo + j * 2048);
+        }
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) acc[i][j] = multiply(pl[i], qh[j], acc[i][j]);
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) acc[i][j] = multiply(ph[i], ql[j], acc[i][j]);
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) acc[i][j] = multiply(ph[i], qh[j], acc[i][j]);
+        stage = stage == NS - 1 ? 0 : stage + 1;
+    }
+    wait_loads_and_barrier<0>();
+
+    // the tile leaves through the wave's own LDS in runs of eight values along either side
+    float* const mine = reinterpret_cast<float*>(smem) + wave * (TM * 16 * kPitch);
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) mine[(i * 16 + (lane >> 4) * 4 + r) * kPitch + j * 16 + (lane & 15)] = acc[i][j][r];
+    __syncthreads();
+    const int iw = i0 + wm * TM * 16, jw = j0 + wn * TN * 16;
+    constexpr int RA = TN * 2, RB = TM * 2;                        // runs of a row, of a column
+    const bool along = KIND != kLast || !t.tall, turned = KIND == kNext || (KIND <= kSquare && ti != tj) || (KIND == kLast && t.tall);
+    const int columns = KIND <= kSquare ? M : N;
+    const auto leave = [&](int row, int col, const float* v) __attribute__((always_inline)) {        // eight results from (row, col) of the matrix as it lies
+        if (row >= t.rows || col >= t.cols) return;
+        const long long at = (long long)row * t.cols + col;
+        const int n = t.cols - col;
+        float o[8];
+        if constexpr (MUON) {
+            Packed<float> w;
+            if (n >= 8) w.load(t.w + at);
+            else w.load_some(t.w + at, n, 0u);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[e] = fmaf(-t.step, v[e], fmaf(-t.lr_decay, w.get(e), w.get(e)));
+            lc_store8(t.w + at, o, n);
+            if (t.out) lc_store8(static_cast<uint16_t*>(t.out) + at, o, n);
+        } else {
+            lc_store8(static_cast<T*>(t.out) + at, v, n);
+        }
+    };
+#pragma unroll 2
+    for (int it = 0; it < TM * 16 * RA / 64; ++it) {
+        const int row = it * (64 / RA) + lane / RA, run = lane % RA * 8, gi = iw + row, gj = jw + run;
+        float* const p = mine + row * kPitch + run;
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = p[e];
+        if (gi < M && gj < columns) {
+            if constexpr (KIND == kGram) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] *= kInvScale;
+                store_pairs(t.a() + pair_at(gi, gj, M), v);
+            } else {
+                float o[8];
+                load_pairs(o, KIND == kSquare ? t.a() + pair_at(gi, gj, M) : t.x() + pair_at(gi, gj, N));
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = KIND == kSquare ? fmaf(kC * kInvScale, v[e], kB * o[e]) : fmaf(kInvScale, v[e], kA * o[e]);
+                if constexpr (KIND == kSquare) {
+                    store_pairs(t.b() + pair_at(gi, gj, M), v);
+                } else if constexpr (KIND == kNext) {
+                    store_pairs(t.x() + pair_at(gi, gj, N), v);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] *= kInvScale;
+                    if (along) leave(gi, gj, v);
+                }
+            }
+        }
+        if (turned) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) p[e] = v[e];
+        }
+    }
+    if (!turned) return;
+    __syncthreads();
+#pragma unroll 2
+    for (int it = 0; it < TN * 16 * RB / 64; ++it) {
+        const int col = it * (64 / RB) + lane / RB, run = lane % RB * 8, gj = jw + col, gi = iw + run;
+        if (gj >= columns || gi >= M) continue;
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = mine[(run + e) * kPitch + col];
+        if constexpr (KIND == kGram) store_pairs(t.a() + pair_at(gj, gi, M), v);
+        else if constexpr (KIND == kSquare) store_pairs(t.b() + pair_at(gj, gi, M), v);
+        else if constexpr (KIND == kNext) store_pairs(t.xt(args.s.which ^ 1) + pair_at(gj, gi, M), v);
+        else leave(gj, gi, v);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- host
+
+constexpr int kMostSide = 1 << 16;
+constexpr int kMostIterations = 64;
+constexpr long long kGroupBytes = 2ll << 30;       // of workspace that matrices go through the steps in together
+
+long long padded(long long side) { return (side + kPad - 1) / kPad * kPad; }
+long long bytes_of(long long rows, long long cols) {
+    const long long M = padded(std::min(rows, cols)), N = padded(std::max(rows, cols));
+    return kMostParts * 8 + 12 * M * N + 8 * M * M;
+}
+
+struct Matrix {                                    // of a call, before it has a place
+    const void* in;
+    float *m, *w;
+    void* out;
+    long long ld;
+    int rows, cols;
+    float step, lr_decay;
+};
+
+// Matrices by the length of their products, the longest first, so that a launch ends with short ones; in groups that share the workspace one after another.
+template <typename F>
+void for_groups(std::vector<int>& order, const int* rows, const int* cols, F&& f) {
+    std::stable_sort(order.begin(), order.end(), [&](int a, int b) { return std::max(rows[a], cols[a]) > std::max(rows[b], cols[b]); });
+    for (size_t first = 0; first < order.size();) {
+        long long bytes = 0;
+        size_t n = 0;
+        while (first + n < order.size() && n < kTable) {
+            const long long more = bytes_of(rows[order[first + n]], cols[order[first + n]]);
+            if (n > 0 && bytes + more > kGroupBytes) break;
+            bytes += more;
+            ++n;
+        }
+        f(first, n, bytes);
+        first += n;
+    }
+}
+
+size_t workspace_of(std::vector<int>& order, const int* rows, const int* cols) {
+    long long most = 0;
+    for_groups(order, rows, cols, [&](size_t, size_t, long long bytes) { most = std::max(most, bytes); });
+    return (size_t)(most + 255) & ~(size_t)255;
+}
+
+template <int TABLE, typename F>
+int set_starts(Args<TABLE>& args, F&& blocks) {
+    long long at = 0;
+    for (int i = 0; i < args.s.count; ++i) {
+        args.start[i] = (int)at;
+        at += blocks(args.t[i]);
+    }
+    std::fill(args.start + args.s.count, args.start + (TABLE + 63) / 64 * 64, 0x7fffffff);
+    return (int)at;
+}
+
+template <Product KIND, bool MUON, typename T, int TABLE>
+bool launch_product(Args<TABLE>& args, hipStream_t stream) {
+    constexpr int TM = 4, TN = 4, WM = 2, WN = 2, NS = 2;
+    constexpr int lds = std::max(NS * (TM * WM + TN * WN) * 16 * 128, WM * WN * TM * 16 * (TN * 16 + 4) * 4);
+    const int blocks = set_starts(args, [](const Mat& t) { return tiles_of<KIND>(t, 16 * TM * WM, 16 * TN * WN); });
+    static const bool once = hipFuncSetAttribute(reinterpret_cast<const void*>(ns_product_kernel<KIND, MUON, T, TM, TN, WM, WN, NS, TABLE>),
+                                                 hipFuncAttributeMaxDynamicSharedMemorySize, lds) == hipSuccess;
+    if (once) hipLaunchKernelGGL((ns_product_kernel<KIND, MUON, T, TM, TN, WM, WN, NS, TABLE>), dim3((unsigned)blocks), dim3(WM * WN * 64), lds, stream, args);
+    return once;
+}
+
+template <bool MUON, typename T, int TABLE>
+lc_status run_group(Args<TABLE>& args, int iterations, hipStream_t stream) {
+    int blocks = set_starts(args, [](const Mat& t) {
+        const long long v = MUON ? ((long long)t.rows * t.cols + 3) / 4 : (long long)t.rows * ((t.cols + 3) / 4);
+        return (v + t.chunk - 1) / t.chunk;
+    });
+    hipLaunchKernelGGL((ns_squares_kernel<T, MUON, TABLE>), dim3((unsigned)blocks), dim3(256), 0, stream, args);
+    blocks = set_starts(args, [](const Mat& t) { return (long long)((t.M + 63) / 64) * ((t.N + 63) / 64); });
+    hipLaunchKernelGGL((ns_split_kernel<T, MUON, TABLE>), dim3((unsigned)blocks), dim3(256), 0, stream, args);
+    bool ok = true;
+    for (int i = 0; i < iterations && ok; ++i) {
+        args.s.which = i & 1;
+        ok = launch_product<kGram, false, float>(args, stream) && launch_product<kSquare, false, float>(args, stream) &&
+             (i + 1 < iterations ? launch_product<kNext, false, float>(args, stream) : launch_product<kLast, MUON, std::conditional_t<MUON, float, T>>(args, stream));
+    }
+    return ok ? LC_OK : LC_ERR_LAUNCH;
+}
+
+template <bool MUON, typename T, int TABLE>
+lc_status run_group(const std::vector<Matrix>& all, const std::vector<int>& order, size_t first, size_t n, const Scalars& s, int iterations, void* workspace,
+                    hipStream_t stream) {
+    Args<TABLE> args;
+    args.s = s;
+    args.s.count = (int)n;
+    unsigned char* base = static_cast<unsigned char*>(workspace);
+    for (size_t i = 0; i < n; ++i) {
+        const Matrix& a = all[order[first + i]];
+        const long long vectors = MUON ? ((long long)a.rows * a.cols + 3) / 4 : (long long)a.rows * ((a.cols + 3) / 4);
+        Mat& t = args.t[i];
+        t = Mat{a.in, a.m, a.w, a.out, a.ld, a.rows, a.cols, (int)padded(std::min(a.rows, a.cols)), (int)padded(std::max(a.rows, a.cols)), a.rows > a.cols,
+                (int)std::max<long long>(1024, ((vectors + kMostParts - 1) / kMostParts + 255) / 256 * 256), base, a.step, a.lr_decay};
+        base += bytes_of(a.rows, a.cols);
+    }
+    return run_group<MUON, T, TABLE>(args, iterations, stream);
+}
+
+template <bool MUON, typename T>
+lc_status run_all(const std::vector<Matrix>& all, std::vector<int>& order, const int* rows, const int* cols, const Scalars& s, int iterations, void* workspace,
+                  hipStream_t stream) {
+    lc_status st = LC_OK;
+    for_groups(order, rows, cols, [&](size_t first, size_t n, long long) {
+        if (st != LC_OK) return;
+        st = n <= kSmallTable ? run_group<MUON, T, kSmallTable>(all, order, first, n, s, iterations, workspace, stream)
+                              : run_group<MUON, T, kTable>(all, order, first, n, s, iterations, workspace, stream);
+    });
+    return st;
+}
+
+bool bad_side(int n) { return n < 0 || n > kMostSide; }
+
+lc_status check_desc(const lc_newton_schulz_desc* d) {
+    if (!d) return LC_ERR_NULL;
+    if (d->dtype != LC_F32 && d->dtype != LC_BF16) return LC_ERR_UNSUPPORTED;
+    if (d->batch < 0 || d->rows <= 0 || d->cols <= 0 || bad_side(d->rows) || bad_side(d->cols) || (d->ld && d->ld < d->cols) || d->ld > (int64_t)1 << 40) return LC_ERR_SHAPE;
+    long long bytes;
+    if (__builtin_mul_overflow((long long)d->batch * d->rows, std::max<long long>(d->ld, d->cols), &bytes) || __builtin_mul_overflow(bytes, 4ll, &bytes)) return LC_ERR_SHAPE;
+    if (d->iterations < 1 || d->iterations > kMostIterations || !(d->eps >= 0.f)) return LC_ERR_UNSUPPORTED;
+    return LC_OK;
+}
+
+// Whether a list's sides are right; the places of what is not empty.
+lc_status check_sides(int n, const int* rows, const int* cols, std::vector<int>* order) {
+    if (n < 0) return LC_ERR_SHAPE;
+    if (n > 0 && (!rows || !cols)) return LC_ERR_NULL;
+    for (int i = 0; i < n; ++i) {
+        if (bad_side(rows[i]) || bad_side(cols[i])) return LC_ERR_SHAPE;
+        if (rows[i] && cols[i]) order->push_back(i);
+    }
+    return LC_OK;
+}
+
+size_t ns_bytes(const lc_newton_schulz_desc* d) {
+    std::vector<int> order(std::min(d->batch, kTable)), rows(order.size(), d->rows), cols(order.size(), d->cols);
+    for (size_t i = 0; i < order.size(); ++i) order[i] = (int)i;
+    return workspace_of(order, rows.data(), cols.data());
+}
+
+}  // namespace
+
+extern "C" size_t newton_schulz_workspace_bytes(const lc_newton_schulz_desc* desc) {
+    if (check_desc(desc) != LC_OK) return 0;
+    try {
+        return ns_bytes(desc);
+    } catch (...) {
+        return 0;
+    }
+}
+
+extern "C" lc_status newton_schulz(const lc_newton_schulz_desc* desc, const void* x, void* y, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    const lc_status st = check_desc(desc);
+    if (st != LC_OK) return st;
+    if (desc->batch == 0) return LC_OK;
+    if (!x || !y) return LC_ERR_NULL;
+    const size_t e = desc->dtype == LC_BF16 ? 2 : 4;
+    if (lc_off_element(x, e) || lc_off_element(y, e)) return LC_ERR_ALIGN;
+    try {
+        if (!workspace || (((uintptr_t)workspace) & 255) || workspace_bytes < ns_bytes(desc)) return LC_ERR_WORKSPACE;
+        const long long ld = desc->ld ? desc->ld : desc->cols;
+        std::vector<Matrix> all(desc->batch);
+        std::vector<int> order(desc->batch), rows(desc->batch, desc->rows), cols(desc->batch, desc->cols);
+        for (int i = 0; i < desc->batch; ++i) {
+            order[i] = i;
+            all[i] = Matrix{static_cast<const unsigned char*>(x) + (size_t)i * desc->rows * ld * e, nullptr, nullptr,
+                            static_cast<unsigned char*>(y) + (size_t)i * desc->rows * desc->cols * e, ld, desc->rows, desc->cols, 0.f, 0.f};
+        }
+        const Scalars s{0, nullptr, 0.f, desc->eps, 0, 0};
+        lc_begin_call();
+        const lc_status run = desc->dtype == LC_BF16
+                                  ? run_all<false, uint16_t>(all, order, rows.data(), cols.data(), s, desc->iterations, workspace, static_cast<hipStream_t>(hip_stream))
+                                  : run_all<false, float>(all, order, rows.data(), cols.data(), s, desc->iterations, workspace, static_cast<hipStream_t>(hip_stream));
+        const lc_status end = lc_end_call();
+        return run != LC_OK ? run : end;
+    } catch (...) {                                 // (host lists that do not fit)
+        return LC_ERR_SHAPE;
+    }
+}
+
+extern "C" size_t muon_workspace_bytes(int n_tensors, const int* rows, const int* cols) {
+    try {
+        std::vector<int> order;
+        return check_sides(n_tensors, rows, cols, &order) == LC_OK ? workspace_of(order, rows, cols) : 0;
+    } catch (...) {
+        return 0;
+    }
+}
+
+extern "C" lc_status muon_step(int n_tensors, float* const* w, const void* const* g, lc_dtype g_dtype, float* const* m, const int* rows, const int* cols, float lr,
+                               float momentum, int nesterov, float weight_decay, int iterations, float eps, const float* scale_per_tensor,
+                               const float* weight_decay_per_tensor, const float* grad_scale, void* const* w_lowp_out, void* workspace, size_t workspace_bytes,
+                               void* hip_stream) {
+    if (g_dtype != LC_F32 && g_dtype != LC_BF16) return LC_ERR_UNSUPPORTED;
+    if (iterations < 1 || iterations > kMostIterations || !(eps >= 0.f) || !(momentum >= 0.f && momentum < 1.f)) return LC_ERR_UNSUPPORTED;
+    try {
+        std::vector<int> order;
+        const lc_status st = check_sides(n_tensors, rows, cols, &order);
+        if (st != LC_OK) return st;
+        if (order.empty()) return LC_OK;
+        if (!w || !g || !m) return LC_ERR_NULL;
+        if (lc_off_element(grad_scale, 4)) return LC_ERR_ALIGN;
+        std::vector<Matrix> all(n_tensors);
+        for (int i : order) {
+            if (!w[i] || !g[i] || !m[i]) return LC_ERR_NULL;
+            void* const lowp = w_lowp_out ? w_lowp_out[i] : nullptr;
+            if (lc_off_element(w[i], 4) || lc_off_element(m[i], 4) || lc_off_element(g[i], g_dtype == LC_BF16 ? 2 : 4) || lc_off_element(lowp, 2)) return LC_ERR_ALIGN;
+            const double scale = scale_per_tensor ? scale_per_tensor[i] : std::sqrt(std::max(1.0, (double)rows[i] / cols[i]));
+            all[i] = Matrix{g[i], m[i], w[i], lowp, cols[i], rows[i], cols[i], (float)(lr * scale),
+                            (float)((double)lr * (weight_decay_per_tensor ? weight_decay_per_tensor[i] : weight_decay))};
+        }
+        if (!workspace || (((uintptr_t)workspace) & 255) || workspace_bytes < workspace_of(order, rows, cols)) return LC_ERR_WORKSPACE;
+        const Scalars s{0, grad_scale, momentum, eps, nesterov != 0, 0};
+        lc_begin_call();
+        const lc_status run = g_dtype == LC_BF16 ? run_all<true, uint16_t>(all, order, rows, cols, s, iterations, workspace, static_cast<hipStream_t>(hip_stream))
+                                                 : run_all<true, float>(all, order, rows, cols, s, iterations, workspace, static_cast<hipStream_t>(hip_stream));
+        const lc_status end = lc_end_call();
+        return run != LC_OK ? run : end;
+    } catch (...) {
+        return LC_ERR_SHAPE;
+    }
+}

@@ -33,6 +33,7 @@ EXPORTS = ["conv2d_out_shape", "conv2d_workspace_bytes", "conv2d_fwd", "conv2d_b
            "layernorm_fwd", "layernorm_bwd_workspace_bytes", "layernorm_bwd",
            "token_logprob_workspace_bytes", "token_logprob_fwd", "token_logprob_bwd",
            "adamw_step", "adamw_step_q8",
+           "newton_schulz_workspace_bytes", "newton_schulz", "muon_workspace_bytes", "muon_step",
            "lc_status_string", "lc_last_error_detail"]
 
 
@@ -126,6 +127,25 @@ class TokenDesc(_Kept):
 
     def c_struct(self) -> lc_token_desc:
         return lc_token_desc(self.rows, self.vocab, self.ld, self.dtype, self.top)
+
+
+class lc_newton_schulz_desc(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int), ("rows", ctypes.c_int), ("cols", ctypes.c_int), ("ld", ctypes.c_int64), ("iterations", ctypes.c_int),
+                ("eps", ctypes.c_float), ("dtype", ctypes.c_int)]
+
+
+@dataclass(frozen=True)
+class NewtonSchulzDesc(_Kept):
+    batch: int
+    rows: int
+    cols: int
+    ld: int = 0
+    iterations: int = 5
+    eps: float = 1e-7
+    dtype: int = LC_F32
+
+    def c_struct(self) -> lc_newton_schulz_desc:
+        return lc_newton_schulz_desc(self.batch, self.rows, self.cols, self.ld, self.iterations, self.eps, self.dtype)
 
 
 _lib = None
@@ -252,6 +272,15 @@ def lib() -> ctypes.CDLL:
         L.adamw_step.argtypes = [i32, vp, vp, i32, vp, vp, vp, f32, f64, f64, f32, f32, i64, vp, vp, vp, vp]
         L.adamw_step_q8.restype = i32
         L.adamw_step_q8.argtypes = [i32, vp, vp, i32, vp, vp, vp, vp, vp, f32, f64, f64, f32, f32, i64, ctypes.c_uint32, vp, vp, vp, vp]
+        mp = ctypes.POINTER(lc_newton_schulz_desc)
+        L.newton_schulz_workspace_bytes.restype = sz
+        L.newton_schulz_workspace_bytes.argtypes = [mp]
+        L.newton_schulz.restype = i32
+        L.newton_schulz.argtypes = [mp, vp, vp, vp, sz, vp]
+        L.muon_workspace_bytes.restype = sz
+        L.muon_workspace_bytes.argtypes = [i32, vp, vp]
+        L.muon_step.restype = i32
+        L.muon_step.argtypes = [i32, vp, vp, i32, vp, vp, vp, f32, f32, i32, f32, i32, f32, vp, vp, vp, vp, vp, sz, vp]
         L.lc_status_string.restype = ctypes.c_char_p
         L.lc_status_string.argtypes = [i32]
         L.lc_last_error_detail.restype = ctypes.c_char_p
@@ -776,3 +805,47 @@ def adamw_step_q8(args: AdamWQ8Args, lr: float, beta1: float, beta2: float, eps:
     _check(lib().adamw_step_q8(args.n, args.w, args.g, args.g_dtype, args.m, args.m_scale, args.v, args.v_scale, args.numel_arr, lr, beta1, beta2,
                                eps, weight_decay, step, seed & 0xFFFFFFFF, _decays(args, weight_decay_per_tensor), _one_float(grad_scale), args.w_lowp,
                                _stream(stream)), "adamw_step_q8")
+
+
+# ---- orthogonalised updates ----
+
+def newton_schulz_workspace_bytes(desc) -> int:
+    return int(lib().newton_schulz_workspace_bytes(_c(desc)))
+
+
+def newton_schulz(desc, x, y, workspace=None, stream=None, workspace_bytes: Optional[int] = None) -> None:
+    nb = _nbytes(workspace) if workspace_bytes is None else workspace_bytes
+    _check(lib().newton_schulz(_c(desc), _ptr(x), _ptr(y), _ptr(workspace), nb, _stream(stream)), "newton_schulz")
+
+
+class MuonArgs:
+    """Host-side pointer and size arrays of a list of matrices, marshalled once and reusable.  A tensor of more than two dimensions is a matrix of its first one's rows; `shapes` gives
+    (rows, cols) in the place of the tensors' own.  Lists of tensors are checked here, as AdamWArgs checks them; plain addresses are taken as they are."""
+
+    def __init__(self, w: Sequence, g: Sequence, m: Sequence, w_lowp: Optional[Sequence] = None, g_dtype: int = LC_F32, shapes: Optional[Sequence] = None):
+        if shapes is None:
+            shapes = [(t.shape[0], t.numel() // t.shape[0] if t.shape[0] else 0) for t in w]
+        self.n, self.shapes, self.g_dtype = len(w), [(operator.index(r), operator.index(c)) for r, c in shapes], g_dtype
+        if len(self.shapes) != self.n:
+            raise ValueError(f"{len(self.shapes)} shapes for {self.n} matrices")
+        self.numel = [r * c for r, c in self.shapes]
+        for name, tensors, types in (("w", w, ("torch.float32",)), ("g", g, ("torch.bfloat16" if g_dtype == LC_BF16 else "torch.float32",)),
+                                     ("m", m, ("torch.float32",)), ("w_lowp", w_lowp, ("torch.bfloat16",))):
+            if tensors is not None:
+                AdamWArgs._check(self, name, tensors, types)
+        self.w, self.g, self.m = _ptr_array(w), _ptr_array(g), _ptr_array(m)
+        self.rows, self.cols = ((ctypes.c_int * max(self.n, 1))(*[s[k] for s in self.shapes]) for k in (0, 1))
+        self.w_lowp = _ptr_array(w_lowp) if w_lowp is not None else None
+        self._keep = [list(a) for a in (w, g, m, w_lowp or [])]
+
+
+def muon_workspace_bytes(args: MuonArgs) -> int:
+    return int(lib().muon_workspace_bytes(args.n, args.rows, args.cols))
+
+
+def muon_step(args: MuonArgs, lr: float, momentum: float, weight_decay: float, workspace=None, nesterov: bool = True, iterations: int = 5, eps: float = 1e-7,
+              scale_per_tensor=None, weight_decay_per_tensor=None, grad_scale=None, stream=None, workspace_bytes: Optional[int] = None) -> None:
+    nb = _nbytes(workspace) if workspace_bytes is None else workspace_bytes
+    _check(lib().muon_step(args.n, args.w, args.g, args.g_dtype, args.m, args.rows, args.cols, lr, momentum, int(bool(nesterov)), weight_decay, iterations, eps,
+                           _decays(args, scale_per_tensor), _decays(args, weight_decay_per_tensor), _one_float(grad_scale), args.w_lowp, _ptr(workspace), nb,
+                           _stream(stream)), "muon_step")
