@@ -348,6 +348,28 @@ lc_status batchnorm_fwd_pair_t(lc_dtype dtype, const void* x, const float* gamma
                                float* save_invstd2, int n, int c, int h, int w, float eps, int relu, lc_layout layout, void* workspace,
                                size_t workspace_bytes, void* hip_stream);
 
+/* ---- The input side of a token model ----
+ * rows tokens, looked up in a table of vocab x c values; table_ld: elements from one row of the table to the next (0: c; otherwise >= c). */
+typedef struct {
+    int64_t rows;          /* at most 2^30 */
+    int vocab, c;          /* at most 2^30 each */
+    int64_t table_ld;
+    float scale;           /* multiplies the table's values, and the gradient (sqrt(c) for instance; 1 for none) */
+    lc_dtype table_dtype;  /* type of table */
+    lc_dtype dtype;        /* type of out and dout; dtable is fp32 */
+} lc_embedding_desc;
+
+/* out[i] = scale * table[tokens[i]] (fp32 product, rounded once); tokens: DEVICE, rows int32 values; a token outside [0, vocab) marks a position that does not count: zeros.
+ * out: [rows][c], contiguous.  Alignment: one element; zero rows are no work. */
+lc_status embedding_fwd(const lc_embedding_desc* desc, const void* table, const int32_t* tokens, void* out, void* hip_stream);
+
+/* Gradient of the table: dtable[v] = scale * sum of dout[i] over the positions whose token is v (zeros for a token that does not occur), or, with `accumulate`, that added to what dtable
+ * holds (a table that is the classifier's too; rows of tokens that do not occur are then neither read nor written).  dtable: [vocab][c] fp32, contiguous; dout: [rows][c], contiguous.  Sums are
+ * fp32 in an order fixed by tokens, rows and c (no atomics on values: reruns are bit-identical); a token may occur any number of times. */
+size_t embedding_bwd_workspace_bytes(const lc_embedding_desc* desc);
+lc_status embedding_bwd(const lc_embedding_desc* desc, const int32_t* tokens, const void* dout, float* dtable, int accumulate, void* workspace,
+                        size_t workspace_bytes, void* hip_stream);
+
 /* ---- The output side of a token model ----
  * What training and serving a model over tokens needs beside the layers above: the norm in front of its classifier (a 1x1
  * convolution over one pixel per token), the log probabilities of given tokens with their gradient, and an AdamW step over the

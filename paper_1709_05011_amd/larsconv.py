@@ -29,6 +29,7 @@ EXPORTS = ["conv2d_out_shape", "conv2d_workspace_bytes", "conv2d_fwd", "conv2d_b
            "batchnorm_fwd_t", "batchnorm_bwd_t", "maxpool_fwd_t", "maxpool_bwd_t", "relu_add_bwd_t", "global_avgpool_fwd_t",
            "global_avgpool_bwd_t", "relu_add_bwd_bnsums_t", "relu_add_bwd_bnsums_grid_t", "batchnorm_bwd_presummed_t",
            "conv2d_fwd_stats_count", "conv2d_fwd_stats", "batchnorm_fwd_pre", "batchnorm_fwd_pair_t",
+           "embedding_fwd", "embedding_bwd_workspace_bytes", "embedding_bwd",
            "rmsnorm_fwd", "rmsnorm_fwd_q8", "rmsnorm_bwd_workspace_bytes", "rmsnorm_bwd",
            "layernorm_fwd", "layernorm_bwd_workspace_bytes", "layernorm_bwd",
            "token_logprob_workspace_bytes", "token_logprob_fwd", "token_logprob_bwd",
@@ -127,6 +128,25 @@ class TokenDesc(_Kept):
 
     def c_struct(self) -> lc_token_desc:
         return lc_token_desc(self.rows, self.vocab, self.ld, self.dtype, self.top)
+
+
+class lc_embedding_desc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("vocab", ctypes.c_int), ("c", ctypes.c_int), ("table_ld", ctypes.c_int64), ("scale", ctypes.c_float),
+                ("table_dtype", ctypes.c_int), ("dtype", ctypes.c_int)]
+
+
+@dataclass(frozen=True)
+class EmbeddingDesc(_Kept):
+    rows: int
+    vocab: int
+    c: int
+    table_ld: int = 0
+    scale: float = 1.0
+    table_dtype: int = LC_F32
+    dtype: int = LC_F32
+
+    def c_struct(self) -> lc_embedding_desc:
+        return lc_embedding_desc(self.rows, self.vocab, self.c, self.table_ld, self.scale, self.table_dtype, self.dtype)
 
 
 class lc_newton_schulz_desc(ctypes.Structure):
@@ -244,6 +264,13 @@ def lib() -> ctypes.CDLL:
                                            i32, i32, vp, sz, vp]
         L.batchnorm_fwd_pre.restype = i32
         L.batchnorm_fwd_pre.argtypes = [i32, vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, ctypes.c_float, i32, i32, vp, sz, vp, sz, vp]
+        ep = ctypes.POINTER(lc_embedding_desc)
+        L.embedding_fwd.restype = i32
+        L.embedding_fwd.argtypes = [ep, vp, vp, vp, vp]
+        L.embedding_bwd_workspace_bytes.restype = sz
+        L.embedding_bwd_workspace_bytes.argtypes = [ep]
+        L.embedding_bwd.restype = i32
+        L.embedding_bwd.argtypes = [ep, vp, vp, vp, i32, vp, sz, vp]
         rp = ctypes.POINTER(lc_rmsnorm_desc)
         L.rmsnorm_fwd.restype = i32
         L.rmsnorm_fwd.argtypes = [rp, vp, vp, vp, vp, vp, vp, vp]
@@ -656,7 +683,7 @@ def batchnorm_fwd_pre(dtype: int, x, gamma, beta, residual, y, save_mean, save_i
                                    _ptr(workspace), _nbytes(workspace), _stream(stream)), "batchnorm_fwd_pre")
 
 
-# ---- the output side of a token model: RMS norm with the residual's addition ----
+# ---- token models: embeddings; RMS norm with the residual's addition ----
 
 def _c(desc):
     """The C structure of a descriptor (made once for each: descriptors do not change), or of a structure as it is."""
@@ -667,6 +694,19 @@ def _c(desc):
         made = ctypes.byref(desc.c_struct())
         object.__setattr__(desc, "_c_ref", made)
     return made
+
+
+def embedding_fwd(desc, table, tokens, out, stream=None) -> None:
+    _check(lib().embedding_fwd(_c(desc), _ptr(table), _ptr(tokens), _ptr(out), _stream(stream)), "embedding_fwd")
+
+
+def embedding_bwd_workspace_bytes(desc) -> int:
+    return int(lib().embedding_bwd_workspace_bytes(_c(desc)))
+
+
+def embedding_bwd(desc, tokens, dout, dtable, workspace=None, accumulate: bool = False, stream=None, workspace_bytes: Optional[int] = None) -> None:
+    nb = _nbytes(workspace) if workspace_bytes is None else workspace_bytes
+    _check(lib().embedding_bwd(_c(desc), _ptr(tokens), _ptr(dout), _ptr(dtable), int(bool(accumulate)), _ptr(workspace), nb, _stream(stream)), "embedding_bwd")
 
 
 def rmsnorm_fwd(desc, x, residual, gamma, total, y, save_rstd=None, stream=None) -> None:

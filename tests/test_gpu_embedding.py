@@ -1,0 +1,175 @@
+"""GPU parity of the embeddings' lookup and of the gradient of their table against oracle/token_model_ops.py in float64.
+
+Tolerances count roundings of u = 2^-24 (fp32): the lookup has one product, and half a step, 2^-8, where it is stored as bf16; a token's sum over n places has n additions at most (its
+parts' among them), a product with the scale and one addition to what is there: (n + 4) u of the magnitudes."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import token_model_ops as ops
+from paper_1709_05011_amd import larsconv as lc
+from paper_1709_05011_amd import synth
+
+import gpu_util as gu
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+TYPES = {"f32": (lc.LC_F32, torch.float32, 0.0), "bf16": (lc.LC_BF16, torch.bfloat16, 2.0 ** -8)}
+# rows, vocab, c: one token to lists that are sorted in one, two and three passes; one column to several blocks a row
+SHAPES = [(1, 1, 1), (1, 70000, 8), (2, 3, 5), (7, 50, 2056), (64, 10, 33), (65, 1000, 64), (100, 7, 4100), (1000, 33, 9), (4096, 3000, 20), (4097, 1000, 96), (5000, 1023, 8), (5000, 1024, 7),
+          (9000, 70000, 24), (20000, 300, 136), (140000, 1 << 21, 3)]
+
+
+def f64(t):
+    return t.double().cpu().numpy()
+
+
+def tokens_of(rows, vocab, seed, how):
+    t = synth.uniform_int(rows, seed, vocab).astype(np.int64)
+    if how == "one often":
+        t[synth.uniform01(rows, seed + 1) < 0.6] = vocab // 2
+    if how == "all the same":
+        t[:] = vocab - 1
+    if how == "some outside":
+        u = synth.uniform01(rows, seed + 2)
+        t[u < 0.2] = -1
+        t[(u > 0.8)] = vocab
+        t[(u > 0.9)] = 2 ** 31 - 1
+        t[(u > 0.95)] = -2 ** 31
+    if how == "none":
+        t[:] = -1
+    return t.astype(np.int32)
+
+
+@pytest.mark.parametrize("table_kind,kind", [("f32", "f32"), ("bf16", "bf16"), ("f32", "bf16"), ("bf16", "f32")])
+@pytest.mark.parametrize("rows,vocab,c", SHAPES)
+@pytest.mark.parametrize("how,pad,offset,scale", [("uniform", 0, 0, 1.0), ("some outside", 5, 1, 11.3)])
+def test_lookup(table_kind, kind, rows, vocab, c, how, pad, offset, scale):
+    tt, (dtype, t, half) = TYPES[table_kind], TYPES[kind]
+    whole = torch.full((vocab * (c + pad) + offset,), float("nan"), dtype=tt[1], device=gu.DEV)
+    table = whole[offset:].view(vocab, c + pad)[:, :c]
+    table.copy_(torch.from_numpy(synth.normal((vocab, c), 1)))
+    tokens = tokens_of(rows, vocab, 2, how)
+    out, check = gu.guarded((rows, c), t, offset=4 * offset)
+    lc.embedding_fwd(lc.EmbeddingDesc(rows, vocab, c, table_ld=c + pad, scale=scale, table_dtype=tt[0], dtype=dtype), table, gu.dev(tokens), out)
+    torch.cuda.synchronize()
+    check()
+    want = ops.embedding(f64(table), tokens, float(np.float32(scale)))
+    assert np.all(np.abs(f64(out) - want) <= (half * (1 + half) + U) * np.abs(want))
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,vocab,c", SHAPES)
+@pytest.mark.parametrize("how,accumulate,offset,scale", [("uniform", False, 0, 1.0), ("one often", True, 1, 3.7), ("all the same", False, 1, 0.5), ("some outside", True, 0, 1.0),
+                                                         ("some outside", False, 1, 11.3), ("none", False, 0, 1.0), ("none", True, 0, 1.0)])
+def test_gradient_of_the_table(kind, rows, vocab, c, how, accumulate, offset, scale):
+    dtype, t, _ = TYPES[kind]
+    tokens = tokens_of(rows, vocab, 3, how)
+    dout = torch.full((rows * c + offset,), float("nan"), dtype=t, device=gu.DEV)[offset:].view(rows, c)
+    dout.copy_(torch.from_numpy(synth.normal((rows, c), 4)))
+    dtable, check = gu.guarded((vocab, c), torch.float32, offset=4 * offset)
+    before = None
+    if accumulate:
+        before = synth.normal((vocab, c), 5)
+        dtable.copy_(torch.from_numpy(before))
+    d = lc.EmbeddingDesc(rows, vocab, c, scale=scale, dtype=dtype)
+    ws = gu.workspace(lc.embedding_bwd_workspace_bytes(d))
+    ws.fill_(0x7f)
+    first = dtable.clone()
+    lc.embedding_bwd(d, gu.dev(tokens), dout, dtable, ws, accumulate=accumulate)
+    torch.cuda.synchronize()
+    check()
+    want, size, counts = ops.embedding_bwd(vocab, tokens, f64(dout), float(np.float32(scale)), before)
+    got = f64(dtable)
+    limit = (counts[:, None] + 4) * U * (size + (0 if before is None else np.abs(before)))
+    limit[counts == 0] = 0.0
+    assert np.all(np.abs(got - want) <= limit)
+    again = first                                          # the same bits once more
+    ws.fill_(0xff)
+    lc.embedding_bwd(d, gu.dev(tokens), dout, again, ws, accumulate=accumulate)
+    torch.cuda.synchronize()
+    assert torch.equal(again, dtable)
+
+
+def test_the_gradient_against_differences():
+    """The lookup is linear: a step of 2 in one value of the table moves the sum of out * dout by twice its gradient, exact but for fp32 sums."""
+    rows, vocab, c = 40, 6, 12
+    tokens, dout = tokens_of(rows, vocab, 6, "some outside"), synth.normal((rows, c), 7)
+    table, d = synth.normal((vocab, c), 8), lc.EmbeddingDesc(rows, vocab, c, scale=2.5)
+    out, dtable = torch.empty((rows, c), device=gu.DEV), torch.empty((vocab, c), device=gu.DEV)
+
+    def forward(a):
+        lc.embedding_fwd(d, gu.dev(a), gu.dev(tokens), out)
+        return float(np.sum(f64(out) * dout))
+
+    lc.embedding_bwd(d, gu.dev(tokens), gu.dev(dout), dtable, gu.workspace(lc.embedding_bwd_workspace_bytes(d)))
+    got = f64(dtable)
+    for v, j in [(0, 0), (3, 11), (5, 4)]:
+        up, down = table.copy(), table.copy()
+        up[v, j] += 1
+        down[v, j] -= 1
+        assert abs((forward(up) - forward(down)) / float(np.float64(up[v, j]) - down[v, j]) - got[v, j]) < 1e-4 * (1 + abs(got[v, j]))
+
+
+def test_no_rows():
+    d = lc.EmbeddingDesc(0, 70, 9)
+    dtable = torch.full((70, 9), 3.0, device=gu.DEV)
+    lc.embedding_bwd(d, None, None, dtable, None, accumulate=True)
+    assert bool((dtable == 3).all())
+    lc.embedding_bwd(d, None, None, dtable, None)
+    assert bool((dtable == 0).all())
+    lc.embedding_fwd(d, None, None, None)
+
+
+def test_numbers_that_are_none_stay_with_their_token():
+    rows, vocab, c = 5000, 40, 64
+    tokens = tokens_of(rows, vocab, 9, "uniform")
+    dout = synth.normal((rows, c), 10)
+    dout[np.nonzero(tokens == 7)[0][3], 5] = np.nan
+    dtable, d = torch.empty((vocab, c), device=gu.DEV), lc.EmbeddingDesc(rows, vocab, c)
+    lc.embedding_bwd(d, gu.dev(tokens), gu.dev(dout), dtable, gu.workspace(lc.embedding_bwd_workspace_bytes(d)))
+    bad = np.isnan(f64(dtable))
+    assert bad[7, 5] and bad.sum() == 1
+
+
+def test_a_large_table_whose_offsets_pass_32_bits():
+    vocab, c = 600_000, 4096                               # 2.4 billion values
+    table = torch.empty((vocab, c), dtype=torch.bfloat16, device=gu.DEV)
+    rows = torch.tensor([0, 524287, 524288, vocab - 1], device=gu.DEV)
+    table[rows] = torch.randn((4, c), device=gu.DEV).to(torch.bfloat16)
+    d = lc.EmbeddingDesc(4, vocab, c, table_dtype=lc.LC_BF16, dtype=lc.LC_BF16)
+    out = torch.empty((4, c), dtype=torch.bfloat16, device=gu.DEV)
+    lc.embedding_fwd(d, table, rows.int(), out)
+    assert torch.equal(out, table[rows])
+    del table
+    dtable = torch.zeros((vocab, c), device=gu.DEV)
+    lc.embedding_bwd(d, rows.int(), out, dtable, gu.workspace(lc.embedding_bwd_workspace_bytes(d)), accumulate=True)
+    assert torch.equal(dtable[rows], out.float()) and float(dtable[1].abs().max()) == 0.0
+    dtable.fill_(1.0)
+    lc.embedding_bwd(d, rows.int(), out, dtable, gu.workspace(lc.embedding_bwd_workspace_bytes(d)))
+    assert torch.equal(dtable[rows], out.float()) and int((dtable != 0).any(1).sum()) == 4
+
+
+def test_a_captured_call_on_another_stream_replays():
+    rows, vocab, c = 6000, 900, 200
+    tokens, dout = gu.dev(tokens_of(rows, vocab, 11, "one often")), torch.randn((rows, c), device=gu.DEV)
+    d, dtable = lc.EmbeddingDesc(rows, vocab, c), torch.empty((vocab, c), device=gu.DEV)
+    ws = gu.workspace(lc.embedding_bwd_workspace_bytes(d))
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        lc.embedding_bwd(d, tokens, dout, dtable, ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        lc.embedding_bwd(d, tokens, dout, dtable, ws)
+    for seed in range(3):
+        tokens.copy_(gu.dev(tokens_of(rows, vocab, 20 + seed, "some outside")))
+        lc.embedding_bwd(d, tokens, dout, dtable, ws)
+        want = dtable.clone()
+        torch.cuda.synchronize()
+        dtable.fill_(float("nan"))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(dtable, want)
