@@ -233,13 +233,15 @@ __host__ __device__ inline int tiles_of(const Mat& t, int BM, int BN) {
 
 __device__ __forceinline__ f32x4 multiply(const f16x8& a, const f16x8& b, const f32x4& c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
+constexpr int leaving_columns(int TN) { return TN > 4 ? TN / 2 : TN; }
+
 // Rows P[i] times rows Q[j] along their sum.  A block has WM x WN waves of 16 TM x 16 TN values each; NS stages of LDS, the next ones arriving while one is multiplied.
 template <Product KIND, bool MUON, typename T, int TM, int TN, int WM, int WN, int NS, int TABLE>
 __global__ void __launch_bounds__(WM * WN * 64, 2) ns_product_kernel(const Args<TABLE> args) {
     constexpr int BM = 16 * TM * WM, BN = 16 * TN * WN, NW = WM * WN;
     constexpr int LP = BM / 8 / NW, LQ = BN / 8 / NW;              // loads of a wave a stage
     constexpr int STAGE = (BM + BN) * 128;
-    constexpr int kPitch = TN * 16 + 4;                           // floats
+    constexpr int TC = leaving_columns(TN), kPitch = TC * 16 + 4;   // floats
     static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && NW % 2 == 0, "tile shape");
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
 
@@ -289,52 +291,57 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) ns_product_kernel(const Args<
     const int hi = ((fp ^ sw) & 7) * 16, lo = (((4 + fp) ^ sw) & 7) * 16;
     const unsigned char* const p_lane = smem + (wm * TM * 16 + (lane & 15)) * 128;
     const unsigned char* const q_lane = smem + BM * 128 + (wn * TN * 16 + (lane & 15)) * 128;
-#pragma unroll
-    for (int s = 0; s < NS - 1; ++s) load(s, s);
-    int stage = 0, next = NS - 1;
-    for (int k = 0; k < steps; ++k) {
-        wait_loads_and_barrier<(NS - 2) * (LP + LQ)>();             // this stage has arrived, and all waves have read the one before
-        load(k + NS - 1, next);
-        next = stage;
+    f16x8 ph[2][TM], pl[2][TM], qh[2][TN], ql[2][TN];
+    const auto read = [&](int to, int stage) __attribute__((always_inline)) {
         const int at = stage * STAGE;
-        f16x8 ph[TM], pl[TM], qh[TN], ql[TN];
 #pragma unroll
-        for (int i = 0; i < TM; ++i) {
-            ph[i] = *reinterpret_cast<const f16x8*>(p_lane + at + hi + i * 2048);
-            pl[i] = *reinterpret_cast<const f16x8*>(p_lane + at + lo + i * 2048);
-        }
+        for (int i = 0; i < TM; ++i) pl[to][i] = *reinterpret_cast<const f16x8*>(p_lane + at + lo + i * 2048);
 #pragma unroll
-        for (int j = 0; j < TN; ++j) {
-            qh[j] = *reinterpret_cast<const f16x8*>(q_lane + at + hi + j * 2048);
-            ql[j] = *reinterpret_cast<const f16x8*>(q_lane + at + lo + j * 2048);
-        }
+        for (int j = 0; j < TN; ++j) qh[to][j] = *reinterpret_cast<const f16x8*>(q_lane + at + hi + j * 2048);
 #pragma unroll
-        for (int i = 0; i < TM; ++i)
+        for (int i = 0; i < TM; ++i) ph[to][i] = *reinterpret_cast<const f16x8*>(p_lane + at + hi + i * 2048);
 #pragma unroll
-            for (int j = 0; j < TN; ++j) acc[i][j] = multiply(pl[i], qh[j], acc[i][j]);
-#pragma unroll
-        for (int i = 0; i < TM; ++i)
-#pragma unroll
-            for (int j = 0; j < TN; ++j) acc[i][j] = multiply(ph[i], ql[j], acc[i][j]);
-#pragma unroll
-        for (int i = 0; i < TM; ++i)
-#pragma unroll
-            for (int j = 0; j < TN; ++j) acc[i][j] = multiply(ph[i], qh[j], acc[i][j]);
+        for (int j = 0; j < TN; ++j) ql[to][j] = *reinterpret_cast<const f16x8*>(q_lane + at + lo + j * 2048);
+    };
+    // fragments of the next step are read while this one's are multiplied: with them read first a step took two and a half times its matrix instructions where a SIMD has one wave
+    int stage = 0;
+    const auto step = [&]<int BUF>(std::integral_constant<int, BUF>, int k) __attribute__((always_inline)) {
+        wait_loads_and_barrier<(NS - 2) * (LP + LQ)>();             // the next stage has arrived, and all waves have read this one
+        load(k + NS, stage);
         stage = stage == NS - 1 ? 0 : stage + 1;
+        read(BUF ^ 1, stage);
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) acc[i][j] = multiply(pl[BUF][i], qh[BUF][j], acc[i][j]);
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) acc[i][j] = multiply(ph[BUF][i], ql[BUF][j], acc[i][j]);
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) acc[i][j] = multiply(ph[BUF][i], qh[BUF][j], acc[i][j]);
+#pragma unroll
+        for (int i = 0; i < 2 * (TM + TN); ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, std::max(1, 3 * TM * TN / (2 * (TM + TN))), 0);
+        }
+    };
+#pragma unroll
+    for (int s = 0; s < NS; ++s) load(s, s);
+    wait_loads_and_barrier<(NS - 1) * (LP + LQ)>();
+    read(0, 0);
+    for (int k = 0; k < steps; k += 2) {
+        step(std::integral_constant<int, 0>{}, k);
+        if (k + 1 < steps) step(std::integral_constant<int, 1>{}, k + 1);
     }
     wait_loads_and_barrier<0>();
 
-    // the tile leaves through the wave's own LDS in runs of eight values along either side
+    // the tile leaves through the wave's own LDS, some columns of pieces at a time, in runs of eight values along either side
     float* const mine = reinterpret_cast<float*>(smem) + wave * (TM * 16 * kPitch);
-#pragma unroll
-    for (int i = 0; i < TM; ++i)
-#pragma unroll
-        for (int j = 0; j < TN; ++j)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) mine[(i * 16 + (lane >> 4) * 4 + r) * kPitch + j * 16 + (lane & 15)] = acc[i][j][r];
-    __syncthreads();
-    const int iw = i0 + wm * TM * 16, jw = j0 + wn * TN * 16;
-    constexpr int RA = TN * 2, RB = TM * 2;                        // runs of a row, of a column
+    const int iw = i0 + wm * TM * 16;
+    constexpr int RA = TC * 2, RB = TM * 2;                        // runs of a row, of a column
     const bool along = KIND != kLast || !t.tall, turned = KIND == kNext || (KIND <= kSquare && ti != tj) || (KIND == kLast && t.tall);
     const int columns = KIND <= kSquare ? M : N;
     const auto leave = [&](int row, int col, const float* v) __attribute__((always_inline)) {        // eight results from (row, col) of the matrix as it lies
@@ -354,52 +361,65 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) ns_product_kernel(const Args<
             lc_store8(static_cast<T*>(t.out) + at, v, n);
         }
     };
+#pragma unroll
+    for (int part = 0; part < TN / TC; ++part) {
+        const int jw = j0 + (wn * TN + part * TC) * 16;
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TC; ++j)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) mine[(i * 16 + (lane >> 4) * 4 + r) * kPitch + j * 16 + (lane & 15)] = acc[i][part * TC + j][r];
+        __syncthreads();
 #pragma unroll 2
-    for (int it = 0; it < TM * 16 * RA / 64; ++it) {
-        const int row = it * (64 / RA) + lane / RA, run = lane % RA * 8, gi = iw + row, gj = jw + run;
-        float* const p = mine + row * kPitch + run;
-        float v[8];
+        for (int at = lane; at < TM * 16 * RA; at += 64) {
+            const int row = at / RA, run = at % RA * 8, gi = iw + row, gj = jw + run;
+            float* const p = mine + row * kPitch + run;
+            float v[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = p[e];
-        if (gi < M && gj < columns) {
-            if constexpr (KIND == kGram) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] *= kInvScale;
-                store_pairs(t.a() + pair_at(gi, gj, M), v);
-            } else {
-                float o[8];
-                load_pairs(o, KIND == kSquare ? t.a() + pair_at(gi, gj, M) : t.x() + pair_at(gi, gj, N));
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = KIND == kSquare ? fmaf(kC * kInvScale, v[e], kB * o[e]) : fmaf(kInvScale, v[e], kA * o[e]);
-                if constexpr (KIND == kSquare) {
-                    store_pairs(t.b() + pair_at(gi, gj, M), v);
-                } else if constexpr (KIND == kNext) {
-                    store_pairs(t.x() + pair_at(gi, gj, N), v);
-                } else {
+            for (int e = 0; e < 8; ++e) v[e] = p[e];
+            if (gi < M && gj < columns) {
+                if constexpr (KIND == kGram) {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) v[e] *= kInvScale;
-                    if (along) leave(gi, gj, v);
+                    store_pairs(t.a() + pair_at(gi, gj, M), v);
+                } else {
+                    float o[8];
+                    load_pairs(o, KIND == kSquare ? t.a() + pair_at(gi, gj, M) : t.x() + pair_at(gi, gj, N));
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = KIND == kSquare ? fmaf(kC * kInvScale, v[e], kB * o[e]) : fmaf(kInvScale, v[e], kA * o[e]);
+                    if constexpr (KIND == kSquare) {
+                        store_pairs(t.b() + pair_at(gi, gj, M), v);
+                    } else if constexpr (KIND == kNext) {
+                        store_pairs(t.x() + pair_at(gi, gj, N), v);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[e] *= kInvScale;
+                        if (along) leave(gi, gj, v);
+                    }
                 }
             }
+            if (turned) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) p[e] = v[e];
+            }
         }
+        __syncthreads();
         if (turned) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) p[e] = v[e];
-        }
-    }
-    if (!turned) return;
-    __syncthreads();
 #pragma unroll 2
-    for (int it = 0; it < TN * 16 * RB / 64; ++it) {
-        const int col = it * (64 / RB) + lane / RB, run = lane % RB * 8, gj = jw + col, gi = iw + run;
-        if (gj >= columns || gi >= M) continue;
-        float v[8];
+            for (int at = lane; at < TC * 16 * RB; at += 64) {
+                const int col = at / RB, run = at % RB * 8, gj = jw + col, gi = iw + run;
+                if (gj >= columns || gi >= M) continue;
+                float v[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = mine[(run + e) * kPitch + col];
-        if constexpr (KIND == kGram) store_pairs(t.a() + pair_at(gj, gi, M), v);
-        else if constexpr (KIND == kSquare) store_pairs(t.b() + pair_at(gj, gi, M), v);
-        else if constexpr (KIND == kNext) store_pairs(t.xt(args.s.which ^ 1) + pair_at(gj, gi, M), v);
-        else leave(gj, gi, v);
+                for (int e = 0; e < 8; ++e) v[e] = mine[(run + e) * kPitch + col];
+                if constexpr (KIND == kGram) store_pairs(t.a() + pair_at(gj, gi, M), v);
+                else if constexpr (KIND == kSquare) store_pairs(t.b() + pair_at(gj, gi, M), v);
+                else if constexpr (KIND == kNext) store_pairs(t.xt(args.s.which ^ 1) + pair_at(gj, gi, M), v);
+                else leave(gj, gi, v);
+            }
+        }
+        if (part + 1 < TN / TC) __syncthreads();
     }
 }
 
@@ -459,15 +479,65 @@ int set_starts(Args<TABLE>& args, F&& blocks) {
     return (int)at;
 }
 
-template <Product KIND, bool MUON, typename T, int TABLE>
+// The tile of a launch's products.  Small ones leave most units idle with large tiles, and a unit alone fetches some 55 GB/s from beyond its die's L2, which is what a k-step then takes (0.27 us at 64 x 64, 0.63 at
+// 128 x 128, four stages or two, four waves or eight).  us of all products of a kind at 128 x 128 with two blocks a unit / 64 x 64 / 128 x 128 with eight waves and four stages: A and B of a 1024 x 1024 matrix (36 tiles of 128) 280 / 130 / 230,
+// of 1536 x 1536 (78) 390 / 210 / 290, of 2048 x 2048 (136) 500 / 465 / 400, of two such (272) 700 / 740 / 780; X of 1024 x 1024 (64 tiles) 150 / 70 / 115, 1536 x 1536 (144) 235 / 205 / 185, 2048 x 2048
+// (256) 270 / 380 / 220, of two such (512) 490 / 840 / 510.  With more tiles than units the launch's last round counts: tiles of 192 x 192 or (X alone) 256 x 128 where they end evenly (4096 x 4096, ms, all three: 128 x 128 4.04,
+// 192 x 192 for A and B 3.63, and 256 x 128 for X 3.44).
+enum Tile { kTile64, kTile128One, kTile128, kTile192, kTile256 };
+struct TileCost {
+    int rows, cols, slots;
+    double step;             // us of a k-step with all slots at work
+};
+constexpr TileCost kTiles[] = {{64, 64, 512, 0.64}, {128, 128, 256, 0.72}, {128, 128, 512, 1.42}, {192, 192, 256, 1.5}, {256, 128, 256, 1.27}};
+template <Product KIND, int TABLE>
+Tile tile_of(const Args<TABLE>& args) {
+    // tiles, the ones of short sums as parts of one of the longest
+    const auto load = [&](int rows, int cols) {
+        double all = 0.0, longest = 0.0;
+        for (int i = 0; i < args.s.count; ++i) {
+            const Mat& t = args.t[i];
+            const double k = KIND == kGram ? t.N : t.M;
+            all += k * tiles_of<KIND>(t, rows, cols);
+            longest = std::max(longest, k);
+        }
+        return all / longest;
+    };
+    const double tiles = load(128, 128);
+    if (tiles <= 100) return kTile64;
+    if (tiles <= 256) return kTile128One;
+    Tile best = kTile128;
+    double least = 1e30;
+    for (Tile t : {kTile128, kTile192, kTile256}) {
+        if (t == kTile256 && KIND <= kSquare) continue;
+        const double cost = std::ceil(load(kTiles[t].rows, kTiles[t].cols) / kTiles[t].slots) * kTiles[t].step;
+        if (cost < least) {
+            least = cost;
+            best = t;
+        }
+    }
+    return best;
+}
+
+template <Product KIND, bool MUON, typename T, int TM, int TN, int WM, int WN, int NS, int TABLE>
 bool launch_product(Args<TABLE>& args, hipStream_t stream) {
-    constexpr int TM = 4, TN = 4, WM = 2, WN = 2, NS = 2;
-    constexpr int lds = std::max(NS * (TM * WM + TN * WN) * 16 * 128, WM * WN * TM * 16 * (TN * 16 + 4) * 4);
+    constexpr int lds = std::max(NS * (TM * WM + TN * WN) * 16 * 128, WM * WN * TM * 16 * (leaving_columns(TN) * 16 + 4) * 4);
     const int blocks = set_starts(args, [](const Mat& t) { return tiles_of<KIND>(t, 16 * TM * WM, 16 * TN * WN); });
     static const bool once = hipFuncSetAttribute(reinterpret_cast<const void*>(ns_product_kernel<KIND, MUON, T, TM, TN, WM, WN, NS, TABLE>),
                                                  hipFuncAttributeMaxDynamicSharedMemorySize, lds) == hipSuccess;
     if (once) hipLaunchKernelGGL((ns_product_kernel<KIND, MUON, T, TM, TN, WM, WN, NS, TABLE>), dim3((unsigned)blocks), dim3(WM * WN * 64), lds, stream, args);
     return once;
+}
+template <Product KIND, bool MUON, typename T, int TABLE>
+bool launch_product(Args<TABLE>& args, hipStream_t stream) {
+    switch (tile_of<KIND>(args)) {
+        case kTile64: return launch_product<KIND, MUON, T, 2, 2, 2, 2, 4>(args, stream);
+        case kTile128One: return launch_product<KIND, MUON, T, 2, 4, 4, 2, 4>(args, stream);
+        case kTile192: return launch_product<KIND, MUON, T, 6, 3, 2, 4, 3>(args, stream);
+        case kTile256:
+            if constexpr (KIND >= kNext) return launch_product<KIND, MUON, T, 4, 4, 4, 2, 3>(args, stream);
+        default: return launch_product<KIND, MUON, T, 4, 4, 2, 2, 2>(args, stream);
+    }
 }
 
 template <bool MUON, typename T, int TABLE>
