@@ -231,6 +231,34 @@ __host__ __device__ inline int tiles_of(const Mat& t, int BM, int BN) {
     return KIND <= kSquare ? nm * (nm + 1) / 2 : nm * nn;
 }
 
+// Row and column of a tile: down the columns of groups of four rows of tiles (by 256 rows), so that the tiles that a die works on at a time are about as high as wide and share what they read.
+template <Product KIND>
+__device__ __forceinline__ void place_of(const Mat& t, int tile, int BM, int BN, int* ti, int* tj) {
+    const int nm = (t.M + BM - 1) / BM, nn = (t.N + BN - 1) / BN;
+    if constexpr (KIND <= kSquare) {
+        constexpr int G = 4;
+        int row = (int)((sqrtf(8.f * (float)tile + 1.f) - 1.f) * 0.5f);
+        while ((row + 1) * (row + 2) / 2 <= tile) ++row;
+        while (row * (row + 1) / 2 > tile) --row;
+        const int first = row / G * G, high = std::min(G, nm - first);
+        int at = tile - first * (first + 1) / 2;
+        if (at < (first + 1) * high) {
+            *tj = at / high;
+            *ti = first + at % high;
+        } else {                                   // the corner on the diagonal
+            at -= (first + 1) * high;
+            int d = 1;
+            for (; at >= high - d; ++d) at -= high - d;
+            *tj = first + d;
+            *ti = *tj + at;
+        }
+    } else {
+        const int G = std::max(1, 1024 / BM), first = tile / (G * nn) * G, high = std::min(G, nm - first), at = tile - first * nn;
+        *tj = at / high;
+        *ti = first + at % high;
+    }
+}
+
 __device__ __forceinline__ f32x4 multiply(const f16x8& a, const f16x8& b, const f32x4& c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
 constexpr int leaving_columns(int TN) { return TN > 4 ? TN / 2 : TN; }
@@ -248,19 +276,14 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) ns_product_kernel(const Args<
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / WN, wn = wave % WN;
     int local;
-    const Mat& t = args.t[owner_of(args, xcd_tile(blockIdx.x, gridDim.x), &local)];
+    const int owner = owner_of(args, blockIdx.x, &local);
+    const Mat& t = args.t[owner];
     const int M = t.M, N = t.N;
+    const int tiles = tiles_of<KIND>(t, BM, BN), per = (tiles + 7) >> 3;
+    const int tile = ((local + owner) & 7) * per + (local >> 3);       // a die takes neighbouring tiles of each matrix; blocks begin at multiples of 8
+    if (tile >= std::min(tiles, (((local + owner) & 7) + 1) * per)) return;
     int ti, tj;
-    if constexpr (KIND <= kSquare) {
-        ti = (int)((sqrtf(8.f * (float)local + 1.f) - 1.f) * 0.5f);
-        while ((ti + 1) * (ti + 2) / 2 <= local) ++ti;
-        while (ti * (ti + 1) / 2 > local) --ti;
-        tj = local - ti * (ti + 1) / 2;
-    } else {
-        const int across = (N + BN - 1) / BN;
-        ti = local / across;
-        tj = local - ti * across;
-    }
+    place_of<KIND>(t, tile, BM, BN, &ti, &tj);
     ti = __builtin_amdgcn_readfirstlane(ti);
     tj = __builtin_amdgcn_readfirstlane(tj);
     const int i0 = ti * BM, j0 = tj * BN;
@@ -522,7 +545,7 @@ Tile tile_of(const Args<TABLE>& args) {
 template <Product KIND, bool MUON, typename T, int TM, int TN, int WM, int WN, int NS, int TABLE>
 bool launch_product(Args<TABLE>& args, hipStream_t stream) {
     constexpr int lds = std::max(NS * (TM * WM + TN * WN) * 16 * 128, WM * WN * TM * 16 * (leaving_columns(TN) * 16 + 4) * 4);
-    const int blocks = set_starts(args, [](const Mat& t) { return tiles_of<KIND>(t, 16 * TM * WM, 16 * TN * WN); });
+    const int blocks = set_starts(args, [](const Mat& t) { return (tiles_of<KIND>(t, 16 * TM * WM, 16 * TN * WN) + 7) / 8 * 8; });
     static const bool once = hipFuncSetAttribute(reinterpret_cast<const void*>(ns_product_kernel<KIND, MUON, T, TM, TN, WM, WN, NS, TABLE>),
                                                  hipFuncAttributeMaxDynamicSharedMemorySize, lds) == hipSuccess;
     if (once) hipLaunchKernelGGL((ns_product_kernel<KIND, MUON, T, TM, TN, WM, WN, NS, TABLE>), dim3((unsigned)blocks), dim3(WM * WN * 64), lds, stream, args);
