@@ -502,41 +502,33 @@ int set_starts(Args<TABLE>& args, F&& blocks) {
     return (int)at;
 }
 
-// The tile of a launch's products.  Small ones leave most units idle with large tiles, and a unit alone fetches some 55 GB/s from beyond its die's L2, which is what a k-step then takes (0.27 us at 64 x 64, 0.63 at
-// 128 x 128, four stages or two, four waves or eight).  us of all products of a kind at 128 x 128 with two blocks a unit / 64 x 64 / 128 x 128 with eight waves and four stages: A and B of a 1024 x 1024 matrix (36 tiles of 128) 280 / 130 / 230,
-// of 1536 x 1536 (78) 390 / 210 / 290, of 2048 x 2048 (136) 500 / 465 / 400, of two such (272) 700 / 740 / 780; X of 1024 x 1024 (64 tiles) 150 / 70 / 115, 1536 x 1536 (144) 235 / 205 / 185, 2048 x 2048
-// (256) 270 / 380 / 220, of two such (512) 490 / 840 / 510.  With more tiles than units the launch's last round counts: tiles of 192 x 192 or (X alone) 256 x 128 where they end evenly (4096 x 4096, ms, all three: 128 x 128 4.04,
-// 192 x 192 for A and B 3.63, and 256 x 128 for X 3.44).
+// The tile of a launch's products, by what a launch is estimated to take, us: rounds of blocks (tiles of sums shorter than the longest count as parts of one), each the k-steps of the longest sum and what begins and ends a
+// tile.  A k-step takes `alone` where a unit has one block (it fetches some 55 GB/s from beyond its die's L2 then, whatever the stages and waves), `step` with all slots at work; the matrix pipe's time at 128 x 128 is 0.32 at full
+// clock.  us of all products of a kind at 128 x 128 with two blocks a unit / 64 x 64 / 128 x 128 with eight waves and four stages: A and B of a 1024 x 1024 matrix (36 tiles of 128) 280 / 130 / 230, of 1536 x 1536 (78)
+// 390 / 210 / 290, of 2048 x 2048 (136) 500 / 465 / 400, of two such (272) 700 / 740 / 780; X of 1024 x 1024 (64 tiles) 150 / 70 / 115, 1536 x 1536 (144) 235 / 205 / 185, 2048 x 2048 (256) 270 / 380 / 220, of two such
+// (512) 490 / 840 / 510.  4096 x 4096, ms, all three: 128 x 128 4.04, 192 x 192 for A and B 3.63, and 256 x 128 for X (which has no triangle to fit) 3.44.
 enum Tile { kTile64, kTile128One, kTile128, kTile192, kTile256 };
 struct TileCost {
     int rows, cols, slots;
-    double step;             // us of a k-step with all slots at work
+    double alone, step, ends;
 };
-constexpr TileCost kTiles[] = {{64, 64, 512, 0.64}, {128, 128, 256, 0.72}, {128, 128, 512, 1.42}, {192, 192, 256, 1.5}, {256, 128, 256, 1.27}};
+constexpr TileCost kTiles[] = {{64, 64, 512, 0.27, 0.64, 3.0}, {128, 128, 256, 0.6, 0.72, 4.0}, {128, 128, 512, 0.8, 1.42, 4.0}, {192, 192, 256, 1.5, 1.5, 8.0}, {256, 128, 256, 1.2, 1.27, 7.0}};
 template <Product KIND, int TABLE>
 Tile tile_of(const Args<TABLE>& args) {
-    // tiles, the ones of short sums as parts of one of the longest
-    const auto load = [&](int rows, int cols) {
-        double all = 0.0, longest = 0.0;
-        for (int i = 0; i < args.s.count; ++i) {
-            const Mat& t = args.t[i];
-            const double k = KIND == kGram ? t.N : t.M;
-            all += k * tiles_of<KIND>(t, rows, cols);
-            longest = std::max(longest, k);
-        }
-        return all / longest;
-    };
-    const double tiles = load(128, 128);
-    if (tiles <= 100) return kTile64;
-    if (tiles <= 256) return kTile128One;
+    double least = 1e30, longest = 0.0;
     Tile best = kTile128;
-    double least = 1e30;
-    for (Tile t : {kTile128, kTile192, kTile256}) {
-        if (t == kTile256 && KIND <= kSquare) continue;
-        const double cost = std::ceil(load(kTiles[t].rows, kTiles[t].cols) / kTiles[t].slots) * kTiles[t].step;
+    for (int i = 0; i < args.s.count; ++i) longest = std::max<double>(longest, KIND == kGram ? args.t[i].N : args.t[i].M);
+    for (Tile tile : {kTile64, kTile128One, kTile128, kTile192, kTile256}) {
+        if (tile == kTile256 && KIND <= kSquare) continue;
+        const TileCost& k = kTiles[tile];
+        double all = 0.0;
+        for (int i = 0; i < args.s.count; ++i) all += (KIND == kGram ? args.t[i].N : args.t[i].M) * (double)tiles_of<KIND>(args.t[i], k.rows, k.cols);
+        const double rounds = all / longest / k.slots, full = std::floor(rounds), rest = rounds - full;
+        const double last = rest == 0.0 ? 0.0 : k.slots > 256 ? std::max(k.alone, k.step * rest) : rounds < 1.0 ? k.alone : k.step;
+        const double cost = longest / 32 * (k.step * full + last) + k.ends * std::ceil(rounds);
         if (cost < least) {
             least = cost;
-            best = t;
+            best = tile;
         }
     }
     return best;
@@ -552,8 +544,8 @@ bool launch_product(Args<TABLE>& args, hipStream_t stream) {
     return once;
 }
 template <Product KIND, bool MUON, typename T, int TABLE>
-bool launch_product(Args<TABLE>& args, hipStream_t stream) {
-    switch (tile_of<KIND>(args)) {
+bool launch_product(Args<TABLE>& args, Tile tile, hipStream_t stream) {
+    switch (tile) {
         case kTile64: return launch_product<KIND, MUON, T, 2, 2, 2, 2, 4>(args, stream);
         case kTile128One: return launch_product<KIND, MUON, T, 2, 4, 4, 2, 4>(args, stream);
         case kTile192: return launch_product<KIND, MUON, T, 6, 3, 2, 4, 3>(args, stream);
@@ -572,11 +564,13 @@ lc_status run_group(Args<TABLE>& args, int iterations, hipStream_t stream) {
     hipLaunchKernelGGL((ns_squares_kernel<T, MUON, TABLE>), dim3((unsigned)blocks), dim3(256), 0, stream, args);
     blocks = set_starts(args, [](const Mat& t) { return (long long)((t.M + 63) / 64) * ((t.N + 63) / 64); });
     hipLaunchKernelGGL((ns_split_kernel<T, MUON, TABLE>), dim3((unsigned)blocks), dim3(256), 0, stream, args);
+    const Tile gram = tile_of<kGram>(args), square = tile_of<kSquare>(args), next = tile_of<kNext>(args);
     bool ok = true;
     for (int i = 0; i < iterations && ok; ++i) {
         args.s.which = i & 1;
-        ok = launch_product<kGram, false, float>(args, stream) && launch_product<kSquare, false, float>(args, stream) &&
-             (i + 1 < iterations ? launch_product<kNext, false, float>(args, stream) : launch_product<kLast, MUON, std::conditional_t<MUON, float, T>>(args, stream));
+        ok = launch_product<kGram, false, float>(args, gram, stream) && launch_product<kSquare, false, float>(args, square, stream) &&
+             (i + 1 < iterations ? launch_product<kNext, false, float>(args, next, stream)
+                                 : launch_product<kLast, MUON, std::conditional_t<MUON, float, T>>(args, next, stream));
     }
     return ok ? LC_OK : LC_ERR_LAUNCH;
 }
