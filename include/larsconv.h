@@ -351,7 +351,7 @@ lc_status batchnorm_fwd_pair_t(lc_dtype dtype, const void* x, const float* gamma
 /* ---- The input side of a token model ----
  * rows tokens, looked up in a table of vocab x c values; table_ld: elements from one row of the table to the next (0: c; otherwise >= c). */
 typedef struct {
-    int64_t rows;          /* at most 2^30 */
+    int64_t rows;          /* at most 2^25 */
     int vocab, c;          /* at most 2^30 each */
     int64_t table_ld;
     float scale;           /* multiplies the table's values, and the gradient (sqrt(c) for instance; 1 for none) */

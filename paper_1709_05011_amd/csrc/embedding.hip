@@ -1,12 +1,13 @@
 // Lookup of token embeddings with a scale, and the gradient of their table, for gfx950.
 //
 // out[i] = scale * table[t_i];  dtable[v] (+)= scale * sum over the places i with t_i = v of dout[i], in a fixed order and without atomics: places are sorted by token (stable), the sorted
-// list is cut into pieces of equal length, and a block sums the rows of a piece, whatever tokens they belong to.  A token that lies within a piece is written at once; one that crosses pieces
-// leaves a part in each, which the block of its first piece adds up in a second launch.  How often a token occurs does not change how long a block takes.  Bound by memory.
+// list is cut into pieces of equal length, and a wave sums the rows of a token within a piece.  A token that lies within one is written at once; one that crosses pieces leaves a part in each, which
+// are added up in a second launch.  A token may occur any number of times.  Bound by memory.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "internal.h"
 #include "token_common.h"
@@ -20,6 +21,23 @@ __device__ __forceinline__ int key_of(const int32_t* tokens, long long i, int vo
     return t >= 0 && t < vocab ? t : kNone;
 }
 
+// Eight columns of a row, loaded (issue) and put in their places (settle) apart, so that loads of several rows are under way; EIGHTS: c is a multiple of 8.
+template <bool EIGHTS, typename T>
+__device__ __forceinline__ void issue(Packed<T>& to, const T* row, int col, int c) {
+    if constexpr (EIGHTS) {
+        to.load(row + col);
+    } else if (c >= 8) {
+        to.load(row + min(col, c - 8));
+    } else {
+        to.load_some(row, c, 0u);
+    }
+}
+template <bool EIGHTS, typename T>
+__device__ __forceinline__ void settle(Packed<T>& x, int col, int c) {
+    if constexpr (!EIGHTS) {
+        if (c >= 8 && c - col < 8) x.shift(8 - (c - col), 0u);
+    }
+}
 // ---------------------------------------------------------------------------------------------- lookup
 
 struct LookupArgs {
@@ -27,25 +45,33 @@ struct LookupArgs {
     const int32_t* tokens;
     void* out;
     long long rows, table_ld;
-    int vocab, c, lanes;       // lanes: of a row, a power of two up to the block's 256
+    int vocab, c, lane_bits;   // a row has 2^lane_bits lanes, up to the block's 256
     float scale;
 };
 
-// Some lanes a row (rows dealt round the grid), eight columns a lane and access.
-template <typename S, typename T>
+// Some lanes a row, eight columns a lane and access, kRowsAhead rows of a block (their tokens, then their values) under way at a time.
+constexpr int kRowsAhead = 4;
+template <typename S, typename T, bool EIGHTS>
 __global__ void __launch_bounds__(256) embedding_fwd_kernel(const LookupArgs p) {
-    const int lane = threadIdx.x & (p.lanes - 1), each = 256 / p.lanes;
-    for (long long row = (long long)blockIdx.x * each + threadIdx.x / p.lanes; row < p.rows; row += (long long)gridDim.x * each) {
-        const int key = key_of(p.tokens, row, p.vocab);
-        const S* from = static_cast<const S*>(p.table) + (key == kNone ? 0 : key) * p.table_ld;
-        T* to = static_cast<T*>(p.out) + row * p.c;
-        for (long long col = lane * 8; col < p.c; col += p.lanes * 8) {
-            Packed<S> x;
-            float v[8];
-            lc_load8(x, from, (int)col, p.c);
+    const int lanes = 1 << p.lane_bits, lane = threadIdx.x & (lanes - 1), each = 256 >> p.lane_bits;
+    const long long stride = (long long)gridDim.x * each;
+    for (long long row = (long long)blockIdx.x * each + (threadIdx.x >> p.lane_bits); row < p.rows; row += stride * kRowsAhead) {
+        int key[kRowsAhead];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = key == kNone ? 0.f : x.get(j) * p.scale;
-            lc_store8(to + col, v, p.c - (int)col);
+        for (int u = 0; u < kRowsAhead; ++u) key[u] = key_of(p.tokens, std::min(row + u * stride, p.rows - 1), p.vocab);
+        for (long long col = lane * 8; col < p.c; col += lanes * 8) {
+            Packed<S> x[kRowsAhead];
+#pragma unroll
+            for (int u = 0; u < kRowsAhead; ++u) issue<EIGHTS>(x[u], static_cast<const S*>(p.table) + (key[u] == kNone ? 0 : key[u]) * p.table_ld, (int)col, p.c);
+#pragma unroll
+            for (int u = 0; u < kRowsAhead; ++u) {
+                if (row + u * stride >= p.rows) break;
+                settle<EIGHTS>(x[u], (int)col, p.c);
+                float v[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = key[u] == kNone ? 0.f : x[u].get(j) * p.scale;
+                lc_store8(static_cast<T*>(p.out) + (row + u * stride) * p.c + col, v, EIGHTS ? 8 : p.c - (int)col);
+            }
         }
     }
 }
@@ -60,11 +86,25 @@ struct SortArgs {
     int* place;
     int* counts;               // [blocks][bins]
     int rows, vocab, per, shift, bits;
+    int sort_blocks;           // blocks behind them write zeros to
+    float* zeros;              // this many bytes (a share of the table, whose rows that do not occur are to be zero)
+    long long zero_bytes;
 };
+
+// Zeros past the caches, by the blocks of a sorting launch that have nothing to sort: few places keep few units busy, and their order is latency.
+__device__ __forceinline__ void fill_share(const SortArgs& p, int threads) {
+    if ((int)blockIdx.x == p.sort_blocks && threadIdx.x < (p.zero_bytes & 15) / 4) p.zeros[p.zero_bytes / 16 * 4 + threadIdx.x] = 0.f;
+    const long long vectors = p.zero_bytes / 16, step = (long long)(gridDim.x - p.sort_blocks) * threads;
+    for (long long v = (long long)(blockIdx.x - p.sort_blocks) * threads + threadIdx.x; v < vectors; v += step) lc_store16<true>(p.zeros + v * 4, lc_u32x4{0u, 0u, 0u, 0u});
+}
 
 // Few places: a block ranks 64 of them against all, which it holds in LDS; each of its 16 waves a share of them.
 constexpr int kRankMost = 4096;
 __global__ void __launch_bounds__(1024) embedding_rank_kernel(const SortArgs p) {
+    if ((int)blockIdx.x >= p.sort_blocks) {
+        fill_share(p, 1024);
+        return;
+    }
     __shared__ __attribute__((aligned(16))) int keys[kRankMost];
     __shared__ int before[16][64];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, padded = (p.rows + 63) & ~63;
@@ -99,6 +139,10 @@ __global__ void __launch_bounds__(1024) embedding_rank_kernel(const SortArgs p) 
 constexpr int kMostBits = 10, kSortBlocks = 128;
 __device__ __forceinline__ int sort_key(const SortArgs& p, int i) { return p.tokens ? min(key_of(p.tokens, i, p.vocab), p.vocab) : p.key_in[i]; }       // (outside: one above the last)
 __global__ void __launch_bounds__(1024) embedding_count_kernel(const SortArgs p) {
+    if ((int)blockIdx.x >= p.sort_blocks) {
+        fill_share(p, 1024);
+        return;
+    }
     __shared__ int count[1 << kMostBits];
     const int bins = 1 << p.bits, first = blockIdx.x * p.per, end = min(p.rows, first + p.per);
     for (int d = threadIdx.x; d < bins; d += 1024) count[d] = 0;
@@ -109,6 +153,10 @@ __global__ void __launch_bounds__(1024) embedding_count_kernel(const SortArgs p)
 }
 // ... and moves it: where a digit's places of the block begin follows from all blocks' counts, where a wave's begin from its share's, and within a wave places keep their order.
 __global__ void __launch_bounds__(1024) embedding_move_kernel(const SortArgs p) {
+    if ((int)blockIdx.x >= p.sort_blocks) {
+        fill_share(p, 1024);
+        return;
+    }
     constexpr int kBins = 1 << kMostBits;
     __shared__ int next[16][kBins];
     __shared__ int sums[16];
@@ -121,7 +169,7 @@ __global__ void __launch_bounds__(1024) embedding_move_kernel(const SortArgs p) 
     int total = 0, before = 0;                     // of digit tid over all blocks; over those before this one
     if (tid < bins) {
 #pragma unroll 8
-        for (int b = 0; b < (int)gridDim.x; ++b) {
+        for (int b = 0; b < p.sort_blocks; ++b) {
             const int n = p.counts[b * bins + tid];
             total += n;
             before += b < blockIdx.x ? n : 0;
@@ -176,174 +224,170 @@ struct SumArgs {
     const void* dout;
     float* dtable;
     float* part;               // [pieces][2][c]: of the token that a piece begins with and an earlier one holds too; of the one that it ends with and that goes on
-    long long pieces;
-    int rows, vocab, c, len, accumulate;
-    int lanes;                 // of a piece; a block has 256 / lanes pieces, or `tiles` blocks have one
-    int tiles;
-    long long sum_blocks;      // the blocks behind them fill the rows of absent tokens
+    long long pieces;          // of kPiece places
+    int rows, vocab, c;
+    int lane_bits, tiles;      // 2^lane_bits lanes take 8 columns each of a part of a row; how many parts a row has
     float scale;
 };
 
-constexpr int kStaged = 2048;      // places of a block's pieces, at most
+constexpr int kPiece = 32;     // places whose rows one wave sums (16: sums as fast, their joining 2 to 13 us slower)
 
-// Eight columns of a row, loaded (issue) and put in their places (settle) apart, so that loads of several rows are under way; EIGHTS: c is a multiple of 8.
-template <bool EIGHTS, bool NT, typename T>
-__device__ __forceinline__ void issue(Packed<T>& to, const T* row, int col, int c) {
-    if constexpr (EIGHTS) {
-        to.template load<NT>(row + col);
-    } else if (c >= 8) {
-        to.template load<NT>(row + min(col, c - 8));
-    } else {
-        to.load_some(row, c, 0u);
-    }
-}
-template <bool EIGHTS, typename T>
-__device__ __forceinline__ void settle(Packed<T>& x, int col, int c) {
-    if constexpr (!EIGHTS) {
-        if (c >= 8 && c - col < 8) x.shift(8 - (c - col), 0u);
-    }
-}
-template <bool EIGHTS>
-__device__ __forceinline__ void add_to(float* to, float* acc, int left, bool accumulate) {
-    if (accumulate) {
-        Packed<float> old;
-        if (EIGHTS || left >= 8) old.load(to);
-        else old.load_some(to, left, 0u);
+// Eight columns of a sum to their place: the table's, where nothing else of the token is, or the piece's part of it.
+template <bool EIGHTS, bool ADD>
+__device__ __forceinline__ void leave(const SumArgs& p, long long piece, int key, bool continued, bool goes_on, int col, const float* acc, Packed<float>& old) {
+    const bool whole = !continued && !goes_on;
+    float* const to = (whole ? p.dtable + (long long)key * p.c : p.part + (piece * 2 + (continued ? 0 : 1)) * p.c) + col;
+    float v[8];
+    if constexpr (ADD) settle<EIGHTS>(old, col, p.c);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) acc[j] += old.get(j);
-    }
-    lc_store8(to, acc, EIGHTS ? 8 : left);
+    for (int j = 0; j < 8; ++j) v[j] = ADD && whole ? fmaf(acc[j], p.scale, old.get(j)) : acc[j] * p.scale;
+    lc_store8(to, v, EIGHTS ? 8 : p.c - col);
 }
 
-template <typename T, bool EIGHTS>
-__device__ __forceinline__ void sum_piece(const SumArgs& p) {
-    __shared__ int keys[kStaged], places[kStaged];
-    const int group = threadIdx.x / p.lanes, lane = threadIdx.x & (p.lanes - 1), each = 256 / p.lanes;
-    const long long block = blockIdx.x / p.tiles, start = block * each * p.len;
-    const int staged = (int)std::min<long long>((long long)each * p.len, p.rows - start);
-    for (int i = threadIdx.x; i < staged; i += 256) {
-        keys[i] = p.key[start + i];
-        places[i] = p.place[start + i];
-    }
-    __syncthreads();
-    const long long piece = block * each + group;
-    const int col = ((int)(blockIdx.x % p.tiles) * p.lanes + lane) * 8;
-    if (piece >= p.pieces || col >= p.c) return;
-    const int first = group * p.len, end = min(staged, first + p.len);
+// A wave sums the rows of a piece, 512 columns of them: keys and places first, then AHEAD rows at a time, then their sums and stores.  No load stands behind a branch, and few behind a store: a wave's loads and stores
+// complete in order, so that waiting for one waits for all before it.  16384 rows of 2048 bf16 (5600 tokens, 107 MB) 31 us, 30011 of 1537 fp32 added to what is there 95 (3.2 TB/s); a wave for each place, most of which are
+// not a token's first, 40 and 90, with a longer joining.  Sequential rows in the place of a token's take as long; without the stores 19: all waves load, then all store.
+template <typename T, bool EIGHTS, bool ADD, int AHEAD>
+__global__ void __launch_bounds__(256) embedding_sum_kernel(const SumArgs p) {
+    const int lane = threadIdx.x & 63;
+    const unsigned wave = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+    const unsigned piece = wave / (unsigned)p.tiles, tile0 = wave - piece * (unsigned)p.tiles;
+    if (piece >= (unsigned)p.pieces) return;
+    const int first = (int)piece * kPiece, n = std::min(kPiece, p.rows - first);
+    const int at = std::min(std::max(first - 1 + lane, 0), p.rows - 1);       // lane 0: the place before the piece, lane n + 1: the one behind it
+    int keys = p.key[at];
+    const int places = p.place[at];
+    if (first - 1 + lane < 0 || first - 1 + lane >= p.rows || keys >= p.vocab) keys = kNone;
     const T* const dout = static_cast<const T*>(p.dout);
-    constexpr int U = 8;                           // rows under way
-    Packed<T> x[U];
+    const auto key_of_place = [&](int k) __attribute__((always_inline)) { return __builtin_amdgcn_readlane(keys, k + 1); };
+    const int before = key_of_place(-1);
+    const int own = ((int)tile0 * 64 + lane) * 8, col = std::min(own, EIGHTS ? p.c - 8 : p.c);
     float acc[8] = {};
-    int key = keys[first];
-    bool continued = start + first > 0 && p.key[start + first - 1] == key;
-    const int behind = start + end < p.rows ? p.key[start + end] : kNone;
-    const auto leave = [&](bool goes_on) __attribute__((always_inline)) {
-        if (key < p.vocab) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) acc[j] *= p.scale;
-            if (continued || goes_on) lc_store8(p.part + (piece * 2 + (continued ? 0 : 1)) * p.c + col, acc, p.c - col);
-            else add_to<EIGHTS>(p.dtable + (long long)key * p.c + col, acc, p.c - col, p.accumulate);
+    for (int ahead = 0; ahead < kPiece; ahead += AHEAD) {
+        if (ahead >= n) break;
+        Packed<T> x[AHEAD];
+        Packed<float> old[ADD ? AHEAD : 1];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const int row = __builtin_amdgcn_readlane(places, std::min(ahead + u, n - 1) + 1);
+            issue<EIGHTS>(x[u], dout + (long long)row * p.c, col, p.c);
+            if constexpr (ADD) {
+                const int key = key_of_place(std::min(ahead + u, n - 1));
+                issue<EIGHTS>(old[u], p.dtable + (long long)(key == kNone ? 0 : key) * p.c, col, p.c);
+            }
         }
 #pragma unroll
-        for (int j = 0; j < 8; ++j) acc[j] = 0.f;
-    };
+        for (int u = 0; u < AHEAD; ++u) {
+            const int k = ahead + u;
+            if (k >= n) break;
+            const int key = key_of_place(k);
+            settle<EIGHTS>(x[u], col, p.c);
 #pragma unroll
-    for (int u = 0; u < U; ++u) issue<EIGHTS, false>(x[u], dout + (long long)places[min(first + u, end - 1)] * p.c, col, p.c);
-    for (int i = first; i < end; i += U) {
+            for (int j = 0; j < 8; ++j) acc[j] += x[u].get(j);
+            const bool last = k + 1 == n, ends = last || key_of_place(k + 1) != key;
+            if (!ends) continue;
+            if (key != kNone && own < p.c)
+                leave<EIGHTS, ADD>(p, piece, key, before == key, last && key_of_place(k + 1) == key, own, acc, old[ADD ? u : 0]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) acc[j] = 0.f;
+        }
+    }
+}
+
+// Rows of fewer columns than a wave takes: 2^lane_bits lanes a row sum a token's rows from a place to the end of its piece, if the token or the piece begins there.
+template <typename T, bool EIGHTS, bool ADD>
+__global__ void __launch_bounds__(256) embedding_sum_narrow_kernel(const SumArgs p) {
+    const int lanes = 1 << p.lane_bits, lane = threadIdx.x & (lanes - 1), of = threadIdx.x & 63 & ~(lanes - 1);       // the first of these lanes in the wave
+    const long long first = ((long long)blockIdx.x * 256 + threadIdx.x) >> p.lane_bits;
+    if (first >= p.rows) return;
+    const int i = (int)first, end = std::min(p.rows, (i / kPiece + 1) * kPiece), at0 = std::min(i + lane, end - 1);
+    const int mine = p.key[at0], place = p.place[at0], before = i > 0 ? p.key[i - 1] : kNone, behind = end < p.rows ? p.key[end] : kNone;
+    const int key = __shfl(mine, of, 64);
+    if (key >= p.vocab || (before == key && i % kPiece != 0)) return;
+    // the token's places: lanes look at the next keys, as many at a time as they are
+    const unsigned long long every = p.lane_bits == 6 ? ~0ull : (1ull << lanes) - 1;
+    const auto run_of = [&](bool same) __attribute__((always_inline)) {
+        const unsigned long long bits = __ballot(same) >> of;
+        return (bits & every) == every ? lanes : __builtin_ctzll(~bits);
+    };
+    int n = run_of(i + lane < end && mine == key);
+    for (int run = n; run == lanes && i + n < end; n += run) run = run_of(i + n + lane < end && p.key[std::min(i + n + lane, end - 1)] == key);
+    const bool goes_on = i + n == end && behind == key, continued = before == key;
+    const T* const dout = static_cast<const T*>(p.dout);
+    const int own = lane * 8, col = std::min(own, EIGHTS ? p.c - 8 : p.c);       // lanes past the row go along: the others ask them for places
+    Packed<float> old;
+    if constexpr (ADD) issue<EIGHTS>(old, p.dtable + (long long)key * p.c, col, p.c);
+    constexpr int U = 4;                           // rows under way
+    float acc[8] = {};
+    int places = place;
+    for (int k = 0; k < n; k += U) {
+        if (k > 0 && (k & (lanes - 1)) == 0) places = p.place[std::min(i + k + lane, end - 1)];
+        Packed<T> x[U];
+        int row[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) row[u] = __shfl(places, of + (std::min(k + u, n - 1) & (lanes - 1)), 64);
+#pragma unroll
+        for (int u = 0; u < U; ++u) issue<EIGHTS>(x[u], dout + (long long)row[u] * p.c, col, p.c);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (i + u < end) {
-                const int k = keys[i + u];
-                if (k != key) {
-                    leave(false);
-                    key = k;
-                    continued = false;
-                }
-                settle<EIGHTS>(x[u], col, p.c);
+            settle<EIGHTS>(x[u], col, p.c);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) acc[j] += x[u].get(j);
-            }
-            issue<EIGHTS, false>(x[u], dout + (long long)places[min(i + u + U, end - 1)] * p.c, col, p.c);
+            for (int j = 0; j < 8; ++j) acc[j] += k + u < n ? x[u].get(j) : 0.f;
         }
     }
-    leave(behind == key);
-}
-
-// Rows of tokens that do not occur: zeros.  A wave takes kFill tokens; each of as many lanes searches for its own.
-constexpr int kFill = 16;
-__device__ __forceinline__ void fill_absent(const SumArgs& p) {
-    const int lane = threadIdx.x & 63;
-    const float zero[8] = {};
-    for (long long v0 = ((blockIdx.x - p.sum_blocks) * 4 + (threadIdx.x >> 6)) * kFill; v0 < p.vocab; v0 += (gridDim.x - p.sum_blocks) * 4 * kFill) {
-        const long long v = v0 + (lane & (kFill - 1));
-        int lo = 0, n = p.rows;                    // the first place with a key >= v is among the n + 1 from lo on
-        while (n > 0) {
-            const int half = n >> 1;
-            const bool below = p.key[lo + half] < v;
-            lo = below ? lo + half + 1 : lo;
-            n = below ? n - half - 1 : half;
-        }
-        const unsigned there = (unsigned)__ballot(lo < p.rows && p.key[min(lo, p.rows - 1)] == v);
-        const int most = (int)std::min<long long>(kFill, p.vocab - v0);
-        for (int k = 0; k < most; ++k) {
-            if (there >> k & 1) continue;
-            float* row = p.dtable + (v0 + k) * p.c;
-            for (long long col = lane * 8; col < p.c; col += 512) lc_store8(row + col, zero, p.c - (int)col);
-        }
-    }
-}
-
-template <typename T, bool EIGHTS>
-__global__ void __launch_bounds__(256) embedding_sum_kernel(const SumArgs p) {
-    if (blockIdx.x < p.sum_blocks) sum_piece<T, EIGHTS>(p);
-    else fill_absent(p);
+    if (own < p.c) leave<EIGHTS, ADD>(p, i / kPiece, key, continued, goes_on, own, acc, old);
 }
 
 // Tokens that cross pieces: the lanes of the piece where one begins add up its parts in the order of the pieces.
-template <bool EIGHTS>
+template <bool EIGHTS, bool ADD>
 __global__ void __launch_bounds__(256) embedding_join_kernel(const SumArgs p) {
-    const int lane = threadIdx.x & (p.lanes - 1), each = 256 / p.lanes;
-    const long long block = blockIdx.x / p.tiles;
-    const long long piece = block * each + threadIdx.x / p.lanes;
-    const int col = ((int)(blockIdx.x % p.tiles) * p.lanes + lane) * 8;
-    if (piece + 1 >= p.pieces || col >= p.c) return;
-    const long long end = (piece + 1) * p.len;
-    const int key = p.key[end - 1];
-    if (key >= p.vocab || p.key[end] != key) return;
-    if (piece > 0 && p.key[piece * p.len - 1] == key) return;                     // it began earlier
-    long long lo = piece + 1, n = p.pieces - lo;   // the first piece that does not begin with it
-    while (n > 0) {
-        const long long half = n >> 1;
-        const bool same = p.key[(lo + half) * p.len] == key;
-        lo = same ? lo + half + 1 : lo;
-        n = same ? n - half - 1 : half;
-    }
-    constexpr int U = 8;
+    const int lanes = 1 << p.lane_bits, lane = threadIdx.x & (lanes - 1), of = threadIdx.x & 63 & ~(lanes - 1);
+    const unsigned group = (blockIdx.x * 256u + threadIdx.x) >> p.lane_bits, piece = group / (unsigned)p.tiles, tile = group - piece * (unsigned)p.tiles;
+    if ((long long)piece + 1 >= p.pieces) return;
+    const long long end = ((long long)piece + 1) * kPiece;
+    const int key = p.key[end - 1], behind = p.key[end], start = p.key[end - kPiece], before = piece > 0 ? p.key[end - kPiece - 1] : kNone;
+    if (key >= p.vocab || behind != key || (start == key && before == key)) return;          // (the last: it began earlier)
+    const unsigned long long every = p.lane_bits == 6 ? ~0ull : (1ull << lanes) - 1;
+    const int own = ((int)tile * lanes + lane) * 8, col = std::min(own, EIGHTS ? p.c - 8 : p.c);
+    constexpr int U = 8;                           // parts under way
     float acc[8];
-    Packed<float> x[U];
-    issue<EIGHTS, false>(x[0], p.part + (piece * 2 + 1) * p.c, col, p.c);
+    Packed<float> x[U], old;
+    issue<EIGHTS>(x[0], p.part + ((long long)piece * 2 + 1) * p.c, col, p.c);
+    if constexpr (ADD) issue<EIGHTS>(old, p.dtable + (long long)key * p.c, col, p.c);
     settle<EIGHTS>(x[0], col, p.c);
 #pragma unroll
     for (int j = 0; j < 8; ++j) acc[j] = x[0].get(j);
-    for (long long next = piece + 1; next < lo; next += U) {
+    for (long long next = (long long)piece + 1;;) {       // lanes look at the next pieces' first keys, as many at a time as they are
+        const long long mine = next + lane;
+        const unsigned long long bits = __ballot(mine < p.pieces && p.key[std::min(mine, p.pieces - 1) * kPiece] == key) >> of;
+        const int run = (bits & every) == every ? lanes : __builtin_ctzll(~bits);
+        for (int k = 0; k < run; k += U) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) issue<EIGHTS, false>(x[u], p.part + std::min(next + u, lo - 1) * 2 * p.c, col, p.c);
+            for (int u = 0; u < U; ++u) issue<EIGHTS>(x[u], p.part + (next + std::min(k + u, run - 1)) * 2 * p.c, col, p.c);
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (next + u < lo) {
+            for (int u = 0; u < U; ++u) {
                 settle<EIGHTS>(x[u], col, p.c);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) acc[j] += x[u].get(j);
+                for (int j = 0; j < 8; ++j) acc[j] += k + u < run ? x[u].get(j) : 0.f;
             }
         }
+        next += run;
+        if (run < lanes) break;
     }
-    add_to<EIGHTS>(p.dtable + (long long)key * p.c + col, acc, p.c - col, p.accumulate);
+    if (own >= p.c) return;
+    if constexpr (ADD) {
+        settle<EIGHTS>(old, col, p.c);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[j] += old.get(j);
+    }
+    lc_store8(p.dtable + (long long)key * p.c + own, acc, EIGHTS ? 8 : p.c - own);
 }
 
 // ---------------------------------------------------------------------------------------------- host
 
 constexpr long long kMostBlocks = 1 << 20;
-constexpr long long kMostRows = 1ll << 30;
+constexpr long long kMostRows = 1ll << 25;        // a launch holds fewer than 2^32 threads, and a row has 64 of them at most
 
 lc_status check_desc(const lc_embedding_desc* d) {
     if (!d) return LC_ERR_NULL;
@@ -362,18 +406,17 @@ int lanes_of(int c) {                              // the smallest power of two 
     return lanes;
 }
 
-// How the gradient is made: places of a piece, pieces, and where things lie in the workspace.
+// How the gradient is made, and where things lie in the workspace.
 struct Plan {
-    int len, lanes, tiles, passes, bits, per, sort_blocks;
+    int lanes, tiles, passes, bits, per, sort_blocks;
     long long pieces, part_at, bytes;
 };
 Plan plan_of(const lc_embedding_desc* d) {
     Plan p{};
     const long long rows = d->rows;
-    p.lanes = lanes_of(d->c);
+    p.lanes = std::min(64, lanes_of(d->c));
     p.tiles = (int)(((long long)d->c + p.lanes * 8 - 1) / (p.lanes * 8));
-    p.len = (int)std::min<long long>(kStaged * p.lanes / 256, std::min<long long>(256, std::max<long long>(16, rows / 1024)));
-    p.pieces = (rows + p.len - 1) / p.len;
+    p.pieces = (rows + kPiece - 1) / kPiece;
     if (rows > kRankMost) {
         int bits = 1;
         while (bits < 31 && (1ll << bits) <= d->vocab) ++bits;                     // keys up to vocab
@@ -397,17 +440,17 @@ extern "C" lc_status embedding_fwd(const lc_embedding_desc* desc, const void* ta
     if (!table || !tokens || !out) return LC_ERR_NULL;
     if (lc_off_element(table, desc->table_dtype == LC_BF16 ? 2 : 4) || lc_off_element(out, desc->dtype == LC_BF16 ? 2 : 4) || lc_off_element(tokens, 4)) return LC_ERR_ALIGN;
     const int lanes = lanes_of(desc->c);
-    const LookupArgs a{table, tokens, out, desc->rows, desc->table_ld ? desc->table_ld : desc->c, desc->vocab, desc->c, lanes, desc->scale};
-    const dim3 grid((unsigned)std::min<long long>((desc->rows + 256 / lanes - 1) / (256 / lanes), kMostBlocks));
+    const LookupArgs a{table, tokens, out, desc->rows, desc->table_ld ? desc->table_ld : desc->c, desc->vocab, desc->c, __builtin_ctz(lanes), desc->scale};
+    const long long blocks = (desc->rows + 256 / lanes - 1) / (256 / lanes);
+    const dim3 grid((unsigned)std::min<long long>(blocks <= 1024 ? blocks : (blocks + kRowsAhead - 1) / kRowsAhead, kMostBlocks));
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     lc_begin_call();
-    if (desc->table_dtype == LC_BF16) {
-        if (desc->dtype == LC_BF16) hipLaunchKernelGGL((embedding_fwd_kernel<uint16_t, uint16_t>), grid, dim3(256), 0, stream, a);
-        else hipLaunchKernelGGL((embedding_fwd_kernel<uint16_t, float>), grid, dim3(256), 0, stream, a);
-    } else {
-        if (desc->dtype == LC_BF16) hipLaunchKernelGGL((embedding_fwd_kernel<float, uint16_t>), grid, dim3(256), 0, stream, a);
-        else hipLaunchKernelGGL((embedding_fwd_kernel<float, float>), grid, dim3(256), 0, stream, a);
-    }
+    const auto launch = [&]<typename S, typename T>() {
+        if (desc->c % 8 == 0) hipLaunchKernelGGL((embedding_fwd_kernel<S, T, true>), grid, dim3(256), 0, stream, a);
+        else hipLaunchKernelGGL((embedding_fwd_kernel<S, T, false>), grid, dim3(256), 0, stream, a);
+    };
+    if (desc->table_dtype == LC_BF16) desc->dtype == LC_BF16 ? launch.template operator()<uint16_t, uint16_t>() : launch.template operator()<uint16_t, float>();
+    else desc->dtype == LC_BF16 ? launch.template operator()<float, uint16_t>() : launch.template operator()<float, float>();
     return lc_end_call();
 }
 
@@ -437,11 +480,23 @@ extern "C" lc_status embedding_bwd(const lc_embedding_desc* desc, const int32_t*
     const long long list = (desc->rows * 4 + 255) & ~255ll;
     int* lists[4];
     for (int i = 0; i < 4; ++i) lists[i] = reinterpret_cast<int*>(ws + list * i);
-    SortArgs s{tokens, nullptr, nullptr, lists[0], lists[1], nullptr, (int)desc->rows, desc->vocab, plan.per, 0, plan.bits};
+    // the whole table is set to zero by the launches that sort, in equal shares: what tokens then write is written twice, and the rest costs no search for what is absent and hides the launches' latency
+    // (32768 rows of 2048, 16384 places: by the sums' launch, absent rows alone, 121 us with the lookup, so 117)
+    const long long launches = std::max(1, 2 * plan.passes), fill = accumulate ? 0 : (long long)desc->vocab * desc->c * 4, share = ((fill + launches - 1) / launches + 15) & ~15ll;
+    long long zeroed = 0;
+    SortArgs s{tokens, nullptr, nullptr, lists[0], lists[1], nullptr, (int)desc->rows, desc->vocab, plan.per, 0, plan.bits, 0, dtable, 0};
+    const auto grid_of = [&](int sort_blocks) {
+        s.sort_blocks = sort_blocks;
+        s.zeros = dtable + zeroed / 4;
+        s.zero_bytes = std::min(share, fill - zeroed);
+        zeroed += s.zero_bytes;
+        return dim3((unsigned)(sort_blocks + std::min<long long>((s.zero_bytes + 16 * 1024 * 4 - 1) / (16 * 1024 * 4), 1024)));
+    };
     lc_begin_call();
     int last = 0;                                    // the pair of lists that holds the order
     if (plan.passes == 0) {
-        hipLaunchKernelGGL(embedding_rank_kernel, dim3((unsigned)((desc->rows + 63) / 64)), dim3(1024), 0, stream, s);
+        const dim3 grid = grid_of((int)((desc->rows + 63) / 64));
+        hipLaunchKernelGGL(embedding_rank_kernel, grid, dim3(1024), 0, stream, s);
     } else {
         s.counts = reinterpret_cast<int*>(ws + list * (plan.passes > 1 ? 4 : 2));
         for (int pass = 0; pass < plan.passes; ++pass) {
@@ -452,20 +507,24 @@ extern "C" lc_status embedding_bwd(const lc_embedding_desc* desc, const int32_t*
             s.key = lists[last ? 2 : 0];
             s.place = lists[last ? 3 : 1];
             s.shift = pass * plan.bits;
-            hipLaunchKernelGGL(embedding_count_kernel, dim3((unsigned)plan.sort_blocks), dim3(1024), 0, stream, s);
-            hipLaunchKernelGGL(embedding_move_kernel, dim3((unsigned)plan.sort_blocks), dim3(1024), 0, stream, s);
+            dim3 grid = grid_of(plan.sort_blocks);
+            hipLaunchKernelGGL(embedding_count_kernel, grid, dim3(1024), 0, stream, s);
+            grid = grid_of(plan.sort_blocks);
+            hipLaunchKernelGGL(embedding_move_kernel, grid, dim3(1024), 0, stream, s);
         }
     }
-    const int each = 256 / plan.lanes;
-    SumArgs a{lists[last ? 2 : 0], lists[last ? 3 : 1], dout, dtable, reinterpret_cast<float*>(ws + plan.part_at), plan.pieces, (int)desc->rows, desc->vocab, desc->c,
-              plan.len, accumulate != 0, plan.lanes, plan.tiles, (plan.pieces + each - 1) / each * plan.tiles, desc->scale};
-    const long long fill = accumulate ? 0 : std::min<long long>(kMostBlocks, ((long long)desc->vocab + 4 * kFill - 1) / (4 * kFill));
-    const dim3 grid((unsigned)(a.sum_blocks + fill));
-    const auto launch = [&]<bool EIGHTS>() {
-        if (desc->dtype == LC_BF16) hipLaunchKernelGGL((embedding_sum_kernel<uint16_t, EIGHTS>), grid, dim3(256), 0, stream, a);
-        else hipLaunchKernelGGL((embedding_sum_kernel<float, EIGHTS>), grid, dim3(256), 0, stream, a);
-        if (plan.pieces > 1) hipLaunchKernelGGL((embedding_join_kernel<EIGHTS>), dim3((unsigned)a.sum_blocks), dim3(256), 0, stream, a);
+    const SumArgs a{lists[last ? 2 : 0], lists[last ? 3 : 1], dout, dtable, reinterpret_cast<float*>(ws + plan.part_at), plan.pieces, (int)desc->rows, desc->vocab, desc->c,
+                    __builtin_ctz(plan.lanes), plan.tiles, desc->scale};
+    const auto launch = [&]<typename T, bool EIGHTS, bool ADD>() {
+        const auto blocks = [](long long threads) { return dim3((unsigned)((threads + 255) / 256)); };
+        if (plan.lanes < 64) hipLaunchKernelGGL((embedding_sum_narrow_kernel<T, EIGHTS, ADD>), blocks(desc->rows * plan.lanes), dim3(256), 0, stream, a);
+        else hipLaunchKernelGGL((embedding_sum_kernel<T, EIGHTS, ADD, 8>), blocks(plan.pieces * plan.tiles * 64), dim3(256), 0, stream, a);
+        if (plan.pieces > 1) hipLaunchKernelGGL((embedding_join_kernel<EIGHTS, ADD>), blocks(plan.pieces * plan.tiles * plan.lanes), dim3(256), 0, stream, a);
     };
-    desc->c % 8 == 0 ? launch.template operator()<true>() : launch.template operator()<false>();
+    const auto with_type = [&]<typename T>() {
+        if (desc->c % 8 == 0) accumulate ? launch.template operator()<T, true, true>() : launch.template operator()<T, true, false>();
+        else accumulate ? launch.template operator()<T, false, true>() : launch.template operator()<T, false, false>();
+    };
+    desc->dtype == LC_BF16 ? with_type.template operator()<uint16_t>() : with_type.template operator()<float>();
     return lc_end_call();
 }
