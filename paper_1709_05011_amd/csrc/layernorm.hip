@@ -2,8 +2,8 @@
 //
 // total = x + residual, mean and variance over the row, rstd = 1/sqrt(variance + eps), n = (total - mean) * rstd, y = n * gamma + beta; with a = dy * gamma,
 // dx = rstd * (a - mean(a) - n * mean(a * n)) + dtotal, dgamma = sum over rows of dy * n, dbeta = sum over rows of dy.  Bound by memory, as the RMS norm (rmsnorm.hip), whose
-// division of rows over threads it has: a row is read once into registers.  The sum gives a first mean; deviations from it are summed with their squares, and what their sum says
-// the first mean lacks is taken off both, so that a mean far from zero costs no places (one more sum over registers instead of a second rounding of the mean).
+// division of rows over threads it has: a row is read once into registers.  A wave's sum gives a mean near its own; deviations from it are summed with their squares, and what their sum says
+// that mean lacks is taken off both, so that a mean far from zero costs no places; waves are then joined by their means' differences, with one barrier a row.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -38,17 +38,17 @@ __device__ __forceinline__ double inverse_root(double x) {
     return ldexp(fabs(better) < INFINITY ? better : r, -half);         // (x = 0 or infinite: the estimate is the value)
 }
 
-// What a row's deviations from the first mean, `first`, say: what that mean lacks, and the inverse deviation.  All in units of 2^e.
+// What deviations from a mean near the row's, `first`, say: `lack`, what the row's mean is above it, and the inverse deviation.  All in units of 2^e.
 struct Moments {
     float first, lack, n_scale;      // n = (total / 2^e - first - lack) * n_scale
     double mean, rstd;
 };
-__device__ __forceinline__ Moments moments_of(const LayerArgs& p, float first, float sum, float squares, int e) {
+__device__ __forceinline__ Moments moments_of(const LayerArgs& p, float first, float lack, float squares, int e) {
     Moments m;
-    const double lack = (double)sum * p.inv_c, var = fmax(fma((double)squares, p.inv_c, -lack * lack), (double)squares * 0.0);      // (a NaN stays one)
+    const double var = fmax((double)squares * p.inv_c, (double)squares * 0.0);         // (rounding leaves nothing under zero; a NaN stays one)
     m.first = first;
-    m.lack = (float)lack;
-    m.mean = ldexp((double)first + lack, e);
+    m.lack = lack;
+    m.mean = ldexp((double)first + (double)lack, e);
     m.rstd = inverse_root(ldexp(var, 2 * e) + (double)p.eps);
     m.n_scale = (float)ldexp(m.rstd, e);
     return m;
@@ -92,7 +92,7 @@ __device__ __forceinline__ void row_sums(float& a, float& b, int waves, float (*
     }
 }
 
-// A block per row (rows dealt round the grid), or LANES lanes of a wave for a narrow one; all of a row's loads are under way at once and it is read once.  NT, ENDS: as the RMS norm's.
+// A block walks rows blockIdx, blockIdx + gridDim, ... (LANES: narrow ones, several of a wave), with scale and shift in its registers and the next row's loads under way.  NT, ENDS: as the RMS norm's.
 template <typename T, int CH, bool NT, Ends ENDS, int LANES = 0>
 __global__ void __launch_bounds__(LANES ? kNarrowThreads : kMostWaves * 64) layernorm_fwd_kernel(const LayerArgs p) {
     __shared__ float red[2][7][kMostWaves];
@@ -100,16 +100,26 @@ __global__ void __launch_bounds__(LANES ? kNarrowThreads : kMostWaves * 64) laye
     const int tid = Of::tid(), c = p.c, waves = blockDim.x >> 6, threads = LANES ? LANES : blockDim.x;
     const auto column = [=](int i) { return (i * threads + tid) * 8; };
     const auto inside = [&](int i) { return ENDS == kWhole ? 8 : ENDS == kEights ? (column(i) < c ? 8 : 0) : c - column(i); };
+    Packed<T> px[CH], pr[CH], nx[CH], nr[CH];
+    Packed<float> pg[CH], pb[CH];
+    const auto issue = [&](long long row) __attribute__((always_inline)) {
+        lc_issue8<ENDS, NT>(nx, static_cast<const T*>(p.x) + row * p.x_ld, column, c);
+        if (p.r) lc_issue8<ENDS, NT>(nr, static_cast<const T*>(p.r) + row * p.r_ld, column, c);
+    };
+    if (Of::first() < p.rows) issue(Of::first());
+    lc_issue8<ENDS>(pg, p.gamma, column, c);
+    if (p.beta) lc_issue8<ENDS>(pb, p.beta, column, c);
+    lc_settle8<ENDS>(pg, column, c);
+    if (p.beta) lc_settle8<ENDS>(pb, column, c);
     int parity = 0;
     for (long long row = Of::first(); row < p.rows; row += Of::step(), parity ^= 1) {
-        const T* x = static_cast<const T*>(p.x) + row * p.x_ld;
-        Packed<T> px[CH], pr[CH];
-        Packed<float> pg[CH], pb[CH];
         float h[CH][8];
-        lc_issue8<ENDS, NT>(px, x, column, c);
-        if (p.r) lc_issue8<ENDS, NT>(pr, static_cast<const T*>(p.r) + row * p.r_ld, column, c);
-        lc_issue8<ENDS>(pg, p.gamma, column, c);
-        if (p.beta) lc_issue8<ENDS>(pb, p.beta, column, c);
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            px[i] = nx[i];
+            pr[i] = nr[i];
+        }
+        if (row + Of::step() < p.rows) issue(row + Of::step());
         lc_settle8<ENDS>(px, column, c);
         if (p.r) {
             lc_settle8<ENDS>(pr, column, c);
@@ -128,12 +138,14 @@ __global__ void __launch_bounds__(LANES ? kNarrowThreads : kMostWaves * 64) laye
 #pragma unroll
             for (int i = 0; i < CH; ++i) lc_store8<NT>(t + column(i), h[i], inside(i));
         }
-        float s = 0.f;
+        const auto sum_of = [&]() __attribute__((always_inline)) {
+            float s = 0.f;
 #pragma unroll
-        for (int i = 0; i < CH; ++i)
+            for (int i = 0; i < CH; ++i)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) s += h[i][j];
-        const float first = (float)((double)row_sum<Of>(s, waves, red[parity][0]) * p.inv_c);
+                for (int j = 0; j < 8; ++j) s += h[i][j];
+            return s;
+        };
         const auto deviations = [&](float from, float& sum, float& squares) __attribute__((always_inline)) {        // h becomes its deviation; what lies past the row stays 0
             sum = squares = 0.f;
 #pragma unroll
@@ -145,9 +157,43 @@ __global__ void __launch_bounds__(LANES ? kNarrowThreads : kMostWaves * 64) laye
                     squares = fmaf(h[i][j], h[i][j], squares);
                 }
         };
-        float sum, squares;
-        deviations(first, sum, squares);
-        row_sums<LANES>(sum, squares, waves, red[parity] + 1);
+        float first, sum, squares;
+        if constexpr (LANES == 0) {
+            // deviations from the wave's own mean; a block's waves are joined as sums of squares around means are: by what each mean is off the first wave's
+            const auto columns_of = [&](int w) __attribute__((always_inline)) {
+                int n = 0;
+#pragma unroll
+                for (int i = 0; i < CH; ++i) n += ENDS == kWhole ? 512 : min(max(c - (i * threads + w * 64) * 8, 0), 512);
+                return (float)n;
+            };
+            const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+            first = lc_wave_sum(sum_of()) * __builtin_amdgcn_rcpf(columns_of(wave));
+            deviations(first, sum, squares);
+            sum = lc_wave_sum(sum);
+            squares = lc_wave_sum(squares);
+            if (waves > 1) {
+                if (lane == 0) {
+                    red[parity][0][wave] = first;
+                    red[parity][1][wave] = sum;
+                    red[parity][2][wave] = squares;
+                }
+                __syncthreads();
+                const bool in = lane < waves;
+                const float n = columns_of(lane), inv_n = __builtin_amdgcn_rcpf(n), base = red[parity][0][0], s = in ? red[parity][1][lane] : 0.f;
+                const float off = in ? fmaf(s, inv_n, red[parity][0][lane] - base) : 0.f, all = (float)((double)lc_wave_sum(in ? off * n : 0.f) * p.inv_c), d = off - all;
+                squares = lc_wave_sum(in ? fmaf(n * d, d, fmaf(-s * s, inv_n, red[parity][2][lane])) : 0.f);
+                sum = (base - first) + all;         // the row's mean less the wave's
+            } else {
+                sum *= (float)p.inv_c;
+                squares = fmaf(-sum * sum, (float)c, squares);
+            }
+        } else {
+            first = (float)((double)row_sum<Of>(sum_of(), waves, red[parity][0]) * p.inv_c);
+            deviations(first, sum, squares);
+            row_sums<LANES>(sum, squares, waves, red[parity] + 1);
+            sum *= (float)p.inv_c;
+            squares = fmaf(-sum * sum, (float)c, squares);
+        }
         Moments m;
         if (squares_serve(p, squares)) {
             m = moments_of(p, first, sum, squares, 0);
@@ -179,14 +225,13 @@ __global__ void __launch_bounds__(LANES ? kNarrowThreads : kMostWaves * 64) laye
             const float from = (float)((double)row_sum<Of>(again, waves, red[parity][4]) * p.inv_c);
             deviations(from, sum, squares);
             row_sums<LANES>(sum, squares, waves, red[parity] + 5);
-            m = moments_of(p, from, sum, squares, e);
+            sum *= (float)p.inv_c;
+            m = moments_of(p, from, sum, fmaf(-sum * sum, (float)c, squares), e);
         }
         if (tid == 0) {
             if (p.mean) p.mean[row] = (float)m.mean;
             if (p.rstd) p.rstd[row] = (float)m.rstd;
         }
-        lc_settle8<ENDS>(pg, column, c);
-        if (p.beta) lc_settle8<ENDS>(pb, column, c);
         T* y = static_cast<T*>(p.y) + row * (long long)c;
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
@@ -264,7 +309,8 @@ __global__ void __launch_bounds__(1024) layernorm_fwd_wide_kernel(const LayerArg
             deviations(first, e);
             row_sums<0>(sum, squares, WAVES, red[parity] + 5);
         }
-        const Moments m = moments_of(p, first, sum, squares, e);
+        sum *= (float)p.inv_c;
+        const Moments m = moments_of(p, first, sum, fmaf(-sum * sum, (float)c, squares), e);
         if (tid == 0) {
             if (p.mean) p.mean[row] = (float)m.mean;
             if (p.rstd) p.rstd[row] = (float)m.rstd;
@@ -474,16 +520,22 @@ lc_status check_desc(const lc_layernorm_desc* d) {
     return LC_OK;
 }
 
+// Blocks of the forward pass: as many waves as the chip holds at once.  us, bf16, with 4096, 8192 and a block a row: 8192 x 4096 48.2, 48.6, 49.4, 2048 x 16384 51, 51, 59, 5000 x 5000 53, 48, 53; fp32 7000 x 4096 81, 83,
+// 86; 3000 x 10240 122, 117, 117.  (Scale and shift read again for every row: 53 for the first.)
+constexpr int kFwdWaves = 8192;
+long long fwd_blocks(int waves) { return std::max(256, kFwdWaves / waves); }
+
 template <typename T, int CH, bool NT>
 void launch_fwd(const LayerArgs& a, hipStream_t stream) {
-    const dim3 grid((unsigned)std::min(a.rows, kMostBlocks)), block((a.c + 512 * CH - 1) / (512 * CH) * 64);
+    const int waves = (a.c + 512 * CH - 1) / (512 * CH);
+    const dim3 grid((unsigned)std::min<long long>(a.rows, fwd_blocks(waves))), block(waves * 64);
     if (a.c % (512 * CH) == 0) hipLaunchKernelGGL((layernorm_fwd_kernel<T, CH, NT, kWhole>), grid, block, 0, stream, a);
     else if (a.c % 8 == 0) hipLaunchKernelGGL((layernorm_fwd_kernel<T, CH, NT, kEights>), grid, block, 0, stream, a);
     else if constexpr (CH * sizeof(T) < 8) hipLaunchKernelGGL((layernorm_fwd_kernel<T, CH, NT, kAny>), grid, block, 0, stream, a);
 }
 template <typename T, bool NT, int LANES>
 void launch_fwd_narrow(const LayerArgs& a, hipStream_t stream) {
-    const dim3 grid((unsigned)std::min((a.rows + Rows<LANES>::kEach - 1) / Rows<LANES>::kEach, kMostBlocks)), block(kNarrowThreads);
+    const dim3 grid((unsigned)std::min<long long>((a.rows + Rows<LANES>::kEach - 1) / Rows<LANES>::kEach, fwd_blocks(4))), block(kNarrowThreads);
     if (a.c % 8 == 0) hipLaunchKernelGGL((layernorm_fwd_kernel<T, 1, NT, kEights, LANES>), grid, block, 0, stream, a);
     else hipLaunchKernelGGL((layernorm_fwd_kernel<T, 1, NT, kAny, LANES>), grid, block, 0, stream, a);
 }

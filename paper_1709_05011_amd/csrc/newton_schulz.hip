@@ -1,10 +1,10 @@
 // Newton-Schulz steps that orthogonalise matrices, and the optimizer's step around them (momentum, orthogonalised update, decay), for gfx950.
 //
 // X = u / (|u| + eps), then `iterations` times X <- a X + (b A + c A A) X with A = X X^T on the shorter side: the singular values go through a x + b x^3 + c x^5, which takes all but the
-// smallest near 1.  Three products a step, A and B = b A + c A A symmetric: of those only tiles on and below the diagonal are made and written twice.
+// smallest near 1.  Three products a step, A and B = a I + b A + c A A symmetric: of those only tiles on and below the diagonal are made and written twice.
 //
-// Values are pairs of fp16, hi = x rounded, lo = (x - hi) rounded, 22 bits, scaled by 2^12: singular values stay below 1.21, hence every value of X below 1.21, of A below 1.46 and of B below 2.81,
-// and fp16's range leaves room for five times that; a product is three matrix instructions, lo hi + hi lo + hi hi, summed in fp32.  One fp16 (or bf16) value each, a third of the instructions, was simulated in 64 bits and
+// Values are pairs of fp16, hi = x rounded, lo = (x - hi) rounded, 22 bits, scaled by 2^12: singular values stay below 1.21, hence every value of X below 1.21, of A below 1.46 and of B below 3.45,
+// and fp16's range leaves room for more than four times that; a product is three matrix instructions, lo hi + hi lo + hi hi, summed in fp32.  One fp16 (or bf16) value each, a third of the instructions, was simulated in 64 bits and
 // left: small singular values grow by up to 3.4445 a step, and the first rounding with them: errors of 1.4e-3 (bf16 1.3e-2) on a random matrix and 1.4e-2 (0.11) on one of rank 8 and noise, pairs 3e-7 to 3e-6, fp32 products
 // 1e-6 to 6e-5.
 //
@@ -222,7 +222,8 @@ __global__ void __launch_bounds__(256) ns_split_kernel(const Args<TABLE> args) {
     }
 }
 
-// What a product makes: A = X X^T; B = b A + c A A; X <- a X + B X, both ways round; the same as the result.
+// What a product makes: A = X X^T; B = a I + b A + c A A; X <- B X, both ways round; the same as the result.  (a on B's diagonal costs X a rounding of 2^-22, as its own is, and saves reading X once more:
+// ResNet-50's filters 118 to 130 us a product of X with it added at the end.)
 enum Product { kGram, kSquare, kNext, kLast };
 
 template <Product KIND>
@@ -402,24 +403,18 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) ns_product_kernel(const Args<
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = p[e];
             if (gi < M && gj < columns) {
-                if constexpr (KIND == kGram) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] *= kInvScale;
-                    store_pairs(t.a() + pair_at(gi, gj, M), v);
-                } else {
+                if constexpr (KIND == kSquare) {
                     float o[8];
-                    load_pairs(o, KIND == kSquare ? t.a() + pair_at(gi, gj, M) : t.x() + pair_at(gi, gj, N));
+                    load_pairs(o, t.a() + pair_at(gi, gj, M));
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] = KIND == kSquare ? fmaf(kC * kInvScale, v[e], kB * o[e]) : fmaf(kInvScale, v[e], kA * o[e]);
-                    if constexpr (KIND == kSquare) {
-                        store_pairs(t.b() + pair_at(gi, gj, M), v);
-                    } else if constexpr (KIND == kNext) {
-                        store_pairs(t.x() + pair_at(gi, gj, N), v);
-                    } else {
+                    for (int e = 0; e < 8; ++e) v[e] = fmaf(kC * kInvScale, v[e], kB * o[e]) + (gi == gj + e ? kA * kScale : 0.f);
+                    store_pairs(t.b() + pair_at(gi, gj, M), v);
+                } else {
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) v[e] *= kInvScale;
-                        if (along) leave(gi, gj, v);
-                    }
+                    for (int e = 0; e < 8; ++e) v[e] *= KIND == kLast ? kInvScale * kInvScale : kInvScale;
+                    if constexpr (KIND == kGram) store_pairs(t.a() + pair_at(gi, gj, M), v);
+                    else if constexpr (KIND == kNext) store_pairs(t.x() + pair_at(gi, gj, N), v);
+                    else if (along) leave(gi, gj, v);
                 }
             }
             if (turned) {
