@@ -100,6 +100,27 @@ __device__ __forceinline__ void load4(float* to, const uint16_t* p, int n) {
     for (int j = 0; j < 4; ++j) to[j] = __uint_as_float(j & 1 ? x[j >> 1] & 0xffff0000u : x[j >> 1] << 16);
 }
 
+// The first n of four values (none for n <= 0).
+__device__ __forceinline__ void put4(float* p, const float* v, int n) {
+    if (n >= 4) {
+        lc_store16(p, lc_u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])});
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (j < n) p[j] = v[j];
+    }
+}
+__device__ __forceinline__ void put4(uint16_t* p, const float* v, int n) {
+    const u32x2 x = {lc_bf16x2_rne(v[0], v[1]), lc_bf16x2_rne(v[2], v[3])};
+    if (n >= 4) {
+        *reinterpret_cast<u32x2_any*>(p) = x;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (j < n) p[j] = (uint16_t)(x[j >> 1] >> (16 * (j & 1)));
+    }
+}
+
 // The momentum's update and the sum of squares, in double, of what is orthogonalised: one block a chunk.
 template <typename T, bool MUON, int TABLE>
 __global__ void __launch_bounds__(256) ns_squares_kernel(const Args<TABLE> args) {
@@ -125,12 +146,7 @@ __global__ void __launch_bounds__(256) ns_squares_kernel(const Args<TABLE> args)
                 m[j] = fmaf(mu, m[j], g);
                 u[j] = args.s.nesterov ? fmaf(mu, m[j], g) : m[j];
             }
-            if (n == 4) {
-                lc_store16(t.m + at, lc_u32x4{__float_as_uint(m[0]), __float_as_uint(m[1]), __float_as_uint(m[2]), __float_as_uint(m[3])});
-            } else {
-                for (int j = 0; j < 4; ++j)
-                    if (j < n) t.m[at + j] = m[j];
-            }
+            put4(t.m + at, m, n);
         } else {
             const unsigned row = (unsigned)v / per_row, col = ((unsigned)v - row * per_row) * 4;
             load4(u, static_cast<const T*>(t.in) + (long long)row * t.ld + col, t.cols - (int)col);
@@ -145,16 +161,28 @@ __global__ void __launch_bounds__(256) ns_squares_kernel(const Args<TABLE> args)
     if (threadIdx.x == 0) reinterpret_cast<double*>(t.base)[part] = (red[0] + red[1]) + (red[2] + red[3]);
 }
 
+// Four values as pairs: two conversions at a time, and the rest by an operation that takes hi as it is.
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ void split4(const float* v, f16x4* hi, f16x4* lo) {
+#pragma unroll
+    for (int j = 0; j < 4; j += 2) {
+        const f16x2 h = __builtin_convertvector((f32x2{v[j], v[j + 1]}), f16x2);
+        const f16x2 l = __builtin_convertvector((f32x2{fmaf((float)h[0], -1.f, v[j]), fmaf((float)h[1], -1.f, v[j + 1])}), f16x2);
+        (*hi)[j] = h[0];
+        (*hi)[j + 1] = h[1];
+        (*lo)[j] = l[0];
+        (*lo)[j + 1] = l[1];
+    }
+}
 // Eight scaled values as pairs: hi in the first 16 bytes' place, lo 64 bytes behind.
 __device__ __forceinline__ void store_pairs(unsigned char* p, const float* v) {
-    f16x8 hi, lo;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        hi[j] = (_Float16)v[j];
-        lo[j] = (_Float16)(v[j] - (float)hi[j]);
-    }
-    *reinterpret_cast<f16x8*>(p) = hi;
-    *reinterpret_cast<f16x8*>(p + 64) = lo;
+    f16x4 hi[2], lo[2];
+    split4(v, hi, lo);
+    split4(v + 4, hi + 1, lo + 1);
+    *reinterpret_cast<f16x8*>(p) = __builtin_shufflevector(hi[0], hi[1], 0, 1, 2, 3, 4, 5, 6, 7);
+    *reinterpret_cast<f16x8*>(p + 64) = __builtin_shufflevector(lo[0], lo[1], 0, 1, 2, 3, 4, 5, 6, 7);
 }
 __device__ __forceinline__ void load_pairs(float* v, const unsigned char* p) {
     const f16x8 hi = *reinterpret_cast<const f16x8*>(p), lo = *reinterpret_cast<const f16x8*>(p + 64);
@@ -441,6 +469,232 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) ns_product_kernel(const Args<
     }
 }
 
+// ---------------------------------------------------------------------------------------------- small matrices
+
+// Sides up to 64 and 256: a block takes a matrix through all steps in LDS (X both ways round and A, 144 KB), where launches for each product would be nearly all of the time (twelve matrices of 64 x 64 and 64 x 256 80 us).
+constexpr int kSmallM = 64, kSmallN = 256, kSmallThreads = 512;
+bool small(int M, int N) { return M <= kSmallM && N <= kSmallN; }
+
+// A row in LDS: blocks of 32 columns of 128 bytes (16-byte pieces: 0 to 3 hi, 4 to 7 lo).  Sixteen rows' pieces lie on all banks: rows of an odd number of blocks begin on either half of them by themselves, others have
+// their blocks swapped in pairs from eight rows to the next; pieces are turned by the row.  Rows 16 apart differ by the rows' bytes alone.
+struct LdsRow {
+    int base, turn, flip;
+    __device__ __forceinline__ LdsRow(int row, int blocks) : base(row * blocks * 128), turn(((blocks & 1 ? row >> 1 : row) & 7) * 16), flip(blocks & 1 ? 0 : row * 16 & 128) {}
+    __device__ __forceinline__ int block(int kb) const { return base + (kb * 128 ^ flip); }
+    __device__ __forceinline__ int piece(int n) const { return n * 16 ^ turn; }                                       // within a block
+    __device__ __forceinline__ int hi(int col) const { return block(col >> 5) + piece((col & 31) >> 3) + (col & 7) * 2; }
+    __device__ __forceinline__ int lo(int col) const { return block(col >> 5) + piece(4 + ((col & 31) >> 3)) + (col & 7) * 2; }
+};
+
+template <typename T, bool MUON, int TABLE>
+__global__ void __launch_bounds__(kSmallThreads) ns_small_kernel(const Args<TABLE> args, int iterations) {
+    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+    __shared__ double red[8];
+    const Mat& t = args.t[blockIdx.x];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int M = t.M, N = t.N, mb = M / 32, nb = N / 32;          // blocks of 32 columns of a row of A and of the transpose, of X
+    unsigned char* const X = smem;
+    unsigned char* const XT = smem + kSmallM * kSmallN * 4;
+    unsigned char* const A = XT + kSmallM * kSmallN * 4;
+    for (int i = tid; i < 2 * kSmallM * kSmallN * 4 / 16; i += kSmallThreads) *reinterpret_cast<lc_u32x4*>(smem + i * 16) = lc_u32x4{0u, 0u, 0u, 0u};
+    // the matrix, its momentum's update and its norm
+    // (a wave takes 16 rows of 16 columns a time: their values the other way round lie on neighbouring banks)
+    constexpr int kVectors = kSmallM * kSmallN / 4 / kSmallThreads;
+    const int wide = (t.cols + 15) / 16;
+    const float gs = args.s.grad_scale ? *args.s.grad_scale : 1.f, mu = args.s.momentum;
+    float u[kVectors][4], m[kVectors][4];
+    int row_of[kVectors], col_of[kVectors], count_of[kVectors];
+#pragma unroll
+    for (int k = 0; k < kVectors; ++k) {
+        const int part = wave + 8 * k, down = part / wide;
+        row_of[k] = down * 16 + (lane & 15);
+        col_of[k] = (part - down * wide) * 16 + (lane >> 4) * 4;
+        count_of[k] = row_of[k] < t.rows ? std::min(4, t.cols - col_of[k]) : 0;
+        const int n = count_of[k];
+        load4(u[k], static_cast<const T*>(t.in) + (n > 0 ? row_of[k] * t.ld + col_of[k] : 0), n);
+        if constexpr (MUON) load4(m[k], t.m + (n > 0 ? row_of[k] * t.cols + col_of[k] : 0), n);
+    }
+    double sum = 0.0;
+#pragma unroll
+    for (int k = 0; k < kVectors; ++k) {
+        if constexpr (MUON) {
+            const int row = row_of[k], col = col_of[k], n = count_of[k];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float g = u[k][j] * gs;
+                m[k][j] = fmaf(mu, m[k][j], g);
+                u[k][j] = args.s.nesterov ? fmaf(mu, m[k][j], g) : m[k][j];
+            }
+            put4(t.m + row * t.cols + col, m[k], n);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sum = fma((double)u[k][j], (double)u[k][j], sum);
+    }
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
+    if (lane == 0) red[wave] = sum;
+    __syncthreads();
+    sum = ((red[0] + red[1]) + (red[2] + red[3])) + ((red[4] + red[5]) + (red[6] + red[7]));
+    const double inv = sum == 0.0 ? 0.0 : (double)kScale / (sqrt(sum) + (double)args.s.eps);
+    unsigned char* const along = t.tall ? XT : X;
+    unsigned char* const turned = t.tall ? X : XT;
+    const int ab = t.tall ? mb : nb, tb = t.tall ? nb : mb;
+#pragma unroll
+    for (int k = 0; k < kVectors; ++k) {
+        const int row = row_of[k], col = col_of[k];
+        f16x4 hi, lo;                                             // (columns past the matrix are zeros)
+        float x[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = (float)((double)u[k][j] * inv);
+        split4(x, &hi, &lo);
+        if (count_of[k] > 0) {
+            const LdsRow to(row, ab);
+            *reinterpret_cast<f16x4*>(along + to.hi(col)) = hi;
+            *reinterpret_cast<f16x4*>(along + to.lo(col)) = lo;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const LdsRow turn(col + j, tb);
+                *reinterpret_cast<_Float16*>(turned + turn.hi(row)) = hi[j];
+                *reinterpret_cast<_Float16*>(turned + turn.lo(row)) = lo[j];
+            }
+        }
+    }
+    __syncthreads();
+
+    // rows P[i] times rows Q[j] of pieces of 16 x 16, COUNT of them a time: the rows of one operand are the same, of the other `far` rows further for each; a lane then holds four neighbouring i of one j
+    int lr = lane & 15, fp = lane >> 4;
+    // (with `other` the same the other way round as well, a lane holding four neighbouring j of one i)
+    const auto products = [&]<int COUNT, bool SAME_P>(std::integral_constant<int, COUNT>, std::integral_constant<bool, SAME_P>, f32x4 (&acc)[COUNT], f32x4* other,
+                                                     const unsigned char* P, int i0, const unsigned char* Q, int j0, int far, int count, int blocks) __attribute__((always_inline)) {
+        const LdsRow row((SAME_P ? i0 : j0) + lr, blocks), first((SAME_P ? j0 : i0) + lr, blocks);
+        const unsigned char* const one = (SAME_P ? P : Q) + row.base;
+        const unsigned char* const more = (SAME_P ? Q : P) + first.base;
+        const int hi = row.piece(fp), lo = row.piece(4 + fp), his = first.piece(fp), los = first.piece(4 + fp), apart = far * blocks * 128;
+#pragma unroll
+        for (int q = 0; q < COUNT; ++q) {
+            acc[q] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if constexpr (SAME_P) other[q] = acc[q];
+        }
+        const auto block = [&]<int BLOCKS>(std::integral_constant<int, BLOCKS>, int kb) __attribute__((always_inline)) {       // that many blocks' pieces read before the first product
+            f16x8 h[BLOCKS], l[BLOCKS], hs[BLOCKS][COUNT], ls[BLOCKS][COUNT];
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b) {
+                const unsigned char *at = one + ((kb + b) * 128 ^ row.flip), *ats = more + ((kb + b) * 128 ^ first.flip);
+                h[b] = *reinterpret_cast<const f16x8*>(at + hi);
+                l[b] = *reinterpret_cast<const f16x8*>(at + lo);
+#pragma unroll
+                for (int q = 0; q < COUNT; ++q) {
+                    const unsigned char* const from = ats + std::min(q, count - 1) * apart;
+                    hs[b][q] = *reinterpret_cast<const f16x8*>(from + his);
+                    ls[b][q] = *reinterpret_cast<const f16x8*>(from + los);
+                }
+            }
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b) {
+#pragma unroll
+                for (int q = 0; q < COUNT; ++q) acc[q] = SAME_P ? multiply(l[b], hs[b][q], acc[q]) : multiply(ls[b][q], h[b], acc[q]);
+#pragma unroll
+                for (int q = 0; q < COUNT; ++q) acc[q] = SAME_P ? multiply(h[b], ls[b][q], acc[q]) : multiply(hs[b][q], l[b], acc[q]);
+#pragma unroll
+                for (int q = 0; q < COUNT; ++q) acc[q] = SAME_P ? multiply(h[b], hs[b][q], acc[q]) : multiply(hs[b][q], h[b], acc[q]);
+                if constexpr (SAME_P) {                           // (the same products in the same order: the same bits)
+#pragma unroll
+                    for (int q = 0; q < COUNT; ++q) other[q] = multiply(hs[b][q], l[b], other[q]);
+#pragma unroll
+                    for (int q = 0; q < COUNT; ++q) other[q] = multiply(ls[b][q], h[b], other[q]);
+#pragma unroll
+                    for (int q = 0; q < COUNT; ++q) other[q] = multiply(hs[b][q], h[b], other[q]);
+                }
+            }
+        };
+        int kb = 0;
+        if constexpr (COUNT <= 2) {
+            for (; kb + 4 <= blocks; kb += 4) block(std::integral_constant<int, 4>{}, kb);
+        }
+        for (; kb < blocks; ++kb) block(std::integral_constant<int, 1>{}, kb);
+    };
+    const auto store4 = [&](unsigned char* hi_to, unsigned char* lo_to, const f32x4& v) __attribute__((always_inline)) {
+        const float f[4] = {v[0], v[1], v[2], v[3]};
+        f16x4 hi, lo;
+        split4(f, &hi, &lo);
+        *reinterpret_cast<f16x4*>(hi_to) = hi;
+        *reinterpret_cast<f16x4*>(lo_to) = lo;
+    };
+    // pieces of a wave: of A column wave % across, rows from wave / across on; of X row wave % across, columns likewise
+    constexpr int kSquares = kSmallM / 16 * (kSmallM / 16) / 8, kPieces = kSmallM / 16 * (kSmallN / 16) / 8;
+    const int across = M / 16, step = 8 / across, own = wave & (across - 1), from = wave / across;
+    const int squares = std::max(0, (across - from + step - 1) / step), pieces = std::max(0, (N / 16 - from + step - 1) / step);
+    const std::integral_constant<int, kSquares> few;
+    const std::integral_constant<int, kPieces> many;
+    for (int it = 0; it < iterations; ++it) {
+        asm volatile("" : "+v"(lr), "+v"(fp));                  // (addresses are made anew: kept over the steps they are more than the registers hold)
+        f32x4 s[kSquares], x[kPieces], y[kPieces];
+        const LdsRow col_a(own * 16 + lr, mb), row_x(own * 16 + lr, nb), row_t(from * 16 + lr, mb);
+        if (squares) {
+            products(few, std::false_type{}, s, nullptr, X, from * 16, X, own * 16, step * 16, squares, nb);
+#pragma unroll
+            for (int q = 0; q < kSquares; ++q)
+                if (q < squares) store4(A + col_a.hi((from + q * step) * 16 + fp * 4), A + col_a.lo((from + q * step) * 16 + fp * 4), s[q] * kInvScale);      // (symmetric: the column's place)
+        }
+        __syncthreads();
+        if (squares) {
+            products(few, std::false_type{}, s, nullptr, A, from * 16, A, own * 16, step * 16, squares, mb);
+#pragma unroll
+            for (int q = 0; q < kSquares; ++q) {
+                const int row = own * 16 + lr, col = (from + std::min(q, squares - 1) * step) * 16 + fp * 4;
+                const f16x4 hi = *reinterpret_cast<const f16x4*>(A + col_a.hi(col)), lo = *reinterpret_cast<const f16x4*>(A + col_a.lo(col));
+#pragma unroll
+                for (int r = 0; r < 4; ++r) s[q][r] = fmaf(kC * kInvScale, s[q][r], kB * ((float)hi[r] + (float)lo[r])) + (row == col + r ? kA * kScale : 0.f);
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < kSquares; ++q)
+            if (q < squares) store4(A + col_a.hi((from + q * step) * 16 + fp * 4), A + col_a.lo((from + q * step) * 16 + fp * 4), s[q]);
+        __syncthreads();
+        if (pieces) products(many, std::true_type{}, x, y, A, own * 16, XT, from * 16, step * 16, pieces, mb);
+        __syncthreads();
+        const bool last = it + 1 == iterations;
+        const int i0 = own * 16 + fp * 4;
+        if (!last) {
+#pragma unroll
+            for (int q = 0; q < kPieces; ++q) {
+                if (q < pieces) {
+                    store4(XT + row_t.hi(i0) + q * step * 16 * mb * 128, XT + row_t.lo(i0) + q * step * 16 * mb * 128, x[q] * kInvScale);
+                    store4(X + row_x.hi((from + q * step) * 16 + fp * 4), X + row_x.lo((from + q * step) * 16 + fp * 4), y[q] * kInvScale);
+                }
+            }
+        } else {
+            // four neighbouring values of a row of the matrix as it lies
+            const auto row_of_piece = [&](int q) __attribute__((always_inline)) { return t.tall ? (from + q * step) * 16 + lr : own * 16 + lr; };
+            const auto col_of_piece = [&](int q) __attribute__((always_inline)) { return t.tall ? i0 : (from + q * step) * 16 + fp * 4; };
+            const auto count = [&](int q) __attribute__((always_inline)) { return q < pieces && row_of_piece(q) < t.rows ? t.cols - col_of_piece(q) : 0; };
+            float w[kPieces][4];
+            if constexpr (MUON) {
+#pragma unroll
+                for (int q = 0; q < kPieces; ++q) load4(w[q], t.w + (count(q) > 0 ? row_of_piece(q) * t.cols + col_of_piece(q) : 0), count(q));
+            }
+#pragma unroll
+            for (int q = 0; q < kPieces; ++q) {
+                const int n = count(q), at = row_of_piece(q) * t.cols + col_of_piece(q);
+                float o[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    o[r] = (t.tall ? x[q][r] : y[q][r]) * (kInvScale * kInvScale);
+                    if constexpr (MUON) o[r] = fmaf(-t.step, o[r], fmaf(-t.lr_decay, w[q][r], w[q][r]));
+                }
+                if constexpr (MUON) {
+                    put4(t.w + at, o, n);
+                    if (t.out) put4(static_cast<uint16_t*>(t.out) + at, o, n);
+                } else {
+                    put4(static_cast<T*>(t.out) + at, o, n);
+                }
+            }
+        }
+        __syncthreads();
+    }
+}
+
 // ---------------------------------------------------------------------------------------------- host
 
 constexpr int kMostSide = 1 << 16;
@@ -551,7 +805,13 @@ bool launch_product(Args<TABLE>& args, Tile tile, hipStream_t stream) {
 }
 
 template <bool MUON, typename T, int TABLE>
-lc_status run_group(Args<TABLE>& args, int iterations, hipStream_t stream) {
+lc_status run_group(Args<TABLE>& args, int iterations, bool all_small, hipStream_t stream) {
+    if (all_small) {
+        constexpr int lds = 2 * kSmallM * kSmallN * 4 + kSmallM * kSmallM * 4;
+        static const bool once = hipFuncSetAttribute(reinterpret_cast<const void*>(ns_small_kernel<T, MUON, TABLE>), hipFuncAttributeMaxDynamicSharedMemorySize, lds) == hipSuccess;
+        if (once) hipLaunchKernelGGL((ns_small_kernel<T, MUON, TABLE>), dim3((unsigned)args.s.count), dim3(kSmallThreads), lds, stream, args, iterations);
+        return once ? LC_OK : LC_ERR_LAUNCH;
+    }
     int blocks = set_starts(args, [](const Mat& t) {
         const long long v = MUON ? ((long long)t.rows * t.cols + 3) / 4 : (long long)t.rows * ((t.cols + 3) / 4);
         return (v + t.chunk - 1) / t.chunk;
@@ -571,8 +831,8 @@ lc_status run_group(Args<TABLE>& args, int iterations, hipStream_t stream) {
 }
 
 template <bool MUON, typename T, int TABLE>
-lc_status run_group(const std::vector<Matrix>& all, const std::vector<int>& order, size_t first, size_t n, const Scalars& s, int iterations, void* workspace,
-                    hipStream_t stream) {
+lc_status run_group(const std::vector<Matrix>& all, const std::vector<int>& order, size_t first, size_t n, const Scalars& s, int iterations, bool all_small,
+                    void* workspace, hipStream_t stream) {
     Args<TABLE> args;
     args.s = s;
     args.s.count = (int)n;
@@ -585,17 +845,19 @@ lc_status run_group(const std::vector<Matrix>& all, const std::vector<int>& orde
                 (int)std::max<long long>(1024, ((vectors + kMostParts - 1) / kMostParts + 255) / 256 * 256), base, a.step, a.lr_decay};
         base += bytes_of(a.rows, a.cols);
     }
-    return run_group<MUON, T, TABLE>(args, iterations, stream);
+    return run_group<MUON, T, TABLE>(args, iterations, all_small, stream);
 }
 
 template <bool MUON, typename T>
 lc_status run_all(const std::vector<Matrix>& all, std::vector<int>& order, const int* rows, const int* cols, const Scalars& s, int iterations, void* workspace,
                   hipStream_t stream) {
     lc_status st = LC_OK;
+    // (beside larger ones small matrices cost next to nothing; a launch of their own would be one more)
+    const bool all_small = std::all_of(order.begin(), order.end(), [&](int i) { return small((int)padded(std::min(rows[i], cols[i])), (int)padded(std::max(rows[i], cols[i]))); });
     for_groups(order, rows, cols, [&](size_t first, size_t n, long long) {
         if (st != LC_OK) return;
-        st = n <= kSmallTable ? run_group<MUON, T, kSmallTable>(all, order, first, n, s, iterations, workspace, stream)
-                              : run_group<MUON, T, kTable>(all, order, first, n, s, iterations, workspace, stream);
+        st = n <= kSmallTable ? run_group<MUON, T, kSmallTable>(all, order, first, n, s, iterations, all_small, workspace, stream)
+                              : run_group<MUON, T, kTable>(all, order, first, n, s, iterations, all_small, workspace, stream);
     });
     return st;
 }
