@@ -8,8 +8,9 @@
 // left: small singular values grow by up to 3.4445 a step, and the first rounding with them: errors of 1.4e-3 (bf16 1.3e-2) on a random matrix and 1.4e-2 (0.11) on one of rank 8 and noise, pairs 3e-7 to 3e-6, fp32 products
 // 1e-6 to 6e-5.
 //
-// In memory a matrix is [row][32 columns: 32 hi, 32 lo], sides filled up with zeros to multiples of 32: a k-step of 32 is 128 bytes of a row, a whole line, and LDS holds it as the bf16 products of conv_dma.h do.  X is
-// kept both ways round, so that all three products read rows along their sum.
+// In memory a matrix is [row][32 columns: 32 hi, 32 lo], sides filled up with zeros to multiples of 32: a k-step of 32 is 128 bytes of a row, a whole line, and LDS holds it as the bf16 products of conv_dma.h do.  A
+// and B are symmetric, so that two products read rows along their sums; B X reads rows of X from LDS the other way round.  (X kept both ways round as well, ResNet-50's filters,
+// 94 MB: 110 us for B X, so 84; two layers of width 2048 1094, so 1003.)
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -45,9 +46,8 @@ struct Mat {
     unsigned char* base;     // its part of the workspace
     float step, lr_decay;    // lr * scale, lr * decay
     __host__ __device__ long long side() const { return (long long)M * N * 4; }
-    __host__ __device__ unsigned char* x() const { return base + kMostParts * 8; }
-    __host__ __device__ unsigned char* xt(int which) const { return x() + (1 + which) * side(); }
-    __host__ __device__ unsigned char* a() const { return x() + 3 * side(); }
+    __host__ __device__ unsigned char* x(int which) const { return base + kMostParts * 8 + which * side(); }
+    __host__ __device__ unsigned char* a() const { return x(2); }
     __host__ __device__ unsigned char* b() const { return a() + (long long)M * M * 4; }
 };
 
@@ -56,7 +56,7 @@ struct Scalars {
     const float* grad_scale;
     float momentum, eps;
     int nesterov;
-    int which;               // of the two transposes, the one that is read
+    int which;               // of the two places of X, the one that is read
 };
 
 template <int TABLE>
@@ -192,7 +192,7 @@ __device__ __forceinline__ void load_pairs(float* v, const unsigned char* p) {
 // Byte of element (row, col) of a matrix with `k` columns in memory, col a multiple of 8.
 __device__ __forceinline__ long long pair_at(long long row, int col, int k) { return row * k * 4 + (col >> 5) * 128 + (col & 31) * 2; }
 
-// u / (|u| + eps) as pairs, both ways round: a block 64 x 64 values.
+// u / (|u| + eps) as pairs: a block 64 x 64 values.
 template <typename T, bool MUON, int TABLE>
 __global__ void __launch_bounds__(256) ns_split_kernel(const Args<TABLE> args) {
     __shared__ double red[4];
@@ -200,7 +200,7 @@ __global__ void __launch_bounds__(256) ns_split_kernel(const Args<TABLE> args) {
     int local;
     const Mat& t = args.t[owner_of(args, blockIdx.x, &local)];
     const int tid = threadIdx.x;
-    const int prows = t.tall ? t.N : t.M, pcols = t.tall ? t.M : t.N;           // sides in memory as the matrix lies
+    const int pcols = t.tall ? t.M : t.N;          // of the sides in memory, along the matrix's rows
     const int across = (pcols + 63) / 64, r0 = local / across * 64, c0 = local % across * 64;
     const float gs = args.s.grad_scale ? *args.s.grad_scale : 1.f, mu = args.s.momentum;
     float u[4][4];
@@ -231,27 +231,20 @@ __global__ void __launch_bounds__(256) ns_split_kernel(const Args<TABLE> args) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) tile[(tid >> 4) + 16 * k][4 * (tid & 15) + j] = (float)((double)u[k][j] * inv);
     __syncthreads();
-    unsigned char* const along = t.tall ? t.xt(0) : t.x();
-    unsigned char* const turned = t.tall ? t.x() : t.xt(0);
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
         const int line = (tid >> 3) + 32 * k, run = (tid & 7) * 8;
+        const int row = (t.tall ? c0 : r0) + line, col = (t.tall ? r0 : c0) + run;
+        if (row >= t.M || col >= t.N) continue;
         float v[8];
-        if (r0 + line < prows && c0 + run < pcols) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = tile[line][run + j];
-            store_pairs(along + pair_at(r0 + line, c0 + run, pcols), v);
-        }
-        if (c0 + line < pcols && r0 + run < prows) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = tile[run + j][line];
-            store_pairs(turned + pair_at(c0 + line, r0 + run, prows), v);
-        }
+        for (int j = 0; j < 8; ++j) v[j] = t.tall ? tile[run + j][line] : tile[line][run + j];
+        store_pairs(t.x(0) + pair_at(row, col, t.N), v);
     }
 }
 
-// What a product makes: A = X X^T; B = a I + b A + c A A; X <- B X, both ways round; the same as the result.  (a on B's diagonal costs X a rounding of 2^-22, as its own is, and saves reading X once more:
-// ResNet-50's filters 118 to 130 us a product of X with it added at the end.)
+// What a product makes: A = X X^T; B = a I + b A + c A A; X <- B X, to the other place; the same as the result.  (a on B's diagonal costs X a rounding of 2^-22, as its own is, and saves reading X once more:
+// ResNet-50's filters 124 us for X with it added at the end, so 110.)
 enum Product { kGram, kSquare, kNext, kLast };
 
 template <Product KIND>
@@ -316,23 +309,37 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) ns_product_kernel(const Args<
     ti = __builtin_amdgcn_readfirstlane(ti);
     tj = __builtin_amdgcn_readfirstlane(tj);
     const int i0 = ti * BM, j0 = tj * BN;
-    const int K = KIND == kGram ? N : M, rowsQ = KIND <= kSquare ? M : N;
-    const unsigned pitch = (unsigned)K * 4u;
-    const unsigned char* const P = KIND == kGram ? t.x() : KIND == kSquare ? t.a() : t.b();
-    const unsigned char* const Q = KIND == kGram ? t.x() : KIND == kSquare ? t.a() : t.xt(args.s.which);
-    // rows past the matrix lie past the end of the buffer: zeros
+    constexpr bool TURN = KIND >= kNext;           // Q[j] is column j of X: rows of X are loaded, and read from LDS the other way round
+    const int K = KIND == kGram ? N : M;
+    const unsigned pitch = (unsigned)K * 4u, x_pitch = (unsigned)N * 4u;
+    const unsigned char* const P = KIND == kGram ? t.x(args.s.which) : KIND == kSquare ? t.a() : t.b();
+    const unsigned char* const Q = KIND == kGram ? P : KIND == kSquare ? P : t.x(args.s.which) + (long long)j0 * 4;
+    // rows past the matrix lie past the end of the buffer: zeros.  (Of TURN, columns past it are the next row's, or past the end; what they make is not stored.)
     const u32x4 p_rsrc = buffer_words(P + (long long)i0 * pitch, (unsigned)std::min(BM, M - i0) * pitch);
-    const u32x4 q_rsrc = buffer_words(Q + (long long)j0 * pitch, (unsigned)std::min(BN, rowsQ - j0) * pitch);
+    u32x4 q_rsrc = TURN ? buffer_words(Q, 32u * x_pitch - (unsigned)j0 * 4u) : buffer_words(Q + (long long)j0 * pitch, (unsigned)std::min(BN, M - j0) * pitch);
     const int lrow = lane >> 3, piece = (lane & 7) ^ (((wave & 1) * 4 + (lrow >> 1)) & 7);
     const unsigned voff = (unsigned)(wave * 8 + lrow) * pitch + piece * 16;
+    // TURN: LDS holds 32 rows of BN columns; pieces of 16 bytes at piece ^ 2 (row % 4 + row / 8 % 2 * 4), so that the 16 rows of a turning read lie on all banks
+    unsigned q_voff[LQ];
+#pragma unroll
+    for (int l = 0; l < LQ; ++l) {
+        const int at = (l * NW + wave) * 64 + lane, row = at / (BN / 4), slot = at - row * (BN / 4);
+        q_voff[l] = TURN ? (unsigned)row * x_pitch + (slot ^ ((row & 3) | (row >> 1 & 4)) << 1) * 16 : voff + (unsigned)(l * NW * 8) * pitch;
+    }
     const unsigned lds0 = lds_address(smem);
     const int steps = K / 32;
-    const auto load = [&](int k, int stage) __attribute__((always_inline)) {
+    unsigned long long q_base = (unsigned long long)q_rsrc[1] << 32 | q_rsrc[0];
+    const auto load = [&](int k, int stage) __attribute__((always_inline)) {       // (called for k = 0, 1, 2, ...)
         const unsigned past = k < steps ? 0u : kBufferBytes;       // (behind the last step the loads fetch nothing, and their number stays the same)
 #pragma unroll
         for (int l = 0; l < LP; ++l) load_to_lds(p_rsrc, (voff + (unsigned)(l * NW * 8) * pitch) | past, k * 128, lds0 + stage * STAGE + (l * NW + wave) * 1024);
 #pragma unroll
-        for (int l = 0; l < LQ; ++l) load_to_lds(q_rsrc, (voff + (unsigned)(l * NW * 8) * pitch) | past, k * 128, lds0 + stage * STAGE + BM * 128 + (l * NW + wave) * 1024);
+        for (int l = 0; l < LQ; ++l) load_to_lds(q_rsrc, q_voff[l] | past, TURN ? 0 : k * 128, lds0 + stage * STAGE + BM * 128 + (l * NW + wave) * 1024);
+        if constexpr (TURN) {
+            q_base += 32ull * x_pitch;
+            q_rsrc[0] = (unsigned)q_base;
+            q_rsrc[1] = (unsigned)(q_base >> 32);
+        }
     };
     f32x4 acc[TM][TN];
 #pragma unroll
@@ -343,17 +350,40 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) ns_product_kernel(const Args<
     const int hi = ((fp ^ sw) & 7) * 16, lo = (((4 + fp) ^ sw) & 7) * 16;
     const unsigned char* const p_lane = smem + (wm * TM * 16 + (lane & 15)) * 128;
     const unsigned char* const q_lane = smem + BM * 128 + (wn * TN * 16 + (lane & 15)) * 128;
+    // TURN: a lane's four columns of a row, whose columns it then holds as 16 lanes' four rows: rows 8 (lane / 16) + 0 .. 3, and four further for the other half of its eight
+    const unsigned char* turn_lane[TN][2];
+    if constexpr (TURN) {
+        const int row = (lane >> 4) * 8 + ((lane >> 2) & 3), turn = (((lane >> 2) & 3) | (lane >> 2 & 4)) << 1;
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+            const int col = (wn * TN + j) * 16, first = col / 32 * 8 + (col & 16) / 8;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) turn_lane[j][h] = smem + BM * 128 + row * (BN * 4) + (((first + 4 * h) ^ turn) + ((lane >> 1) & 1)) * 16 + (lane & 1) * 8;
+        }
+    }
     f16x8 ph[2][TM], pl[2][TM], qh[2][TN], ql[2][TN];
+    const auto read_q = [&](int j, int h, int at) __attribute__((always_inline)) {
+        if constexpr (TURN) {
+            const auto four = [&](int rows) __attribute__((always_inline)) {
+                const unsigned char* const from = turn_lane[j][h] + at + rows * (BN * 4);
+                return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(uintptr_t)from);
+            };
+            const s16x4 a = four(0), b = four(4);
+            return __builtin_bit_cast(f16x8, s16x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]});
+        } else {
+            return *reinterpret_cast<const f16x8*>(q_lane + at + (h ? lo : hi) + j * 2048);
+        }
+    };
     const auto read = [&](int to, int stage) __attribute__((always_inline)) {
         const int at = stage * STAGE;
 #pragma unroll
         for (int i = 0; i < TM; ++i) pl[to][i] = *reinterpret_cast<const f16x8*>(p_lane + at + lo + i * 2048);
 #pragma unroll
-        for (int j = 0; j < TN; ++j) qh[to][j] = *reinterpret_cast<const f16x8*>(q_lane + at + hi + j * 2048);
+        for (int j = 0; j < TN; ++j) qh[to][j] = read_q(j, 0, at);
 #pragma unroll
         for (int i = 0; i < TM; ++i) ph[to][i] = *reinterpret_cast<const f16x8*>(p_lane + at + hi + i * 2048);
 #pragma unroll
-        for (int j = 0; j < TN; ++j) ql[to][j] = *reinterpret_cast<const f16x8*>(q_lane + at + lo + j * 2048);
+        for (int j = 0; j < TN; ++j) ql[to][j] = read_q(j, 1, at);
     };
     // fragments of the next step are read while this one's are multiplied: with them read first a step took two and a half times its matrix instructions where a SIMD has one wave
     int stage = 0;
@@ -375,9 +405,9 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) ns_product_kernel(const Args<
 #pragma unroll
             for (int j = 0; j < TN; ++j) acc[i][j] = multiply(ph[BUF][i], qh[BUF][j], acc[i][j]);
 #pragma unroll
-        for (int i = 0; i < 2 * (TM + TN); ++i) {
+        for (int i = 0; i < 2 * TM + (TURN ? 4 : 2) * TN; ++i) {
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(0x008, std::max(1, 3 * TM * TN / (2 * (TM + TN))), 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, std::max(1, 3 * TM * TN / (2 * TM + (TURN ? 4 : 2) * TN)), 0);
         }
     };
 #pragma unroll
@@ -394,7 +424,7 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) ns_product_kernel(const Args<
     float* const mine = reinterpret_cast<float*>(smem) + wave * (TM * 16 * kPitch);
     const int iw = i0 + wm * TM * 16;
     constexpr int RA = TC * 2, RB = TM * 2;                        // runs of a row, of a column
-    const bool along = KIND != kLast || !t.tall, turned = KIND == kNext || (KIND <= kSquare && ti != tj) || (KIND == kLast && t.tall);
+    const bool along = KIND != kLast || !t.tall, turned = (KIND <= kSquare && ti != tj) || (KIND == kLast && t.tall);
     const int columns = KIND <= kSquare ? M : N;
     const auto leave = [&](int row, int col, const float* v) __attribute__((always_inline)) {        // eight results from (row, col) of the matrix as it lies
         if (row >= t.rows || col >= t.cols) return;
@@ -441,7 +471,7 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) ns_product_kernel(const Args<
 #pragma unroll
                     for (int e = 0; e < 8; ++e) v[e] *= KIND == kLast ? kInvScale * kInvScale : kInvScale;
                     if constexpr (KIND == kGram) store_pairs(t.a() + pair_at(gi, gj, M), v);
-                    else if constexpr (KIND == kNext) store_pairs(t.x() + pair_at(gi, gj, N), v);
+                    else if constexpr (KIND == kNext) store_pairs(t.x(args.s.which ^ 1) + pair_at(gi, gj, N), v);
                     else if (along) leave(gi, gj, v);
                 }
             }
@@ -461,8 +491,7 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) ns_product_kernel(const Args<
                 for (int e = 0; e < 8; ++e) v[e] = mine[(run + e) * kPitch + col];
                 if constexpr (KIND == kGram) store_pairs(t.a() + pair_at(gj, gi, M), v);
                 else if constexpr (KIND == kSquare) store_pairs(t.b() + pair_at(gj, gi, M), v);
-                else if constexpr (KIND == kNext) store_pairs(t.xt(args.s.which ^ 1) + pair_at(gj, gi, M), v);
-                else leave(gj, gi, v);
+                else if constexpr (KIND == kLast) leave(gj, gi, v);
             }
         }
         if (part + 1 < TN / TC) __syncthreads();
@@ -704,7 +733,7 @@ constexpr long long kGroupBytes = 2ll << 30;       // of workspace that matrices
 long long padded(long long side) { return (side + kPad - 1) / kPad * kPad; }
 long long bytes_of(long long rows, long long cols) {
     const long long M = padded(std::min(rows, cols)), N = padded(std::max(rows, cols));
-    return kMostParts * 8 + 12 * M * N + 8 * M * M;
+    return kMostParts * 8 + 8 * M * N + 8 * M * M;
 }
 
 struct Matrix {                                    // of a call, before it has a place

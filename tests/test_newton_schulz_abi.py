@@ -35,7 +35,7 @@ def test_pointers_and_workspace():
     assert ns(OK, x=None) == lc.LC_ERR_NULL and ns(OK, y=None) == lc.LC_ERR_NULL
     assert ns(OK, x=FAKE + 2) == lc.LC_ERR_ALIGN and ns(OK, y=FAKE + 2) == lc.LC_ERR_ALIGN
     need = lc.newton_schulz_workspace_bytes(OK)
-    assert need % 256 == 0 and need >= 2 * (12 * 64 * 32 + 8 * 32 * 32)
+    assert need % 256 == 0 and need >= 2 * (8 * 64 * 32 + 8 * 32 * 32)
     assert ns(OK, ws=None) == lc.LC_ERR_WORKSPACE and ns(OK, ws=FAKE + 128) == lc.LC_ERR_WORKSPACE and ns(OK, nb=need - 1) == lc.LC_ERR_WORKSPACE
 
 
@@ -73,8 +73,8 @@ def test_lists():
 def test_workspace_is_shared_by_groups():
     of = lambda *shapes: lc.muon_workspace_bytes(lc.MuonArgs([FAKE] * len(shapes), [FAKE] * len(shapes), [FAKE] * len(shapes), shapes=shapes))
     single = of((4096, 4096))
-    assert 20 * 4096 * 4096 <= single <= 20 * 4096 * 4096 + 16384
-    assert of(*[(4096, 4096)] * 40) == 6 * single <= 2 << 30                          # as many as 2 GiB hold
+    assert 16 * 4096 * 4096 <= single <= 16 * 4096 * 4096 + 16384
+    assert of(*[(4096, 4096)] * 40) == 7 * single <= 2 << 30                          # as many as 2 GiB hold
     assert of(*[(64, 64)] * 200) == of(*[(64, 64)] * 64)
     assert of((65536, 65536)) > 2 << 30
     assert of((100, 300), (4096, 4096)) == of((4096, 4096), (100, 300))
