@@ -63,6 +63,7 @@ template <int TABLE>
 struct Args {
     Mat t[TABLE];
     int start[(TABLE + 63) / 64 * 64];   // first block of each, past the last the largest int
+    uint8_t dies[TABLE], die[TABLE];     // products: how many dies take a matrix, from which on
     Scalars s;
 };
 
@@ -301,9 +302,10 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) ns_product_kernel(const Args<
     const int owner = owner_of(args, blockIdx.x, &local);
     const Mat& t = args.t[owner];
     const int M = t.M, N = t.N;
-    const int tiles = tiles_of<KIND>(t, BM, BN), per = (tiles + 7) >> 3;
-    const int tile = ((local + owner) & 7) * per + (local >> 3);       // a die takes neighbouring tiles of each matrix; blocks begin at multiples of 8
-    if (tile >= std::min(tiles, (((local + owner) & 7) + 1) * per)) return;
+    // blocks are dealt round the dies, a matrix's begin at a multiple of 8: its dies take neighbouring tiles each, the others' blocks have nothing to do
+    const int dies = args.dies[owner], part = (local - args.die[owner]) & 7;
+    const int tiles = tiles_of<KIND>(t, BM, BN), per = (tiles + dies - 1) / dies, tile = part * per + (local >> 3);
+    if (part >= dies || tile >= std::min(tiles, (part + 1) * per)) return;
     int ti, tj;
     place_of<KIND>(t, tile, BM, BN, &ti, &tj);
     ti = __builtin_amdgcn_readfirstlane(ti);
@@ -812,18 +814,70 @@ Tile tile_of(const Args<TABLE>& args) {
     return best;
 }
 
+// How a launch's products are made: its tile, and the dies of each matrix.  A die has an L2 of its own, and what several dies work on each of them fetches: a matrix is shared by as few dies as leave their loads even, a
+// part being half of a die's load at most.  Steps over a list, us, all dies a part of each / so: ResNet-50's filters 965 / 895 (A: 418 MB fetched for 94), twelve layers of width 256 530 / 484, four of 512 670 / 632, two of
+// 2048 9810 / 9780, three of 333 285 / 294.
+template <int TABLE>
+struct LaunchPlan {
+    Tile tile;
+    uint8_t dies[TABLE], die[TABLE];
+};
+template <Product KIND, int TABLE>
+LaunchPlan<TABLE> plan_of(const Args<TABLE>& args) {
+    LaunchPlan<TABLE> plan{tile_of<KIND>(args), {}, {}};
+    const TileCost& k = kTiles[plan.tile];
+    double cost[TABLE], all = 0.0, load[8] = {};
+    int order[TABLE];
+    for (int i = 0; i < args.s.count; ++i) {
+        cost[i] = (double)tiles_of<KIND>(args.t[i], k.rows, k.cols) * ((KIND == kGram ? args.t[i].N : args.t[i].M) / 32 * k.step + k.ends);
+        all += cost[i];
+        order[i] = i;
+    }
+    for (int i = 0; i < args.s.count; ++i) {
+        int dies = 1;
+        while (dies < 8 && cost[i] / dies > all / 16) dies *= 2;
+        plan.dies[i] = (uint8_t)dies;
+        cost[i] /= dies;
+    }
+    std::stable_sort(order, order + args.s.count, [&](int a, int b) { return cost[a] > cost[b]; });
+    for (int n = 0; n < args.s.count; ++n) {             // the largest parts first, each to the dies that have least
+        const int i = order[n], dies = plan.dies[i];
+        int best = n & 7;                                // (for all dies: another one begins each time)
+        if (dies < 8) {
+            double least = 1e30;
+            for (int d = 0; d < 8; ++d) {
+                double most = 0.0;
+                for (int q = 0; q < dies; ++q) most = std::max(most, load[(d + q) & 7]);
+                if (most < least) {
+                    least = most;
+                    best = d;
+                }
+            }
+        }
+        plan.die[i] = (uint8_t)best;
+        for (int q = 0; q < dies; ++q) load[(best + q) & 7] += cost[i];
+    }
+    return plan;
+}
+
 template <Product KIND, bool MUON, typename T, int TM, int TN, int WM, int WN, int NS, int TABLE>
 bool launch_product(Args<TABLE>& args, hipStream_t stream) {
     constexpr int lds = std::max(NS * (TM * WM + TN * WN) * 16 * 128, WM * WN * TM * 16 * (leaving_columns(TN) * 16 + 4) * 4);
-    const int blocks = set_starts(args, [](const Mat& t) { return (tiles_of<KIND>(t, 16 * TM * WM, 16 * TN * WN) + 7) / 8 * 8; });
+    const uint8_t* dies = args.dies;
+    const int blocks = set_starts(args, [&](const Mat& t) {
+        const int shared = *dies++;
+        return (tiles_of<KIND>(t, 16 * TM * WM, 16 * TN * WN) + shared - 1) / shared * 8;
+    });
     static const bool once = hipFuncSetAttribute(reinterpret_cast<const void*>(ns_product_kernel<KIND, MUON, T, TM, TN, WM, WN, NS, TABLE>),
                                                  hipFuncAttributeMaxDynamicSharedMemorySize, lds) == hipSuccess;
     if (once) hipLaunchKernelGGL((ns_product_kernel<KIND, MUON, T, TM, TN, WM, WN, NS, TABLE>), dim3((unsigned)blocks), dim3(WM * WN * 64), lds, stream, args);
     return once;
 }
 template <Product KIND, bool MUON, typename T, int TABLE>
-bool launch_product(Args<TABLE>& args, Tile tile, hipStream_t stream) {
-    switch (tile) {
+bool launch_product(Args<TABLE>& args, const LaunchPlan<TABLE>& plan, hipStream_t stream) {
+    std::copy(plan.dies, plan.dies + TABLE, args.dies);
+    std::copy(plan.die, plan.die + TABLE, args.die);
+    switch (plan.tile) {
         case kTile64: return launch_product<KIND, MUON, T, 2, 2, 2, 2, 4>(args, stream);
         case kTile128One: return launch_product<KIND, MUON, T, 2, 4, 4, 2, 4>(args, stream);
         case kTile192: return launch_product<KIND, MUON, T, 6, 3, 2, 4, 3>(args, stream);
@@ -848,7 +902,7 @@ lc_status run_group(Args<TABLE>& args, int iterations, bool all_small, hipStream
     hipLaunchKernelGGL((ns_squares_kernel<T, MUON, TABLE>), dim3((unsigned)blocks), dim3(256), 0, stream, args);
     blocks = set_starts(args, [](const Mat& t) { return (long long)((t.M + 63) / 64) * ((t.N + 63) / 64); });
     hipLaunchKernelGGL((ns_split_kernel<T, MUON, TABLE>), dim3((unsigned)blocks), dim3(256), 0, stream, args);
-    const Tile gram = tile_of<kGram>(args), square = tile_of<kSquare>(args), next = tile_of<kNext>(args);
+    const auto gram = plan_of<kGram>(args), square = plan_of<kSquare>(args), next = plan_of<kNext>(args);
     bool ok = true;
     for (int i = 0; i < iterations && ok; ++i) {
         args.s.which = i & 1;
