@@ -218,3 +218,52 @@ def test_a_captured_step_on_another_stream_replays():
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(w + m, want))
         g[0].mul_(0.5)
+
+
+def on_the_device(x, dtype):
+    """The steps as plain products of one type (2-D, ordinary layouts)."""
+    x = x.to(dtype)
+    tall = x.shape[0] > x.shape[1]
+    x = x.T.contiguous() if tall else x
+    x = x / (x.double().norm().to(dtype) + 1e-7)
+    for _ in range(5):
+        a = x @ x.T.contiguous()
+        x = 3.4445 * x + (-4.7750 * a + 2.0315 * (a @ a)) @ x
+    return x.T if tall else x
+
+
+@pytest.mark.parametrize("batch,rows,cols", [(1, 2048, 2048), (2, 2000, 2100), (1, 4096, 4096), (1, 3001, 2900), (3, 1024, 4100), (12, 700, 500)])
+def test_every_tile_is_as_near_as_fp32_products(batch, rows, cols):
+    """Sizes that take tiles of 128 (one block a unit and two), 192 and 256 x 128: errors against 64 bits at most twice those of fp32 products, and 2e-6."""
+    torch.manual_seed(rows)
+    x = torch.randn((batch, rows, cols), device=gu.DEV) * torch.exp(0.7 * torch.randn((batch, rows, 1), device=gu.DEV))
+    y, d = torch.empty_like(x), lc.NewtonSchulzDesc(batch, rows, cols)
+    lc.newton_schulz(d, x, y, gu.workspace(lc.newton_schulz_workspace_bytes(d)))
+    for i in range(batch):
+        want, plain = on_the_device(x[i], torch.float64), on_the_device(x[i], torch.float32)
+        off = lambda v: float((v.double() - want).norm() / want.norm())
+        assert off(y[i]) <= 2 * off(plain) + 2e-6
+
+
+@pytest.mark.parametrize("shapes", [[(cs.k, cs.weight_numel // cs.k) for cs in synth.resnet50_convs(1)], [(300, 300)] * 9 + [(1200, 300), (300, 1200)] * 3 + [(17, 2000)]])
+def test_a_mixed_list_against_64_bits(shapes):
+    """Matrices shared by one to eight dies, among them ones smaller than a tile: the update of each, and the same bits once more."""
+    torch.manual_seed(len(shapes))
+    w, g, m = ([torch.randn(s, device=gu.DEV) * std for s in shapes] for std in (0.02, 1e-3, 4e-3))
+    start = [[t.clone() for t in v] for v in (w, m)]
+    args = lc.MuonArgs(w, g, m)
+    ws = gu.workspace(lc.muon_workspace_bytes(args))
+    lc.muon_step(args, 0.02, 0.95, 0.1, ws)
+    for i, s in enumerate(shapes):
+        m64 = 0.95 * start[1][i].double() + g[i].double()
+        moved = g[i].double() + 0.95 * m64
+        want = on_the_device(moved, torch.float64) * max(1.0, s[0] / s[1]) ** 0.5
+        got = ((1 - 0.02 * 0.1) * start[0][i].double() - w[i].double()) / 0.02
+        # w's own rounding, 2^-24 of it twice, is 50 times as much of the update's unit
+        assert float((got - want).norm()) <= 1e-5 * float(want.norm()) + 50 * 2.0 ** -23 * float(start[0][i].double().norm()), (i, s)
+    first = [t.clone() for t in w + m]
+    for now, then in zip((w, m), start):
+        for a, b in zip(now, then):
+            a.copy_(b)
+    lc.muon_step(args, 0.02, 0.95, 0.1, ws)
+    assert all(torch.equal(a, b) for a, b in zip(w + m, first))
