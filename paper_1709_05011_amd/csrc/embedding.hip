@@ -21,13 +21,13 @@ __device__ __forceinline__ int key_of(const int32_t* tokens, long long i, int vo
     return t >= 0 && t < vocab ? t : kNone;
 }
 
-// Eight columns of a row, loaded (issue) and put in their places (settle) apart, so that loads of several rows are under way; EIGHTS: c is a multiple of 8.
-template <bool EIGHTS, typename T>
+// Eight columns of a row, loaded (issue) and put in their places (settle) apart, so that loads of several rows are under way; EIGHTS: c is a multiple of 8; NT: past the caches.
+template <bool EIGHTS, bool NT = false, typename T>
 __device__ __forceinline__ void issue(Packed<T>& to, const T* row, int col, int c) {
     if constexpr (EIGHTS) {
-        to.load(row + col);
+        to.template load<NT>(row + col);
     } else if (c >= 8) {
-        to.load(row + min(col, c - 8));
+        to.template load<NT>(row + min(col, c - 8));
     } else {
         to.load_some(row, c, 0u);
     }
@@ -49,9 +49,9 @@ struct LookupArgs {
     float scale;
 };
 
-// Some lanes a row, eight columns a lane and access, kRowsAhead rows of a block (their tokens, then their values) under way at a time.
+// Some lanes a row, eight columns a lane and access, kRowsAhead rows of a block (their tokens, then their values) under way at a time.  PAST: out goes past the caches.
 constexpr int kRowsAhead = 4;
-template <typename S, typename T, bool EIGHTS>
+template <typename S, typename T, bool EIGHTS, bool PAST>
 __global__ void __launch_bounds__(256) embedding_fwd_kernel(const LookupArgs p) {
     const int lanes = 1 << p.lane_bits, lane = threadIdx.x & (lanes - 1), each = 256 >> p.lane_bits;
     const long long stride = (long long)gridDim.x * each;
@@ -70,7 +70,7 @@ __global__ void __launch_bounds__(256) embedding_fwd_kernel(const LookupArgs p) 
                 float v[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[j] = key[u] == kNone ? 0.f : x[u].get(j) * p.scale;
-                lc_store8(static_cast<T*>(p.out) + (row + u * stride) * p.c + col, v, EIGHTS ? 8 : p.c - (int)col);
+                lc_store8<PAST>(static_cast<T*>(p.out) + (row + u * stride) * p.c + col, v, EIGHTS ? 8 : p.c - (int)col);
             }
         }
     }
@@ -246,7 +246,8 @@ __device__ __forceinline__ void leave(const SumArgs& p, long long piece, int key
 
 // A wave sums the rows of a piece, 512 columns of them: keys and places first, then AHEAD rows at a time, then their sums and stores.  No load stands behind a branch, and few behind a store: a wave's loads and stores
 // complete in order, so that waiting for one waits for all before it.  16384 rows of 2048 bf16 (5600 tokens, 107 MB) 31 us, 30011 of 1537 fp32 added to what is there 95 (3.2 TB/s); a wave for each place, most of which are
-// not a token's first, 40 and 90, with a longer joining.  Sequential rows in the place of a token's take as long; without the stores 19: all waves load, then all store.
+// not a token's first, 40 and 90, with a longer joining.  Rows in whole lines are read past the caches, which nothing asks for them again (behind what
+// wrote them: 16384 of 2048 bf16 109 us for 114, 30000 159 for 173; fp32, a line of which takes two loads, 155 for 155 and 81 for 78).  Sequential rows in the place of a token's take as long; without the stores 19: all waves load, then all store.
 template <typename T, bool EIGHTS, bool ADD, int AHEAD>
 __global__ void __launch_bounds__(256) embedding_sum_kernel(const SumArgs p) {
     const int lane = threadIdx.x & 63;
@@ -271,7 +272,7 @@ __global__ void __launch_bounds__(256) embedding_sum_kernel(const SumArgs p) {
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
             const int row = __builtin_amdgcn_readlane(places, std::min(ahead + u, n - 1) + 1);
-            issue<EIGHTS>(x[u], dout + (long long)row * p.c, col, p.c);
+            issue<EIGHTS, EIGHTS && sizeof(T) == 2>(x[u], dout + (long long)row * p.c, col, p.c);
             if constexpr (ADD) {
                 const int key = key_of_place(std::min(ahead + u, n - 1));
                 issue<EIGHTS>(old[u], p.dtable + (long long)(key == kNone ? 0 : key) * p.c, col, p.c);
@@ -389,6 +390,10 @@ __global__ void __launch_bounds__(256) embedding_join_kernel(const SumArgs p) {
 constexpr long long kMostBlocks = 1 << 20;
 constexpr long long kMostRows = 1ll << 25;        // a launch holds fewer than 2^32 threads, and a row has 64 of them at most
 
+// Bytes of out from which it goes past the caches.  us, three sets in turn, ordinary / past: 24000 x 2048 bf16 (98 MB) 32.3 / 24.6, 40000 (164 MB) 51 / 39, 30011 x 1537 fp32 (184 MB) with the gradient 193 / 181; but with a
+// layer norm of out behind it 30000 x 2048 bf16 84 / 86, 40000 113 / 114, 60000 162 / 163, 100000 273 / 272, fp32 16000 (131 MB) 111 / 117, 20000 136 / 143, 30011 x 1537 160 / 161.
+constexpr long long kPastBytes = 160 << 20;
+
 lc_status check_desc(const lc_embedding_desc* d) {
     if (!d) return LC_ERR_NULL;
     if ((d->dtype != LC_F32 && d->dtype != LC_BF16) || (d->table_dtype != LC_F32 && d->table_dtype != LC_BF16)) return LC_ERR_UNSUPPORTED;
@@ -445,9 +450,11 @@ extern "C" lc_status embedding_fwd(const lc_embedding_desc* desc, const void* ta
     const dim3 grid((unsigned)std::min<long long>(blocks <= 1024 ? blocks : (blocks + kRowsAhead - 1) / kRowsAhead, kMostBlocks));
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     lc_begin_call();
+    const bool past = (long long)desc->rows * desc->c * (desc->dtype == LC_BF16 ? 2 : 4) >= kPastBytes;
     const auto launch = [&]<typename S, typename T>() {
-        if (desc->c % 8 == 0) hipLaunchKernelGGL((embedding_fwd_kernel<S, T, true>), grid, dim3(256), 0, stream, a);
-        else hipLaunchKernelGGL((embedding_fwd_kernel<S, T, false>), grid, dim3(256), 0, stream, a);
+        const auto kernel = desc->c % 8 == 0 ? (past ? embedding_fwd_kernel<S, T, true, true> : embedding_fwd_kernel<S, T, true, false>)
+                                             : (past ? embedding_fwd_kernel<S, T, false, true> : embedding_fwd_kernel<S, T, false, false>);
+        hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a);
     };
     if (desc->table_dtype == LC_BF16) desc->dtype == LC_BF16 ? launch.template operator()<uint16_t, uint16_t>() : launch.template operator()<uint16_t, float>();
     else desc->dtype == LC_BF16 ? launch.template operator()<float, uint16_t>() : launch.template operator()<float, float>();

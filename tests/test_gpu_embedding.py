@@ -173,3 +173,19 @@ def test_a_captured_call_on_another_stream_replays():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(dtable, want)
+
+
+@pytest.mark.parametrize("table_kind,kind", [("f32", "f32"), ("bf16", "bf16"), ("f32", "bf16"), ("bf16", "f32")])
+@pytest.mark.parametrize("c", [2048, 1537])
+def test_outputs_past_the_caches(table_kind, kind, c):
+    """Outputs of 160 MB and more: a row per place, values that need no rounding, nothing behind the last."""
+    rows, vocab, tt, (dtype, t, _) = (172 << 20) // (c * (2 if kind == "bf16" else 4)) + 1, 1000, TYPES[table_kind], TYPES[kind]
+    table = torch.randn((vocab, c), device=gu.DEV).to(torch.bfloat16).to(tt[1])
+    tokens = torch.from_numpy(tokens_of(rows, vocab, 3, "some outside")).to(gu.DEV)
+    out, check = gu.guarded((rows, c), t)
+    lc.embedding_fwd(lc.EmbeddingDesc(rows, vocab, c, scale=0.5, table_dtype=tt[0], dtype=dtype), table, tokens, out)
+    torch.cuda.synchronize()
+    check()
+    inside = (tokens >= 0) & (tokens < vocab)
+    want = torch.where(inside[:, None], table[tokens.clamp(0, vocab - 1).long()].to(t) * 0.5, torch.zeros((), dtype=t, device=gu.DEV))
+    assert torch.equal(out, want)
