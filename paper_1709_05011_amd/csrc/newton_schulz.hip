@@ -78,9 +78,10 @@ __device__ __forceinline__ int owner_of(const Args<TABLE>& args, int bid, int* l
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef u32x2 u32x2_any __attribute__((aligned(2)));
+template <bool NT = false>
 __device__ __forceinline__ void load4(float* to, const float* p, int n) {
     if (n >= 4) {
-        const lc_u32x4 x = lc_load16(p);
+        const lc_u32x4 x = lc_load16<NT>(p);
 #pragma unroll
         for (int j = 0; j < 4; ++j) to[j] = __uint_as_float(x[j]);
     } else {
@@ -88,10 +89,12 @@ __device__ __forceinline__ void load4(float* to, const float* p, int n) {
         for (int j = 0; j < 4; ++j) to[j] = j < n ? p[j] : 0.f;
     }
 }
+template <bool NT = false>
 __device__ __forceinline__ void load4(float* to, const uint16_t* p, int n) {
     u32x2 x = {0u, 0u};
     if (n >= 4) {
-        x = *reinterpret_cast<const u32x2_any*>(p);
+        if constexpr (NT) x = __builtin_nontemporal_load(reinterpret_cast<const u32x2_any*>(p));
+        else x = *reinterpret_cast<const u32x2_any*>(p);
     } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
@@ -193,7 +196,8 @@ __device__ __forceinline__ void load_pairs(float* v, const unsigned char* p) {
 // Byte of element (row, col) of a matrix with `k` columns in memory, col a multiple of 8.
 __device__ __forceinline__ long long pair_at(long long row, int col, int k) { return row * k * 4 + (col >> 5) * 128 + (col & 31) * 2; }
 
-// u / (|u| + eps) as pairs: a block 64 x 64 values.
+// u / (|u| + eps) as pairs: a block 64 x 64 values.  A step reads its gradient and momentum for the last time here, past the caches, which X then finds emptier (ResNet-50's filters 907 us, so 880; twelve layers of width 256
+// 520 / 512).
 template <typename T, bool MUON, int TABLE>
 __global__ void __launch_bounds__(256) ns_split_kernel(const Args<TABLE> args) {
     __shared__ double red[4];
@@ -209,10 +213,10 @@ __global__ void __launch_bounds__(256) ns_split_kernel(const Args<TABLE> args) {
     for (int k = 0; k < 4; ++k) {
         const int row = r0 + (tid >> 4) + 16 * k, col = c0 + 4 * (tid & 15);
         const int n = row < t.rows ? t.cols - col : 0;
-        load4(u[k], static_cast<const T*>(t.in) + (n > 0 ? (long long)row * t.ld + col : 0), n);
+        load4<MUON>(u[k], static_cast<const T*>(t.in) + (n > 0 ? (long long)row * t.ld + col : 0), n);
         if constexpr (MUON) {
             float m[4];
-            load4(m, t.m + (n > 0 ? (long long)row * t.cols + col : 0), n);
+            load4<true>(m, t.m + (n > 0 ? (long long)row * t.cols + col : 0), n);
 #pragma unroll
             for (int j = 0; j < 4; ++j) u[k][j] = args.s.nesterov ? fmaf(mu, m[j], u[k][j] * gs) : m[j];
         }
