@@ -520,10 +520,17 @@ lc_status check_desc(const lc_layernorm_desc* d) {
     return LC_OK;
 }
 
-// Blocks of the forward pass: as many waves as the chip holds at once.  us, bf16, with 4096, 8192 and a block a row: 8192 x 4096 48.2, 48.6, 49.4, 2048 x 16384 51, 51, 59, 5000 x 5000 53, 48, 53; fp32 7000 x 4096 81, 83,
-// 86; 3000 x 10240 122, 117, 117.  (Scale and shift read again for every row: 53 for the first.)
-constexpr int kFwdWaves = 8192;
-long long fwd_blocks(int waves) { return std::max(256, kFwdWaves / waves); }
+// Blocks of the forward pass: as many waves as the chip holds at once, the same number of blocks for each of its 256 units.  us, bf16, with 4096 waves, 8192 and a block a row: 8192 x 4096 48.2, 48.6, 49.4,
+// 2048 x 16384 51, 51, 59; fp32 7000 x 4096 81, 83, 86; 3000 x 10240 122, 117, 117.  (Scale and shift read again for every row: 53 for the first.)
+constexpr int kFwdWaves = 8192, kUnits = 256;
+long long fwd_blocks(int waves) { return std::max(kUnits, kFwdWaves / waves / kUnits * kUnits); }
+
+// Blocks of the backward pass: the RMS norm's number, in multiples of the units where a block has whole rows.  us, bf16, forward and backward, the RMS norm's / so, both passes': 7084 rows of 1536 50 / 46.5, 2816 77.5 / 66.5,
+// 5120 116 / 110, 6144 152 / 137, 7168 181 / 152, 10240 325 / 281; fp32 4000 x 6144 171 / 154, 16409 x 1344 152 / 148; 2048, 4096 and 8192 columns have the same blocks.
+long long grad_blocks(lc_dtype dtype, long long rows, int c) {
+    const long long blocks = bwd_blocks(dtype, rows, c);
+    return in_passes(dtype, c) || narrow(rows, c) || blocks < kUnits ? blocks : blocks / kUnits * kUnits;
+}
 
 template <typename T, int CH, bool NT>
 void launch_fwd(const LayerArgs& a, hipStream_t stream) {
@@ -617,7 +624,7 @@ extern "C" lc_status layernorm_fwd(const lc_layernorm_desc* desc, const void* x,
 
 extern "C" size_t layernorm_bwd_workspace_bytes(const lc_layernorm_desc* desc) {
     if (check_desc(desc) != LC_OK) return 0;
-    return ((size_t)bwd_blocks(desc->dtype, desc->rows, desc->c) * 2 * desc->c * sizeof(float) + 255) & ~(size_t)255;
+    return ((size_t)grad_blocks(desc->dtype, desc->rows, desc->c) * 2 * desc->c * sizeof(float) + 255) & ~(size_t)255;
 }
 
 extern "C" lc_status layernorm_bwd(const lc_layernorm_desc* desc, const void* total, int64_t h_ld, const void* dy, const void* dtotal, const float* gamma,
@@ -643,7 +650,7 @@ extern "C" lc_status layernorm_bwd(const lc_layernorm_desc* desc, const void* to
         lc_off_element(save_mean, 4) || lc_off_element(save_rstd, 4))
         return LC_ERR_ALIGN;
     if (!workspace || (((uintptr_t)workspace) & 255) || workspace_bytes < layernorm_bwd_workspace_bytes(desc)) return LC_ERR_WORKSPACE;
-    const int blocks = (int)bwd_blocks(desc->dtype, desc->rows, desc->c);
+    const int blocks = (int)grad_blocks(desc->dtype, desc->rows, desc->c);
     const LayerBwdArgs a{total, dy, dtotal, gamma, save_mean, save_rstd, dx, static_cast<float*>(workspace), desc->rows, h_ld ? h_ld : desc->c,
                          (dbeta ? 2ll : 1ll) * desc->c, desc->c};
     lc_begin_call();
