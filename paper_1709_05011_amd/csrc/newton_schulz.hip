@@ -11,6 +11,9 @@
 // In memory a matrix is [row][32 columns: 32 hi, 32 lo], sides filled up with zeros to multiples of 32: a k-step of 32 is 128 bytes of a row, a whole line, and LDS holds it as the bf16 products of conv_dma.h do.  A
 // and B are symmetric, so that two products read rows along their sums; B X reads rows of X from LDS the other way round.  (X kept both ways round as well, ResNet-50's filters,
 // 94 MB: 110 us for B X, so 84; two layers of width 2048 1094, so 1003.)
+//
+// Bound by the matrix pipe and the card's power where products are large (4096 x 4096: 3.3 to 3.5 ms from card to card, B X 315 to 330 us, 1.25 to 1.3 PFLOP/s of the pairs' products, as a large library product of fp16), by
+// what a unit fetches from L2 in between, by launches where they are small (three of 517 x 1031: 17 launches of 6 to 13 us, 181).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -125,7 +128,7 @@ __device__ __forceinline__ void put4(uint16_t* p, const float* v, int n) {
     }
 }
 
-// The momentum's update and the sum of squares, in double, of what is orthogonalised: one block a chunk.
+// The momentum's update and the sum of squares, in double, of what is orthogonalised: one block a chunk.  ResNet-50's filters (275 MB) 53 us, 5.2 TB/s.
 template <typename T, bool MUON, int TABLE>
 __global__ void __launch_bounds__(256) ns_squares_kernel(const Args<TABLE> args) {
     __shared__ double red[4];
@@ -506,7 +509,7 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) ns_product_kernel(const Args<
 
 // ---------------------------------------------------------------------------------------------- small matrices
 
-// Sides up to 64 and 256: a block takes a matrix through all steps in LDS (X both ways round and A, 144 KB), where launches for each product would be nearly all of the time (twelve matrices of 64 x 64 and 64 x 256 80 us).
+// Sides up to 64 and 256: a block takes a matrix through all steps in LDS (X both ways round and A, 144 KB), where launches for each product would be nearly all of the time (twelve matrices of 64 x 64 and 64 x 256 80 us, so 42).
 constexpr int kSmallM = 64, kSmallN = 256, kSmallThreads = 512;
 bool small(int M, int N) { return M <= kSmallM && N <= kSmallN; }
 
@@ -787,10 +790,12 @@ int set_starts(Args<TABLE>& args, F&& blocks) {
 }
 
 // The tile of a launch's products, by what a launch is estimated to take, us: rounds of blocks (tiles of sums shorter than the longest count as parts of one), each the k-steps of the longest sum and what begins and ends a
-// tile.  A k-step takes `alone` where a unit has one block (it fetches some 55 GB/s from beyond its die's L2 then, whatever the stages and waves), `step` with all slots at work; the matrix pipe's time at 128 x 128 is 0.32 at full
-// clock.  us of all products of a kind at 128 x 128 with two blocks a unit / 64 x 64 / 128 x 128 with eight waves and four stages: A and B of a 1024 x 1024 matrix (36 tiles of 128) 280 / 130 / 230, of 1536 x 1536 (78)
-// 390 / 210 / 290, of 2048 x 2048 (136) 500 / 465 / 400, of two such (272) 700 / 740 / 780; X of 1024 x 1024 (64 tiles) 150 / 70 / 115, 1536 x 1536 (144) 235 / 205 / 185, 2048 x 2048 (256) 270 / 380 / 220, of two such
-// (512) 490 / 840 / 510.  4096 x 4096, ms, all three: 128 x 128 4.04, 192 x 192 for A and B 3.63, and 256 x 128 for X (which has no triangle to fit) 3.44.
+// tile.  A k-step takes `alone` where a unit has one block (it fetches some 55 GB/s from beyond its die's L2 then, whatever the stages and waves), `step` with all slots at work; the matrix pipe's time at 128 x 128 is 0.32
+// at full clock.  us of five iterations by the rule, with A and B in tiles of 64 / 128 with eight waves and four stages / 128 with two blocks a unit / 192, and with X in 64 / 128 and one / 128 and two / 256 x 128:
+//   1024 x 1024     191    191   304   353   523    192   236   256   297      2048 x 2048     631    680   632   716   988    687   633   649   713
+//   1024 x 4096     362    362   587   686  1015    385   364   369   408      two of them    1147   1119  1237  1147  1171   1301  1196  1163  1150
+//   1536 x 1536     392    392   470   563   762    413   393   419   481      4096 x 4096    3338   3853  3855  3727  3342   4564  3545  3372  3346
+//   ResNet-50's     891    885  1022  1143  1446   1060   942   874   899      twelve layers of width 256 496  498 555 638 732  563 537 513 557
 enum Tile { kTile64, kTile128One, kTile128, kTile192, kTile256 };
 struct TileCost {
     int rows, cols, slots;

@@ -1,4 +1,4 @@
-// Shared by the kernels of a token model's output side (rmsnorm.hip, token_logprob.hip, adamw.hip): accesses of eight elements at any
+// Shared by the kernels of a token model (embedding.hip, rmsnorm.hip, layernorm.hip, token_logprob.hip, adamw.hip, newton_schulz.hip): accesses of eight elements at any
 // element's alignment, sums and maxima over a wave and a block.
 #pragma once
 
