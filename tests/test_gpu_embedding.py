@@ -189,3 +189,21 @@ def test_outputs_past_the_caches(table_kind, kind, c):
     inside = (tokens >= 0) & (tokens < vocab)
     want = torch.where(inside[:, None], table[tokens.clamp(0, vocab - 1).long()].to(t) * 0.5, torch.zeros((), dtype=t, device=gu.DEV))
     assert torch.equal(out, want)
+
+
+def test_the_longest_list():
+    """2^25 places, the most that a call takes: sums of some 6700 places each, in two passes of digits, against float64."""
+    rows, vocab, c = 1 << 25, 5000, 3
+    tokens = torch.randint(0, vocab, (rows,), dtype=torch.int32, device=gu.DEV, generator=torch.Generator(gu.DEV).manual_seed(1))
+    dout = torch.randn((rows, c), device=gu.DEV, generator=torch.Generator(gu.DEV).manual_seed(2))
+    d = lc.EmbeddingDesc(rows, vocab, c, scale=0.5)
+    dtable = torch.empty((vocab, c), device=gu.DEV)
+    lc.embedding_bwd(d, tokens, dout, dtable, gu.workspace(lc.embedding_bwd_workspace_bytes(d)))
+    want, size = (torch.zeros((vocab, c), dtype=torch.float64, device=gu.DEV).index_add_(0, tokens.long(), v) * 0.5 for v in (dout.double(), dout.double().abs()))
+    n = torch.bincount(tokens.long(), minlength=vocab)[:, None]
+    assert bool(((dtable.double() - want).abs() <= (n + 4) * U * size).all())
+    out = torch.empty((rows, c), device=gu.DEV)
+    lc.embedding_fwd(d, dtable, tokens, out)
+    assert torch.equal(out, dtable[tokens.long()] * 0.5)
+    with pytest.raises(lc.LarsConvError):
+        lc.embedding_fwd(lc.EmbeddingDesc(rows + 1, vocab, c), dtable, tokens, out)

@@ -247,3 +247,25 @@ def test_a_captured_call_on_another_stream_replays():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(outs, want))
+
+
+def test_offsets_past_32_bits():
+    """1.1 million rows of 4096 bf16, 9 GB each of input and output, with the gradient: the first and last rows against float64, and rows behind the last as they were."""
+    rows, c, u8 = 1100000, 4096, 2.0 ** -8
+    x = torch.randn((64, c), device=gu.DEV, generator=torch.Generator(gu.DEV).manual_seed(1)).to(torch.bfloat16).repeat((rows + 63) // 64, 1)[:rows]
+    y, dx = torch.empty_like(x), torch.empty((rows + 1, c), dtype=torch.bfloat16, device=gu.DEV)
+    dx[rows] = 7.0
+    gamma, mean, rstd = torch.ones(c, device=gu.DEV), torch.empty(rows, device=gu.DEV), torch.empty(rows, device=gu.DEV)
+    d = lc.LayerNormDesc(rows, c, dtype=lc.LC_BF16)
+    lc.layernorm_fwd(d, x, None, gamma, None, None, y, mean, rstd)
+    dgamma, dbeta = torch.empty(c, device=gu.DEV), torch.empty(c, device=gu.DEV)
+    lc.layernorm_bwd(d, x, y, None, gamma, mean, rstd, dx[:rows], dgamma, dbeta, gu.workspace(lc.layernorm_bwd_workspace_bytes(d)))
+    for part in (slice(0, 64), slice(rows - 64, rows)):
+        v = x[part].double()
+        n = (v - v.mean(1, keepdim=True)) / torch.sqrt(v.var(1, unbiased=False, keepdim=True) + 1e-5)
+        assert bool(((y[part].double() - n).abs() <= (u8 + 1e-4) * n.abs() + 1e-5).all())
+    # rows repeat every 64: so do their gradients, bit for bit
+    assert torch.equal(dx[:64], dx[64 * ((rows - 64) // 64):][:64]) and bool((dx[rows] == 7.0).all())
+    # dy = y and gamma = 1: dbeta sums y, dgamma y n.  Sums of rows in a fixed order, 1100000 roundings at most of what they have reached
+    ys, counts = y[:64].double(), torch.tensor([(rows - i + 63) // 64 for i in range(64)], dtype=torch.float64, device=gu.DEV)[:, None]
+    assert bool(((dbeta.double() - (ys * counts).sum(0)).abs() <= rows * 2.0 ** -24 * (ys.abs() * counts).sum(0)).all())

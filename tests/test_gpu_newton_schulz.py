@@ -267,3 +267,23 @@ def test_a_mixed_list_against_64_bits(shapes):
             a.copy_(b)
     lc.muon_step(args, 0.02, 0.95, 0.1, ws)
     assert all(torch.equal(a, b) for a, b in zip(w + m, first))
+
+
+@pytest.mark.parametrize("tall", [False, True])
+def test_the_longest_side_and_offsets_past_32_bits(tall):
+    """17000 x 65536 (pairs take 4.5 GB): v in one place of each row, in columns of their own.  The rows are orthogonal, so that each singular value goes through the polynomial by itself and
+    the result has ops' value of it in the same places; between products it is stored 15 times with 2^-22 and the polynomial's slope multiplies that by up to 3.4445 a step."""
+    rows, cols, v = 17000, 65536, 0.37
+    at = torch.randperm(cols, generator=torch.Generator().manual_seed(1))[:rows].to(gu.DEV)
+    x = torch.zeros((rows, cols), dtype=torch.bfloat16, device=gu.DEV)
+    x[torch.arange(rows, device=gu.DEV), at] = v
+    x = x.T.contiguous() if tall else x
+    d = lc.NewtonSchulzDesc(1, *x.shape, iterations=3, dtype=lc.LC_BF16)
+    lc.newton_schulz(d, x, x, gu.workspace(lc.newton_schulz_workspace_bytes(d)))
+    y = x.T if tall else x
+    s, (a, b, c) = 1 / np.sqrt(rows), ops.COEFFICIENTS
+    for _ in range(3):
+        s = a * s + b * s ** 3 + c * s ** 5
+    got = y[torch.arange(rows, device=gu.DEV), at].double()
+    assert float((got - s).abs().max()) <= s * (2.0 ** -8 + 15 * 3.4445 ** 3 * 2.0 ** -22)
+    assert int((y != 0).sum()) == rows
