@@ -21,23 +21,23 @@ __device__ __forceinline__ int key_of(const int32_t* tokens, long long i, int vo
     return t >= 0 && t < vocab ? t : kNone;
 }
 
-// Eight columns of a row, loaded (issue) and put in their places (settle) apart, so that loads of several rows are under way; EIGHTS: c is a multiple of 8; NT: past the caches.
-template <bool EIGHTS, bool NT = false, typename T>
+// What a row's columns are: a multiple of 8, another number from 8 on, or fewer.
+enum Columns { kByEights, kFromEight, kUnderEight };
+
+// Eight columns of a row, loaded (issue) and put in their places (settle) apart, so that loads of several rows are under way.  NT: past the caches.
+template <Columns COLS, bool NT = false, typename T>
 __device__ __forceinline__ void issue(Packed<T>& to, const T* row, int col, int c) {
-    if constexpr (EIGHTS) {
-        to.template load<NT>(row + col);
-    } else if (c >= 8) {
-        to.template load<NT>(row + min(col, c - 8));
-    } else {
-        to.load_some(row, c, 0u);
-    }
+    if constexpr (COLS == kByEights) to.template load<NT>(row + col);
+    else if constexpr (COLS == kFromEight) to.template load<NT>(row + min(col, c - 8));
+    else to.load_some(row, c, 0u);
 }
-template <bool EIGHTS, typename T>
+template <Columns COLS, typename T>
 __device__ __forceinline__ void settle(Packed<T>& x, int col, int c) {
-    if constexpr (!EIGHTS) {
-        if (c >= 8 && c - col < 8) x.shift(8 - (c - col), 0u);
+    if constexpr (COLS == kFromEight) {
+        if (c - col < 8) x.shift(8 - (c - col), 0u);
     }
 }
+
 // ---------------------------------------------------------------------------------------------- lookup
 
 struct LookupArgs {
@@ -52,7 +52,7 @@ struct LookupArgs {
 // Some lanes a row, eight columns a lane and access, kRowsAhead rows of a block (their tokens, then their values) under way at a time.  16384 of 2048 bf16 20.5 us (5.2 TB/s), one 2.0.
 // PAST: out goes past the caches.
 constexpr int kRowsAhead = 4;
-template <typename S, typename T, bool EIGHTS, bool PAST>
+template <typename S, typename T, Columns COLS, bool PAST>
 __global__ void __launch_bounds__(256) embedding_fwd_kernel(const LookupArgs p) {
     const int lanes = 1 << p.lane_bits, lane = threadIdx.x & (lanes - 1), each = 256 >> p.lane_bits;
     const long long stride = (long long)gridDim.x * each;
@@ -63,15 +63,15 @@ __global__ void __launch_bounds__(256) embedding_fwd_kernel(const LookupArgs p) 
         for (long long col = lane * 8; col < p.c; col += lanes * 8) {
             Packed<S> x[kRowsAhead];
 #pragma unroll
-            for (int u = 0; u < kRowsAhead; ++u) issue<EIGHTS>(x[u], static_cast<const S*>(p.table) + (key[u] == kNone ? 0 : key[u]) * p.table_ld, (int)col, p.c);
+            for (int u = 0; u < kRowsAhead; ++u) issue<COLS>(x[u], static_cast<const S*>(p.table) + (key[u] == kNone ? 0 : key[u]) * p.table_ld, (int)col, p.c);
 #pragma unroll
             for (int u = 0; u < kRowsAhead; ++u) {
                 if (row + u * stride >= p.rows) break;
-                settle<EIGHTS>(x[u], (int)col, p.c);
+                settle<COLS>(x[u], (int)col, p.c);
                 float v[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[j] = key[u] == kNone ? 0.f : x[u].get(j) * p.scale;
-                lc_store8<PAST>(static_cast<T*>(p.out) + (row + u * stride) * p.c + col, v, EIGHTS ? 8 : p.c - (int)col);
+                lc_store8<PAST>(static_cast<T*>(p.out) + (row + u * stride) * p.c + col, v, COLS == kByEights ? 8 : p.c - (int)col);
             }
         }
     }
@@ -234,22 +234,22 @@ struct SumArgs {
 constexpr int kPiece = 32;     // places whose rows one wave sums (16: sums as fast, their joining 2 to 13 us slower)
 
 // Eight columns of a sum to their place: the table's, where nothing else of the token is, or the piece's part of it.
-template <bool EIGHTS, bool ADD>
+template <Columns COLS, bool ADD>
 __device__ __forceinline__ void leave(const SumArgs& p, long long piece, int key, bool continued, bool goes_on, int col, const float* acc, Packed<float>& old) {
     const bool whole = !continued && !goes_on;
     float* const to = (whole ? p.dtable + (long long)key * p.c : p.part + (piece * 2 + (continued ? 0 : 1)) * p.c) + col;
     float v[8];
-    if constexpr (ADD) settle<EIGHTS>(old, col, p.c);
+    if constexpr (ADD) settle<COLS>(old, col, p.c);
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = ADD && whole ? fmaf(acc[j], p.scale, old.get(j)) : acc[j] * p.scale;
-    lc_store8(to, v, EIGHTS ? 8 : p.c - col);
+    lc_store8(to, v, COLS == kByEights ? 8 : p.c - col);
 }
 
 // A wave sums the rows of a piece, 512 columns of them: keys and places first, then AHEAD rows at a time, then their sums and stores.  No load stands behind a branch, and few behind a store: a wave's loads and stores
 // complete in order, so that waiting for one waits for all before it.  16384 rows of 2048 bf16 (5600 tokens, 117 MB) 27.5 us, 30011 of 1537 fp32 added to what is there 80 (321 MB, 4.0 TB/s); a wave for each place, most of which are
 // not a token's first, 40 where this took 31, with a longer joining.  Rows in whole lines are read past the caches, which nothing asks for them again (behind what
 // wrote them: 16384 of 2048 bf16 109 us for 114, 30000 159 for 173; fp32, a line of which takes two loads, 155 for 155 and 81 for 78).  Sequential rows in the place of a token's take as long; without the stores 19 of 31: all waves load, then all store.
-template <typename T, bool EIGHTS, bool ADD, int AHEAD>
+template <typename T, Columns COLS, bool ADD, int AHEAD>
 __global__ void __launch_bounds__(256) embedding_sum_kernel(const SumArgs p) {
     const int lane = threadIdx.x & 63;
     const unsigned wave = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
@@ -263,7 +263,7 @@ __global__ void __launch_bounds__(256) embedding_sum_kernel(const SumArgs p) {
     const T* const dout = static_cast<const T*>(p.dout);
     const auto key_of_place = [&](int k) __attribute__((always_inline)) { return __builtin_amdgcn_readlane(keys, k + 1); };
     const int before = key_of_place(-1);
-    const int own = ((int)tile0 * 64 + lane) * 8, col = std::min(own, EIGHTS ? p.c - 8 : p.c);
+    const int own = ((int)tile0 * 64 + lane) * 8, col = std::min(own, COLS == kByEights ? p.c - 8 : p.c);
     float acc[8] = {};
 #pragma unroll
     for (int ahead = 0; ahead < kPiece; ahead += AHEAD) {
@@ -273,10 +273,10 @@ __global__ void __launch_bounds__(256) embedding_sum_kernel(const SumArgs p) {
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
             const int row = __builtin_amdgcn_readlane(places, std::min(ahead + u, n - 1) + 1);
-            issue<EIGHTS, EIGHTS && sizeof(T) == 2>(x[u], dout + (long long)row * p.c, col, p.c);
+            issue<COLS, COLS == kByEights && sizeof(T) == 2>(x[u], dout + (long long)row * p.c, col, p.c);
             if constexpr (ADD) {
                 const int key = key_of_place(std::min(ahead + u, n - 1));
-                issue<EIGHTS>(old[u], p.dtable + (long long)(key == kNone ? 0 : key) * p.c, col, p.c);
+                issue<COLS>(old[u], p.dtable + (long long)(key == kNone ? 0 : key) * p.c, col, p.c);
             }
         }
 #pragma unroll
@@ -284,13 +284,13 @@ __global__ void __launch_bounds__(256) embedding_sum_kernel(const SumArgs p) {
             const int k = ahead + u;
             if (k >= n) break;
             const int key = key_of_place(k);
-            settle<EIGHTS>(x[u], col, p.c);
+            settle<COLS>(x[u], col, p.c);
 #pragma unroll
             for (int j = 0; j < 8; ++j) acc[j] += x[u].get(j);
             const bool last = k + 1 == n, ends = last || key_of_place(k + 1) != key;
             if (!ends) continue;
             if (key != kNone && own < p.c)
-                leave<EIGHTS, ADD>(p, piece, key, before == key, last && key_of_place(k + 1) == key, own, acc, old[ADD ? u : 0]);
+                leave<COLS, ADD>(p, piece, key, before == key, last && key_of_place(k + 1) == key, own, acc, old[ADD ? u : 0]);
 #pragma unroll
             for (int j = 0; j < 8; ++j) acc[j] = 0.f;
         }
@@ -298,7 +298,7 @@ __global__ void __launch_bounds__(256) embedding_sum_kernel(const SumArgs p) {
 }
 
 // Rows of fewer columns than a wave takes: 2^lane_bits lanes a row sum a token's rows from a place to the end of its piece, if the token or the piece begins there.
-template <typename T, bool EIGHTS, bool ADD>
+template <typename T, Columns COLS, bool ADD>
 __global__ void __launch_bounds__(256) embedding_sum_narrow_kernel(const SumArgs p) {
     const int lanes = 1 << p.lane_bits, lane = threadIdx.x & (lanes - 1), of = threadIdx.x & 63 & ~(lanes - 1);       // the first of these lanes in the wave
     const long long first = ((long long)blockIdx.x * 256 + threadIdx.x) >> p.lane_bits;
@@ -317,9 +317,9 @@ __global__ void __launch_bounds__(256) embedding_sum_narrow_kernel(const SumArgs
     for (int run = n; run == lanes && i + n < end; n += run) run = run_of(i + n + lane < end && p.key[std::min(i + n + lane, end - 1)] == key);
     const bool goes_on = i + n == end && behind == key, continued = before == key;
     const T* const dout = static_cast<const T*>(p.dout);
-    const int own = lane * 8, col = std::min(own, EIGHTS ? p.c - 8 : p.c);       // lanes past the row go along: the others ask them for places
+    const int own = lane * 8, col = std::min(own, COLS == kByEights ? p.c - 8 : p.c);       // lanes past the row go along: the others ask them for places
     Packed<float> old;
-    if constexpr (ADD) issue<EIGHTS>(old, p.dtable + (long long)key * p.c, col, p.c);
+    if constexpr (ADD) issue<COLS>(old, p.dtable + (long long)key * p.c, col, p.c);
     constexpr int U = 4;                           // rows under way
     float acc[8] = {};
     int places = place;
@@ -330,19 +330,19 @@ __global__ void __launch_bounds__(256) embedding_sum_narrow_kernel(const SumArgs
 #pragma unroll
         for (int u = 0; u < U; ++u) row[u] = __shfl(places, of + (std::min(k + u, n - 1) & (lanes - 1)), 64);
 #pragma unroll
-        for (int u = 0; u < U; ++u) issue<EIGHTS>(x[u], dout + (long long)row[u] * p.c, col, p.c);
+        for (int u = 0; u < U; ++u) issue<COLS>(x[u], dout + (long long)row[u] * p.c, col, p.c);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            settle<EIGHTS>(x[u], col, p.c);
+            settle<COLS>(x[u], col, p.c);
 #pragma unroll
             for (int j = 0; j < 8; ++j) acc[j] += k + u < n ? x[u].get(j) : 0.f;
         }
     }
-    if (own < p.c) leave<EIGHTS, ADD>(p, i / kPiece, key, continued, goes_on, own, acc, old);
+    if (own < p.c) leave<COLS, ADD>(p, i / kPiece, key, continued, goes_on, own, acc, old);
 }
 
 // Tokens that cross pieces: the lanes of the piece where one begins add up its parts in the order of the pieces.
-template <bool EIGHTS, bool ADD>
+template <Columns COLS, bool ADD>
 __global__ void __launch_bounds__(256) embedding_join_kernel(const SumArgs p) {
     const int lanes = 1 << p.lane_bits, lane = threadIdx.x & (lanes - 1), of = threadIdx.x & 63 & ~(lanes - 1);
     const unsigned group = (blockIdx.x * 256u + threadIdx.x) >> p.lane_bits, piece = group / (unsigned)p.tiles, tile = group - piece * (unsigned)p.tiles;
@@ -351,13 +351,13 @@ __global__ void __launch_bounds__(256) embedding_join_kernel(const SumArgs p) {
     const int key = p.key[end - 1], behind = p.key[end], start = p.key[end - kPiece], before = piece > 0 ? p.key[end - kPiece - 1] : kNone;
     if (key >= p.vocab || behind != key || (start == key && before == key)) return;          // (the last: it began earlier)
     const unsigned long long every = p.lane_bits == 6 ? ~0ull : (1ull << lanes) - 1;
-    const int own = ((int)tile * lanes + lane) * 8, col = std::min(own, EIGHTS ? p.c - 8 : p.c);
+    const int own = ((int)tile * lanes + lane) * 8, col = std::min(own, COLS == kByEights ? p.c - 8 : p.c);
     constexpr int U = 8;                           // parts under way
     float acc[8];
     Packed<float> x[U], old;
-    issue<EIGHTS>(x[0], p.part + ((long long)piece * 2 + 1) * p.c, col, p.c);
-    if constexpr (ADD) issue<EIGHTS>(old, p.dtable + (long long)key * p.c, col, p.c);
-    settle<EIGHTS>(x[0], col, p.c);
+    issue<COLS>(x[0], p.part + ((long long)piece * 2 + 1) * p.c, col, p.c);
+    if constexpr (ADD) issue<COLS>(old, p.dtable + (long long)key * p.c, col, p.c);
+    settle<COLS>(x[0], col, p.c);
 #pragma unroll
     for (int j = 0; j < 8; ++j) acc[j] = x[0].get(j);
     for (long long next = (long long)piece + 1;;) {       // lanes look at the next pieces' first keys, as many at a time as they are
@@ -366,10 +366,10 @@ __global__ void __launch_bounds__(256) embedding_join_kernel(const SumArgs p) {
         const int run = (bits & every) == every ? lanes : __builtin_ctzll(~bits);
         for (int k = 0; k < run; k += U) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) issue<EIGHTS>(x[u], p.part + (next + std::min(k + u, run - 1)) * 2 * p.c, col, p.c);
+            for (int u = 0; u < U; ++u) issue<COLS>(x[u], p.part + (next + std::min(k + u, run - 1)) * 2 * p.c, col, p.c);
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                settle<EIGHTS>(x[u], col, p.c);
+                settle<COLS>(x[u], col, p.c);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) acc[j] += k + u < run ? x[u].get(j) : 0.f;
             }
@@ -379,11 +379,11 @@ __global__ void __launch_bounds__(256) embedding_join_kernel(const SumArgs p) {
     }
     if (own >= p.c) return;
     if constexpr (ADD) {
-        settle<EIGHTS>(old, col, p.c);
+        settle<COLS>(old, col, p.c);
 #pragma unroll
         for (int j = 0; j < 8; ++j) acc[j] += old.get(j);
     }
-    lc_store8(p.dtable + (long long)key * p.c + own, acc, EIGHTS ? 8 : p.c - own);
+    lc_store8(p.dtable + (long long)key * p.c + own, acc, COLS == kByEights ? 8 : p.c - own);
 }
 
 // ---------------------------------------------------------------------------------------------- host
@@ -404,6 +404,11 @@ lc_status check_desc(const lc_embedding_desc* d) {
         __builtin_mul_overflow((long long)d->vocab, std::max<long long>(d->table_ld, d->c), &bytes) || __builtin_mul_overflow(bytes, 4ll, &bytes))
         return LC_ERR_SHAPE;
     return LC_OK;
+}
+
+template <typename F>
+void by_columns(int c, F&& f) {
+    c % 8 == 0 ? f.template operator()<kByEights>() : c > 8 ? f.template operator()<kFromEight>() : f.template operator()<kUnderEight>();
 }
 
 int lanes_of(int c) {                              // the smallest power of two from 8 on that takes a row at once, a block's threads at most
@@ -453,9 +458,10 @@ extern "C" lc_status embedding_fwd(const lc_embedding_desc* desc, const void* ta
     lc_begin_call();
     const bool past = (long long)desc->rows * desc->c * (desc->dtype == LC_BF16 ? 2 : 4) >= kPastBytes;
     const auto launch = [&]<typename S, typename T>() {
-        const auto kernel = desc->c % 8 == 0 ? (past ? embedding_fwd_kernel<S, T, true, true> : embedding_fwd_kernel<S, T, true, false>)
-                                             : (past ? embedding_fwd_kernel<S, T, false, true> : embedding_fwd_kernel<S, T, false, false>);
-        hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a);
+        by_columns(desc->c, [&]<Columns COLS>() {
+            if (past) hipLaunchKernelGGL((embedding_fwd_kernel<S, T, COLS, true>), grid, dim3(256), 0, stream, a);
+            else hipLaunchKernelGGL((embedding_fwd_kernel<S, T, COLS, false>), grid, dim3(256), 0, stream, a);
+        });
     };
     if (desc->table_dtype == LC_BF16) desc->dtype == LC_BF16 ? launch.template operator()<uint16_t, uint16_t>() : launch.template operator()<uint16_t, float>();
     else desc->dtype == LC_BF16 ? launch.template operator()<float, uint16_t>() : launch.template operator()<float, float>();
@@ -523,15 +529,14 @@ extern "C" lc_status embedding_bwd(const lc_embedding_desc* desc, const int32_t*
     }
     const SumArgs a{lists[last ? 2 : 0], lists[last ? 3 : 1], dout, dtable, reinterpret_cast<float*>(ws + plan.part_at), plan.pieces, (int)desc->rows, desc->vocab, desc->c,
                     __builtin_ctz(plan.lanes), plan.tiles, desc->scale};
-    const auto launch = [&]<typename T, bool EIGHTS, bool ADD>() {
+    const auto launch = [&]<typename T, Columns COLS, bool ADD>() {
         const auto blocks = [](long long threads) { return dim3((unsigned)((threads + 255) / 256)); };
-        if (plan.lanes < 64) hipLaunchKernelGGL((embedding_sum_narrow_kernel<T, EIGHTS, ADD>), blocks(desc->rows * plan.lanes), dim3(256), 0, stream, a);
-        else hipLaunchKernelGGL((embedding_sum_kernel<T, EIGHTS, ADD, 8>), blocks(plan.pieces * plan.tiles * 64), dim3(256), 0, stream, a);
-        if (plan.pieces > 1) hipLaunchKernelGGL((embedding_join_kernel<EIGHTS, ADD>), blocks(plan.pieces * plan.tiles * plan.lanes), dim3(256), 0, stream, a);
+        if (plan.lanes < 64) hipLaunchKernelGGL((embedding_sum_narrow_kernel<T, COLS, ADD>), blocks(desc->rows * plan.lanes), dim3(256), 0, stream, a);
+        else if constexpr (COLS != kUnderEight) hipLaunchKernelGGL((embedding_sum_kernel<T, COLS, ADD, 8>), blocks(plan.pieces * plan.tiles * 64), dim3(256), 0, stream, a);
+        if (plan.pieces > 1) hipLaunchKernelGGL((embedding_join_kernel<COLS, ADD>), blocks(plan.pieces * plan.tiles * plan.lanes), dim3(256), 0, stream, a);
     };
     const auto with_type = [&]<typename T>() {
-        if (desc->c % 8 == 0) accumulate ? launch.template operator()<T, true, true>() : launch.template operator()<T, true, false>();
-        else accumulate ? launch.template operator()<T, false, true>() : launch.template operator()<T, false, false>();
+        by_columns(desc->c, [&]<Columns COLS>() { accumulate ? launch.template operator()<T, COLS, true>() : launch.template operator()<T, COLS, false>(); });
     };
     desc->dtype == LC_BF16 ? with_type.template operator()<uint16_t>() : with_type.template operator()<float>();
     return lc_end_call();
