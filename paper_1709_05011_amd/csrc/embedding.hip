@@ -49,14 +49,16 @@ struct LookupArgs {
     float scale;
 };
 
-// Some lanes a row, eight columns a lane and access, kRowsAhead rows of a block (their tokens, then their values) under way at a time.  16384 of 2048 bf16 20.5 us (5.2 TB/s), one 2.0.
+// Some lanes a row, eight columns a lane and access, kRowsAhead rows of a block (their tokens, then their values) under way at a time, neighbours unless every block has one at most.  16384 of 2048 bf16 19.5 us (5.5 TB/s), one 2.0.
+// (By themselves, us, four rows a grid apart / two neighbours: 16384 x 2048 bf16 22.4 / 21.0, 30000 39.0 / 37.6, 8000 x 8200 52.6 / 50.6, 30011 x 1537 fp32 60 / 56.)
 // PAST: out goes past the caches.
-constexpr int kRowsAhead = 4;
+constexpr int kRowsAhead = 2;
 template <typename S, typename T, Columns COLS, bool PAST>
 __global__ void __launch_bounds__(256) embedding_fwd_kernel(const LookupArgs p) {
     const int lanes = 1 << p.lane_bits, lane = threadIdx.x & (lanes - 1), each = 256 >> p.lane_bits;
-    const long long stride = (long long)gridDim.x * each;
-    for (long long row = (long long)blockIdx.x * each + (threadIdx.x >> p.lane_bits); row < p.rows; row += stride * kRowsAhead) {
+    const bool few = gridDim.x * (long long)each >= p.rows;
+    const long long stride = few ? (long long)gridDim.x * each : each;
+    for (long long row = (long long)blockIdx.x * each * (few ? 1 : kRowsAhead) + (threadIdx.x >> p.lane_bits); row < p.rows; row += (long long)gridDim.x * each * kRowsAhead) {
         int key[kRowsAhead];
 #pragma unroll
         for (int u = 0; u < kRowsAhead; ++u) key[u] = key_of(p.tokens, std::min(row + u * stride, p.rows - 1), p.vocab);
