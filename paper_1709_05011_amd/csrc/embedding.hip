@@ -49,7 +49,7 @@ struct LookupArgs {
     float scale;
 };
 
-// Some lanes a row, eight columns a lane and access, kRowsAhead rows of a block (their tokens, then their values) under way at a time, neighbours unless every block has one at most.  16384 of 2048 bf16 19.5 us (5.5 TB/s), one 2.0.
+// Some lanes a row, eight columns a lane and access, kRowsAhead rows of a block (their tokens, then their values) under way at a time, neighbours unless every block has one at most.  16384 of 2048 bf16 20 to 22 us (4.9 to 5.4 TB/s), one 2.0.
 // (By themselves, us, four rows a grid apart / two neighbours: 16384 x 2048 bf16 22.4 / 21.0, 30000 39.0 / 37.6, 8000 x 8200 52.6 / 50.6, 30011 x 1537 fp32 60 / 56.)
 // PAST: out goes past the caches.
 constexpr int kRowsAhead = 2;
@@ -249,7 +249,7 @@ __device__ __forceinline__ void leave(const SumArgs& p, long long piece, int key
 }
 
 // A wave sums the rows of a piece, 512 columns of them: keys and places first, then AHEAD rows at a time, then their sums and stores.  No load stands behind a branch, and few behind a store: a wave's loads and stores
-// complete in order, so that waiting for one waits for all before it.  16384 rows of 2048 bf16 (5600 tokens, 117 MB) 27.5 us, 30011 of 1537 fp32 added to what is there 80 (321 MB, 4.0 TB/s); a wave for each place, most of which are
+// complete in order, so that waiting for one waits for all before it.  16384 rows of 2048 bf16 (5600 tokens, 117 MB) 27.5 us, 30011 of 1537 fp32 added to what is there 77 (321 MB, 4.2 TB/s); a wave for each place, most of which are
 // not a token's first, 40 where this took 31, with a longer joining.  Rows in whole lines are read past the caches, which nothing asks for them again (behind what
 // wrote them: 16384 of 2048 bf16 109 us for 114, 30000 159 for 173; fp32, a line of which takes two loads, 155 for 155 and 81 for 78).  Sequential rows in the place of a token's take as long; without the stores 19 of 31: all waves load, then all store.
 template <typename T, Columns COLS, bool ADD, int AHEAD>
@@ -394,7 +394,7 @@ __global__ void __launch_bounds__(256) embedding_join_kernel(const SumArgs p) {
 constexpr long long kMostBlocks = 1 << 20;
 constexpr long long kMostRows = 1ll << 25;        // a launch holds fewer than 2^32 threads, and a row has 64 of them at most
 
-// Bytes of out from which it goes past the caches.  us, three sets in turn, ordinary / past: 24000 x 2048 bf16 (98 MB) 32.3 / 24.6, 40000 (164 MB) 51 / 39, 30011 x 1537 fp32 (184 MB) with the gradient 193 / 181; but with a
+// Bytes of out from which it goes past the caches.  us, three sets in turn, ordinary / past: 24000 x 2048 bf16 (98 MB) 32.3 / 24.6, 40000 (164 MB) 51 / 39, 30011 x 1537 fp32 (184 MB) with the gradient 193 / 181 (then); but with a
 // layer norm of out behind it 30000 x 2048 bf16 84 / 86, 40000 113 / 114, 60000 162 / 163, 100000 273 / 272, fp32 16000 (131 MB) 111 / 117, 20000 136 / 143, 30011 x 1537 160 / 161.
 constexpr long long kPastBytes = 160 << 20;
 

@@ -12,7 +12,7 @@
 // and B are symmetric, so that two products read rows along their sums; B X reads rows of X from LDS the other way round.  (X kept both ways round as well, ResNet-50's filters,
 // 94 MB: 110 us for B X, so 84; two layers of width 2048 1094, so 1003.)
 //
-// Bound by the matrix pipe and the card's power where products are large (4096 x 4096: 3.3 to 3.5 ms from card to card, B X 315 to 330 us, 1.25 to 1.3 PFLOP/s of the pairs' products, as a large library product of fp16), by
+// Bound by the matrix pipe and the card's power where products are large (4096 x 4096: 3.25 to 3.5 ms from card to card, B X 305 to 330 us, 1.25 to 1.35 PFLOP/s of the pairs' products, as a large library product of fp16), by
 // what a unit fetches from L2 in between, by launches where they are small (three of 517 x 1031: 17 launches of 6 to 13 us, 181).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
