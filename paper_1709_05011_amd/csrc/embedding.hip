@@ -103,7 +103,7 @@ __device__ __forceinline__ void fill_share(const SortArgs& p, int threads) {
 }
 
 // Few places (3064 in a table of 10836 x 2048, with the lookup and all else 44 us): a block ranks 64 of them against all, which it holds in LDS; each of its 16 waves a share of them.
-constexpr int kRankMost = 4096;
+constexpr int kRankMost = 6144;
 __global__ void __launch_bounds__(1024) embedding_rank_kernel(const SortArgs p) {
     if ((int)blockIdx.x >= p.sort_blocks) {
         fill_share(p, 1024);
@@ -431,10 +431,12 @@ Plan plan_of(const lc_embedding_desc* d) {
     p.lanes = std::min(64, lanes_of(d->c));
     p.tiles = (int)(((long long)d->c + p.lanes * 8 - 1) / (p.lanes * 8));
     p.pieces = (rows + kPiece - 1) / kPiece;
-    if (rows > kRankMost) {
-        int bits = 1;
-        while (bits < 31 && (1ll << bits) <= d->vocab) ++bits;                     // keys up to vocab
-        p.passes = (bits + kMostBits - 1) / kMostBits;
+    int bits = 1;
+    while (bits < 31 && (1ll << bits) <= d->vocab) ++bits;                         // keys up to vocab
+    const int passes = (bits + kMostBits - 1) / kMostBits;
+    // ranks against all go by the square of the places: 5000 of 256 bf16 columns with the lookup, us, in passes / ranked: one pass 24 / 25, two 32 / 25; 8192 24.6 / 30, 32 / 30, and with 160 MB of zeros 56 / 57
+    if (rows > (passes > 1 ? kRankMost : 4096)) {
+        p.passes = passes;
         p.bits = (bits + p.passes - 1) / p.passes;
         p.per = (int)std::max<long long>(1024, ((rows + kSortBlocks - 1) / kSortBlocks + 1023) / 1024 * 1024);
         p.sort_blocks = (int)((rows + p.per - 1) / p.per);
@@ -498,7 +500,7 @@ extern "C" lc_status embedding_bwd(const lc_embedding_desc* desc, const int32_t*
     int* lists[4];
     for (int i = 0; i < 4; ++i) lists[i] = reinterpret_cast<int*>(ws + list * i);
     // the whole table is set to zero by the launches that sort, in equal shares: what tokens then write is written twice, and the rest costs no search for what is absent and hides the launches' latency
-    // (32768 rows of 2048, 16384 places: by the sums' launch, absent rows alone, 121 us with the lookup, so 117)
+    // (32768 rows of 2048, 16384 places: by the sums' launch, absent rows alone, 121 us with the lookup where this took 117)
     const long long launches = std::max(1, 2 * plan.passes), fill = accumulate ? 0 : (long long)desc->vocab * desc->c * 4, share = ((fill + launches - 1) / launches + 15) & ~15ll;
     long long zeroed = 0;
     SortArgs s{tokens, nullptr, nullptr, lists[0], lists[1], nullptr, (int)desc->rows, desc->vocab, plan.per, 0, plan.bits, 0, dtable, 0};

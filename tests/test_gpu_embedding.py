@@ -16,7 +16,7 @@ pytestmark = pytest.mark.gpu
 U = 2.0 ** -24
 TYPES = {"f32": (lc.LC_F32, torch.float32, 0.0), "bf16": (lc.LC_BF16, torch.bfloat16, 2.0 ** -8)}
 # rows, vocab, c: one token to lists that are sorted in one, two and three passes; one column to several blocks a row
-SHAPES = [(1, 1, 1), (1, 70000, 8), (2, 3, 5), (7, 50, 2056), (64, 10, 33), (65, 1000, 64), (100, 7, 4100), (1000, 33, 9), (4096, 3000, 20), (4097, 1000, 96), (5000, 1023, 8), (5000, 1024, 7),
+SHAPES = [(1, 1, 1), (1, 70000, 8), (2, 3, 5), (7, 50, 2056), (64, 10, 33), (65, 1000, 64), (100, 7, 4100), (1000, 33, 9), (4096, 3000, 20), (4097, 1000, 96), (5000, 1023, 8), (5000, 1024, 7), (6144, 1024, 40), (6145, 1024, 40), (70000, 900, 16),
           (9000, 70000, 24), (20000, 300, 136), (140000, 1 << 21, 3)]
 
 
