@@ -13,7 +13,7 @@
 // 94 MB: 110 us for B X, so 84; two layers of width 2048 1094, so 1003.)
 //
 // Bound by the matrix pipe and the card's power where products are large (4096 x 4096: 3.25 to 3.5 ms from card to card, B X 305 to 330 us, 1.25 to 1.35 PFLOP/s of the pairs' products, as a large library product of fp16), by
-// what a unit fetches from L2 in between, by launches where they are small (three of 517 x 1031: 17 launches of 6 to 13 us, 181).
+// what a unit fetches from L2 in between, by launches where they are small (three of 517 x 1031: 17 launches of 6 to 13 us, 172 to 177).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -67,6 +67,8 @@ struct Args {
     Mat t[TABLE];
     int start[(TABLE + 63) / 64 * 64];   // first block of each, past the last the largest int
     uint8_t dies[TABLE], die[TABLE];     // products: how many dies take a matrix, from which on
+    int cuts;                            // or: the tile that a die begins with, and the one behind its last
+    int cut[TABLE][9];
     Scalars s;
 };
 
@@ -309,10 +311,17 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) ns_product_kernel(const Args<
     const int owner = owner_of(args, blockIdx.x, &local);
     const Mat& t = args.t[owner];
     const int M = t.M, N = t.N;
-    // blocks are dealt round the dies, a matrix's begin at a multiple of 8: its dies take neighbouring tiles each, the others' blocks have nothing to do
-    const int dies = args.dies[owner], part = (local - args.die[owner]) & 7;
-    const int tiles = tiles_of<KIND>(t, BM, BN), per = (tiles + dies - 1) / dies, tile = part * per + (local >> 3);
-    if (part >= dies || tile >= std::min(tiles, (part + 1) * per)) return;
+    // blocks are dealt round the dies, a matrix's begin at a multiple of 8: its dies take neighbouring tiles each, blocks past a die's part have nothing to do
+    int tile;
+    if (args.cuts) {
+        tile = args.cut[owner][local & 7] + (local >> 3);
+        if (tile >= args.cut[owner][(local & 7) + 1]) return;
+    } else {
+        const int dies = args.dies[owner], part = (local - args.die[owner]) & 7;
+        const int tiles = tiles_of<KIND>(t, BM, BN), per = (tiles + dies - 1) / dies;
+        tile = part * per + (local >> 3);
+        if (part >= dies || tile >= std::min(tiles, (part + 1) * per)) return;
+    }
     int ti, tj;
     place_of<KIND>(t, tile, BM, BN, &ti, &tj);
     ti = __builtin_amdgcn_readfirstlane(ti);
@@ -830,17 +839,34 @@ template <int TABLE>
 struct LaunchPlan {
     Tile tile;
     uint8_t dies[TABLE], die[TABLE];
+    bool cuts;
+    int cut[TABLE][9];
 };
+// Where all tiles of a launch have a place at once, loads need not be even to the tile, and the list's tiles, matrix after matrix, are cut into eight parts of the same cost: a die then meets one or two matrices.  us, dies by
+// matrices / so: three of 517 x 1031 177 / 172, four 231 / 209, ten 412 / 318, four of 700 x 700 221 / 204, two of 1024 x 1024 286 / 270, four layers of width 512 640 / 592, two of 700 755 / 700; with twice as many tiles
+// as places ResNet-50's filters 880 / 918, three layers of width 1298 4810 / 5190.
+constexpr double kCutRounds = 1.0;
 template <Product KIND, int TABLE>
 LaunchPlan<TABLE> plan_of(const Args<TABLE>& args) {
-    LaunchPlan<TABLE> plan{tile_of<KIND>(args), {}, {}};
+    LaunchPlan<TABLE> plan{tile_of<KIND>(args), {}, {}, false, {}};
     const TileCost& k = kTiles[plan.tile];
-    double cost[TABLE], all = 0.0, load[8] = {};
+    double cost[TABLE], all = 0.0, number = 0.0, load[8] = {};
     int order[TABLE];
     for (int i = 0; i < args.s.count; ++i) {
         cost[i] = (double)tiles_of<KIND>(args.t[i], k.rows, k.cols) * ((KIND == kGram ? args.t[i].N : args.t[i].M) / 32 * k.step + k.ends);
         all += cost[i];
+        number += tiles_of<KIND>(args.t[i], k.rows, k.cols);
         order[i] = i;
+    }
+    if (number <= kCutRounds * k.slots) {
+        plan.cuts = true;
+        double before = 0.0;
+        for (int i = 0; i < args.s.count; ++i) {
+            const int tiles = tiles_of<KIND>(args.t[i], k.rows, k.cols);
+            for (int d = 0; d <= 8; ++d) plan.cut[i][d] = (int)std::min<double>(tiles, std::max(0.0, std::round((all * d / 8 - before) / cost[i] * tiles)));
+            before += cost[i];
+        }
+        return plan;
     }
     for (int i = 0; i < args.s.count; ++i) {
         int dies = 1;
@@ -872,10 +898,17 @@ LaunchPlan<TABLE> plan_of(const Args<TABLE>& args) {
 template <Product KIND, bool MUON, typename T, int TM, int TN, int WM, int WN, int NS, int TABLE>
 bool launch_product(Args<TABLE>& args, hipStream_t stream) {
     constexpr int lds = std::max(NS * (TM * WM + TN * WN) * 16 * 128, WM * WN * TM * 16 * (leaving_columns(TN) * 16 + 4) * 4);
-    const uint8_t* dies = args.dies;
+    int i = 0;
     const int blocks = set_starts(args, [&](const Mat& t) {
-        const int shared = *dies++;
-        return (tiles_of<KIND>(t, 16 * TM * WM, 16 * TN * WN) + shared - 1) / shared * 8;
+        if (args.cuts) {
+            const int* const cut = args.cut[i++];
+            int most = 0;
+            for (int d = 0; d < 8; ++d) most = std::max(most, cut[d + 1] - cut[d]);
+            return most * 8;
+        } else {
+            const int shared = args.dies[i++];
+            return (tiles_of<KIND>(t, 16 * TM * WM, 16 * TN * WN) + shared - 1) / shared * 8;
+        }
     });
     static const bool once = hipFuncSetAttribute(reinterpret_cast<const void*>(ns_product_kernel<KIND, MUON, T, TM, TN, WM, WN, NS, TABLE>),
                                                  hipFuncAttributeMaxDynamicSharedMemorySize, lds) == hipSuccess;
@@ -886,6 +919,8 @@ template <Product KIND, bool MUON, typename T, int TABLE>
 bool launch_product(Args<TABLE>& args, const LaunchPlan<TABLE>& plan, hipStream_t stream) {
     std::copy(plan.dies, plan.dies + TABLE, args.dies);
     std::copy(plan.die, plan.die + TABLE, args.die);
+    args.cuts = plan.cuts;
+    std::copy(&plan.cut[0][0], &plan.cut[0][0] + TABLE * 9, &args.cut[0][0]);
     switch (plan.tile) {
         case kTile64: return launch_product<KIND, MUON, T, 2, 2, 2, 2, 4>(args, stream);
         case kTile128One: return launch_product<KIND, MUON, T, 2, 4, 4, 2, 4>(args, stream);
