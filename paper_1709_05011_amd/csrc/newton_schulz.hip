@@ -67,8 +67,8 @@ struct Args {
     Mat t[TABLE];
     int start[(TABLE + 63) / 64 * 64];   // first block of each, past the last the largest int
     uint8_t dies[TABLE], die[TABLE];     // products: how many dies take a matrix, from which on
-    int cuts;                            // or: the tile that a die begins with, and the one behind its last
-    int cut[TABLE][9];
+    int cuts;                            // or: start[] counts tiles instead, and the tile of all that a die begins with, and the one behind its last
+    int cut[9];
     Scalars s;
 };
 
@@ -307,21 +307,22 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) ns_product_kernel(const Args<
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / WN, wn = wave % WN;
-    int local;
-    const int owner = owner_of(args, blockIdx.x, &local);
-    const Mat& t = args.t[owner];
-    const int M = t.M, N = t.N;
-    // blocks are dealt round the dies, a matrix's begin at a multiple of 8: its dies take neighbouring tiles each, blocks past a die's part have nothing to do
-    int tile;
+    // blocks are dealt round the dies
+    int tile, owner;
     if (args.cuts) {
-        tile = args.cut[owner][local & 7] + (local >> 3);
-        if (tile >= args.cut[owner][(local & 7) + 1]) return;
-    } else {
+        const int die = blockIdx.x & 7, at = args.cut[die] + (int)(blockIdx.x >> 3);
+        if (at >= args.cut[die + 1]) return;
+        owner = owner_of(args, at, &tile);
+    } else {                                       // a matrix's begin at a multiple of 8: its dies take neighbouring tiles each, the others' blocks have nothing to do
+        int local;
+        owner = owner_of(args, blockIdx.x, &local);
         const int dies = args.dies[owner], part = (local - args.die[owner]) & 7;
-        const int tiles = tiles_of<KIND>(t, BM, BN), per = (tiles + dies - 1) / dies;
+        const int tiles = tiles_of<KIND>(args.t[owner], BM, BN), per = (tiles + dies - 1) / dies;
         tile = part * per + (local >> 3);
         if (part >= dies || tile >= std::min(tiles, (part + 1) * per)) return;
     }
+    const Mat& t = args.t[owner];
+    const int M = t.M, N = t.N;
     int ti, tj;
     place_of<KIND>(t, tile, BM, BN, &ti, &tj);
     ti = __builtin_amdgcn_readfirstlane(ti);
@@ -840,10 +841,10 @@ struct LaunchPlan {
     Tile tile;
     uint8_t dies[TABLE], die[TABLE];
     bool cuts;
-    int cut[TABLE][9];
+    int cut[9];
 };
 // Where all tiles of a launch have a place at once, loads need not be even to the tile, and the list's tiles, matrix after matrix, are cut into eight parts of the same cost: a die then meets one or two matrices.  us, dies by
-// matrices / so: three of 517 x 1031 177 / 172, four 231 / 209, ten 412 / 318, four of 700 x 700 221 / 204, two of 1024 x 1024 286 / 270, four layers of width 512 640 / 592, two of 700 755 / 700; with twice as many tiles
+// matrices / so: three of 517 x 1031 177 / 170, four 231 / 205, ten 412 / 304, four of 700 x 700 221 / 197, two of 1024 x 1024 286 / 267, twenty of 256 x 512 185 / 146, four layers of width 512 640 / 590, two of 700 755 / 700; with twice as many tiles
 // as places ResNet-50's filters 880 / 918, three layers of width 1298 4810 / 5190.
 constexpr double kCutRounds = 1.0;
 template <Product KIND, int TABLE>
@@ -863,7 +864,7 @@ LaunchPlan<TABLE> plan_of(const Args<TABLE>& args) {
         double before = 0.0;
         for (int i = 0; i < args.s.count; ++i) {
             const int tiles = tiles_of<KIND>(args.t[i], k.rows, k.cols);
-            for (int d = 0; d <= 8; ++d) plan.cut[i][d] = (int)std::min<double>(tiles, std::max(0.0, std::round((all * d / 8 - before) / cost[i] * tiles)));
+            for (int d = 0; d <= 8; ++d) plan.cut[d] += (int)std::min<double>(tiles, std::max(0.0, std::round((all * d / 8 - before) / cost[i] * tiles)));
             before += cost[i];
         }
         return plan;
@@ -899,17 +900,14 @@ template <Product KIND, bool MUON, typename T, int TM, int TN, int WM, int WN, i
 bool launch_product(Args<TABLE>& args, hipStream_t stream) {
     constexpr int lds = std::max(NS * (TM * WM + TN * WN) * 16 * 128, WM * WN * TM * 16 * (leaving_columns(TN) * 16 + 4) * 4);
     int i = 0;
-    const int blocks = set_starts(args, [&](const Mat& t) {
-        if (args.cuts) {
-            const int* const cut = args.cut[i++];
-            int most = 0;
-            for (int d = 0; d < 8; ++d) most = std::max(most, cut[d + 1] - cut[d]);
-            return most * 8;
-        } else {
-            const int shared = args.dies[i++];
-            return (tiles_of<KIND>(t, 16 * TM * WM, 16 * TN * WN) + shared - 1) / shared * 8;
-        }
+    int blocks = set_starts(args, [&](const Mat& t) {
+        const int tiles = tiles_of<KIND>(t, 16 * TM * WM, 16 * TN * WN), dies = args.dies[i++];
+        return args.cuts ? tiles : (tiles + dies - 1) / dies * 8;
     });
+    if (args.cuts) {
+        blocks = 0;
+        for (int d = 0; d < 8; ++d) blocks = std::max(blocks, (args.cut[d + 1] - args.cut[d]) * 8);
+    }
     static const bool once = hipFuncSetAttribute(reinterpret_cast<const void*>(ns_product_kernel<KIND, MUON, T, TM, TN, WM, WN, NS, TABLE>),
                                                  hipFuncAttributeMaxDynamicSharedMemorySize, lds) == hipSuccess;
     if (once) hipLaunchKernelGGL((ns_product_kernel<KIND, MUON, T, TM, TN, WM, WN, NS, TABLE>), dim3((unsigned)blocks), dim3(WM * WN * 64), lds, stream, args);
@@ -920,7 +918,7 @@ bool launch_product(Args<TABLE>& args, const LaunchPlan<TABLE>& plan, hipStream_
     std::copy(plan.dies, plan.dies + TABLE, args.dies);
     std::copy(plan.die, plan.die + TABLE, args.die);
     args.cuts = plan.cuts;
-    std::copy(&plan.cut[0][0], &plan.cut[0][0] + TABLE * 9, &args.cut[0][0]);
+    std::copy(plan.cut, plan.cut + 9, args.cut);
     switch (plan.tile) {
         case kTile64: return launch_product<KIND, MUON, T, 2, 2, 2, 2, 4>(args, stream);
         case kTile128One: return launch_product<KIND, MUON, T, 2, 4, 4, 2, 4>(args, stream);
