@@ -13,7 +13,7 @@
 // 94 MB: 110 us for B X, so 84; two layers of width 2048 1094, so 1003.)
 //
 // Bound by the matrix pipe and the card's power where products are large (4096 x 4096: 3.25 to 3.5 ms from card to card, B X 305 to 330 us, 1.25 to 1.35 PFLOP/s of the pairs' products, as a large library product of fp16), by
-// what a unit fetches from L2 in between, by launches where they are small (three of 517 x 1031: 17 launches of 6 to 13 us, 172 to 177).
+// what a unit fetches from L2 in between, by launches where they are small (three of 517 x 1031: 17 launches of 6 to 13 us, 168 to 175).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -843,10 +843,10 @@ struct LaunchPlan {
     bool cuts;
     int cut[9];
 };
-// Where all tiles of a launch have a place at once, loads need not be even to the tile, and the list's tiles, matrix after matrix, are cut into eight parts of the same cost: a die then meets one or two matrices.  us, dies by
+// Where all tiles of a launch have a place at once, or nearly, loads need not be even to the tile, and the list's tiles, matrix after matrix, are cut into eight parts of the same cost: a die then meets one or two matrices.  us, dies by
 // matrices / so: three of 517 x 1031 177 / 170, four 231 / 205, ten 412 / 304, four of 700 x 700 221 / 197, two of 1024 x 1024 286 / 267, twenty of 256 x 512 185 / 146, four layers of width 512 640 / 590, two of 700 755 / 700; with twice as many tiles
-// as places ResNet-50's filters 880 / 918, three layers of width 1298 4810 / 5190.
-constexpr double kCutRounds = 1.0;
+// as places ResNet-50's filters 880 / 895, three layers of width 1298 4800 / 5115 (1.4 times: twelve layers of width 256 460 / 432, those two as before).
+constexpr double kCutRounds = 1.4;
 template <Product KIND, int TABLE>
 LaunchPlan<TABLE> plan_of(const Args<TABLE>& args) {
     LaunchPlan<TABLE> plan{tile_of<KIND>(args), {}, {}, false, {}};
