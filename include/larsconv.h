@@ -433,7 +433,8 @@ lc_status layernorm_fwd(const lc_layernorm_desc* desc, const void* x, const void
 
 /* Gradient: with a = dy * gamma and n = (total - mean) * rstd (total: what the forward pass stored, or its x where there was no residual; h_ld elements from row to row, 0: c),
  *     dx = rstd * (a - mean of a - n * mean of (a * n)) + dtotal,   dgamma = sum over the rows of dy * n,   dbeta = sum over the rows of dy.
- * dtotal as in rmsnorm_bwd, or NULL; dbeta may be NULL.  dy, dtotal, dx: [rows][c], contiguous.  n is formed from save_mean as stored (an error of |mean| * rstd * 2^-24).
+ * dtotal as in rmsnorm_bwd, or NULL; dbeta may be NULL.  dy, dtotal, dx: [rows][c], contiguous.  n is formed from save_mean and save_rstd as stored (an error of |mean| * rstd * 2^-24);
+ * rows whose deviations leave fp32 have finite gradients, rows of deviations under 2^-128 (with an eps of 0), whose rstd leaves it, have none.
  * x_ld and residual_ld of desc are not used.  Buffers must not overlap. */
 size_t layernorm_bwd_workspace_bytes(const lc_layernorm_desc* desc);
 lc_status layernorm_bwd(const lc_layernorm_desc* desc, const void* total, int64_t h_ld, const void* dy, const void* dtotal, const float* gamma,

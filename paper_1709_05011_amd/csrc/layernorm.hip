@@ -344,6 +344,18 @@ struct LayerBwdArgs {
     int c;
 };
 
+// n of a row's values from its saved statistics, (h - mean) * rstd.  Where deviations may leave fp32 (one over 2^127 in a row of up to 2^30 values takes rstd under 2^-112) h and mean are a quarter and rstd four times what they are;
+// elsewhere the same bits as without (h times 1 is exact, and the operation as long as a subtraction).
+template <bool SAME>                                                // the row is the same for a wave
+struct Centred {
+    float part, mean, n_scale;
+    __device__ __forceinline__ Centred(float mean, float rstd) : part(rstd < 0x1p-100f ? 0.25f : 1.f), mean(mean * part), n_scale(rstd < 0x1p-100f ? 4.f * rstd : rstd) {
+        if constexpr (SAME) part = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(part)));
+    }
+    __device__ __forceinline__ float operator()(float h) const { return fmaf(h, part, -mean) * n_scale; }
+    __device__ __forceinline__ float rstd() const { return n_scale * part; }
+};
+
 // A block walks rows blockIdx, blockIdx + gridDim, ...; a thread's columns stay the same, so that its shares of dgamma and dbeta stay in registers and no atomics are needed, and the next
 // row's loads are under way while one is summed.  8192 x 4096 bf16 46 us (268 MB, 5.8 TB/s), 65536 x 256 26, and 4.7 for the sum of the blocks' shares.
 template <typename T, int CH, bool NT, Ends ENDS, int LANES = 0>
@@ -359,7 +371,7 @@ __global__ void __launch_bounds__(LANES ? kNarrowThreads : kMostWaves * 64) laye
     lc_issue8<ENDS>(pg, p.gamma, column, c);
     lc_settle8<ENDS>(pg, column, c);
     Packed<T> ph[CH], pd[CH], pt[CH], nh[CH], nd[CH], nt[CH];
-    float rstd = 0.f, mean = 0.f, next_rstd = 0.f, next_mean = 0.f;
+    float next_rstd = 0.f, next_mean = 0.f;
     const auto issue = [&](long long row) __attribute__((always_inline)) {
         lc_issue8<ENDS, NT>(nh, static_cast<const T*>(p.h) + row * p.h_ld, column, c);
         lc_issue8<ENDS, NT>(nd, static_cast<const T*>(p.dy) + row * (long long)c, column, c);
@@ -376,8 +388,7 @@ __global__ void __launch_bounds__(LANES ? kNarrowThreads : kMostWaves * 64) laye
             pd[i] = nd[i];
             pt[i] = nt[i];
         }
-        rstd = next_rstd;
-        mean = next_mean;
+        const Centred<LANES == 0> n_of(next_mean, next_rstd);
         if (row + Of::step() < p.rows) issue(row + Of::step());
         float s = 0.f, sn = 0.f;
         lc_settle8<ENDS>(ph, column, c);
@@ -387,7 +398,7 @@ __global__ void __launch_bounds__(LANES ? kNarrowThreads : kMostWaves * 64) laye
         for (int i = 0; i < CH; ++i)
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float n = (ph[i].get(j) - mean) * rstd, d = pd[i].get(j), a = d * pg[i].get(j);
+                const float n = n_of(ph[i].get(j)), d = pd[i].get(j), a = d * pg[i].get(j);
                 s += a;
                 sn = fmaf(a, n, sn);
                 acc[i][j] = fmaf(d, n, acc[i][j]);
@@ -402,8 +413,8 @@ __global__ void __launch_bounds__(LANES ? kNarrowThreads : kMostWaves * 64) laye
             float o[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float n = (ph[i].get(j) - mean) * rstd;
-                o[j] = ((pd[i].get(j) * pg[i].get(j) - s) - n * sn) * rstd;
+                const float n = n_of(ph[i].get(j));
+                o[j] = ((pd[i].get(j) * pg[i].get(j) - s) - n * sn) * n_of.rstd();
             }
             if (p.dh) {
 #pragma unroll
@@ -452,10 +463,10 @@ __global__ void __launch_bounds__(256) layernorm_parts_wide_kernel(const LayerBw
         Packed<T> h, d;
         lc_load8(h, static_cast<const T*>(p.h) + row * p.h_ld, col, p.c);
         lc_load8(d, static_cast<const T*>(p.dy) + row * (long long)p.c, col, p.c);
-        const float rstd = p.rstd[row], mean = p.mean[row];
+        const Centred<true> n_of(p.mean[row], p.rstd[row]);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            acc[j] = fmaf(d.get(j), (h.get(j) - mean) * rstd, acc[j]);
+            acc[j] = fmaf(d.get(j), n_of(h.get(j)), acc[j]);
             shift[j] += d.get(j);
         }
     }
@@ -475,7 +486,7 @@ __global__ void __launch_bounds__(1024) layernorm_bwd_wide_kernel(const LayerBwd
         const T* dy = static_cast<const T*>(p.dy) + row * (long long)c;
         const T* dh = p.dh ? static_cast<const T*>(p.dh) + row * (long long)c : nullptr;
         T* dx = static_cast<T*>(p.dx) + row * (long long)c;
-        const float rstd = p.rstd[row], mean = p.mean[row];
+        const Centred<true> n_of(p.mean[row], p.rstd[row]);
         Packed<T> a, b, t;
         Packed<float> g;
         float s = 0.f, sn = 0.f;
@@ -487,7 +498,7 @@ __global__ void __launch_bounds__(1024) layernorm_bwd_wide_kernel(const LayerBwd
             for (int j = 0; j < 8; ++j) {
                 const float d = b.get(j) * g.get(j);
                 s += d;
-                sn = fmaf(d, (a.get(j) - mean) * rstd, sn);
+                sn = fmaf(d, n_of(a.get(j)), sn);
             }
         }
         row_sums<0>(s, sn, WAVES, red[parity]);
@@ -501,7 +512,7 @@ __global__ void __launch_bounds__(1024) layernorm_bwd_wide_kernel(const LayerBwd
             float o[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                o[j] = ((b.get(j) * g.get(j) - s) - (a.get(j) - mean) * rstd * sn) * rstd;
+                o[j] = ((b.get(j) * g.get(j) - s) - n_of(a.get(j)) * sn) * n_of.rstd();
                 if (dh) o[j] += t.get(j);
             }
             lc_store8(dx + at, o, c - (int)at);
