@@ -529,7 +529,7 @@ lc_status newton_schulz(const lc_newton_schulz_desc* desc, const void* x, void* 
  * type g_dtype, read only.  A filter of a convolution is a matrix of k rows and c*r*s columns.  scale_per_tensor: HOST array, or NULL for sqrt(max(1, rows / cols)).
  * weight_decay_per_tensor, grad_scale, w_lowp_out: as adamw_step.  momentum in [0, 1), eps >= 0, iterations 1 to 64 -- LC_ERR_UNSUPPORTED otherwise.  A side of 0 is an empty tensor, n_tensors = 0 a
  * no-op.  Tensors must not overlap.  Host arrays are read during the call and travel as launch arguments.  A list's results are
- * bit-identical in reruns; which kernels and tiles take a matrix goes by the whole list, and with it the last bits of its result.
+ * bit-identical in reruns; which kernels and tiles take a matrix goes by what is in its group, and with it the last bits of its result.
  * Matrices go through the steps in groups that share the workspace: at most 64 and, but for a single larger one, 2 GiB at a time (8 bytes for each value, 8 for each of the
  * square of the shorter side, sides counted in multiples of 32). */
 size_t muon_workspace_bytes(int n_tensors, const int* rows, const int* cols);

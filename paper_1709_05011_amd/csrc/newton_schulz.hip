@@ -977,10 +977,11 @@ template <bool MUON, typename T>
 lc_status run_all(const std::vector<Matrix>& all, std::vector<int>& order, const int* rows, const int* cols, const Scalars& s, int iterations, void* workspace,
                   hipStream_t stream) {
     lc_status st = LC_OK;
-    // (beside larger ones small matrices cost next to nothing; a launch of their own would be one more)
-    const bool all_small = std::all_of(order.begin(), order.end(), [&](int i) { return small((int)padded(std::min(rows[i], cols[i])), (int)padded(std::max(rows[i], cols[i]))); });
     for_groups(order, rows, cols, [&](size_t first, size_t n, long long) {
         if (st != LC_OK) return;
+        // (in a group with larger ones small matrices cost next to nothing; a launch of their own would be one more.  One of 330 x 350 and 300 of 64 x 256 491 us where all groups went by the first's sizes, so 295; each of
+        // the two alone 114 and 219)
+        const bool all_small = std::all_of(order.begin() + first, order.begin() + first + n, [&](int i) { return small((int)padded(std::min(rows[i], cols[i])), (int)padded(std::max(rows[i], cols[i]))); });
         st = n <= kSmallTable ? run_group<MUON, T, kSmallTable>(all, order, first, n, s, iterations, all_small, workspace, stream)
                               : run_group<MUON, T, kTable>(all, order, first, n, s, iterations, all_small, workspace, stream);
     });
