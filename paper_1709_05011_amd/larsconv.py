@@ -859,11 +859,14 @@ def newton_schulz(desc, x, y, workspace=None, stream=None, workspace_bytes: Opti
 
 
 class MuonArgs:
-    """Host-side pointer and size arrays of a list of matrices, marshalled once and reusable.  A tensor of more than two dimensions is a matrix of its first one's rows; `shapes` gives
-    (rows, cols) in the place of the tensors' own.  Lists of tensors are checked here, as AdamWArgs checks them; plain addresses are taken as they are."""
+    """Host-side pointer and size arrays of a list of matrices, marshalled once and reusable.  A tensor of more than two dimensions is a matrix of its first one's rows, one of fewer is refused;
+    `shapes` gives (rows, cols) in the place of the tensors' own.  Lists of tensors are checked here, as AdamWArgs checks them; plain addresses are taken as they are."""
 
     def __init__(self, w: Sequence, g: Sequence, m: Sequence, w_lowp: Optional[Sequence] = None, g_dtype: int = LC_F32, shapes: Optional[Sequence] = None):
         if shapes is None:
+            for i, t in enumerate(w):
+                if t.dim() < 2:
+                    raise ValueError(f"w[{i}]: a matrix is needed, got {tuple(t.shape)}; scales and shifts go to another optimizer's list (or name their rows and columns in `shapes`)")
             shapes = [(t.shape[0], t.numel() // t.shape[0] if t.shape[0] else 0) for t in w]
         self.n, self.shapes, self.g_dtype = len(w), [(operator.index(r), operator.index(c)) for r, c in shapes], g_dtype
         if len(self.shapes) != self.n:
