@@ -447,6 +447,8 @@ Plan plan_of(const lc_embedding_desc* d) {
     if (rows > (passes > 1 ? kRankMost : 4096)) {
         p.passes = passes;
         p.bits = (bits + p.passes - 1) / p.passes;
+        // places a block: fewer, in more blocks, lengthen the sums over blocks that each makes.  Whole gradients, us, 1024 / 512 / 256: 30011 of 50021 x 64 bf16 28.6 / 29.6 / 35.8, x 1537 fp32 110 / 111 / 117, 16384 of 32768 x 64 bf16
+        // 23.4 / 25.2 / 26.5, 65536 of 32000 x 64 31.4 / 35.8 / 36.0
         p.per = (int)std::max<long long>(1024, ((rows + kSortBlocks - 1) / kSortBlocks + 1023) / 1024 * 1024);
         p.sort_blocks = (int)((rows + p.per - 1) / p.per);
     }

@@ -538,7 +538,8 @@ constexpr int kFwdWaves = 8192, kUnits = 256;
 long long fwd_blocks(int waves) { return std::max(kUnits, kFwdWaves / waves / kUnits * kUnits); }
 
 // Blocks of the backward pass: the RMS norm's number, in multiples of the units where a block has whole rows.  us, bf16, forward and backward, the RMS norm's / so, both passes': 7084 rows of 1536 50 / 46.5, 2816 77.5 / 66.5,
-// 5120 116 / 110, 6144 152 / 137, 7168 181 / 152, 10240 325 / 281; fp32 4000 x 6144 171 / 154, 16409 x 1344 152 / 148; 2048, 4096 and 8192 columns have the same blocks.
+// 5120 116 / 110, 6144 152 / 137, 7168 181 / 152, 10240 325 / 281; fp32 4000 x 6144 171 / 154, 16409 x 1344 152 / 148; 2048, 4096 and 8192 columns have the same blocks.  (The step from 7168 to 10240: over
+// 8192 columns a thread has 16, whose scale, two sums, three operands and the next row's three are more than the 128 registers that 1024 threads leave: 35 to 117 are spilled, in fp32's forward pass 16 and 17.)
 long long grad_blocks(lc_dtype dtype, long long rows, int c) {
     const long long blocks = bwd_blocks(dtype, rows, c);
     return in_passes(dtype, c) || narrow(rows, c) || blocks < kUnits ? blocks : blocks / kUnits * kUnits;
